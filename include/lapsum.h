@@ -49,7 +49,8 @@ typedef enum lapsum_error {
     LAPSUM_ERR_WORKSPACE = -5,   /* workspace unknown, too small or built for other dims */
     LAPSUM_ERR_CUDA = -6,        /* a CUDA runtime call failed (see lapsum_last_cuda_error) */
     LAPSUM_ERR_PARAM = -7,       /* a field of lapsum_params is out of range       */
-    LAPSUM_ERR_UNSUPPORTED = -8  /* entry point not available for this configuration */
+    LAPSUM_ERR_UNSUPPORTED = -8, /* entry point not available for this configuration */
+    LAPSUM_ERR_ALIGN = -9        /* a tensor of lapsum_experts_* does not start at a multiple of 16 bytes */
 } lapsum_error;
 
 /* Largest row length accepted (tile look-back words carry 30-bit counts). */
@@ -117,6 +118,9 @@ typedef struct lapsum_params {
                                             limit; the access was skipped, the results are invalid                 */
 #define LAPSUM_ST_BAD_ALPHA 0x100u       /* a row's own temperature (alpha_rows) was zero, not finite or outside
                                             fp32's normal range: that row is void                                */
+
+#define LAPSUM_ST_EXPERTS_TIMEOUT 0x400u /* a bounded wait of an experts kernel gave up: results invalid
+                                            (lapsum_experts_status)                                              */
 
 typedef struct lapsum_stats {
     uint32_t status_bits;   /* OR of LAPSUM_ST_* since workspace_init                       */
@@ -448,6 +452,123 @@ int lapsum_profile_enable(void *ws, uint32_t kernel_mask, int max_records);
 int lapsum_profile_read(void *ws, void *stream, int kernel_id, int64_t *launches, double *total_ms);
 int lapsum_profile_disable(void *ws);
 const char *lapsum_kernel_name(int kernel_id);
+
+/*
+ * Mixture-of-experts operators: what follows a routing score in a model.  route -> dispatch -> experts; the scores may be
+ * a router's logits or the soft mask that lapsum_forward returns.  None of these calls allocates, synchronises or keeps
+ * anything from one call for the next; every buffer is the caller's.
+ *
+ * lapsum_route_forward: per token, from `experts` logits l (rows `stride` elements apart, io_dtype):
+ *   scores   s = softmax(l) | sigmoid(l) | l itself ("given": a soft mask)
+ *   keys     c_i = s_i + bias_i; without a bias l_i (softmax and sigmoid rise with it).  The bias balances the load: it
+ *            enters the choice only, never a weight or a gradient.  It may be NULL.
+ *   groups   experts in `groups` equal runs; the `groups_kept` groups with the largest sum of their best `group_top`
+ *            scores (plus bias) keep their experts (a group with one expert available counts that one)
+ *   choice   idx: the k largest keys, largest first; equal keys (and equal groups) by the lower index
+ *   weights  w_j = scale s_j, with renormalise = 1 scale s_j / sum over the chosen s
+ * An expert whose logit is -inf or NaN (or whose key is) is never chosen.  Where fewer than k are left, the remaining
+ * idx are -1 with weight 0.  A logit of +inf makes the row's softmax weights NaN.  "given" scores that sum to 0 give weights 0.
+ * k <= 32, experts <= 1024, groups <= 32.
+ *
+ * lapsum_route_backward: the gradient of the logits (tokens x experts, io_dtype, written in full) from grad_w (type
+ * grad_w_dtype), with the forward's idx and w.  The choice itself is piecewise constant.
+ *   softmax, renormalised:  g_j = w_j (gw_j - W), W = sum_j gw_j w_j / scale       softmax: p_i (scale [i chosen] gw_i - scale W')
+ *   sigmoid, renormalised:  g_j (1 - s_j)                                          sigmoid: scale gw_j s_j (1 - s_j)
+ *   given,   renormalised:  (scale gw_j - sum gw w) / sum s                        given:   scale gw_j
+ */
+typedef enum lapsum_route_score {
+    LAPSUM_ROUTE_SOFTMAX = 0,
+    LAPSUM_ROUTE_SIGMOID = 1,
+    LAPSUM_ROUTE_GIVEN = 2
+} lapsum_route_score;
+
+typedef struct lapsum_route_params {
+    double scale;         /* factor on the weights, not 0; default 1                  */
+    int32_t score;        /* lapsum_route_score; default softmax                      */
+    int32_t k;            /* experts per token; default 1                             */
+    int32_t groups;       /* 1 (default) = no groups                                  */
+    int32_t groups_kept;  /* default 1                                                */
+    int32_t group_top;    /* 1 or 2 (default) keys count for a group                  */
+    int32_t renormalise;  /* default 1                                                */
+    int32_t io_dtype;     /* lapsum_io_dtype of logits and grad_logits; default fp32  */
+    int32_t grad_w_dtype; /* lapsum_io_dtype of grad_w; default fp32                  */
+} lapsum_route_params;
+
+void lapsum_route_default_params(lapsum_route_params *prm);
+int lapsum_route_forward(const void *logits, int64_t tokens, int64_t experts, int64_t stride, const float *bias,
+                         const lapsum_route_params *prm, int32_t *idx, float *w, void *stream);
+int lapsum_route_backward(const void *grad_w, const void *logits, int64_t tokens, int64_t experts, int64_t stride,
+                          const int32_t *idx, const float *w, const lapsum_route_params *prm, void *grad_logits, void *stream);
+
+/*
+ * lapsum_dispatch: the tables that bring every expert's tokens side by side.  An "entry" is one choice of one token, number
+ * token * k + choice; entries with idx outside [0, experts) are dropped.  A stable counting sort gives the others "slots":
+ * expert e owns the slots offsets[e] .. offsets[e] + counts[e] - 1, in the order of the entries; offsets are multiples of
+ * tile_rows (16, 32, 64 or 128).  Arrays of the buffer (byte offsets from lapsum_dispatch_describe, all int32):
+ *   counts[experts], offsets[experts + 1], slot_of[tokens * k] (-1 = dropped), entry_of[capacity] (-1 = hole),
+ *   tile_expert[tiles] (expert of the slots tile_rows * i ..., -1 beyond the last).
+ * capacity, the slots that a batch may need at most, and so every buffer's size, depends on the shape alone.
+ * lapsum_dispatch_tile_rows gives the row tile that lapsum_experts_* is fastest with, from the mean entries per expert;
+ * training needs 64 or 128.
+ */
+typedef struct lapsum_dispatch_layout {
+    int64_t capacity, tiles;
+    size_t off_counts, off_offsets, off_slot_of, off_entry_of, off_tile_expert, off_partial;
+    size_t bytes;
+} lapsum_dispatch_layout;
+
+int lapsum_dispatch_tile_rows(int64_t tokens, int32_t k, int64_t experts, int32_t training, int32_t *tile_rows);
+int lapsum_dispatch_describe(int64_t tokens, int32_t k, int64_t experts, int32_t tile_rows, lapsum_dispatch_layout *out);
+/* dispatch: 256-byte aligned, `bytes` at least as described */
+int lapsum_dispatch(const int32_t *idx, int64_t tokens, int32_t k, int64_t experts, int32_t tile_rows, void *dispatch,
+                    size_t bytes, void *stream);
+
+/*
+ * lapsum_experts_forward: the gated experts' products on the routed tokens (fp16 or bf16, sums in fp32),
+ *   y_t = sum_j w_tj W_down[e] (silu(g) * u),   [g; u] = W_gate_up[e] x_t,   e = idx_tj.
+ * x: tokens rows of d, x_stride elements apart (a multiple of 8); w_gate_up: experts x 2f x d (f gate rows, then f up
+ * rows); w_down: experts x d x f; w: tokens x k floats; dispatch: the tables of the same idx; y: tokens x d.  d and f are
+ * multiples of 8; every tensor starts at a multiple of 16 bytes.  A token without an entry gets y = 0.
+ * With dims.training the call leaves g, u and the weighted activations in `saved` (256-byte aligned, `saved_bytes` as
+ * described) for lapsum_experts_backward; otherwise saved is NULL.
+ *
+ * lapsum_experts_backward: every gradient: grad_x (tokens x d), grad_w_gate_up, grad_w_down (written in full, zeros for an
+ * expert without tokens), grad_w (tokens x k, in io_dtype, 0 for dropped entries: it is a sum over 16-bit activations).
+ * Results do not depend on scheduling: no sum is formed by atomics.
+ *
+ * One workspace serves one stream at a time.  lapsum_experts_workspace_init clears its status word (enqueued on `stream`);
+ * lapsum_experts_status synchronises and reads it (LAPSUM_ST_EXPERTS_TIMEOUT: a bounded wait inside a kernel gave up).
+ */
+typedef struct lapsum_experts_dims {
+    int64_t tokens, experts, d, f;
+    int32_t k, tile_rows; /* as given to lapsum_dispatch */
+    int32_t io_dtype;     /* LAPSUM_IO_F16 or LAPSUM_IO_BF16 */
+    int32_t training;     /* 1: a forward is followed by a backward */
+} lapsum_experts_dims;
+
+typedef struct lapsum_experts_layout {
+    size_t workspace_bytes, saved_bytes;
+} lapsum_experts_layout;
+
+int lapsum_experts_describe(const lapsum_experts_dims *dims, lapsum_experts_layout *out);
+int lapsum_experts_workspace_init(void *ws, size_t bytes, const lapsum_experts_dims *dims, void *stream);
+int lapsum_experts_status(void *ws, void *stream, uint32_t *status_bits);
+int lapsum_experts_forward(const void *x, int64_t x_stride, const void *w_gate_up, const void *w_down, const float *w,
+                           const void *dispatch, size_t dispatch_bytes, void *saved, size_t saved_bytes, void *y,
+                           const lapsum_experts_dims *dims, void *ws, size_t ws_bytes, void *stream);
+int lapsum_experts_backward(const void *grad_y, int64_t grad_y_stride, const void *x, int64_t x_stride, const void *w_gate_up,
+                            const void *w_down, const float *w, const void *dispatch, size_t dispatch_bytes, const void *saved,
+                            size_t saved_bytes, void *grad_x, void *grad_w_gate_up, void *grad_w_down, void *grad_w,
+                            const lapsum_experts_dims *dims, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Test hook for the bounded waits of the experts' kernels: runs the first product with a producer that brings nothing and a
+ * bound of wait_us (1 .. 100000) microseconds, so that every wait runs out, LAPSUM_ST_EXPERTS_TIMEOUT is raised and the
+ * kernel returns.  Writes nothing but the status word.  bf16, not training.
+ */
+int lapsum_debug_experts_timeout(int64_t wait_us, void *ws, size_t ws_bytes, const void *dispatch, size_t dispatch_bytes,
+                                 const void *x, const void *w_gate_up, const float *w, const lapsum_experts_dims *dims,
+                                 void *stream);
 
 /* Number of kernel launches this library has enqueued since it was loaded. */
 int64_t lapsum_launch_count(void);

@@ -10,4 +10,9 @@ from .binding import (  # noqa: F401
     lapsum_profile_read, KERNELS, lapsum_backward_static, lapsum_backward_scalars, lapsum_forward_backward_host,
     lapsum_describe, lapsum_forward_row_budgets, lapsum_debug_lookback_timeout, lapsum_forward_rows, lapsum_backward_rows, ST_BAD_ALPHA, ST_BOUNDS,
     lapsum_forward_io, lapsum_backward_io, ShardWorkspace, GpuShard, IO_F32, IO_F16, IO_BF16, IO_TORCH, IO_NAMES, lapsum_workspace_bytes, lib, library_path,
+    ST_EXPERTS_TIMEOUT,
+)
+from .experts import (  # noqa: F401
+    Dispatch, ExpertsWorkspace, IO_OF, ROUTE_GIVEN, ROUTE_SCORES, ROUTE_SIGMOID, ROUTE_SOFTMAX, dispatch_tile_rows, lapsum_dispatch,
+    lapsum_dispatch_describe, lapsum_experts_backward, lapsum_experts_forward, lapsum_route_backward, lapsum_route_forward, route_params,
 )

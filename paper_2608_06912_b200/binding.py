@@ -33,6 +33,7 @@ ST_WIDENED = 0x40
 ST_BAD_BUDGET = 0x80
 ST_BAD_ALPHA = 0x100
 ST_BOUNDS = 0x200
+ST_EXPERTS_TIMEOUT = 0x400
 
 EXPORTS = (
     "lapsum_default_params", "lapsum_workspace_bytes", "lapsum_workspace_init", "lapsum_workspace_release",
@@ -44,6 +45,10 @@ EXPORTS = (
     "lapsum_forward_io", "lapsum_backward_io",
     "lapsum_shard_workspace_bytes", "lapsum_shard_workspace_init", "lapsum_shard_describe", "lapsum_shard_sample",
     "lapsum_shard_stream", "lapsum_shard_solve", "lapsum_shard_mask", "lapsum_shard_vjp_partial", "lapsum_shard_vjp_apply",
+    "lapsum_route_default_params", "lapsum_route_forward", "lapsum_route_backward",
+    "lapsum_dispatch_tile_rows", "lapsum_dispatch_describe", "lapsum_dispatch",
+    "lapsum_experts_describe", "lapsum_experts_workspace_init", "lapsum_experts_status", "lapsum_experts_forward",
+    "lapsum_experts_backward", "lapsum_debug_experts_timeout",
 )
 
 KERNELS = ("row_block_forward", "row_block_backward", "rs_histogram", "rs_onesweep", "tile_aggregate", "solve_global",
@@ -79,6 +84,32 @@ class ShardLayout(C.Structure):
         ("off_n_R", C.c_size_t), ("off_tails", C.c_size_t), ("off_bucket_counts", C.c_size_t),
         ("off_bucket_sums", C.c_size_t), ("off_band_keys", C.c_size_t), ("off_vjp_sums", C.c_size_t),
     ]
+
+
+class RouteParams(C.Structure):
+    _fields_ = [
+        ("scale", C.c_double), ("score", C.c_int32), ("k", C.c_int32), ("groups", C.c_int32), ("groups_kept", C.c_int32),
+        ("group_top", C.c_int32), ("renormalise", C.c_int32), ("io_dtype", C.c_int32), ("grad_w_dtype", C.c_int32),
+    ]
+
+
+class DispatchLayout(C.Structure):
+    _fields_ = [
+        ("capacity", C.c_int64), ("tiles", C.c_int64), ("off_counts", C.c_size_t), ("off_offsets", C.c_size_t),
+        ("off_slot_of", C.c_size_t), ("off_entry_of", C.c_size_t), ("off_tile_expert", C.c_size_t), ("off_partial", C.c_size_t),
+        ("bytes", C.c_size_t),
+    ]
+
+
+class ExpertsDims(C.Structure):
+    _fields_ = [
+        ("tokens", C.c_int64), ("experts", C.c_int64), ("d", C.c_int64), ("f", C.c_int64), ("k", C.c_int32),
+        ("tile_rows", C.c_int32), ("io_dtype", C.c_int32), ("training", C.c_int32),
+    ]
+
+
+class ExpertsLayout(C.Structure):
+    _fields_ = [("workspace_bytes", C.c_size_t), ("saved_bytes", C.c_size_t)]
 
 
 class Stats(C.Structure):
@@ -136,6 +167,20 @@ def lib():
         L.lapsum_debug_lookback_timeout.argtypes = [vp, i64, C.c_int, vp, vp]
         L.lapsum_debug_bracket.argtypes = [vp, i64, dbl, dbl, vp, vp, C.c_int, C.c_float, C.c_float, vp, vp]
         L.lapsum_forward_with_bracket.argtypes = [vp, i64, dbl, dbl, C.c_float, C.c_float, vp, vp, vp, vp]
+        i32, sz = C.c_int32, C.c_size_t
+        L.lapsum_route_default_params.argtypes = [C.POINTER(RouteParams)]
+        L.lapsum_route_default_params.restype = None
+        L.lapsum_route_forward.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, vp]
+        L.lapsum_route_backward.argtypes = [vp, vp, i64, i64, i64, vp, vp, vp, vp, vp]
+        L.lapsum_dispatch_tile_rows.argtypes = [i64, i32, i64, i32, C.POINTER(i32)]
+        L.lapsum_dispatch_describe.argtypes = [i64, i32, i64, i32, C.POINTER(DispatchLayout)]
+        L.lapsum_dispatch.argtypes = [vp, i64, i32, i64, i32, vp, sz, vp]
+        L.lapsum_experts_describe.argtypes = [vp, C.POINTER(ExpertsLayout)]
+        L.lapsum_experts_workspace_init.argtypes = [vp, sz, vp, vp]
+        L.lapsum_experts_status.argtypes = [vp, vp, C.POINTER(C.c_uint32)]
+        L.lapsum_experts_forward.argtypes = [vp, i64, vp, vp, vp, vp, sz, vp, sz, vp, vp, vp, sz, vp]
+        L.lapsum_experts_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, sz, vp, sz, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.lapsum_debug_experts_timeout.argtypes = [i64, vp, sz, vp, sz, vp, vp, vp, vp, vp]
         L.lapsum_launch_count.argtypes = []
         L.lapsum_launch_count.restype = i64
         L.lapsum_error_string.argtypes = [C.c_int]

@@ -12,8 +12,9 @@ CSRC = os.path.join(HERE, "csrc")
 # LAPSUM_IN_BOUNDS in csrc/common.cuh): a separate library, built with build(check_bounds=True)
 CHECK = os.environ.get("LAPSUM_B200_CHECK_BUILD", "0") not in ("", "0")
 LIB = os.path.join(HERE, "liblapsum_b200_check.so" if CHECK else "liblapsum_b200.so")
-SOURCES = ["lapsum_api.cu"]
+SOURCES = ["lapsum_api.cu", "experts_api.cu"]
 HEADERS = ["common.cuh", "solve.cuh", "radix_sort.cuh", "row_block.cuh", "global_path.cuh", "bracket_select.cuh",
+           "host.h", "routing.cuh", "experts.cuh",
            os.path.join("..", "..", "include", "lapsum.h")]
 
 
@@ -41,7 +42,7 @@ def build(force: bool = False, verbose: bool = False, check_bounds: bool | None 
         return LIB
     tmp = lib + f".{os.getpid()}.tmp"
     cmd = [nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-rdc=true", "-o", tmp]
+           "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-rdc=true", "--threads", "0", "-o", tmp]
     if check:
         cmd += ["-DLAPSUM_CHECK_BOUNDS"]
     if verbose:

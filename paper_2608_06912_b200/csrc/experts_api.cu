@@ -1,0 +1,505 @@
+// C entries of the mixture-of-experts operators: lapsum_route_*, lapsum_dispatch*, lapsum_experts_*.  Argument checks,
+// buffer layout, tensor maps and launches; nothing is allocated and the host never waits.
+#include <cmath>
+#include <cstring>
+
+#include "../../include/lapsum.h"
+#include "experts.cuh"
+#include "host.h"
+#include "routing.cuh"
+
+using namespace lapsum;
+
+namespace {
+
+inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
+inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+#define CU_OK(x)                                      \
+    do {                                              \
+        const cudaError_t e__ = (x);                  \
+        if (e__ != cudaSuccess) return cuda_fail(e__); \
+    } while (0)
+#define RUN(x)                    \
+    do {                          \
+        const int rc__ = (x);     \
+        if (rc__ != 0) return rc__; \
+    } while (0)
+
+// ------------------------------------------------------------------- route ----
+int route_check(int64_t tokens, int64_t experts, int64_t stride, const lapsum_route_params *p)
+{
+    if (!p) return LAPSUM_ERR_NULL;
+    if (tokens < 0 || tokens > (int64_t)1 << 30 || experts < 1 || experts > ROUTE_MAX_E || stride < experts) return LAPSUM_ERR_SHAPE;
+    if (p->score < LAPSUM_ROUTE_SOFTMAX || p->score > LAPSUM_ROUTE_GIVEN || p->io_dtype < LAPSUM_IO_F32 || p->io_dtype > LAPSUM_IO_BF16 ||
+        p->grad_w_dtype < LAPSUM_IO_F32 || p->grad_w_dtype > LAPSUM_IO_BF16 || p->k < 1 || p->k > ROUTE_MAX_K || p->k > experts ||
+        p->groups < 1 || p->groups > ROUTE_MAX_GROUPS || experts % p->groups || p->groups_kept < 1 || p->groups_kept > p->groups ||
+        p->group_top < 1 || p->group_top > 2 || !std::isfinite(p->scale) || p->scale == 0.0 || (float)p->scale == 0.f ||
+        !std::isfinite((float)p->scale))
+        return LAPSUM_ERR_PARAM;
+    return LAPSUM_OK;
+}
+
+template <typename T, int NV, bool VEC>
+int route_forward_nv(const RouteArgs &A, cudaStream_t st)
+{
+    const unsigned grid = (unsigned)((A.tokens + ROUTE_WARPS - 1) / ROUTE_WARPS);
+    if (A.groups > 1)
+        return launch_pdl(route_forward_kernel<T, NV, VEC, true>, grid, 32 * ROUTE_WARPS, sizeof(float) * ROUTE_WARPS * A.E, st, A);
+    return launch_pdl(route_forward_kernel<T, NV, VEC, false>, grid, 32 * ROUTE_WARPS, 0, st, A);
+}
+template <typename T, int NV, bool VEC>
+int route_backward_nv(const RouteBackArgs &A, cudaStream_t st)
+{
+    return launch_pdl(route_backward_kernel<T, NV, VEC>, (unsigned)((A.tokens + ROUTE_WARPS - 1) / ROUTE_WARPS), 32 * ROUTE_WARPS, 0, st, A);
+}
+#define BY_WIDTH(fn, T, vec, E, ...)                                                                                    \
+    ((E) <= 128   ? ((vec) ? fn<T, 4, true>(__VA_ARGS__) : fn<T, 4, false>(__VA_ARGS__))                               \
+     : (E) <= 256 ? ((vec) ? fn<T, 8, true>(__VA_ARGS__) : fn<T, 8, false>(__VA_ARGS__))                               \
+     : (E) <= 512 ? ((vec) ? fn<T, 16, true>(__VA_ARGS__) : fn<T, 16, false>(__VA_ARGS__))                             \
+                  : ((vec) ? fn<T, 32, true>(__VA_ARGS__) : fn<T, 32, false>(__VA_ARGS__)))
+#define BY_TYPE(fn, dtype, ...)                                  \
+    ((dtype) == LAPSUM_IO_F32   ? fn<float>(__VA_ARGS__)          \
+     : (dtype) == LAPSUM_IO_F16 ? fn<__half>(__VA_ARGS__)         \
+                                : fn<__nv_bfloat16>(__VA_ARGS__))
+
+// four logits per load where every row starts at a multiple of four elements
+template <typename T>
+int route_forward_t(const RouteArgs &A, cudaStream_t st)
+{
+    const bool vec = A.E % 4 == 0 && A.stride % 4 == 0 && aligned(A.logits, 4 * sizeof(T));
+    return BY_WIDTH(route_forward_nv, T, vec, A.E, A, st);
+}
+template <typename T>
+int route_backward_t(const RouteBackArgs &A, cudaStream_t st)
+{
+    const bool vec = A.E % 4 == 0 && A.stride % 4 == 0 && aligned(A.logits, 4 * sizeof(T)) && aligned(A.grad, 4 * sizeof(T));
+    return BY_WIDTH(route_backward_nv, T, vec, A.E, A, st);
+}
+
+// ---------------------------------------------------------------- dispatch ----
+int dispatch_layout(int64_t tokens, int32_t k, int64_t experts, int32_t rows, lapsum_dispatch_layout *L)
+{
+    if (tokens < 0 || k < 1 || k > ROUTE_MAX_K || experts < 1 || experts > ROUTE_MAX_E) return LAPSUM_ERR_SHAPE;
+    if (rows != 16 && rows != 32 && rows != 64 && rows != 128) return LAPSUM_ERR_PARAM;
+    if (tokens > ((int64_t)1 << 30) / k) return LAPSUM_ERR_SHAPE;
+    const int64_t entries = tokens * k;
+    const int64_t used = entries < experts ? entries : experts;
+    L->capacity = (entries + used * (rows - 1)) / rows * rows;
+    L->tiles = L->capacity / rows;
+    size_t at = 0;
+    auto take = [&](size_t words) {
+        const size_t o = at;
+        at += align_up(4 * words);
+        return o;
+    };
+    L->off_counts = take((size_t)experts);
+    L->off_offsets = take((size_t)experts + 1);
+    L->off_slot_of = take((size_t)entries);
+    L->off_entry_of = take((size_t)L->capacity);
+    L->off_tile_expert = take((size_t)L->tiles);
+    L->off_partial = take((size_t)((entries + DISPATCH_CHUNK - 1) / DISPATCH_CHUNK * experts));
+    L->bytes = at;
+    return LAPSUM_OK;
+}
+
+// ----------------------------------------------------------------- experts ----
+struct ExpertsLayout {
+    lapsum_dispatch_layout d;
+    size_t off_slots, off_hw, off_dgu, off_partial, off_gu_saved, off_hw_saved;
+    int nts_dh;
+};
+
+// Columns of an output tile: 256 keep the tensor core fed from shared memory; with 64 or fewer rows a tile is bound by the
+// weights it streams, and narrower tiles give more blocks and a deeper ring.
+constexpr int tile_cols(int rows) { return rows == 128 ? 256 : rows == 64 ? 128 : 64; }
+
+int experts_layout(const lapsum_experts_dims *p, ExpertsLayout &X, lapsum_experts_layout *out)
+{
+    if (!p) return LAPSUM_ERR_NULL;
+    if (p->d < 8 || p->f < 8 || p->d % 8 || p->f % 8 || p->d > 1 << 20 || p->f > 1 << 20) return LAPSUM_ERR_SHAPE;
+    if (p->io_dtype != LAPSUM_IO_F16 && p->io_dtype != LAPSUM_IO_BF16) return LAPSUM_ERR_UNSUPPORTED;
+    if (p->training != 0 && p->training != 1) return LAPSUM_ERR_PARAM;
+    RUN(dispatch_layout(p->tokens, p->k, p->experts, p->tile_rows, &X.d));
+    if (p->training && p->tile_rows < 64) return LAPSUM_ERR_PARAM;
+    const size_t cap = (size_t)X.d.capacity, D = (size_t)p->d, F = (size_t)p->f;
+    X.nts_dh = (int)((p->f + tile_cols(p->tile_rows) - 1) / tile_cols(p->tile_rows));
+    size_t at = 256;  // control block: the status word
+    X.off_slots = at, at += align_up(cap * D * 2);
+    X.off_hw = at, at += p->training ? 0 : align_up(cap * F * 2);
+    X.off_dgu = at, at += p->training ? align_up(cap * F * 4) : 0;
+    X.off_partial = at, at += p->training ? align_up(cap * (size_t)X.nts_dh * 4) : 0;
+    out->workspace_bytes = at;
+    X.off_gu_saved = 0;
+    X.off_hw_saved = align_up(cap * F * 4);
+    out->saved_bytes = p->training ? X.off_hw_saved + align_up(cap * F * 2) : 0;
+    return LAPSUM_OK;
+}
+
+using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                              const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                              CUtensorMapFloatOOBfill);
+EncodeFn encode_fn()
+{
+    static const EncodeFn fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeFn>(p);
+    }();
+    return fn;
+}
+
+// dims from the innermost; strides in elements for dimensions 1..; 128-byte swizzle; reads beyond the tensor give zeros
+int tensor_map(CUtensorMap *map, int dtype, const void *base, int rank, const int64_t *dims, const int64_t *strides, const int *box)
+{
+    const EncodeFn fn = encode_fn();
+    if (!fn) return cuda_fail(cudaErrorNotSupported);
+    cuuint64_t d[3], s[2];
+    cuuint32_t b[3], one[3] = {1, 1, 1};
+    for (int i = 0; i < rank; ++i) d[i] = (cuuint64_t)dims[i], b[i] = (cuuint32_t)box[i];
+    for (int i = 0; i + 1 < rank; ++i) s[i] = (cuuint64_t)strides[i] * 2;
+    const CUresult r = fn(map, dtype == LAPSUM_IO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
+                          const_cast<void *>(base), d, s, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? LAPSUM_OK : cuda_fail(cudaErrorInvalidValue);
+}
+int map_2d(CUtensorMap *m, int dtype, const void *base, int64_t cols, int64_t rows, int64_t stride, int box_rows)
+{
+    const int64_t d[2] = {cols, rows}, s[1] = {stride};
+    const int b[2] = {64, box_rows};
+    return tensor_map(m, dtype, base, 2, d, s, b);
+}
+int map_3d(CUtensorMap *m, int dtype, const void *base, int64_t cols, int64_t rows, int64_t depth, int box_rows)
+{
+    const int64_t d[3] = {cols, rows, depth}, s[2] = {cols, cols * rows};
+    const int b[3] = {64, box_rows, 1};
+    return tensor_map(m, dtype, base, 3, d, s, b);
+}
+
+int sm_count(int *n)
+{
+    static thread_local int dev_known = -1, sms = 0;
+    int dev = 0;
+    CU_OK(cudaGetDevice(&dev));
+    if (dev != dev_known) {
+        CU_OK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+        dev_known = dev;
+    }
+    *n = sms;
+    return LAPSUM_OK;
+}
+
+template <int MODE, int AR, int BN, typename T>
+int run_experts(const CUtensorMap &a, const CUtensorMap &b, const ExpertsArgs &P, int64_t tiles_max, cudaStream_t st)
+{
+    using S = ExpertsShape<MODE, AR, BN>;
+    static thread_local int dev_ready = -1;  // the attribute belongs to the device's context
+    int dev = 0, sms = 0;
+    CU_OK(cudaGetDevice(&dev));
+    RUN(sm_count(&sms));
+    if (dev != dev_ready) {
+        CU_OK(cudaFuncSetAttribute(experts_kernel<MODE, AR, BN, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
+        dev_ready = dev;
+    }
+    const unsigned grid = (unsigned)(tiles_max < sms ? (tiles_max < 1 ? 1 : tiles_max) : sms);
+    return launch_pdl(experts_kernel<MODE, AR, BN, T>, grid, 256, S::SMEM, st, a, b, P);
+}
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct Call {
+    const lapsum_experts_dims *p;
+    ExpertsLayout X;
+    ExpertsArgs A;
+    uint8_t *ws;
+};
+
+int begin_call(const lapsum_experts_dims *p, const void *dispatch, size_t dispatch_bytes, void *ws, size_t ws_bytes, Call &c)
+{
+    lapsum_experts_layout out;
+    RUN(experts_layout(p, c.X, &out));
+    if (!dispatch || !ws) return LAPSUM_ERR_NULL;
+    if (!aligned(ws, 256) || ws_bytes < out.workspace_bytes || !aligned(dispatch, 256) || dispatch_bytes < c.X.d.bytes)
+        return LAPSUM_ERR_WORKSPACE;
+    c.p = p;
+    c.ws = static_cast<uint8_t *>(ws);
+    const uint8_t *d = static_cast<const uint8_t *>(dispatch);
+    std::memset(&c.A, 0, sizeof(c.A));
+    c.A.entry_of = reinterpret_cast<const int32_t *>(d + c.X.d.off_entry_of);
+    c.A.tile_expert = reinterpret_cast<const int32_t *>(d + c.X.d.off_tile_expert);
+    c.A.offsets = reinterpret_cast<const int32_t *>(d + c.X.d.off_offsets);
+    c.A.status = reinterpret_cast<uint32_t *>(ws);
+    c.A.slots = c.X.d.capacity;
+    c.A.wait_ns = 2000000000ull;
+    c.A.E = (int)p->experts, c.A.D = (int)p->d, c.A.F = (int)p->f, c.A.k = p->k, c.A.tokens = (int)p->tokens, c.A.rows = p->tile_rows;
+    return LAPSUM_OK;
+}
+
+template <int MODE, typename T>
+int run_rows(const Call &c, const CUtensorMap &a, const CUtensorMap &b, const ExpertsArgs &P, int64_t cols, cudaStream_t st)
+{
+    const int rows = c.p->tile_rows, step = MODE == GATE_UP ? tile_cols(rows) / 2 : tile_cols(rows);
+    const int64_t tiles = c.X.d.tiles * ceil_div(cols, step);
+    if (rows == 128) return run_experts<MODE, 128, tile_cols(128), T>(a, b, P, tiles, st);
+    if (rows == 64) return run_experts<MODE, 64, tile_cols(64), T>(a, b, P, tiles, st);
+    if constexpr (MODE == GATE_UP || MODE == DOWN) {
+        if (rows == 32) return run_experts<MODE, 32, tile_cols(32), T>(a, b, P, tiles, st);
+        return run_experts<MODE, 16, tile_cols(16), T>(a, b, P, tiles, st);
+    }
+    return LAPSUM_ERR_PARAM;
+}
+
+template <typename T>
+int combine(const Call &c, const uint8_t *dispatch, void *out, int64_t stride, const float *partial, void *grad_w, cudaStream_t st)
+{
+    const int64_t work = c.p->tokens * (c.p->d / 8);
+    return launch_pdl(experts_combine_kernel<T>, (unsigned)ceil_div(work, 256), 256, 0, st, reinterpret_cast<const T *>(c.ws + c.X.off_slots),
+                      reinterpret_cast<const int32_t *>(dispatch + c.X.d.off_slot_of), static_cast<T *>(out), stride, partial,
+                      static_cast<T *>(grad_w), c.p->tokens, (int)c.p->k, (int)c.p->d, c.X.nts_dh);
+}
+
+template <typename T>
+int forward_t(Call &c, const void *x, int64_t x_stride, const void *w_gate_up, const void *w_down, const float *w, const uint8_t *dispatch,
+              uint8_t *saved, void *y, cudaStream_t st)
+{
+    const lapsum_experts_dims &p = *c.p;
+    const int dt = p.io_dtype, rows = p.tile_rows, cols = tile_cols(rows);
+    void *hw = saved ? saved + c.X.off_hw_saved : c.ws + c.X.off_hw;
+    CUtensorMap a, b;
+    RUN(map_2d(&a, dt, x, p.d, p.tokens, x_stride, 1));
+    RUN(map_3d(&b, dt, w_gate_up, p.d, p.f, 2 * p.experts, cols / 2));
+    ExpertsArgs A = c.A;
+    A.w = w;
+    A.out0 = hw;
+    A.out1 = saved ? saved + c.X.off_gu_saved : nullptr;
+    RUN((run_rows<GATE_UP, T>(c, a, b, A, p.f, st)));
+    RUN(map_2d(&a, dt, hw, p.f, c.X.d.capacity, p.f, rows));
+    RUN(map_3d(&b, dt, w_down, p.f, p.d, p.experts, cols));
+    A = c.A;
+    A.out0 = c.ws + c.X.off_slots;
+    RUN((run_rows<DOWN, T>(c, a, b, A, p.d, st)));
+    return combine<T>(c, dispatch, y, p.d, nullptr, nullptr, st);
+}
+
+template <typename T>
+int backward_t(Call &c, const void *grad_y, int64_t gy_stride, const void *x, int64_t x_stride, const void *w_gate_up, const void *w_down,
+               const float *w, const uint8_t *dispatch, const uint8_t *saved, void *grad_x, void *grad_w_gate_up, void *grad_w_down,
+               void *grad_w, cudaStream_t st)
+{
+    const lapsum_experts_dims &p = *c.p;
+    const int dt = p.io_dtype, rows = p.tile_rows;
+    const int64_t cap = c.X.d.capacity;
+    const uint8_t *hw = saved + c.X.off_hw_saved;
+    uint8_t *dgu = c.ws + c.X.off_dgu;
+    float *partial = reinterpret_cast<float *>(c.ws + c.X.off_partial);
+    CUtensorMap a, b;
+    RUN(map_2d(&a, dt, grad_y, p.d, p.tokens, gy_stride, 1));
+    RUN(map_3d(&b, dt, w_down, p.f, p.d, p.experts, 64));
+    ExpertsArgs A = c.A;
+    A.w = w, A.in0 = saved + c.X.off_gu_saved, A.out0 = dgu, A.partial = partial;
+    RUN((run_rows<DH, T>(c, a, b, A, p.f, st)));
+
+    // a = grad_y by token, b = w h by slot
+    RUN(map_2d(&b, dt, hw, p.f, cap, p.f, 64));
+    A = c.A;
+    A.out0 = grad_w_down;
+    RUN((run_experts<DW_DOWN, 128, 256, T>(a, b, A, p.experts * ceil_div(p.d, 128) * ceil_div(p.f, 256), st)));
+
+    RUN(map_2d(&a, dt, dgu, 2 * p.f, cap, 2 * p.f, rows));
+    RUN(map_3d(&b, dt, w_gate_up, p.d, 2 * p.f, p.experts, 64));
+    A = c.A;
+    A.out0 = c.ws + c.X.off_slots;
+    RUN((run_rows<DX, T>(c, a, b, A, p.d, st)));
+    RUN(combine<T>(c, dispatch, grad_x, p.d, partial, grad_w, st));
+
+    RUN(map_2d(&a, dt, dgu, 2 * p.f, cap, 2 * p.f, 64));
+    RUN(map_2d(&b, dt, x, p.d, p.tokens, x_stride, 1));
+    A = c.A;
+    A.out0 = grad_w_gate_up;
+    return run_experts<DW_GATE_UP, 128, 256, T>(a, b, A, p.experts * ceil_div(2 * p.f, 128) * ceil_div(p.d, 256), st);
+}
+
+}  // namespace
+
+extern "C" {
+
+void lapsum_route_default_params(lapsum_route_params *p)
+{
+    if (!p) return;
+    std::memset(p, 0, sizeof(*p));
+    p->scale = 1.0;
+    p->score = LAPSUM_ROUTE_SOFTMAX;
+    p->k = p->groups = p->groups_kept = 1;
+    p->group_top = 2;
+    p->renormalise = 1;
+    p->io_dtype = p->grad_w_dtype = LAPSUM_IO_F32;
+}
+
+int lapsum_route_forward(const void *logits, int64_t tokens, int64_t experts, int64_t stride, const float *bias,
+                         const lapsum_route_params *prm, int32_t *idx, float *w, void *stream)
+{
+    RUN(route_check(tokens, experts, stride, prm));
+    if (tokens == 0) return LAPSUM_OK;
+    if (!logits || !idx || !w) return LAPSUM_ERR_NULL;
+    const RouteArgs A{logits, bias, idx, w, tokens, stride, (int)experts, prm->k, prm->groups, prm->groups_kept, prm->group_top,
+                      prm->score, prm->renormalise != 0, (float)prm->scale};
+    return BY_TYPE(route_forward_t, prm->io_dtype, A, static_cast<cudaStream_t>(stream));
+}
+
+int lapsum_route_backward(const void *grad_w, const void *logits, int64_t tokens, int64_t experts, int64_t stride, const int32_t *idx,
+                          const float *w, const lapsum_route_params *prm, void *grad_logits, void *stream)
+{
+    RUN(route_check(tokens, experts, stride, prm));
+    if (tokens == 0) return LAPSUM_OK;
+    if (!grad_w || !logits || !idx || !w || !grad_logits) return LAPSUM_ERR_NULL;
+    const RouteBackArgs A{grad_w, logits, idx, w, grad_logits, tokens, stride, (int)experts, prm->k, prm->score, prm->renormalise != 0,
+                          prm->grad_w_dtype, (float)prm->scale};
+    return BY_TYPE(route_backward_t, prm->io_dtype, A, static_cast<cudaStream_t>(stream));
+}
+
+int lapsum_dispatch_tile_rows(int64_t tokens, int32_t k, int64_t experts, int32_t training, int32_t *rows)
+{
+    if (!rows) return LAPSUM_ERR_NULL;
+    if (tokens < 0 || k < 1 || k > ROUTE_MAX_K || experts < 1 || experts > ROUTE_MAX_E) return LAPSUM_ERR_SHAPE;
+    const double mean = (double)tokens * k / (double)experts;  // entries per expert
+    *rows = mean > 48 ? 128 : mean > 24 || training ? 64 : mean > 8 ? 32 : 16;
+    return LAPSUM_OK;
+}
+
+int lapsum_dispatch_describe(int64_t tokens, int32_t k, int64_t experts, int32_t tile_rows, lapsum_dispatch_layout *out)
+{
+    if (!out) return LAPSUM_ERR_NULL;
+    return dispatch_layout(tokens, k, experts, tile_rows, out);
+}
+
+int lapsum_dispatch(const int32_t *idx, int64_t tokens, int32_t k, int64_t experts, int32_t tile_rows, void *dispatch, size_t bytes,
+                    void *stream)
+{
+    lapsum_dispatch_layout L;
+    RUN(dispatch_layout(tokens, k, experts, tile_rows, &L));
+    if ((!idx && tokens > 0) || !dispatch) return LAPSUM_ERR_NULL;
+    if (!aligned(dispatch, 256) || bytes < L.bytes) return LAPSUM_ERR_WORKSPACE;
+    uint8_t *d = static_cast<uint8_t *>(dispatch);
+    DispatchArgs A;
+    A.idx = idx;
+    A.entries = tokens * k, A.capacity = L.capacity;
+    A.E = (int)experts, A.rows = tile_rows;
+    A.chunks = (int)ceil_div(A.entries, DISPATCH_CHUNK);
+    if (A.chunks < 1) A.chunks = 1;
+    A.bits = 1;
+    while ((1 << A.bits) <= (int)experts) ++A.bits;  // values 0 .. experts
+    A.counts = reinterpret_cast<int32_t *>(d + L.off_counts), A.offsets = reinterpret_cast<int32_t *>(d + L.off_offsets);
+    A.slot_of = reinterpret_cast<int32_t *>(d + L.off_slot_of), A.entry_of = reinterpret_cast<int32_t *>(d + L.off_entry_of);
+    A.tile_expert = reinterpret_cast<int32_t *>(d + L.off_tile_expert), A.partial = reinterpret_cast<int32_t *>(d + L.off_partial);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (A.chunks > 1) RUN(launch_pdl(dispatch_count_kernel, (unsigned)A.chunks, DISPATCH_THREADS, 4 * (size_t)experts, st, A));
+    const size_t smem = 4 * ((size_t)(DISPATCH_THREADS / 32 + 3) * (size_t)experts + 1);
+    return launch_pdl(dispatch_place_kernel, (unsigned)A.chunks, DISPATCH_THREADS, smem, st, A);
+}
+
+int lapsum_experts_describe(const lapsum_experts_dims *dims, lapsum_experts_layout *out)
+{
+    if (!out) return LAPSUM_ERR_NULL;
+    ExpertsLayout X;
+    return experts_layout(dims, X, out);
+}
+
+int lapsum_experts_workspace_init(void *ws, size_t bytes, const lapsum_experts_dims *dims, void *stream)
+{
+    ExpertsLayout X;
+    lapsum_experts_layout out;
+    RUN(experts_layout(dims, X, &out));
+    if (!ws) return LAPSUM_ERR_NULL;
+    if (!aligned(ws, 256) || bytes < out.workspace_bytes) return LAPSUM_ERR_WORKSPACE;
+    CU_OK(cudaMemsetAsync(ws, 0, 256, static_cast<cudaStream_t>(stream)));
+    return LAPSUM_OK;
+}
+
+int lapsum_experts_status(void *ws, void *stream, uint32_t *status_bits)
+{
+    if (!ws || !status_bits) return LAPSUM_ERR_NULL;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    CU_OK(cudaMemcpyAsync(status_bits, ws, sizeof(uint32_t), cudaMemcpyDeviceToHost, st));
+    CU_OK(cudaStreamSynchronize(st));
+    return LAPSUM_OK;
+}
+
+int lapsum_experts_forward(const void *x, int64_t x_stride, const void *w_gate_up, const void *w_down, const float *w,
+                           const void *dispatch, size_t dispatch_bytes, void *saved, size_t saved_bytes, void *y,
+                           const lapsum_experts_dims *dims, void *ws, size_t ws_bytes, void *stream)
+{
+    Call c;
+    RUN(begin_call(dims, dispatch, dispatch_bytes, ws, ws_bytes, c));
+    if (dims->tokens == 0) return LAPSUM_OK;
+    if (dims->training && !saved) return LAPSUM_ERR_NULL;
+    if (!dims->training && saved) return LAPSUM_ERR_PARAM;
+    lapsum_experts_layout out;
+    RUN(experts_layout(dims, c.X, &out));
+    if (saved && (!aligned(saved, 256) || saved_bytes < out.saved_bytes)) return LAPSUM_ERR_WORKSPACE;
+    if (x_stride < dims->d || x_stride % 8) return LAPSUM_ERR_SHAPE;
+    if (!x || !w_gate_up || !w_down || !w || !y) return LAPSUM_ERR_NULL;
+    if (!aligned(x, 16) || !aligned(w_gate_up, 16) || !aligned(w_down, 16) || !aligned(y, 16)) return LAPSUM_ERR_ALIGN;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const uint8_t *d = static_cast<const uint8_t *>(dispatch);
+    uint8_t *s = static_cast<uint8_t *>(saved);
+    return dims->io_dtype == LAPSUM_IO_BF16 ? forward_t<__nv_bfloat16>(c, x, x_stride, w_gate_up, w_down, w, d, s, y, st)
+                                            : forward_t<__half>(c, x, x_stride, w_gate_up, w_down, w, d, s, y, st);
+}
+
+int lapsum_experts_backward(const void *grad_y, int64_t grad_y_stride, const void *x, int64_t x_stride, const void *w_gate_up,
+                            const void *w_down, const float *w, const void *dispatch, size_t dispatch_bytes, const void *saved,
+                            size_t saved_bytes, void *grad_x, void *grad_w_gate_up, void *grad_w_down, void *grad_w,
+                            const lapsum_experts_dims *dims, void *ws, size_t ws_bytes, void *stream)
+{
+    Call c;
+    RUN(begin_call(dims, dispatch, dispatch_bytes, ws, ws_bytes, c));
+    if (!dims->training) return LAPSUM_ERR_UNSUPPORTED;
+    if (!grad_w_gate_up || !grad_w_down) return LAPSUM_ERR_NULL;
+    if (!aligned(grad_w_gate_up, 16) || !aligned(grad_w_down, 16)) return LAPSUM_ERR_ALIGN;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dims->tokens == 0) {  // no token: every weight's gradient is zero
+        const size_t bytes = (size_t)dims->experts * (size_t)dims->d * (size_t)dims->f * 2;
+        CU_OK(cudaMemsetAsync(grad_w_gate_up, 0, 2 * bytes, st));
+        CU_OK(cudaMemsetAsync(grad_w_down, 0, bytes, st));
+        return LAPSUM_OK;
+    }
+    lapsum_experts_layout out;
+    RUN(experts_layout(dims, c.X, &out));
+    if (!saved) return LAPSUM_ERR_NULL;
+    if (!aligned(saved, 256) || saved_bytes < out.saved_bytes) return LAPSUM_ERR_WORKSPACE;
+    if (x_stride < dims->d || x_stride % 8 || grad_y_stride < dims->d || grad_y_stride % 8) return LAPSUM_ERR_SHAPE;
+    if (!grad_y || !x || !w_gate_up || !w_down || !w || !grad_x || !grad_w) return LAPSUM_ERR_NULL;
+    if (!aligned(grad_y, 16) || !aligned(x, 16) || !aligned(w_gate_up, 16) || !aligned(w_down, 16) || !aligned(grad_x, 16))
+        return LAPSUM_ERR_ALIGN;
+    const uint8_t *d = static_cast<const uint8_t *>(dispatch), *s = static_cast<const uint8_t *>(saved);
+    return dims->io_dtype == LAPSUM_IO_BF16
+               ? backward_t<__nv_bfloat16>(c, grad_y, grad_y_stride, x, x_stride, w_gate_up, w_down, w, d, s, grad_x, grad_w_gate_up,
+                                           grad_w_down, grad_w, st)
+               : backward_t<__half>(c, grad_y, grad_y_stride, x, x_stride, w_gate_up, w_down, w, d, s, grad_x, grad_w_gate_up, grad_w_down,
+                                    grad_w, st);
+}
+
+int lapsum_debug_experts_timeout(int64_t wait_us, void *ws, size_t ws_bytes, const void *dispatch, size_t dispatch_bytes, const void *x,
+                                 const void *w_gate_up, const float *w, const lapsum_experts_dims *dims, void *stream)
+{
+    Call c;
+    RUN(begin_call(dims, dispatch, dispatch_bytes, ws, ws_bytes, c));
+    if (!x || !w_gate_up || !w) return LAPSUM_ERR_NULL;
+    if (dims->tokens < 1 || dims->training || dims->io_dtype != LAPSUM_IO_BF16) return LAPSUM_ERR_UNSUPPORTED;
+    if (wait_us < 1 || wait_us > 100000) return LAPSUM_ERR_PARAM;
+    if (!aligned(x, 16) || !aligned(w_gate_up, 16)) return LAPSUM_ERR_ALIGN;
+    CUtensorMap a, b;
+    RUN(map_2d(&a, dims->io_dtype, x, dims->d, dims->tokens, dims->d, 1));
+    RUN(map_3d(&b, dims->io_dtype, w_gate_up, dims->d, dims->f, 2 * dims->experts, tile_cols(dims->tile_rows) / 2));
+    ExpertsArgs A = c.A;
+    A.w = w;
+    A.out0 = c.ws + c.X.off_hw;
+    A.wait_ns = (unsigned long long)wait_us * 1000;
+    A.hold = 1;
+    return run_rows<GATE_UP, __nv_bfloat16>(c, a, b, A, dims->f, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

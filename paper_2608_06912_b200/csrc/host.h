@@ -1,0 +1,30 @@
+// Host helpers shared by the library's translation units: launch counting, the thread's last CUDA error, and the
+// launch itself (programmatic stream serialisation, see pdl_wait in common.cuh).
+#pragma once
+#include <cuda_runtime.h>
+
+#include "../../include/lapsum.h"
+
+namespace lapsum {
+
+int cuda_fail(cudaError_t e);  // remembers e for lapsum_last_cuda_error, returns LAPSUM_ERR_CUDA
+int post_launch();             // counts a launch and picks up its error
+
+template <typename... KArgs, typename... Args>
+int launch_pdl(void (*kernel)(KArgs...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, const Args &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+    return e != cudaSuccess ? cuda_fail(e) : post_launch();
+}
+
+}  // namespace lapsum

@@ -14,6 +14,7 @@
 #include "common.cuh"
 #include "bracket_select.cuh"
 #include "global_path.cuh"
+#include "host.h"
 #include "radix_sort.cuh"
 #include "row_block.cuh"
 #include "solve.cuh"
@@ -102,11 +103,15 @@ struct WsHandle {
     WsInfo *W = nullptr;
 };
 
+}  // namespace
+namespace lapsum {
 int cuda_fail(cudaError_t e)
 {
     g_last_cuda = (int)e;
     return LAPSUM_ERR_CUDA;
 }
+}  // namespace lapsum
+namespace {
 #define CU(x)                                   \
     do {                                        \
         cudaError_t e__ = (x);                  \
@@ -235,6 +240,8 @@ int lock_ws(void *ws, WsHandle &h)
     return LAPSUM_OK;
 }
 
+}  // namespace
+namespace lapsum {
 int post_launch()
 {
     g_launches.fetch_add(1, std::memory_order_relaxed);
@@ -242,6 +249,8 @@ int post_launch()
     if (e != cudaSuccess) return cuda_fail(e);
     return LAPSUM_OK;
 }
+}  // namespace lapsum
+namespace {
 int prof_begin(WsInfo &W, int kid, cudaStream_t st);
 void prof_end(WsInfo &W, int slot, cudaStream_t st);
 // launch `...` as kernel `kid` of workspace W on stream st, optionally bracketed by profiling events
@@ -1924,6 +1933,7 @@ const char *lapsum_error_string(int err)
     case LAPSUM_ERR_WORKSPACE: return "workspace unknown, misaligned, too small or built for other dimensions";
     case LAPSUM_ERR_CUDA: return "CUDA runtime error";
     case LAPSUM_ERR_PARAM: return "lapsum_params field out of range";
+    case LAPSUM_ERR_ALIGN: return "a tensor does not start at a multiple of 16 bytes";
     case LAPSUM_ERR_UNSUPPORTED: return "entry point not available for this workspace configuration";
     default: return "unknown error";
     }
