@@ -9,8 +9,7 @@
 //   DW_GATE_UP    dW_gate_up = [dg; du]^T x
 //
 // A block per SM walks over output tiles.  Warp 0 brings operand tiles of 64 along the contraction into a ring of
-// shared-memory stages by TMA (rows of x and dy are gathered by token, four per instruction, so nothing is permuted in
-// memory), one thread of warp 1 issues tcgen05.mma into one of two accumulators in TMEM, warps 4-7 read the other one
+// shared-memory stages by TMA, one thread of warp 1 issues tcgen05.mma into one of two accumulators in TMEM, warps 4-7 read the other one
 // and finish the previous tile.  Operands that the contraction runs along the rows of (W_down in DH, W_gate_up in DX, both
 // sides of the weight gradients) are read as they lie in memory: the tensor core takes them "MN-major".
 //
@@ -178,11 +177,15 @@ __device__ __forceinline__ float sigmoid_fast(float g) { return __fdividef(1.f, 
 // ---------------------------------------------------------------- the kernel ----
 // AR: rows of the A tile that are brought (the slots of a row tile; 128 = M for the weight gradients).  The tensor core
 // always works on M = 128 rows: with AR < 128 it reads the next stages' bytes as rows AR..127, whose results nobody reads.
+// Row tiles up to GATHER_ROWS take their tokens' rows from x by TMA gather, four rows per instruction.  A gather takes about 40
+// cycles whatever the reuse (measured: 32 of them per step of 64 made the first product of 131072 slots 2.43 ms instead of
+// 0.9), so wider tiles read a copy of x in slot order that gather_rows_kernel writes at memory speed.
+constexpr int GATHER_ROWS = 32;
+
 template <int MODE, int AR, int BN>
 struct ExpertsShape {
     static constexpr bool WGRAD = MODE == DW_DOWN || MODE == DW_GATE_UP;
-    static constexpr bool A_GATHER = MODE == GATE_UP || MODE == DH || MODE == DW_DOWN;
-    static constexpr bool B_GATHER = MODE == DW_GATE_UP;
+    static constexpr bool A_GATHER = MODE == GATE_UP && AR <= GATHER_ROWS;
     static constexpr bool A_MN = WGRAD, B_MN = MODE >= DH;
     static constexpr int A_BYTES = AR * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
     static constexpr int STAGES = (196608 / STAGE) < 16 ? (196608 / STAGE) : 16;
@@ -267,7 +270,7 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         for (int64_t i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
             const Tile t = tile_at(i);
             int4 rows = make_int4(0, 0, 0, 0);
-            if constexpr (S::A_GATHER && !S::WGRAD)
+            if constexpr (S::A_GATHER)
                 if (lane < AR / 4) rows = tokens4(t.m0 + 4 * lane);
             for (int kb = 0; kb < t.nkb; ++kb, ++fill) {
                 const uint32_t s = fill % S::STAGES, phase = (fill / S::STAGES) & 1;
@@ -280,16 +283,8 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 const int k0 = kb * 64;
                 if constexpr (S::WGRAD) {
                     const int slot = t.kb + k0;
-                    rows = tokens4(slot + 4 * (lane & 15));  // 16 groups of four slots; the half warps take alternate column chunks
-                    if constexpr (MODE == DW_DOWN) {
-                        tma_gather4(a + (lane >> 4) * 8192 + (lane & 15) * 512, &map_a, t.m0 + (lane >> 4) * 64, rows, bar);
-                        if (lane < BN / 64) tma_load_2d(b + lane * 8192, &map_b, t.n0 + lane * 64, slot, bar);
-                    } else {
-                        if (lane < 2) tma_load_2d(a + lane * 8192, &map_a, t.m0 + lane * 64, slot, bar);
-#pragma unroll
-                        for (int c = lane >> 4; c < BN / 64; c += 2)
-                            tma_gather4(b + c * 8192 + (lane & 15) * 512, &map_b, t.n0 + c * 64, rows, bar);
-                    }
+                    if (lane < 2) tma_load_2d(a + lane * 8192, &map_a, t.m0 + lane * 64, slot, bar);
+                    if (lane >= 2 && lane < 2 + BN / 64) tma_load_2d(b + (lane - 2) * 8192, &map_b, t.n0 + (lane - 2) * 64, slot, bar);
                 } else {
                     if constexpr (S::A_GATHER) {
                         if (lane < AR / 4) tma_gather4(a + lane * 512, &map_a, k0, rows, bar);
@@ -466,6 +461,30 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
 }
 
+// Rows of a matrix in slot order, a warp per slot; holes become zeros.  Bound by memory: it writes 2 D bytes a slot and reads
+// every token's row once from HBM, k - 1 times from L2.
+template <typename T>
+__global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t stride, const int32_t *entry_of, const int32_t *used, T *out,
+                                                             int k, int D)
+{
+    pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t slot = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (slot >= __ldg(used)) return;
+    const int entry = __ldg(entry_of + slot);
+    const uint4 *const from = reinterpret_cast<const uint4 *>(x + (int64_t)(entry < 0 ? 0 : entry / k) * stride);
+    uint4 *const to = reinterpret_cast<uint4 *>(out + slot * D);
+    const int n = D / 8;
+    for (int i = lane; i < n; i += 256) {
+        uint4 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (entry >= 0 && i + 32 * j < n) ? __ldg(from + i + 32 * j) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i + 32 * j < n) to[i + 32 * j] = v[j];
+    }
+}
+
 // y_t = sum over the token's slots, in the order of its choices, eight columns per thread; dropped entries (-1) add nothing.
 // With `partial` also grad_w of the token's entries: the column tiles' sums in order.
 template <typename T>
@@ -480,12 +499,17 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(const T *slots, co
     const int c = (int)(id - t * per);
     float sum[8] = {};
     const int32_t *const at = slot_of + t * k;
-#pragma unroll 4
-    for (int j = 0; j < k; ++j) {
-        const int s = __ldg(at + j);
-        if (s >= 0) {
+    for (int j0 = 0; j0 < k; j0 += 8) {  // eight slots' loads in flight
+        int s[8];
+        uint4 q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = j0 + j < k ? __ldg(at + j0 + j) : -1;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = s[j] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(slots + (int64_t)s[j] * D + 8 * c)) : Io<T>::zero();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
             float v[8];
-            load8(slots + (int64_t)s * D + 8 * c, v);
+            Io<T>::unpack(q[j], v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += v[i];
         }

@@ -98,7 +98,7 @@ int dispatch_layout(int64_t tokens, int32_t k, int64_t experts, int32_t rows, la
     L->off_slot_of = take((size_t)entries);
     L->off_entry_of = take((size_t)L->capacity);
     L->off_tile_expert = take((size_t)L->tiles);
-    L->off_partial = take((size_t)((entries + DISPATCH_CHUNK - 1) / DISPATCH_CHUNK * experts));
+    L->off_partial = take((size_t)((entries + DISPATCH_CHUNK - 1) / DISPATCH_CHUNK * dispatch_stride((int)experts)));
     L->bytes = at;
     return LAPSUM_OK;
 }
@@ -253,6 +253,13 @@ int run_rows(const Call &c, const CUtensorMap &a, const CUtensorMap &b, const Ex
 }
 
 template <typename T>
+int gather(const Call &c, const void *x, int64_t stride, cudaStream_t st)
+{
+    return launch_pdl(experts_gather_kernel<T>, (unsigned)ceil_div(c.X.d.capacity, 8), 256, 0, st, static_cast<const T *>(x), stride,
+                      c.A.entry_of, c.A.offsets + c.A.E, reinterpret_cast<T *>(c.ws + c.X.off_slots), (int)c.p->k, (int)c.p->d);
+}
+
+template <typename T>
 int combine(const Call &c, const uint8_t *dispatch, void *out, int64_t stride, const float *partial, void *grad_w, cudaStream_t st)
 {
     const int64_t work = c.p->tokens * (c.p->d / 8);
@@ -269,7 +276,12 @@ int forward_t(Call &c, const void *x, int64_t x_stride, const void *w_gate_up, c
     const int dt = p.io_dtype, rows = p.tile_rows, cols = tile_cols(rows);
     void *hw = saved ? saved + c.X.off_hw_saved : c.ws + c.X.off_hw;
     CUtensorMap a, b;
-    RUN(map_2d(&a, dt, x, p.d, p.tokens, x_stride, 1));
+    if (rows > GATHER_ROWS) {  // x in slot order, where the second product's result goes later
+        RUN(gather<T>(c, x, x_stride, st));
+        RUN(map_2d(&a, dt, c.ws + c.X.off_slots, p.d, c.X.d.capacity, p.d, rows));
+    } else {
+        RUN(map_2d(&a, dt, x, p.d, p.tokens, x_stride, 1));
+    }
     RUN(map_3d(&b, dt, w_gate_up, p.d, p.f, 2 * p.experts, cols / 2));
     ExpertsArgs A = c.A;
     A.w = w;
@@ -295,31 +307,32 @@ int backward_t(Call &c, const void *grad_y, int64_t gy_stride, const void *x, in
     const uint8_t *hw = saved + c.X.off_hw_saved;
     uint8_t *dgu = c.ws + c.X.off_dgu;
     float *partial = reinterpret_cast<float *>(c.ws + c.X.off_partial);
+    void *rowbuf = c.ws + c.X.off_slots;  // in turn: grad_y in slot order, x in slot order, grad_x per slot
     CUtensorMap a, b;
-    RUN(map_2d(&a, dt, grad_y, p.d, p.tokens, gy_stride, 1));
+    RUN(gather<T>(c, grad_y, gy_stride, st));
+    RUN(map_2d(&a, dt, rowbuf, p.d, cap, p.d, rows));
     RUN(map_3d(&b, dt, w_down, p.f, p.d, p.experts, 64));
     ExpertsArgs A = c.A;
     A.w = w, A.in0 = saved + c.X.off_gu_saved, A.out0 = dgu, A.partial = partial;
     RUN((run_rows<DH, T>(c, a, b, A, p.f, st)));
 
-    // a = grad_y by token, b = w h by slot
+    RUN(map_2d(&a, dt, rowbuf, p.d, cap, p.d, 64));
     RUN(map_2d(&b, dt, hw, p.f, cap, p.f, 64));
     A = c.A;
     A.out0 = grad_w_down;
     RUN((run_experts<DW_DOWN, 128, 256, T>(a, b, A, p.experts * ceil_div(p.d, 128) * ceil_div(p.f, 256), st)));
 
+    RUN(gather<T>(c, x, x_stride, st));
+    RUN(map_2d(&a, dt, dgu, 2 * p.f, cap, 2 * p.f, 64));
+    RUN(map_2d(&b, dt, rowbuf, p.d, cap, p.d, 64));
+    A.out0 = grad_w_gate_up;
+    RUN((run_experts<DW_GATE_UP, 128, 256, T>(a, b, A, p.experts * ceil_div(2 * p.f, 128) * ceil_div(p.d, 256), st)));
+
     RUN(map_2d(&a, dt, dgu, 2 * p.f, cap, 2 * p.f, rows));
     RUN(map_3d(&b, dt, w_gate_up, p.d, 2 * p.f, p.experts, 64));
-    A = c.A;
-    A.out0 = c.ws + c.X.off_slots;
+    A.out0 = rowbuf;
     RUN((run_rows<DX, T>(c, a, b, A, p.d, st)));
-    RUN(combine<T>(c, dispatch, grad_x, p.d, partial, grad_w, st));
-
-    RUN(map_2d(&a, dt, dgu, 2 * p.f, cap, 2 * p.f, 64));
-    RUN(map_2d(&b, dt, x, p.d, p.tokens, x_stride, 1));
-    A = c.A;
-    A.out0 = grad_w_gate_up;
-    return run_experts<DW_GATE_UP, 128, 256, T>(a, b, A, p.experts * ceil_div(2 * p.f, 128) * ceil_div(p.d, 256), st);
+    return combine<T>(c, dispatch, grad_x, p.d, partial, grad_w, st);
 }
 
 }  // namespace
@@ -395,8 +408,9 @@ int lapsum_dispatch(const int32_t *idx, int64_t tokens, int32_t k, int64_t exper
     A.slot_of = reinterpret_cast<int32_t *>(d + L.off_slot_of), A.entry_of = reinterpret_cast<int32_t *>(d + L.off_entry_of);
     A.tile_expert = reinterpret_cast<int32_t *>(d + L.off_tile_expert), A.partial = reinterpret_cast<int32_t *>(d + L.off_partial);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (A.chunks > 1) RUN(launch_pdl(dispatch_count_kernel, (unsigned)A.chunks, DISPATCH_THREADS, 4 * (size_t)experts, st, A));
-    const size_t smem = 4 * ((size_t)(DISPATCH_THREADS / 32 + 3) * (size_t)experts + 1);
+    if (A.chunks > 1) RUN(launch_pdl(dispatch_count_kernel, (unsigned)A.chunks, DISPATCH_THREADS, 4 * (size_t)dispatch_stride((int)experts), st, A));
+    A.shift = tile_rows == 16 ? 4 : tile_rows == 32 ? 5 : tile_rows == 64 ? 6 : 7;
+    const size_t smem = 4 * (size_t)(DISPATCH_THREADS / 32 + 3) * (size_t)dispatch_stride((int)experts) + 16;
     return launch_pdl(dispatch_place_kernel, (unsigned)A.chunks, DISPATCH_THREADS, smem, st, A);
 }
 
@@ -492,7 +506,7 @@ int lapsum_debug_experts_timeout(int64_t wait_us, void *ws, size_t ws_bytes, con
     if (wait_us < 1 || wait_us > 100000) return LAPSUM_ERR_PARAM;
     if (!aligned(x, 16) || !aligned(w_gate_up, 16)) return LAPSUM_ERR_ALIGN;
     CUtensorMap a, b;
-    RUN(map_2d(&a, dims->io_dtype, x, dims->d, dims->tokens, dims->d, 1));
+    RUN(map_2d(&a, dims->io_dtype, x, dims->d, dims->tokens, dims->d, dims->tile_rows > GATHER_ROWS ? dims->tile_rows : 1));
     RUN(map_3d(&b, dims->io_dtype, w_gate_up, dims->d, dims->f, 2 * dims->experts, tile_cols(dims->tile_rows) / 2));
     ExpertsArgs A = c.A;
     A.w = w;

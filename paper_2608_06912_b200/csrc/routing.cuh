@@ -328,11 +328,12 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_backward_kernel(const 
 
 // ------------------------------------------------------------------ dispatch ----
 constexpr int DISPATCH_THREADS = 256, DISPATCH_CHUNK = 4096;  // entries per block; a warp takes 512 neighbours
+__host__ __device__ constexpr int dispatch_stride(int E) { return (E + 3) & ~3; }  // words of one row of counts: 16-byte rows
 
 struct DispatchArgs {
     const int32_t *idx;
     int64_t entries, capacity;
-    int E, rows, chunks, bits;
+    int E, rows, shift, chunks, bits;  // rows = 1 << shift
     int32_t *counts, *offsets, *slot_of, *entry_of, *tile_expert, *partial;
 };
 
@@ -340,67 +341,76 @@ struct DispatchArgs {
 __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_count_kernel(const DispatchArgs A)
 {
     extern __shared__ int32_t dispatch_sh[];
+    const int stride = dispatch_stride(A.E);
+    for (int e = threadIdx.x; e < stride; e += DISPATCH_THREADS) dispatch_sh[e] = 0;
     pdl_wait();
-    for (int e = threadIdx.x; e < A.E; e += DISPATCH_THREADS) dispatch_sh[e] = 0;
     __syncthreads();
     const int64_t begin = (int64_t)blockIdx.x * DISPATCH_CHUNK;
     const int n = (int)min((int64_t)DISPATCH_CHUNK, A.entries - begin);
+#pragma unroll 8
     for (int i = threadIdx.x; i < n; i += DISPATCH_THREADS) {
         const int e = __ldg(A.idx + begin + i);
         if ((unsigned)e < (unsigned)A.E) atomicAdd(dispatch_sh + e, 1);
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < A.E; e += DISPATCH_THREADS) A.partial[(int64_t)blockIdx.x * A.E + e] = dispatch_sh[e];
+    for (int e = threadIdx.x; e < stride; e += DISPATCH_THREADS) A.partial[(int64_t)blockIdx.x * stride + e] = dispatch_sh[e];
 }
 
 // Positions.  Every block sums the chunks' counts itself (chunks x E words from L2: less than another launch), scans the
 // experts' padded lengths, then gives its entries their slots in order: a warp's 32 entries find their equals by ballot.
 __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_place_kernel(const DispatchArgs A)
 {
-    extern __shared__ int32_t dispatch_sh[];
+    extern __shared__ __align__(16) int32_t dispatch_sh[];
     constexpr int W = DISPATCH_THREADS / 32;
-    const int E = A.E;
-    int32_t *const hist = dispatch_sh;         // [W][E]: a warp's entries per expert, then its next slot
-    int32_t *const before = hist + W * E;      // [E]: entries of the chunks before this one
-    int32_t *const count = before + E;         // [E]: entries of all chunks
-    int32_t *const offset = count + E;         // [E + 1]
+    const int E = A.E, stride = dispatch_stride(E);
+    int32_t *const hist = dispatch_sh;          // [W][stride]: a warp's entries per expert, then its next slot
+    int32_t *const before = hist + W * stride;  // [stride]: entries of the chunks before this one
+    int32_t *const count = before + stride;     // [stride]: entries of all chunks
+    int32_t *const offset = count + stride;     // [E + 1]
     __shared__ int32_t scan[W];
-    pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int64_t begin = (int64_t)blockIdx.x * DISPATCH_CHUNK;
-    const int n = (int)min((int64_t)DISPATCH_CHUNK, A.entries - begin);
-    const int per = DISPATCH_CHUNK / W;
-    const int w0 = warp * per, w1 = min(n, w0 + per);
-
-    for (int i = tid; i < W * E; i += DISPATCH_THREADS) hist[i] = 0;
+    for (int i = tid; i < (W + 2) * stride; i += DISPATCH_THREADS) hist[i] = 0;
+    pdl_wait();
     __syncthreads();
+    const int64_t begin = (int64_t)blockIdx.x * DISPATCH_CHUNK;
+    const int n = max(0, (int)min((int64_t)DISPATCH_CHUNK, A.entries - begin));
+    const int per = (n + 32 * W - 1) / (32 * W) * 32;  // entries of a warp: neighbours, so that the order is kept
+    const int w0 = min(n, warp * per), w1 = min(n, w0 + per);
+#pragma unroll 8
     for (int i = w0 + lane; i < w1; i += 32) {
         const int e = __ldg(A.idx + begin + i);
-        if ((unsigned)e < (unsigned)E) atomicAdd(hist + warp * E + e, 1);
-    }
-    __syncthreads();
-    for (int e = tid; e < E; e += DISPATCH_THREADS) {
-        int b = 0, all = 0;
-        if (A.chunks > 1) {
-            for (int c = 0; c < A.chunks; ++c) {
-                const int v = __ldg(A.partial + (int64_t)c * E + e);
-                b += c < (int)blockIdx.x ? v : 0;
-                all += v;
-            }
-        } else {
-            for (int w = 0; w < W; ++w) all += hist[w * E + e];
+        if ((unsigned)e < (unsigned)E) {
+            atomicAdd(hist + warp * stride + e, 1);
+            if (A.chunks == 1) atomicAdd(count + e, 1);
         }
-        before[e] = b;
-        count[e] = all;
+    }
+    if (A.chunks > 1) {  // four experts of one chunk per load
+        const int quads = stride / 4;
+        const int4 *const p = reinterpret_cast<const int4 *>(A.partial);
+#pragma unroll 8
+        for (int i = tid; i < A.chunks * quads; i += DISPATCH_THREADS) {
+            const int4 v = __ldg(p + i);
+            const int c = i / quads, q = 4 * (i - c * quads);
+            int32_t *const all = count + q, *const b = before + q;
+            if (v.x) atomicAdd(all, v.x);
+            if (v.y) atomicAdd(all + 1, v.y);
+            if (v.z) atomicAdd(all + 2, v.z);
+            if (v.w) atomicAdd(all + 3, v.w);
+            if (c < (int)blockIdx.x) {
+                if (v.x) atomicAdd(b, v.x);
+                if (v.y) atomicAdd(b + 1, v.y);
+                if (v.z) atomicAdd(b + 2, v.z);
+                if (v.w) atomicAdd(b + 3, v.w);
+            }
+        }
     }
     __syncthreads();
     // exclusive scan of the padded lengths: a thread takes `own` neighbouring experts
     const int own = (E + DISPATCH_THREADS - 1) / DISPATCH_THREADS;
+    auto padded = [&](int e) { return (count[e] + A.rows - 1) >> A.shift << A.shift; };
     int sum = 0;
-    for (int j = 0; j < own; ++j) {
-        const int e = tid * own + j;
-        if (e < E) sum += (count[e] + A.rows - 1) / A.rows * A.rows;
-    }
+    for (int j = 0; j < own; ++j)
+        if (tid * own + j < E) sum += padded(tid * own + j);
     int run = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -413,20 +423,17 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_place_kernel(const 
     for (int w = 0; w < warp; ++w) base += scan[w];
     for (int j = 0; j < own; ++j) {
         const int e = tid * own + j;
-        if (e < E) {
-            offset[e] = base;
-            base += (count[e] + A.rows - 1) / A.rows * A.rows;
-            if (e == E - 1) offset[E] = base;
-        }
-    }
-    __syncthreads();
-    for (int e = tid; e < E; e += DISPATCH_THREADS) {
-        int next = offset[e] + before[e];
+        if (e >= E) break;
+        offset[e] = base;
+        int next = base + before[e];
+#pragma unroll
         for (int w = 0; w < W; ++w) {
-            const int v = hist[w * E + e];
-            hist[w * E + e] = next;
+            const int v = hist[w * stride + e];
+            hist[w * stride + e] = next;
             next += v;
         }
+        base += padded(e);
+        if (e == E - 1) offset[E] = base;
     }
     __syncthreads();
     for (int i = w0; i < w1; i += 32) {
@@ -442,26 +449,27 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_place_kernel(const 
         }
         const int rank = __popc(peers & ((1u << lane) - 1u));
         int slot = -1;
-        if (there) slot = hist[warp * E + e] + rank;
+        if (there) slot = hist[warp * stride + e] + rank;
         __syncwarp();
-        if (there && rank == 0) hist[warp * E + e] += __popc(peers);
+        if (there && rank == 0) hist[warp * stride + e] += __popc(peers);
         __syncwarp();
         if (at < w1) {
             A.slot_of[begin + at] = slot;
             if (there) A.entry_of[slot] = (int32_t)(begin + at);
         }
     }
-    // the tables' rest: holes of the slots, experts of the row tiles, counts and offsets; the blocks share the experts
-    for (int e = blockIdx.x; e < E; e += gridDim.x) {
-        for (int s = offset[e] + count[e] + tid; s < offset[e + 1]; s += DISPATCH_THREADS) A.entry_of[s] = -1;
-        for (int r = offset[e] / A.rows + tid; r < offset[e + 1] / A.rows; r += DISPATCH_THREADS) A.tile_expert[r] = e;
-        if (tid == 0) A.counts[e] = count[e], A.offsets[e] = offset[e];
+    // the tables' rest: holes of the slots, experts of the row tiles, counts and offsets; a warp per expert
+    for (int e = blockIdx.x * W + warp; e < E; e += gridDim.x * W) {
+        const int lo = offset[e], hi = offset[e + 1], c = count[e];
+        for (int s = lo + c + lane; s < hi; s += 32) A.entry_of[s] = -1;
+        for (int r = (lo >> A.shift) + lane; r < (hi >> A.shift); r += 32) A.tile_expert[r] = e;
+        if (lane == 0) A.counts[e] = c, A.offsets[e] = lo;
     }
-    if (blockIdx.x == 0 && tid == 0) A.offsets[E] = offset[E];
-    for (int64_t s = offset[E] + (int64_t)blockIdx.x * DISPATCH_THREADS + tid; s < A.capacity; s += (int64_t)gridDim.x * DISPATCH_THREADS) {
-        A.entry_of[s] = -1;
-        if (s % A.rows == 0) A.tile_expert[s / A.rows] = -1;
-    }
+    const int all = offset[E];
+    if (blockIdx.x == 0 && tid == 0) A.offsets[E] = all;
+    for (int64_t s = all + (int64_t)blockIdx.x * DISPATCH_THREADS + tid; s < A.capacity; s += (int64_t)gridDim.x * DISPATCH_THREADS) A.entry_of[s] = -1;
+    for (int64_t r = (all >> A.shift) + (int64_t)blockIdx.x * DISPATCH_THREADS + tid; r < (A.capacity >> A.shift); r += (int64_t)gridDim.x * DISPATCH_THREADS)
+        A.tile_expert[r] = -1;
 }
 
 }  // namespace lapsum
