@@ -504,12 +504,12 @@ int lapsum_route_backward(const void *grad_w, const void *logits, int64_t tokens
  * lapsum_dispatch: the tables that bring every expert's tokens side by side.  An "entry" is one choice of one token, number
  * token * k + choice; entries with idx outside [0, experts) are dropped.  A stable counting sort gives the others "slots":
  * expert e owns the slots offsets[e] .. offsets[e] + counts[e] - 1, in the order of the entries; offsets are multiples of
- * tile_rows (16, 32, 64 or 128).  Arrays of the buffer (byte offsets from lapsum_dispatch_describe, all int32):
+ * tile_rows (16, 32, 64, 128 or 256).  Arrays of the buffer (byte offsets from lapsum_dispatch_describe, all int32):
  *   counts[experts], offsets[experts + 1], slot_of[tokens * k] (-1 = dropped), entry_of[capacity] (-1 = hole),
  *   tile_expert[tiles] (expert of the slots tile_rows * i ..., -1 beyond the last).
  * capacity, the slots that a batch may need at most, and so every buffer's size, depends on the shape alone.
  * lapsum_dispatch_tile_rows gives the row tile that lapsum_experts_* is fastest with, from the mean entries per expert;
- * training needs 64 or 128.
+ * training needs 64 or more.
  */
 typedef struct lapsum_dispatch_layout {
     int64_t capacity, tiles;

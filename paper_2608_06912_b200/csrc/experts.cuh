@@ -30,13 +30,11 @@ enum ExpertsMode { GATE_UP = 0, DOWN = 1, DH = 2, DX = 3, DW_DOWN = 4, DW_GATE_U
 struct ExpertsArgs {
     const int32_t *entry_of, *tile_expert, *offsets;
     const float *w;                 // per entry (token, choice)
-    void *out0, *out1;              // per mode, see the epilogues
-    const void *in0;                // DH: the saved [g, u]
     float *partial;                 // DH: per slot and column tile, <dh, h>
     uint32_t *status;
-    int64_t slots;                  // capacity of the slot buffers
     unsigned long long wait_ns;     // bound of every wait
-    int E, D, F, k, tokens, rows;   // rows: slots per row tile
+    int E, D, F, k, tokens;
+    int keep;                       // GATE_UP: store g and u
     int hold;                       // test hook: the producer brings nothing, so the waits run out
 };
 
@@ -50,14 +48,14 @@ __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void mbar_arrive(uint32_t bar)
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)  // a shared::cluster address
 {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
                  : "=r"(ok)
                  : "r"(bar), "r"(parity)
                  : "memory");
@@ -80,6 +78,51 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
     asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
                  "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
                  : "memory");
+}
+// The same by one block of a pair: the bytes are counted by a barrier of the pair's first block (a shared::cluster address).
+__device__ __forceinline__ void tma_pair_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tma_pair_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int x, int y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, uint32_t src, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void tma_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank)  // the address of another block's copy of a shared variable
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // four rows of a matrix, 64 columns each; a row index beyond the matrix reads as zeros
 __device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map, int x, int4 r, uint32_t bar)
@@ -113,15 +156,27 @@ __device__ __forceinline__ void tmem_wait_ld(float (&v)[16])
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(uint32_t bar)
+template <bool PAIR>
+__device__ __forceinline__ void tc_commit(uint32_t bar)  // PAIR: on the barrier of this name in both blocks
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                     "h"((uint16_t)3)
+                     : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+template <bool PAIR>
 __device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a),
-                 "l"(b), "r"(idesc), "r"(accumulate)
-                 : "memory");
+    if constexpr (PAIR)
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+                     "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+                     : "memory");
+    else
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+                     "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+                     : "memory");
 }
 
 // Shared-memory matrix descriptor, 128-byte swizzle.  K-major: rows of 64 elements along the contraction, groups of 8 rows
@@ -175,68 +230,99 @@ __device__ __forceinline__ void load8(const T *p, float *v)
 __device__ __forceinline__ float sigmoid_fast(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
 
 // ---------------------------------------------------------------- the kernel ----
-// AR: rows of the A tile that are brought (the slots of a row tile; 128 = M for the weight gradients).  The tensor core
-// always works on M = 128 rows: with AR < 128 it reads the next stages' bytes as rows AR..127, whose results nobody reads.
 // Row tiles up to GATHER_ROWS take their tokens' rows from x by TMA gather, four rows per instruction.  A gather takes about 40
 // cycles whatever the reuse (measured: 32 of them per step of 64 made the first product of 131072 slots 2.43 ms instead of
-// 0.9), so wider tiles read a copy of x in slot order that gather_rows_kernel writes at memory speed.
+// 0.97), so wider tiles read a copy of x in slot order that experts_gather_kernel writes at memory speed.
 constexpr int GATHER_ROWS = 32;
 
-template <int MODE, int AR, int BN>
+// AR: rows of the row tile (slots), or of the output tile of a weight gradient (128 or 256).
+//   256   a cluster of two blocks works on one 256 x 256 tile (cta_group::2): each block brings 128 rows of A and half of B, and
+//         the tensor cores of both read both halves.  A single block's 128 x 256 tile needs 96 bytes per clock of shared memory
+//         for the operands and another 96 for the copies, more than the 128 there are; the pair needs 64 + 64.
+//   128   one block, M = 128.
+//   < 128 the tensor core still works on M = 128: rows AR..127 are whatever the following stages hold, and nobody reads their
+//         results.  Such tiles are bound by the weights they stream.
+// KS: steps of 64 along the contraction in one stage.  With few rows a stage of several steps lets a row of weights arrive in
+// runs of 128 KS bytes.
+template <int MODE, int AR, int BN, int KS_>
 struct ExpertsShape {
+    static constexpr bool PAIR = AR == 256;
     static constexpr bool WGRAD = MODE == DW_DOWN || MODE == DW_GATE_UP;
     static constexpr bool A_GATHER = MODE == GATE_UP && AR <= GATHER_ROWS;
     static constexpr bool A_MN = WGRAD, B_MN = MODE >= DH;
-    static constexpr int A_BYTES = AR * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
-    static constexpr int STAGES = (196608 / STAGE) < 16 ? (196608 / STAGE) : 16;
-    static constexpr int ACC = 2;                       // accumulators
-    static constexpr int TMEM = ACC * BN < 32 ? 32 : ACC * BN;
+    static constexpr int KS = KS_;
+    static constexpr int ROWS = PAIR ? 128 : AR, COLS = PAIR ? BN / 2 : BN;  // what one block brings of A and B
+    static constexpr int A_SUB = ROWS * 128, B_SUB = COLS * 128;             // bytes of one step
+    static constexpr int A_BYTES = KS * A_SUB, B_BYTES = KS * B_SUB, STAGE = A_BYTES + B_BYTES;
+    static constexpr int SLAB = 4096;                                        // 32 rows x 64 columns of results of one epilogue warp
+    static constexpr int SLABS = MODE == GATE_UP ? 3 : MODE == DH ? 4 : 2;   // per warp
+    static constexpr int FIT = (229376 - 4 * SLABS * SLAB) / STAGE;
+    static constexpr int STAGES = FIT < 12 ? FIT : 12;
+    static constexpr int ACC = 2;  // accumulators: one is finished while the next is computed
+    static constexpr int TMEM = ACC * BN;
     static constexpr int NSTEP = MODE == GATE_UP ? BN / 2 : BN;  // output columns of a tile
+    static constexpr int SMEM = STAGES * STAGE + 4 * SLABS * SLAB + 1024 + 512;
     // the A ring comes first: M = 128 rows read from its last stage stay inside the B ring behind it
-    static constexpr int SMEM = STAGES * STAGE + 1024 + 512;
-    static_assert(STAGES * B_BYTES >= 16384 - A_BYTES, "the A operand's 128 rows must stay inside the allocation");
+    static_assert(STAGES >= 2 && STAGES * B_BYTES >= 16384 - A_SUB && TMEM <= 512 && NSTEP % 64 == 0, "tile does not fit");
 };
 
-template <int MODE, int AR, int BN, typename T>
-__global__ void __launch_bounds__(256, 1)
-experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ExpertsArgs P)
+struct ExpertsMaps {
+    CUtensorMap a, b;    // operands
+    CUtensorMap out;     // results: 64 columns x min(32, AR) rows
+    CUtensorMap gu;      // g and u of a slot as [capacity][2][F]: stored by GATE_UP (training), loaded by DH
+};
+
+template <int MODE, int AR, int BN, int KS, typename T>
+__global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__ ExpertsMaps maps, const ExpertsArgs P)
 {
-    using S = ExpertsShape<MODE, AR, BN>;
+    using S = ExpertsShape<MODE, AR, BN, KS>;
+    constexpr bool PAIR = S::PAIR;
     extern __shared__ uint8_t raw[];
-    const uint32_t raw_at = smem_u32(raw), ring_a = (raw_at + 1023) & ~1023u, ring_b = ring_a + S::STAGES * S::A_BYTES;
-    const uint32_t bars = ring_b + S::STAGES * S::B_BYTES;
-    const uint32_t full = bars, empty = bars + 8 * S::STAGES, acc_full = empty + 8 * S::STAGES, acc_empty = acc_full + 8 * S::ACC,
-                   drain = acc_empty + 8 * S::ACC;
+    const uint32_t ring_a = (smem_u32(raw) + 1023) & ~1023u, ring_b = ring_a + S::STAGES * S::A_BYTES;
+    const uint32_t slabs = ring_b + S::STAGES * S::B_BYTES, bars = slabs + 4 * S::SLABS * S::SLAB;
+    const uint32_t full = bars, empty = full + 8 * S::STAGES, acc_full = empty + 8 * S::STAGES, acc_empty = acc_full + 8 * S::ACC,
+                   drain = acc_empty + 8 * S::ACC, loaded = drain + 8;  // loaded: DH, two per epilogue warp
     __shared__ uint32_t tmem_at;
     __shared__ int abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = PAIR ? cluster_rank() : 0;
 
     if (tid == 0) {
         abort_flag = 0;
         for (int s = 0; s < S::STAGES; ++s) mbar_init(full + 8 * s, 1), mbar_init(empty + 8 * s, 1);
-        for (int a = 0; a < S::ACC; ++a) mbar_init(acc_full + 8 * a, 1), mbar_init(acc_empty + 8 * a, 128);
+        for (int a = 0; a < S::ACC; ++a) mbar_init(acc_full + 8 * a, 1), mbar_init(acc_empty + 8 * a, PAIR ? 8 : 4);
         mbar_init(drain, 1);
+        if constexpr (MODE == DH)
+            for (int i = 0; i < 8; ++i) mbar_init(loaded + 8 * i, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        fence_async_smem();
     }
     if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_at)), "n"(S::TMEM) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_at)), "n"(S::TMEM) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_at)), "n"(S::TMEM) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
         tc_fence_before();
     }
     __syncthreads();
+    if constexpr (PAIR) cluster_barrier();
     tc_fence_after();
     const uint32_t tmem = tmem_at;
     pdl_wait();
 
+    constexpr int MT = PAIR ? 256 : 128;                                           // output rows of a weight gradient's tile
     const int M = MODE == DW_DOWN ? P.D : 2 * P.F;                                 // weight gradients only
     const int N = (MODE == DOWN || MODE == DX || MODE == DW_GATE_UP) ? P.D : P.F;  // output columns
     const int K = (MODE == GATE_UP || MODE == DH) ? P.D : MODE == DOWN ? P.F : 2 * P.F;
-    const int nts = (N + S::NSTEP - 1) / S::NSTEP, mts = S::WGRAD ? (M + 127) / 128 : __ldg(P.offsets + P.E) / P.rows;
+    const int nts = (N + S::NSTEP - 1) / S::NSTEP, mts = S::WGRAD ? (M + MT - 1) / MT : __ldg(P.offsets + P.E) / AR;
     const int64_t tiles = S::WGRAD ? (int64_t)P.E * mts * nts : (int64_t)mts * nts;
+    const int64_t tile0 = PAIR ? blockIdx.x / 2 : blockIdx.x, tile_step = PAIR ? gridDim.x / 2 : gridDim.x;
 
     struct Tile {
-        int e, m0, n0, kb, nkb;  // expert, first slot (or output row), first output column, first slot of the contraction, steps
+        int e, m0, n0, kb, nkb;  // expert, first slot (or output row), first output column, first slot of the contraction, stages
     };
     auto tile_at = [&](int64_t i) {
         Tile t;
@@ -245,58 +331,83 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         t.n0 = nt * S::NSTEP;
         if constexpr (S::WGRAD) {
             t.e = (int)(rest / mts);
-            t.m0 = (int)(rest % mts) * 128;
+            t.m0 = (int)(rest % mts) * MT + (int)rank * 128;
             t.kb = __ldg(P.offsets + t.e);
             t.nkb = (__ldg(P.offsets + t.e + 1) - t.kb) / 64;
         } else {
             t.e = __ldg(P.tile_expert + rest);
-            t.m0 = (int)rest * P.rows;
+            t.m0 = (int)rest * AR + (int)rank * 128;
             t.kb = 0;
-            t.nkb = (K + 63) / 64;
+            t.nkb = (K + 64 * KS - 1) / (64 * KS);  // columns beyond K read as zeros
         }
         return t;
     };
     Waits waits{&abort_flag, P.status, P.wait_ns};
 
     if (warp == 0) {
-        // ------------------------------------------------ producer: all lanes, one gather (four rows) each
+        // ------------------------------------------------ producer
         uint32_t fill = 0;
         bool ok = true;
-        auto tokens4 = [&](int slot) {  // the tokens of four neighbouring slots; holes give a row beyond the matrix
-            const int4 e = __ldg(reinterpret_cast<const int4 *>(P.entry_of + slot));
-            return make_int4(e.x < 0 ? P.tokens : e.x / P.k, e.y < 0 ? P.tokens : e.y / P.k, e.z < 0 ? P.tokens : e.z / P.k,
-                             e.w < 0 ? P.tokens : e.w / P.k);
+        auto load_2d = [&](uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+            if constexpr (PAIR) tma_pair_2d(dst, map, x, y, bar);
+            else tma_load_2d(dst, map, x, y, bar);
         };
-        for (int64_t i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
-            const Tile t = tile_at(i);
-            int4 rows = make_int4(0, 0, 0, 0);
+        auto load_3d = [&](uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+            if constexpr (PAIR) tma_pair_3d(dst, map, x, y, z, bar);
+            else tma_load_3d(dst, map, x, y, z, bar);
+        };
+        // The next tile's expert and tokens are on their way while this tile's copies are issued.
+        Tile next = {};
+        int4 entries = make_int4(0, 0, 0, 0);
+        auto look_ahead = [&](int64_t i) {
+            if (i >= tiles) return;
+            next = tile_at(i);
+            if constexpr (S::A_GATHER)  // four neighbouring slots per lane
+                if (lane < AR / 4) entries = __ldg(reinterpret_cast<const int4 *>(P.entry_of + next.m0 + 4 * lane));
+        };
+        look_ahead(tile0);
+        for (int64_t i = tile0; i < tiles && ok; i += tile_step) {
+            const Tile t = next;
+            int4 rows = make_int4(0, 0, 0, 0);  // their tokens; holes give a row beyond the matrix, which reads as zeros
             if constexpr (S::A_GATHER)
-                if (lane < AR / 4) rows = tokens4(t.m0 + 4 * lane);
+                rows = make_int4(entries.x < 0 ? P.tokens : entries.x / P.k, entries.y < 0 ? P.tokens : entries.y / P.k,
+                                 entries.z < 0 ? P.tokens : entries.z / P.k, entries.w < 0 ? P.tokens : entries.w / P.k);
+            look_ahead(i + tile_step);
             for (int kb = 0; kb < t.nkb; ++kb, ++fill) {
                 const uint32_t s = fill % S::STAGES, phase = (fill / S::STAGES) & 1;
                 ok = waits.wait(empty + 8 * s, phase ^ 1);
                 ok = __all_sync(FULL, ok);
                 if (!ok || P.hold) break;
-                const uint32_t a = ring_a + s * S::A_BYTES, b = ring_b + s * S::B_BYTES, bar = full + 8 * s;
-                if (lane == 0) mbar_expect_tx(bar, S::STAGE);
+                const uint32_t a = ring_a + s * S::A_BYTES, b = ring_b + s * S::B_BYTES;
+                const uint32_t bar = PAIR ? in_block(full + 8 * s, 0) : full + 8 * s;  // the pair's first block counts for both
+                if (lane == 0 && rank == 0) mbar_expect_tx(full + 8 * s, PAIR ? 2 * S::STAGE : S::STAGE);
                 __syncwarp();
-                const int k0 = kb * 64;
                 if constexpr (S::WGRAD) {
-                    const int slot = t.kb + k0;
-                    if (lane < 2) tma_load_2d(a + lane * 8192, &map_a, t.m0 + lane * 64, slot, bar);
-                    if (lane >= 2 && lane < 2 + BN / 64) tma_load_2d(b + (lane - 2) * 8192, &map_b, t.n0 + (lane - 2) * 64, slot, bar);
+                    const int slot = t.kb + kb * 64, n0 = t.n0 + (int)rank * S::COLS;
+                    if (lane < 2) load_2d(a + lane * 8192, &maps.a, t.m0 + lane * 64, slot, bar);
+                    if (lane >= 2 && lane < 2 + S::COLS / 64) load_2d(b + (lane - 2) * 8192, &maps.b, n0 + (lane - 2) * 64, slot, bar);
                 } else {
-                    if constexpr (S::A_GATHER) {
-                        if (lane < AR / 4) tma_gather4(a + lane * 512, &map_a, k0, rows, bar);
-                    } else {
-                        if (lane == 0) tma_load_2d(a, &map_a, k0, t.m0, bar);
-                    }
-                    if constexpr (MODE == GATE_UP) {
-                        if (lane < 2) tma_load_3d(b + lane * (S::B_BYTES / 2), &map_b, k0, t.n0, 2 * t.e + lane, bar);
-                    } else if constexpr (MODE == DOWN) {
-                        if (lane == 0) tma_load_3d(b, &map_b, k0, t.n0, t.e, bar);
-                    } else {
-                        if (lane < BN / 64) tma_load_3d(b + lane * 8192, &map_b, t.n0 + lane * 64, k0, t.e, bar);
+#pragma unroll
+                    for (int q = 0; q < KS; ++q) {
+                        const int k0 = (kb * KS + q) * 64;
+                        const uint32_t aq = a + q * S::A_SUB, bq = b + q * S::B_SUB;
+                        if constexpr (S::A_GATHER) {
+                            if (lane < AR / 4) tma_gather4(aq + lane * 512, &maps.a, k0, rows, bar);
+                        } else {
+                            if (lane == 0) load_2d(aq, &maps.a, k0, t.m0, bar);
+                        }
+                        if constexpr (MODE == GATE_UP) {  // gate rows, then up rows; a pair's blocks bring one kind each
+                            if constexpr (PAIR) {
+                                if (lane == 0) load_3d(bq, &maps.b, k0, t.n0, 2 * t.e + (int)rank, bar);
+                            } else {
+                                if (lane < 2) load_3d(bq + lane * (S::B_SUB / 2), &maps.b, k0, t.n0, 2 * t.e + lane, bar);
+                            }
+                        } else if constexpr (MODE == DOWN) {
+                            if (lane == 0) load_3d(bq, &maps.b, k0, t.n0 + (int)rank * S::COLS, t.e, bar);
+                        } else {
+                            if (lane < S::COLS / 64)
+                                load_3d(bq + lane * 8192, &maps.b, t.n0 + (int)rank * S::COLS + lane * 64, k0, t.e, bar);
+                        }
                     }
                 }
             }
@@ -306,19 +417,19 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const uint32_t first = fill > S::STAGES ? fill - S::STAGES : 0;
         for (uint32_t f = first; f < fill; ++f) {
             const uint32_t s = f % S::STAGES, phase = (f / S::STAGES) & 1;
-            waits.plain(full + 8 * s, phase, false);
+            if (rank == 0) waits.plain(full + 8 * s, phase, false);
             if (ok) waits.wait(empty + 8 * s, phase);
         }
     } else if (warp == 1) {
-        // ------------------------------------------------ one thread issues the products
-        if (lane == 0) {
-            constexpr uint32_t type = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
+        // ------------------------------------------------ one thread issues the products (a pair's: one of its first block)
+        if (lane == 0 && rank == 0) {
+            constexpr uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
             constexpr uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | ((S::A_MN ? 1u : 0u) << 15) |
-                                       ((S::B_MN ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+                                       ((S::B_MN ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
             constexpr uint32_t step_a = S::A_MN ? 2048 : 32, step_b = S::B_MN ? 2048 : 32;  // 16 along the contraction
             uint32_t fill = 0, it = 0;
             bool ok = true, any = false;
-            for (int64_t i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+            for (int64_t i = tile0; i < tiles && ok; i += tile_step) {
                 const Tile t = tile_at(i);
                 if (t.nkb == 0) continue;
                 const uint32_t buf = it % S::ACC, phase = (it / S::ACC) & 1;
@@ -332,132 +443,202 @@ experts_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     ok = waits.wait(full + 8 * s, (fill / S::STAGES) & 1);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint64_t a = smem_desc(ring_a + s * S::A_BYTES, S::A_MN), b = smem_desc(ring_b + s * S::B_BYTES, S::B_MN);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        tc_mma(d, a + q * (step_a >> 4), b + q * (step_b >> 4), idesc, (kb | q) != 0);
+                    for (int h = 0; h < KS; ++h) {
+                        const uint64_t a = smem_desc(ring_a + s * S::A_BYTES + h * S::A_SUB, S::A_MN),
+                                       b = smem_desc(ring_b + s * S::B_BYTES + h * S::B_SUB, S::B_MN);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            tc_mma<PAIR>(d, a + q * (step_a >> 4), b + q * (step_b >> 4), idesc, (kb | h | q) != 0);
+                    }
                     any = true;
-                    tc_commit(empty + 8 * s);
+                    tc_commit<PAIR>(empty + 8 * s);
                 }
-                if (ok) tc_commit(acc_full + 8 * buf);
+                if (ok) tc_commit<PAIR>(acc_full + 8 * buf);
             }
             if (!ok && any) {  // a wait ran out: the products already issued end before the block does
-                tc_commit(drain);
+                tc_commit<PAIR>(drain);
                 waits.plain(drain, 0, false);
             }
         }
     } else if (warp >= 4) {
-        // ------------------------------------------------ epilogue: one accumulator row per thread
-        const int row = tid - 128;
-        const uint32_t lanes = (uint32_t)(warp - 4) << 21;  // 32 TMEM lanes per warp, lane index in the upper half
-        uint32_t it = 0;
+        // ------------------------------------------------ epilogue: one accumulator row per thread, 64 columns at a time.
+        // A warp puts its 32 rows x 64 columns as 16-bit values into a slab of its own (rows of 128 bytes, 16-byte pieces
+        // exchanged by the row's low three bits, as TMA's 128-byte swizzle has it) and stores it with one TMA instruction:
+        // a row per thread written directly costs the load / store unit 32 lines per instruction.
+        const int ew = warp - 4, row = tid - 128;
+        const uint32_t lanes = (uint32_t)ew << 21;  // 32 TMEM lanes per warp, lane index in the upper half
+        const uint32_t slab = slabs + ew * S::SLABS * S::SLAB;
+        const bool live = ew * 32 < S::ROWS, mine = row < S::ROWS;  // live: uniform in the warp
+        auto piece = [&](uint32_t base, int j) { return base + lane * 128 + ((j ^ (lane & 7)) << 4); };  // 8 columns of my row
+        auto put = [&](uint32_t base, int j, const float *v) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = v[i];
+            const uint4 q = Io<T>::pack(x);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece(base, j)), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
+        };
+        auto get = [&](uint32_t base, int j, float *v) {
+            uint4 q;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(piece(base, j)) : "memory");
+            float x[8];
+            Io<T>::unpack(q, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = x[i];
+        };
+        uint32_t it = 0, chunk = 0;  // chunk: slabs used so far (DH: pairs)
         bool ok = true;
-        for (int64_t i = blockIdx.x; i < tiles; i += gridDim.x) {
+        auto bring = [&](const Tile &t, int c, uint32_t q) {  // DH: g and u of 64 columns into pair q & 1
+            const uint32_t at = slab + (q & 1) * 2 * S::SLAB, bar = loaded + 8 * (2 * ew + (q & 1));
+            if (lane == 0) {
+                mbar_expect_tx(bar, 2 * S::SLAB);
+                tma_load_3d(at, &maps.gu, t.n0 + c, 0, t.m0 + 32 * ew, bar);
+                tma_load_3d(at + S::SLAB, &maps.gu, t.n0 + c, 1, t.m0 + 32 * ew, bar);
+            }
+        };
+        for (int64_t i = tile0; i < tiles; i += tile_step) {
             const Tile t = tile_at(i);
             const uint32_t buf = it % S::ACC, phase = (it / S::ACC) & 1;
+            int entry = -1;
+            float w = 0.f, dot = 0.f;
+            if constexpr (MODE == GATE_UP || MODE == DH) {
+                if (mine) entry = __ldg(P.entry_of + t.m0 + row);
+                if (entry >= 0) w = __ldg(P.w + entry);
+            }
+            if constexpr (MODE == DH) {
+                if (live) {
+                    if (lane == 0) tma_store_wait_read<0>();
+                    __syncwarp();
+                    bring(t, 0, chunk);
+                }
+            }
             if (t.nkb > 0) {
                 ++it;
                 ok = waits.wait(acc_full + 8 * buf, phase);
-                if (!__all_sync(FULL, ok)) break;
+                if (!__all_sync(FULL, ok)) {
+                    if (MODE == DH && live) waits.plain(loaded + 8 * (2 * ew + (chunk & 1)), (chunk >> 1) & 1, false);  // the copy in flight
+                    break;
+                }
                 tc_fence_after();
             }
             const uint32_t d = tmem + buf * BN + lanes;
-            const bool live = (warp - 4) * 32 < (S::WGRAD ? min(128, M - t.m0) : AR);  // uniform in the warp
-            if (live) {
-                const bool mine = S::WGRAD ? t.m0 + row < M : row < AR;
-                const int64_t slot = t.m0 + row;  // row modes
-                if constexpr (MODE == GATE_UP) {
-                    const int entry = mine ? __ldg(P.entry_of + slot) : -1;
-                    const float w = entry >= 0 ? __ldg(P.w + entry) : 0.f;
-                    T *const hw = reinterpret_cast<T *>(P.out0) + slot * P.F;
-                    T *const gu = P.out1 ? reinterpret_cast<T *>(P.out1) + slot * 2 * P.F : nullptr;
+            if (live && (!S::WGRAD || t.m0 + 32 * ew < M)) {
 #pragma unroll 1
-                    for (int c = 0; c < BN / 2 && t.n0 + c < P.F; c += 16) {
-                        float g[16], u[16], h[16];
-                        tmem_ld16(d + c, g);
-                        tmem_ld16(d + BN / 2 + c, u);
-                        tmem_wait_ld(g);
-                        tmem_pin(u);
+                for (int c = 0; c < S::NSTEP && t.n0 + c < N; c += 64, ++chunk) {
+                    if constexpr (MODE == GATE_UP) {
+                        // slabs: w h, g, u
+                        if (lane == 0) tma_store_wait_read<0>();
+                        __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) h[j] = entry >= 0 ? w * (g[j] * sigmoid_fast(g[j]) * u[j]) : 0.f;
-                        if (mine) {
+                        for (int j = 0; j < 64 && c + j < S::NSTEP; j += 16) {
+                            float g[16], u[16], h[16];
+                            tmem_ld16(d + c + j, g);
+                            tmem_ld16(d + BN / 2 + c + j, u);
+                            tmem_wait_ld(g);
+                            tmem_pin(u);
 #pragma unroll
-                            for (int j = 0; j < 16; j += 8) {
-                                const int f = t.n0 + c + j;
-                                if (f < P.F) {
-                                    store8(hw + f, h + j);
-                                    if (gu && entry >= 0) store8(gu + f, g + j), store8(gu + P.F + f, u + j);
+                            for (int v = 0; v < 16; ++v) h[v] = entry >= 0 ? w * (g[v] * sigmoid_fast(g[v]) * u[v]) : 0.f;
+                            if (mine) {
+                                put(slab, j / 8, h), put(slab, j / 8 + 1, h + 8);
+                                if (P.keep) {
+                                    put(slab + S::SLAB, j / 8, g), put(slab + S::SLAB, j / 8 + 1, g + 8);
+                                    put(slab + 2 * S::SLAB, j / 8, u), put(slab + 2 * S::SLAB, j / 8 + 1, u + 8);
                                 }
                             }
                         }
-                    }
-                } else if constexpr (MODE == DH) {
-                    const int entry = mine ? __ldg(P.entry_of + slot) : -1;
-                    const float w = entry >= 0 ? __ldg(P.w + entry) : 0.f;
-                    const T *const gu = reinterpret_cast<const T *>(P.in0) + slot * 2 * P.F;
-                    T *const dgu = reinterpret_cast<T *>(P.out0) + slot * 2 * P.F;
-                    float dot = 0.f;
-#pragma unroll 1
-                    for (int c = 0; c < BN && t.n0 + c < P.F; c += 16) {
-                        float dh[16];
-                        tmem_ld16(d + c, dh);
-                        tmem_wait_ld(dh);
-                        if (mine) {
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tma_store_2d(&maps.out, slab, t.n0 + c, t.m0 + 32 * ew);
+                            if (P.keep) {
+                                tma_store_3d(&maps.gu, slab + S::SLAB, t.n0 + c, 0, t.m0 + 32 * ew);
+                                tma_store_3d(&maps.gu, slab + 2 * S::SLAB, t.n0 + c, 1, t.m0 + 32 * ew);
+                            }
+                            tma_store_commit();
+                        }
+                    } else if constexpr (MODE == DH) {
+                        // the pair of slabs holds g and u and takes dg and du in their place; the other pair is filled meanwhile
+                        const uint32_t at = slab + (chunk & 1) * 2 * S::SLAB;
+                        if (c + 64 < S::NSTEP && t.n0 + c + 64 < N) {
+                            if (lane == 0) tma_store_wait_read<0>();
+                            __syncwarp();
+                            bring(t, c + 64, chunk + 1);
+                        }
+                        ok = waits.wait(loaded + 8 * (2 * ew + (chunk & 1)), (chunk >> 1) & 1);
 #pragma unroll
-                            for (int j = 0; j < 16; j += 8) {
-                                const int f = t.n0 + c + j;
-                                if (f < P.F) {
-                                    float g[8] = {}, u[8] = {};
-                                    if (entry >= 0) {  // a hole's gradients are zeros whatever the weights hold
-                                        load8(gu + f, g);
-                                        load8(gu + P.F + f, u);
+                        for (int j = 0; j < 64; j += 16) {
+                            float dh[16];
+                            tmem_ld16(d + c + j, dh);
+                            tmem_wait_ld(dh);
 #pragma unroll
-                                        for (int v = 0; v < 8; ++v) {
-                                            const float s = sigmoid_fast(g[v]), a = g[v] * s, x = dh[j + v], xw = x * w;
-                                            dot += x * a * u[v];
-                                            g[v] = xw * u[v] * (s + a * (1.f - s));
-                                            u[v] = xw * a;
-                                        }
-                                    }
-                                    store8(dgu + f, g);
-                                    store8(dgu + P.F + f, u);
+                            for (int p = 0; p < 2; ++p) {
+                                float g[8], u[8];
+                                get(at, j / 8 + p, g);
+                                get(at + S::SLAB, j / 8 + p, u);
+                                // a hole's gradients are zeros whatever the weights and the buffers hold; so are columns beyond F
+                                const bool real = entry >= 0 && t.n0 + c + j + 8 * p < N;
+#pragma unroll
+                                for (int v = 0; v < 8; ++v) {
+                                    const float s = sigmoid_fast(g[v]), a = g[v] * s, x = dh[8 * p + v], xw = x * w, uv = u[v];
+                                    dot += real ? x * a * uv : 0.f;
+                                    g[v] = real ? xw * uv * (s + a * (1.f - s)) : 0.f;
+                                    u[v] = real ? xw * a : 0.f;
                                 }
+                                put(at, j / 8 + p, g);
+                                put(at + S::SLAB, j / 8 + p, u);
                             }
                         }
-                    }
-                    if (mine) P.partial[slot * nts + t.n0 / S::NSTEP] = dot;
-                } else {
-                    T *const out = S::WGRAD ? reinterpret_cast<T *>(P.out0) + ((int64_t)t.e * M + slot) * N
-                                            : reinterpret_cast<T *>(P.out0) + slot * N;
-#pragma unroll 1
-                    for (int c = 0; c < BN && t.n0 + c < N; c += 16) {
-                        float v[16];
-                        if (t.nkb > 0) {
-                            tmem_ld16(d + c, v);
-                            tmem_wait_ld(v);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) v[j] = 0.f;
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            tma_store_3d(&maps.out, at, t.n0 + c, 0, t.m0 + 32 * ew);
+                            tma_store_3d(&maps.out, at + S::SLAB, t.n0 + c, 1, t.m0 + 32 * ew);
+                            tma_store_commit();
                         }
-                        if (mine) {
+                    } else {
+                        const uint32_t at = slab + (chunk & 1) * S::SLAB;
+                        if (lane == 0) tma_store_wait_read<1>();
+                        __syncwarp();
 #pragma unroll
-                            for (int j = 0; j < 16; j += 8)
-                                if (t.n0 + c + j < N) store8(out + t.n0 + c + j, v + j);
+                        for (int j = 0; j < 64; j += 16) {
+                            float v[16];
+                            if (t.nkb > 0) {
+                                tmem_ld16(d + c + j, v);
+                                tmem_wait_ld(v);
+                            } else {  // an expert without tokens
+#pragma unroll
+                                for (int q = 0; q < 16; ++q) v[q] = 0.f;
+                            }
+                            if (mine) put(at, j / 8, v), put(at, j / 8 + 1, v + 8);
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if constexpr (S::WGRAD) tma_store_3d(&maps.out, at, t.n0 + c, t.m0 + 32 * ew, t.e);
+                            else tma_store_2d(&maps.out, at, t.n0 + c, t.m0 + 32 * ew);
+                            tma_store_commit();
                         }
                     }
                 }
             }
+            if (MODE == DH && mine) P.partial[(int64_t)(t.m0 + row) * nts + t.n0 / S::NSTEP] = dot;
             if (t.nkb > 0) {
                 tc_fence_before();
-                mbar_arrive(acc_empty + 8 * buf);
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(PAIR ? in_block(acc_empty + 8 * buf, 0) : acc_empty + 8 * buf);
             }
         }
+        if (lane == 0) tma_store_wait_all();
     }
     __syncwarp();
     __syncthreads();
+    if constexpr (PAIR) cluster_barrier();
     if (warp == 2) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::TMEM) : "memory");
+        if constexpr (PAIR)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::TMEM) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::TMEM) : "memory");
     }
 }
 

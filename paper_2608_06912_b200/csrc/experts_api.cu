@@ -81,7 +81,7 @@ int route_backward_t(const RouteBackArgs &A, cudaStream_t st)
 int dispatch_layout(int64_t tokens, int32_t k, int64_t experts, int32_t rows, lapsum_dispatch_layout *L)
 {
     if (tokens < 0 || k < 1 || k > ROUTE_MAX_K || experts < 1 || experts > ROUTE_MAX_E) return LAPSUM_ERR_SHAPE;
-    if (rows != 16 && rows != 32 && rows != 64 && rows != 128) return LAPSUM_ERR_PARAM;
+    if (rows != 16 && rows != 32 && rows != 64 && rows != 128 && rows != 256) return LAPSUM_ERR_PARAM;
     if (tokens > ((int64_t)1 << 30) / k) return LAPSUM_ERR_SHAPE;
     const int64_t entries = tokens * k;
     const int64_t used = entries < experts ? entries : experts;
@@ -107,12 +107,19 @@ int dispatch_layout(int64_t tokens, int32_t k, int64_t experts, int32_t rows, la
 struct ExpertsLayout {
     lapsum_dispatch_layout d;
     size_t off_slots, off_hw, off_dgu, off_partial, off_gu_saved, off_hw_saved;
-    int nts_dh;
+    int nts_dh;    // column tiles of DH
+    bool wide_dh;  // of 256 columns
 };
 
-// Columns of an output tile: 256 keep the tensor core fed from shared memory; with 64 or fewer rows a tile is bound by the
-// weights it streams, and narrower tiles give more blocks and a deeper ring.
-constexpr int tile_cols(int rows) { return rows == 128 ? 256 : rows == 64 ? 128 : 64; }
+// Columns of an output tile: 256, the most that two accumulators in TMEM allow; 128 for narrow row tiles where 256 would leave
+// SMs without work (fewer than two tiles for each).  Measured, bf16 / fp16: 48 tokens on 128 experts 210 us with 256 columns and
+// 215 us with 128, one token on 8 experts 43 us and 35 us.
+constexpr int MIN_TILES = 2 * 148;
+inline bool wide_tiles(const lapsum_experts_dims *p, const lapsum_dispatch_layout &d, int64_t cols, bool gate_up)
+{
+    const int step = gate_up ? 128 : 256;
+    return p->tile_rows >= 128 || d.tiles * ((cols + step - 1) / step) >= MIN_TILES;
+}
 
 int experts_layout(const lapsum_experts_dims *p, ExpertsLayout &X, lapsum_experts_layout *out)
 {
@@ -123,7 +130,8 @@ int experts_layout(const lapsum_experts_dims *p, ExpertsLayout &X, lapsum_expert
     RUN(dispatch_layout(p->tokens, p->k, p->experts, p->tile_rows, &X.d));
     if (p->training && p->tile_rows < 64) return LAPSUM_ERR_PARAM;
     const size_t cap = (size_t)X.d.capacity, D = (size_t)p->d, F = (size_t)p->f;
-    X.nts_dh = (int)((p->f + tile_cols(p->tile_rows) - 1) / tile_cols(p->tile_rows));
+    X.wide_dh = wide_tiles(p, X.d, p->f, false);
+    X.nts_dh = (int)((p->f + (X.wide_dh ? 255 : 127)) / (X.wide_dh ? 256 : 128));
     size_t at = 256;  // control block: the status word
     X.off_slots = at, at += align_up(cap * D * 2);
     X.off_hw = at, at += p->training ? 0 : align_up(cap * F * 2);
@@ -179,6 +187,14 @@ int map_3d(CUtensorMap *m, int dtype, const void *base, int64_t cols, int64_t ro
     return tensor_map(m, dtype, base, 3, d, s, b);
 }
 
+// [slots][2][F]: g and u, or their gradients, 64 columns of one of the two
+int map_gu(CUtensorMap *m, int dtype, const void *base, int64_t f, int64_t slots, int box_rows)
+{
+    const int64_t d[3] = {f, 2, slots}, s[2] = {f, 2 * f};
+    const int b[3] = {64, 1, box_rows};
+    return tensor_map(m, dtype, base, 3, d, s, b);
+}
+
 int sm_count(int *n)
 {
     static thread_local int dev_known = -1, sms = 0;
@@ -192,20 +208,21 @@ int sm_count(int *n)
     return LAPSUM_OK;
 }
 
-template <int MODE, int AR, int BN, typename T>
-int run_experts(const CUtensorMap &a, const CUtensorMap &b, const ExpertsArgs &P, int64_t tiles_max, cudaStream_t st)
+template <int MODE, int AR, int BN, int KS, typename T>
+int run_experts(const ExpertsMaps &maps, const ExpertsArgs &P, int64_t tiles_max, cudaStream_t st)
 {
-    using S = ExpertsShape<MODE, AR, BN>;
+    using S = ExpertsShape<MODE, AR, BN, KS>;
     static thread_local int dev_ready = -1;  // the attribute belongs to the device's context
     int dev = 0, sms = 0;
     CU_OK(cudaGetDevice(&dev));
     RUN(sm_count(&sms));
+    const auto kernel = experts_kernel<MODE, AR, BN, KS, T>;
     if (dev != dev_ready) {
-        CU_OK(cudaFuncSetAttribute(experts_kernel<MODE, AR, BN, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
+        CU_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
         dev_ready = dev;
     }
-    const unsigned grid = (unsigned)(tiles_max < sms ? (tiles_max < 1 ? 1 : tiles_max) : sms);
-    return launch_pdl(experts_kernel<MODE, AR, BN, T>, grid, 256, S::SMEM, st, a, b, P);
+    const int64_t units = S::PAIR ? sms / 2 : sms, n = tiles_max < 1 ? 1 : tiles_max < units ? tiles_max : units;
+    return launch_clusters(S::PAIR ? 2 : 1, kernel, (unsigned)(S::PAIR ? 2 * n : n), 256, S::SMEM, st, maps, P);
 }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -232,24 +249,38 @@ int begin_call(const lapsum_experts_dims *p, const void *dispatch, size_t dispat
     c.A.tile_expert = reinterpret_cast<const int32_t *>(d + c.X.d.off_tile_expert);
     c.A.offsets = reinterpret_cast<const int32_t *>(d + c.X.d.off_offsets);
     c.A.status = reinterpret_cast<uint32_t *>(ws);
-    c.A.slots = c.X.d.capacity;
     c.A.wait_ns = 2000000000ull;
-    c.A.E = (int)p->experts, c.A.D = (int)p->d, c.A.F = (int)p->f, c.A.k = p->k, c.A.tokens = (int)p->tokens, c.A.rows = p->tile_rows;
+    c.A.E = (int)p->experts, c.A.D = (int)p->d, c.A.F = (int)p->f, c.A.k = p->k, c.A.tokens = (int)p->tokens;
     return LAPSUM_OK;
 }
 
+// One of the four products whose rows are slots
 template <int MODE, typename T>
-int run_rows(const Call &c, const CUtensorMap &a, const CUtensorMap &b, const ExpertsArgs &P, int64_t cols, cudaStream_t st)
+int run_rows(const Call &c, const ExpertsMaps &maps, const ExpertsArgs &P, int64_t cols, bool wide, cudaStream_t st)
 {
-    const int rows = c.p->tile_rows, step = MODE == GATE_UP ? tile_cols(rows) / 2 : tile_cols(rows);
+    constexpr bool BACK = MODE == DH || MODE == DX;
+    const int step = (wide ? 256 : 128) / (MODE == GATE_UP ? 2 : 1);
     const int64_t tiles = c.X.d.tiles * ceil_div(cols, step);
-    if (rows == 128) return run_experts<MODE, 128, tile_cols(128), T>(a, b, P, tiles, st);
-    if (rows == 64) return run_experts<MODE, 64, tile_cols(64), T>(a, b, P, tiles, st);
-    if constexpr (MODE == GATE_UP || MODE == DOWN) {
-        if (rows == 32) return run_experts<MODE, 32, tile_cols(32), T>(a, b, P, tiles, st);
-        return run_experts<MODE, 16, tile_cols(16), T>(a, b, P, tiles, st);
+    switch (c.p->tile_rows) {
+    case 256: return run_experts<MODE, 256, 256, 1, T>(maps, P, tiles, st);
+    case 128: return run_experts<MODE, 128, 256, 1, T>(maps, P, tiles, st);
+    case 64: return wide ? run_experts<MODE, 64, 256, 1, T>(maps, P, tiles, st) : run_experts<MODE, 64, 128, 2, T>(maps, P, tiles, st);
+    default: break;
+    }
+    if constexpr (!BACK) {
+        if (c.p->tile_rows == 32)
+            return wide ? run_experts<MODE, 32, 256, 1, T>(maps, P, tiles, st) : run_experts<MODE, 32, 128, 2, T>(maps, P, tiles, st);
+        if (c.p->tile_rows == 16)
+            return wide ? run_experts<MODE, 16, 256, 1, T>(maps, P, tiles, st) : run_experts<MODE, 16, 128, 2, T>(maps, P, tiles, st);
     }
     return LAPSUM_ERR_PARAM;
+}
+template <int MODE, typename T>
+int run_weights(const Call &c, const ExpertsMaps &maps, int64_t m, int64_t n, cudaStream_t st)
+{
+    if (c.p->tile_rows == 256)
+        return run_experts<MODE, 256, 256, 1, T>(maps, c.A, c.p->experts * ceil_div(m, 256) * ceil_div(n, 256), st);
+    return run_experts<MODE, 128, 256, 1, T>(maps, c.A, c.p->experts * ceil_div(m, 128) * ceil_div(n, 256), st);
 }
 
 template <typename T>
@@ -270,29 +301,38 @@ int combine(const Call &c, const uint8_t *dispatch, void *out, int64_t stride, c
 
 template <typename T>
 int forward_t(Call &c, const void *x, int64_t x_stride, const void *w_gate_up, const void *w_down, const float *w, const uint8_t *dispatch,
-              uint8_t *saved, void *y, cudaStream_t st)
+              uint8_t *saved, void *y, int hold, cudaStream_t st)
 {
     const lapsum_experts_dims &p = *c.p;
-    const int dt = p.io_dtype, rows = p.tile_rows, cols = tile_cols(rows);
+    const int dt = p.io_dtype, rows = p.tile_rows < 128 ? p.tile_rows : 128, out_rows = rows < 32 ? rows : 32;
+    const int64_t cap = c.X.d.capacity;
+    const bool pair = p.tile_rows == 256;
+    uint8_t *rowbuf = c.ws + c.X.off_slots;  // in turn: x in slot order, the second product's results
     void *hw = saved ? saved + c.X.off_hw_saved : c.ws + c.X.off_hw;
-    CUtensorMap a, b;
-    if (rows > GATHER_ROWS) {  // x in slot order, where the second product's result goes later
-        RUN(gather<T>(c, x, x_stride, st));
-        RUN(map_2d(&a, dt, c.ws + c.X.off_slots, p.d, c.X.d.capacity, p.d, rows));
+    ExpertsMaps m;
+    if (rows > GATHER_ROWS) {
+        if (!hold) RUN(gather<T>(c, x, x_stride, st));
+        RUN(map_2d(&m.a, dt, rowbuf, p.d, cap, p.d, rows));
     } else {
-        RUN(map_2d(&a, dt, x, p.d, p.tokens, x_stride, 1));
+        RUN(map_2d(&m.a, dt, x, p.d, p.tokens, x_stride, 1));
     }
-    RUN(map_3d(&b, dt, w_gate_up, p.d, p.f, 2 * p.experts, cols / 2));
+    bool wide = wide_tiles(&p, c.X.d, p.f, true);
+    RUN(map_3d(&m.b, dt, w_gate_up, p.d, p.f, 2 * p.experts, wide ? 128 : 64));
+    RUN(map_2d(&m.out, dt, hw, p.f, cap, p.f, out_rows));
+    if (saved) RUN(map_gu(&m.gu, dt, saved + c.X.off_gu_saved, p.f, cap, out_rows));
+    else m.gu = m.out;  // not used
     ExpertsArgs A = c.A;
     A.w = w;
-    A.out0 = hw;
-    A.out1 = saved ? saved + c.X.off_gu_saved : nullptr;
-    RUN((run_rows<GATE_UP, T>(c, a, b, A, p.f, st)));
-    RUN(map_2d(&a, dt, hw, p.f, c.X.d.capacity, p.f, rows));
-    RUN(map_3d(&b, dt, w_down, p.f, p.d, p.experts, cols));
-    A = c.A;
-    A.out0 = c.ws + c.X.off_slots;
-    RUN((run_rows<DOWN, T>(c, a, b, A, p.d, st)));
+    A.keep = saved != nullptr;
+    A.hold = hold;
+    RUN((run_rows<GATE_UP, T>(c, m, A, p.f, wide, st)));
+    if (hold) return LAPSUM_OK;
+
+    wide = wide_tiles(&p, c.X.d, p.d, false);
+    RUN(map_2d(&m.a, dt, hw, p.f, cap, p.f, rows));
+    RUN(map_3d(&m.b, dt, w_down, p.f, p.d, p.experts, wide && !pair ? 256 : 128));
+    RUN(map_2d(&m.out, dt, rowbuf, p.d, cap, p.d, out_rows));
+    RUN((run_rows<DOWN, T>(c, m, c.A, p.d, wide, st)));
     return combine<T>(c, dispatch, y, p.d, nullptr, nullptr, st);
 }
 
@@ -302,36 +342,37 @@ int backward_t(Call &c, const void *grad_y, int64_t gy_stride, const void *x, in
                void *grad_w, cudaStream_t st)
 {
     const lapsum_experts_dims &p = *c.p;
-    const int dt = p.io_dtype, rows = p.tile_rows;
+    const int dt = p.io_dtype, rows = p.tile_rows < 128 ? p.tile_rows : 128;
     const int64_t cap = c.X.d.capacity;
     const uint8_t *hw = saved + c.X.off_hw_saved;
     uint8_t *dgu = c.ws + c.X.off_dgu;
     float *partial = reinterpret_cast<float *>(c.ws + c.X.off_partial);
     void *rowbuf = c.ws + c.X.off_slots;  // in turn: grad_y in slot order, x in slot order, grad_x per slot
-    CUtensorMap a, b;
+    ExpertsMaps m;
     RUN(gather<T>(c, grad_y, gy_stride, st));
-    RUN(map_2d(&a, dt, rowbuf, p.d, cap, p.d, rows));
-    RUN(map_3d(&b, dt, w_down, p.f, p.d, p.experts, 64));
+    RUN(map_2d(&m.a, dt, rowbuf, p.d, cap, p.d, rows));
+    RUN(map_3d(&m.b, dt, w_down, p.f, p.d, p.experts, 64));
+    RUN(map_gu(&m.out, dt, dgu, p.f, cap, 32));
+    RUN(map_gu(&m.gu, dt, saved + c.X.off_gu_saved, p.f, cap, 32));
     ExpertsArgs A = c.A;
-    A.w = w, A.in0 = saved + c.X.off_gu_saved, A.out0 = dgu, A.partial = partial;
-    RUN((run_rows<DH, T>(c, a, b, A, p.f, st)));
+    A.w = w, A.partial = partial;
+    RUN((run_rows<DH, T>(c, m, A, p.f, c.X.wide_dh, st)));
 
-    RUN(map_2d(&a, dt, rowbuf, p.d, cap, p.d, 64));
-    RUN(map_2d(&b, dt, hw, p.f, cap, p.f, 64));
-    A = c.A;
-    A.out0 = grad_w_down;
-    RUN((run_experts<DW_DOWN, 128, 256, T>(a, b, A, p.experts * ceil_div(p.d, 128) * ceil_div(p.f, 256), st)));
+    RUN(map_2d(&m.a, dt, rowbuf, p.d, cap, p.d, 64));
+    RUN(map_2d(&m.b, dt, hw, p.f, cap, p.f, 64));
+    RUN(map_3d(&m.out, dt, grad_w_down, p.f, p.d, p.experts, 32));
+    RUN((run_weights<DW_DOWN, T>(c, m, p.d, p.f, st)));
 
     RUN(gather<T>(c, x, x_stride, st));
-    RUN(map_2d(&a, dt, dgu, 2 * p.f, cap, 2 * p.f, 64));
-    RUN(map_2d(&b, dt, rowbuf, p.d, cap, p.d, 64));
-    A.out0 = grad_w_gate_up;
-    RUN((run_experts<DW_GATE_UP, 128, 256, T>(a, b, A, p.experts * ceil_div(2 * p.f, 128) * ceil_div(p.d, 256), st)));
+    RUN(map_2d(&m.a, dt, dgu, 2 * p.f, cap, 2 * p.f, 64));
+    RUN(map_2d(&m.b, dt, rowbuf, p.d, cap, p.d, 64));
+    RUN(map_3d(&m.out, dt, grad_w_gate_up, p.d, 2 * p.f, p.experts, 32));
+    RUN((run_weights<DW_GATE_UP, T>(c, m, 2 * p.f, p.d, st)));
 
-    RUN(map_2d(&a, dt, dgu, 2 * p.f, cap, 2 * p.f, rows));
-    RUN(map_3d(&b, dt, w_gate_up, p.d, 2 * p.f, p.experts, 64));
-    A.out0 = rowbuf;
-    RUN((run_rows<DX, T>(c, a, b, A, p.d, st)));
+    RUN(map_2d(&m.a, dt, dgu, 2 * p.f, cap, 2 * p.f, rows));
+    RUN(map_3d(&m.b, dt, w_gate_up, p.d, 2 * p.f, p.experts, 64));
+    RUN(map_2d(&m.out, dt, rowbuf, p.d, cap, p.d, 32));
+    RUN((run_rows<DX, T>(c, m, c.A, p.d, wide_tiles(&p, c.X.d, p.d, false), st)));
     return combine<T>(c, dispatch, grad_x, p.d, partial, grad_w, st);
 }
 
@@ -378,7 +419,7 @@ int lapsum_dispatch_tile_rows(int64_t tokens, int32_t k, int64_t experts, int32_
     if (!rows) return LAPSUM_ERR_NULL;
     if (tokens < 0 || k < 1 || k > ROUTE_MAX_K || experts < 1 || experts > ROUTE_MAX_E) return LAPSUM_ERR_SHAPE;
     const double mean = (double)tokens * k / (double)experts;  // entries per expert
-    *rows = mean > 48 ? 128 : mean > 24 || training ? 64 : mean > 8 ? 32 : 16;
+    *rows = mean > 384 ? 256 : mean > 48 ? 128 : mean > 24 || training ? 64 : mean > 8 ? 32 : 16;
     return LAPSUM_OK;
 }
 
@@ -409,7 +450,8 @@ int lapsum_dispatch(const int32_t *idx, int64_t tokens, int32_t k, int64_t exper
     A.tile_expert = reinterpret_cast<int32_t *>(d + L.off_tile_expert), A.partial = reinterpret_cast<int32_t *>(d + L.off_partial);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (A.chunks > 1) RUN(launch_pdl(dispatch_count_kernel, (unsigned)A.chunks, DISPATCH_THREADS, 4 * (size_t)dispatch_stride((int)experts), st, A));
-    A.shift = tile_rows == 16 ? 4 : tile_rows == 32 ? 5 : tile_rows == 64 ? 6 : 7;
+    A.shift = 4;
+    while ((1 << A.shift) < tile_rows) ++A.shift;
     const size_t smem = 4 * (size_t)(DISPATCH_THREADS / 32 + 3) * (size_t)dispatch_stride((int)experts) + 16;
     return launch_pdl(dispatch_place_kernel, (unsigned)A.chunks, DISPATCH_THREADS, smem, st, A);
 }
@@ -459,8 +501,8 @@ int lapsum_experts_forward(const void *x, int64_t x_stride, const void *w_gate_u
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     const uint8_t *d = static_cast<const uint8_t *>(dispatch);
     uint8_t *s = static_cast<uint8_t *>(saved);
-    return dims->io_dtype == LAPSUM_IO_BF16 ? forward_t<__nv_bfloat16>(c, x, x_stride, w_gate_up, w_down, w, d, s, y, st)
-                                            : forward_t<__half>(c, x, x_stride, w_gate_up, w_down, w, d, s, y, st);
+    return dims->io_dtype == LAPSUM_IO_BF16 ? forward_t<__nv_bfloat16>(c, x, x_stride, w_gate_up, w_down, w, d, s, y, 0, st)
+                                            : forward_t<__half>(c, x, x_stride, w_gate_up, w_down, w, d, s, y, 0, st);
 }
 
 int lapsum_experts_backward(const void *grad_y, int64_t grad_y_stride, const void *x, int64_t x_stride, const void *w_gate_up,
@@ -505,15 +547,9 @@ int lapsum_debug_experts_timeout(int64_t wait_us, void *ws, size_t ws_bytes, con
     if (dims->tokens < 1 || dims->training || dims->io_dtype != LAPSUM_IO_BF16) return LAPSUM_ERR_UNSUPPORTED;
     if (wait_us < 1 || wait_us > 100000) return LAPSUM_ERR_PARAM;
     if (!aligned(x, 16) || !aligned(w_gate_up, 16)) return LAPSUM_ERR_ALIGN;
-    CUtensorMap a, b;
-    RUN(map_2d(&a, dims->io_dtype, x, dims->d, dims->tokens, dims->d, dims->tile_rows > GATHER_ROWS ? dims->tile_rows : 1));
-    RUN(map_3d(&b, dims->io_dtype, w_gate_up, dims->d, dims->f, 2 * dims->experts, tile_cols(dims->tile_rows) / 2));
-    ExpertsArgs A = c.A;
-    A.w = w;
-    A.out0 = c.ws + c.X.off_hw;
-    A.wait_ns = (unsigned long long)wait_us * 1000;
-    A.hold = 1;
-    return run_rows<GATE_UP, __nv_bfloat16>(c, a, b, A, dims->f, static_cast<cudaStream_t>(stream));
+    c.A.wait_ns = (unsigned long long)wait_us * 1000;
+    return forward_t<__nv_bfloat16>(c, x, dims->d, w_gate_up, nullptr, w, static_cast<const uint8_t *>(dispatch), nullptr, nullptr, 1,
+                                    static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

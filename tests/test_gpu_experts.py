@@ -61,7 +61,7 @@ def test_forward(T, dtype):
     Run(T, 12, 3, 200, 136, dtype, seed=T).check()
 
 
-@pytest.mark.parametrize("rows", [16, 32, 64, 128])
+@pytest.mark.parametrize("rows", [16, 32, 64, 128, 256])
 @pytest.mark.parametrize("d,f", [(8, 8), (64, 64), (72, 40), (256, 128), (520, 264), (1000, 1032)])
 def test_forward_on_every_row_tile(rows, d, f):
     Run(150, 5, 2, d, f, tile_rows=rows, seed=rows + d).check()
@@ -75,9 +75,16 @@ def test_training(T, E, k, d, f, dtype):
     Run(T, E, k, d, f, dtype, training=True, seed=T + d).check()
 
 
-@pytest.mark.parametrize("rows", [64, 128])
-def test_training_on_both_row_tiles(rows):
-    Run(300, 7, 2, 192, 320, training=True, tile_rows=rows, seed=5).check()
+@pytest.mark.parametrize("rows", [64, 128, 256])
+@pytest.mark.parametrize("d,f", [(192, 320), (72, 40), (520, 264)])
+def test_training_on_every_row_tile(rows, d, f):
+    Run(300, 7, 2, d, f, training=True, tile_rows=rows, seed=5).check()
+
+
+@pytest.mark.parametrize("rows", [64, 128, 256])
+def test_training_with_more_tiles_than_processors(rows):
+    """every block walks over several tiles, in both accumulators and round the ring"""
+    Run(3000, 16, 4, 512, 768, training=True, tile_rows=rows, seed=6).check()
 
 
 def test_dropped_entries_and_tokens_without_any():
@@ -102,6 +109,11 @@ def test_nothing_routed():
 
 def test_all_tokens_to_one_expert_on_narrow_tiles():
     Run(500, 64, 1, 136, 72, idx=torch.full((500, 1), 41), tile_rows=16, seed=2).check()
+
+
+@pytest.mark.parametrize("rows", [16, 32, 64])
+def test_wide_column_tiles_on_narrow_row_tiles(rows):
+    Run(200, 60, 4, 264, 1032, tile_rows=rows, seed=3).check()  # enough tiles for 256 columns
 
 
 def test_an_expert_twice_for_one_token():

@@ -204,7 +204,7 @@ def check_dispatch(idx, E, rows):
 
 @pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 128, 8), (5, 3, 2), (33, 60, 6), (512, 128, 8), (513, 128, 8), (700, 1024, 6), (4096, 31, 1),
                                    (4097, 256, 3), (9000, 64, 8)])
-@pytest.mark.parametrize("rows", [16, 32, 64, 128])
+@pytest.mark.parametrize("rows", [16, 32, 64, 128, 256])
 def test_dispatch_tables(T, E, k, rows):
     gen = torch.Generator().manual_seed(T + E)
     check_dispatch(chosen(T, E, k, gen, drop=0.1 if T > 30 else 0.0, device="cpu"), E, rows)
