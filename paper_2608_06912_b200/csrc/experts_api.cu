@@ -40,41 +40,60 @@ int route_check(int64_t tokens, int64_t experts, int64_t stride, const lapsum_ro
     return LAPSUM_OK;
 }
 
-template <typename T, int NV, bool VEC>
-int route_forward_nv(const RouteArgs &A, cudaStream_t st)
-{
-    const unsigned grid = (unsigned)((A.tokens + ROUTE_WARPS - 1) / ROUTE_WARPS);
-    if (A.groups > 1)
-        return launch_pdl(route_forward_kernel<T, NV, VEC, true>, grid, 32 * ROUTE_WARPS, sizeof(float) * ROUTE_WARPS * A.E, st, A);
-    return launch_pdl(route_forward_kernel<T, NV, VEC, false>, grid, 32 * ROUTE_WARPS, 0, st, A);
-}
-template <typename T, int NV, bool VEC>
-int route_backward_nv(const RouteBackArgs &A, cudaStream_t st)
-{
-    return launch_pdl(route_backward_kernel<T, NV, VEC>, (unsigned)((A.tokens + ROUTE_WARPS - 1) / ROUTE_WARPS), 32 * ROUTE_WARPS, 0, st, A);
-}
-#define BY_WIDTH(fn, T, vec, E, ...)                                                                                    \
-    ((E) <= 128   ? ((vec) ? fn<T, 4, true>(__VA_ARGS__) : fn<T, 4, false>(__VA_ARGS__))                               \
-     : (E) <= 256 ? ((vec) ? fn<T, 8, true>(__VA_ARGS__) : fn<T, 8, false>(__VA_ARGS__))                               \
-     : (E) <= 512 ? ((vec) ? fn<T, 16, true>(__VA_ARGS__) : fn<T, 16, false>(__VA_ARGS__))                             \
-                  : ((vec) ? fn<T, 32, true>(__VA_ARGS__) : fn<T, 32, false>(__VA_ARGS__)))
+inline unsigned route_grid(int64_t tokens, int lanes) { return (unsigned)((tokens * lanes + 32 * ROUTE_WARPS - 1) / (32 * ROUTE_WARPS)); }
+
+template <typename T, int L, int NV>
+struct RouteShape {
+    static constexpr int V = 16 / (int)sizeof(T) < NV ? 16 / (int)sizeof(T) : NV;  // elements of a vector access
+    // whole vectors at aligned addresses in every row
+    static bool vec(const void *p, int64_t stride, int E) { return E % V == 0 && stride % V == 0 && aligned(p, V * sizeof(T)); }
+
+    static int forward(const RouteArgs &A, cudaStream_t st)
+    {
+        const bool v = vec(A.logits, A.stride, A.E);
+        const auto kernel = A.groups > 1 ? (v ? route_forward_kernel<T, L, NV, true, true> : route_forward_kernel<T, L, NV, false, true>)
+                                         : (v ? route_forward_kernel<T, L, NV, true, false> : route_forward_kernel<T, L, NV, false, false>);
+        return launch_pdl(kernel, route_grid(A.tokens, L), 32 * ROUTE_WARPS, 0, st, A);
+    }
+    static int dense(const RouteBackArgs &A, cudaStream_t st)
+    {
+        const bool v = vec(A.logits, A.stride, A.E) && vec(A.grad, A.E, A.E);
+        return launch_pdl(v ? route_backward_dense_kernel<T, L, NV, true> : route_backward_dense_kernel<T, L, NV, false>,
+                          route_grid(A.tokens, L), 32 * ROUTE_WARPS, 0, st, A);
+    }
+};
+// Lanes per token: eight with up to 16 logits each, more only where a row is longer (a choice costs a warp the same
+// instructions however many tokens it holds).
+#define BY_WIDTH(T, what, E, ...)                                 \
+    ((E) <= 32    ? RouteShape<T, 8, 4>::what(__VA_ARGS__)        \
+     : (E) <= 64  ? RouteShape<T, 8, 8>::what(__VA_ARGS__)        \
+     : (E) <= 128 ? RouteShape<T, 8, 16>::what(__VA_ARGS__)       \
+     : (E) <= 256 ? RouteShape<T, 16, 16>::what(__VA_ARGS__)      \
+     : (E) <= 512 ? RouteShape<T, 32, 16>::what(__VA_ARGS__)      \
+                  : RouteShape<T, 32, 32>::what(__VA_ARGS__))
 #define BY_TYPE(fn, dtype, ...)                                  \
     ((dtype) == LAPSUM_IO_F32   ? fn<float>(__VA_ARGS__)          \
      : (dtype) == LAPSUM_IO_F16 ? fn<__half>(__VA_ARGS__)         \
                                 : fn<__nv_bfloat16>(__VA_ARGS__))
 
-// four logits per load where every row starts at a multiple of four elements
 template <typename T>
 int route_forward_t(const RouteArgs &A, cudaStream_t st)
 {
-    const bool vec = A.E % 4 == 0 && A.stride % 4 == 0 && aligned(A.logits, 4 * sizeof(T));
-    return BY_WIDTH(route_forward_nv, T, vec, A.E, A, st);
+    return BY_WIDTH(T, forward, A.E, A, st);
+}
+template <typename T, int L>
+int route_sparse(const RouteBackArgs &A, cudaStream_t st)
+{
+    constexpr int V = 16 / (int)sizeof(T);
+    const bool v = (32 / L) * A.E % V == 0 && A.tokens * A.E % V == 0 && aligned(A.grad, 16);  // whole vectors per warp
+    return launch_pdl(v ? route_backward_kernel<T, L, true> : route_backward_kernel<T, L, false>, route_grid(A.tokens, L), 32 * ROUTE_WARPS, 0,
+                      st, A);
 }
 template <typename T>
 int route_backward_t(const RouteBackArgs &A, cudaStream_t st)
 {
-    const bool vec = A.E % 4 == 0 && A.stride % 4 == 0 && aligned(A.logits, 4 * sizeof(T)) && aligned(A.grad, 4 * sizeof(T));
-    return BY_WIDTH(route_backward_nv, T, vec, A.E, A, st);
+    if (A.score == LAPSUM_ROUTE_SOFTMAX && !A.renorm) return BY_WIDTH(T, dense, A.E, A, st);
+    return A.k <= 8 ? route_sparse<T, 8>(A, st) : A.k <= 16 ? route_sparse<T, 16>(A, st) : route_sparse<T, 32>(A, st);
 }
 
 // ---------------------------------------------------------------- dispatch ----

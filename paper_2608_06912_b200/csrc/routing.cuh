@@ -1,9 +1,14 @@
 // Routing of tokens to experts and the dispatch tables that bring every expert's tokens side by side.
 //
-// route    one warp per token, the token's E logits in registers (E <= 1024: 32 per lane).
+// route    L lanes per token (8, 16 or 32), NV neighbouring logits in each lane's registers.
 //          keys   c_i = l_i (softmax or sigmoid without a bias: both rise with the logit), else s_i + bias_i
 //          groups the `kept` groups with the largest sum of their best `group_top` keys keep their experts
 //          choice k largest keys, ties to the lower index; weights from the scores s, never from the bias
+//          Bound by integer instructions, not by memory, so the work per choice is kept small: a lane knows the maxima of
+//          its runs of four keys, log2 L exchanges find the row's largest, a ballot the lane (lanes hold ascending
+//          runs, so the lowest lane is the lowest index), and that lane alone looks into one run in shared memory.
+//          Measured at 65536 x 128, k = 8: a warp per token with its logits spread over all lanes took 47 us (780
+//          instructions a token).
 // dispatch a stable counting sort of the T k entries by expert, integers only.
 #pragma once
 #include "common.cuh"
@@ -11,7 +16,7 @@
 namespace lapsum {
 
 constexpr int ROUTE_MAX_E = 1024, ROUTE_MAX_K = 32, ROUTE_MAX_GROUPS = 32;
-constexpr int ROUTE_WARPS = 8;  // tokens per block
+constexpr int ROUTE_WARPS = 8;  // warps per block
 
 struct RouteArgs {
     const void *logits;
@@ -23,19 +28,6 @@ struct RouteArgs {
     float scale;
 };
 
-__device__ __forceinline__ float warp_sum_f(float v)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-    return v;
-}
-__device__ __forceinline__ float warp_max_f(float v)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
-    return v;
-}
-
 // 0 for an expert that cannot be chosen (-inf or NaN), else the order-preserving key; -0 counts as +0
 __device__ __forceinline__ uint32_t route_key(float x)
 {
@@ -43,81 +35,90 @@ __device__ __forceinline__ uint32_t route_key(float x)
 }
 __device__ __forceinline__ float sigmoid_f(float x) { return 1.f / (1.f + expf(-x)); }
 
-// The lane's NV logits, four neighbours at a time: register 4 q + v holds expert 128 q + 4 lane + v.  With VEC the four
-// arrive in one 16-byte (fp32) or 8-byte (16-bit) load.
-template <typename T, int NV, bool VEC>
-__device__ __forceinline__ void load_row(const T *row, int E, int lane, float (&x)[NV])
+template <int L>
+__device__ __forceinline__ float row_sum_f(float v)
 {
 #pragma unroll
-    for (int q = 0; q < NV / 4; ++q) {
-        const int i = 128 * q + 4 * lane;
-        if constexpr (VEC) {
-            if (i < E) {
-                if constexpr (sizeof(T) == 4) {
-                    const float4 f = __ldg(reinterpret_cast<const float4 *>(row + i));
-                    x[4 * q] = f.x, x[4 * q + 1] = f.y, x[4 * q + 2] = f.z, x[4 * q + 3] = f.w;
-                } else {
-                    const uint2 u = __ldg(reinterpret_cast<const uint2 *>(row + i));
-                    T h[4];
-                    *reinterpret_cast<uint2 *>(h) = u;
+    for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+    return v;
+}
+template <int L>
+__device__ __forceinline__ float row_max_f(float v)
+{
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) x[4 * q + v] = Io<T>::from_storage(h[v]);
-                }
-            } else {
+    for (int o = L / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
+    return v;
+}
+
+// NV neighbouring logits from `first` on, -inf beyond the row's end.  VEC: rows of whole vectors at aligned addresses.
+template <typename T, int NV, bool VEC>
+__device__ __forceinline__ void load_run(const T *row, int first, int E, float (&x)[NV])
+{
+    if constexpr (VEC) {
+        constexpr int V = 16 / sizeof(T) < NV ? 16 / sizeof(T) : NV;  // logits per load
 #pragma unroll
-                for (int v = 0; v < 4; ++v) x[4 * q + v] = -CUDART_INF_F;
+        for (int q = 0; q < NV / V; ++q) {
+            T h[V];
+            if (first + q * V < E) {
+                if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4 *>(h) = __ldg(reinterpret_cast<const uint4 *>(row + first + q * V));
+                else *reinterpret_cast<uint2 *>(h) = __ldg(reinterpret_cast<const uint2 *>(row + first + q * V));
             }
-        } else {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) x[4 * q + v] = (i + v < E) ? Io<T>::load1(row + i + v) : -CUDART_INF_F;
+            for (int v = 0; v < V; ++v) x[q * V + v] = (first + q * V < E) ? Io<T>::from_storage(h[v]) : -CUDART_INF_F;
         }
+    } else {
+#pragma unroll
+        for (int v = 0; v < NV; ++v) x[v] = (first + v < E) ? Io<T>::load1(row + first + v) : -CUDART_INF_F;
     }
 }
 
-// The best `top` keys' sum of every group, by the lanes of the warp: lane l works for group l / per_lanes.  `sh` holds
-// the row's keys as floats (-inf where unavailable).  Returns the mask of the groups that stay.
-__device__ __forceinline__ uint32_t kept_groups(const float *sh, const RouteArgs &A, int lane)
+// The groups that keep their experts, as a bit mask, by the row's L lanes; `c` holds the row's keys as floats (-inf =
+// unavailable), element e at c[place(e)], `strength` 32 floats of the row.
+template <int L, typename Place>
+__device__ __forceinline__ uint32_t kept_groups(const float *c, float *strength, const RouteArgs &A, int r, int row_lane, Place place)
 {
     const int size = A.E / A.groups;
-    int lanes = 1;  // lanes per group: a power of two
-    while (2 * lanes * A.groups <= 32) lanes *= 2;
-    const int g = lane / lanes;
-    float a = -CUDART_INF_F, b = -CUDART_INF_F;  // best and second best
-    if (g < A.groups)
-        for (int i = lane % lanes; i < size; i += lanes) {
-            const float v = sh[g * size + i];
+    for (int g = r; g < A.groups; g += L) {
+        float a = -CUDART_INF_F, b = -CUDART_INF_F;  // best and second best
+        for (int i = g * size; i < (g + 1) * size; ++i) {
+            const float v = c[place(i)];
             b = fmaxf(b, fminf(a, v));
             a = fmaxf(a, v);
         }
-    for (int o = 1; o < lanes; o <<= 1) {
-        const float a2 = __shfl_xor_sync(FULL, a, o), b2 = __shfl_xor_sync(FULL, b, o);
-        b = fmaxf(fmaxf(b, b2), fminf(a, a2));
-        a = fmaxf(a, a2);
+        strength[g] = (A.top > 1 && b > -CUDART_INF_F) ? a + b : a;  // a group with one expert left counts that one
     }
-    const float s = (A.top > 1 && b > -CUDART_INF_F) ? a + b : a;  // a group with one expert left counts that one
-    uint32_t key = (g < A.groups && lane % lanes == 0) ? route_key(s) : 0u;
+    __syncwarp();
     uint32_t keep = 0;
-    for (int j = 0; j < A.kept; ++j) {
-        const uint32_t m = __reduce_max_sync(FULL, key);
-        if (m == 0) break;
-        const int src = __ffs(__ballot_sync(FULL, key == m)) - 1;  // lowest lane = lowest group
-        keep |= 1u << (src / lanes);
-        if (lane == src) key = 0;
+    for (int g0 = 0; g0 < A.groups; g0 += L) {
+        const int g = g0 + r;
+        bool in = false;
+        if (g < A.groups && strength[g] > -CUDART_INF_F) {
+            int ahead = 0;  // groups that come before this one
+            for (int o = 0; o < A.groups; ++o) ahead += strength[o] > strength[g] || (strength[o] == strength[g] && o < g);
+            in = ahead < A.kept;
+        }
+        const uint32_t bal = __ballot_sync(FULL, in) >> row_lane;
+        keep |= (L == 32 ? bal : bal & ((1u << (L & 31)) - 1u)) << g0;
     }
     return keep;
 }
 
-template <typename T, int NV, bool VEC, bool GROUPS>
+template <typename T, int L, int NV, bool VEC, bool GROUPS>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_forward_kernel(const RouteArgs A)
 {
-    extern __shared__ float route_sh[];
+    constexpr int ROWS = 32 / L * ROUTE_WARPS, PITCH = NV + 4;  // a lane's keys: 16-byte pieces of eight lanes meet no bank twice
+    __shared__ __align__(16) uint32_t keys[32 * ROUTE_WARPS * PITCH];
+    __shared__ int choice[ROWS * ROUTE_MAX_K];
+    __shared__ float strength[GROUPS ? ROWS * ROUTE_MAX_GROUPS : 1];
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t t = (int64_t)blockIdx.x * ROUTE_WARPS + warp;
-    if (t >= A.tokens) return;
-    const T *row = reinterpret_cast<const T *>(A.logits) + t * A.stride;
+    const int lane = threadIdx.x & 31, r = lane % L, row_lane = lane - r, row_in_block = threadIdx.x / L;
+    const int64_t t = (int64_t)blockIdx.x * ROWS + row_in_block;
+    const bool live = t < A.tokens;
+    const T *row = reinterpret_cast<const T *>(A.logits) + (live ? t : A.tokens - 1) * A.stride;
+    uint32_t *const mine = keys + threadIdx.x * PITCH;
+    const int first = r * NV;
     float x[NV];
-    load_row<T, NV, VEC>(row, A.E, lane, x);
+    load_run<T, NV, VEC>(row, first, A.E, x);
 
     // softmax over the whole row, where the scores themselves are needed
     const bool by_score = A.bias != nullptr || GROUPS;
@@ -126,100 +127,129 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_forward_kernel(const R
         float m = -CUDART_INF_F;
 #pragma unroll
         for (int i = 0; i < NV; ++i) m = fmaxf(m, x[i]);  // fmaxf skips NaN
-        top = warp_max_f(m);
+        top = row_max_f<L>(m);
         if (top == -CUDART_INF_F) top = 0.f;
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) s += (x[i] > -CUDART_INF_F) ? expf(x[i] - top) : 0.f;
-        total = warp_sum_f(s);
+        total = row_sum_f<L>(s);
     }
-
-    uint32_t key[NV];
-    float *sh = route_sh + warp * A.E;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int e = 128 * (i / 4) + 4 * lane + (i & 3);
-        float c = x[i];
-        if (by_score) {
-            float s = c;
-            if (A.score == LAPSUM_ROUTE_SOFTMAX) s = expf(c - top) / total;
-            else if (A.score == LAPSUM_ROUTE_SIGMOID) s = sigmoid_f(c);
-            const bool there = c > -CUDART_INF_F;
-            if (A.bias != nullptr && e < A.E) s += __ldg(A.bias + e);
-            s = there ? s : -CUDART_INF_F;
-            if (GROUPS && e < A.E) sh[e] = (s > -CUDART_INF_F) ? s : -CUDART_INF_F;  // a NaN (bias) counts as unavailable
-            // without a bias the experts of the kept groups are compared by their logits, which the score rises with
-            if (A.bias != nullptr) c = s;
-        }
-        key[i] = route_key(c);
-    }
-    if constexpr (GROUPS) {
-        __syncwarp();
-        const uint32_t keep = kept_groups(sh, A, lane);
-        const int size = A.E / A.groups;
+    if (by_score) {
+        float c[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int e = 128 * (i / 4) + 4 * lane + (i & 3);
-            if (e < A.E && !((keep >> (e / size)) & 1u)) key[i] = 0u;
+            float s = x[i];
+            if (A.score == LAPSUM_ROUTE_SOFTMAX) s = expf(s - top) / total;
+            else if (A.score == LAPSUM_ROUTE_SIGMOID) s = sigmoid_f(s);
+            if (A.bias != nullptr && first + i < A.E) s += __ldg(A.bias + first + i);
+            c[i] = (x[i] > -CUDART_INF_F && s > -CUDART_INF_F) ? s : -CUDART_INF_F;  // a NaN counts as unavailable
         }
-    }
-
-    // k times the warp's largest key; among equal keys the lowest expert
-    int mine = -1;  // lane j keeps the j-th choice
-    uint32_t best = 0;
-    int at = 0;
+        if constexpr (GROUPS) {
+            float *const f = reinterpret_cast<float *>(mine);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if (key[i] > best) best = key[i], at = i;
-    for (int j = 0; j < A.k; ++j) {
-        const uint32_t m = __reduce_max_sync(FULL, best);
-        if (m == 0) break;
-        const uint32_t e = 128 * (at / 4) + 4 * lane + (at & 3);
-        const uint32_t win = __reduce_min_sync(FULL, best == m ? e : 0xffffffffu);
-        if (lane == j) mine = (int)win;
-        if (best == m && e == win) {
-            best = 0;
-            int next = 0;
+            for (int i = 0; i < NV; ++i) f[i] = c[i];
+            __syncwarp();
+            const float *const all = reinterpret_cast<const float *>(keys + (threadIdx.x - r) * PITCH);
+            const uint32_t keep = kept_groups<L>(all, strength + row_in_block * ROUTE_MAX_GROUPS, A, r, row_lane,
+                                                 [](int e) { return e / NV * PITCH + e % NV; });
+            __syncwarp();
+            const int size = A.E / A.groups;
+            int g = first / size, left = (g + 1) * size - first;  // experts until the next group
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (i == at) key[i] = 0u;
-                if (key[i] > best) best = key[i], next = i;
+                if (!((keep >> (g & 31)) & 1u)) c[i] = x[i] = -CUDART_INF_F;
+                if (--left == 0) ++g, left = size;
             }
-            at = next;
+        }
+        // without a bias the experts of the kept groups are compared by their logits, which the score rises with
+        if (A.bias != nullptr) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) x[i] = c[i];
         }
     }
 
-    // weights: lane j holds its choice's logit again
-    const float l = (mine >= 0) ? Io<T>::load1(row + mine) : -CUDART_INF_F;
-    float w = 0.f;
-    if (A.score == LAPSUM_ROUTE_SOFTMAX) {
-        if (A.renorm) {  // the softmax of the chosen logits alone: never 0 / 0
-            const float m = warp_max_f(l);
-            w = (mine >= 0) ? expf(l - m) : 0.f;
-            const float s = warp_sum_f(w);
-            w = (mine >= 0) ? w / s : 0.f;
-        } else {
-            w = (mine >= 0) ? expf(l - top) / total : 0.f;
-        }
-    } else if (A.score == LAPSUM_ROUTE_SIGMOID) {
-        if (A.renorm) {  // s_j e^{-m} = 1 / (e^m + e^{m - l}), m = min(0, largest l): the sum cannot underflow
-            const float m = fminf(0.f, warp_max_f(l));
-            w = (mine >= 0) ? 1.f / (expf(m) + expf(m - l)) : 0.f;
-            const float s = warp_sum_f(w);
-            w = (mine >= 0) ? w / s : 0.f;
-        } else {
-            w = (mine >= 0) ? sigmoid_f(l) : 0.f;
-        }
-    } else {
-        w = (mine >= 0) ? l : 0.f;
-        if (A.renorm) {
-            const float s = warp_sum_f(w);
-            w = (s != 0.f) ? w / s : 0.f;
+    // maxima of the lane's runs of four keys
+    uint32_t run[NV / 4];
+    uint32_t best = 0;
+#pragma unroll
+    for (int q = 0; q < NV / 4; ++q) {
+        const uint4 k4 = make_uint4(route_key(x[4 * q]), route_key(x[4 * q + 1]), route_key(x[4 * q + 2]), route_key(x[4 * q + 3]));
+        *reinterpret_cast<uint4 *>(mine + 4 * q) = k4;
+        run[q] = max(max(k4.x, k4.y), max(k4.z, k4.w));
+        best = max(best, run[q]);
+    }
+    int *const out = choice + row_in_block * ROUTE_MAX_K;
+    for (int j = 0; j < A.k; ++j) {
+        uint32_t m = best;
+#pragma unroll
+        for (int o = L / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(FULL, m, o));
+        const uint32_t bal = __ballot_sync(FULL, best == m);
+        const uint32_t owners = (L == 32) ? bal : (bal >> row_lane) & ((1u << (L & 31)) - 1u);
+        if (r == __ffs(owners) - 1) {
+            int e = -1;
+            if (m != 0u) {
+                int q = NV / 4 - 1;
+#pragma unroll
+                for (int i = NV / 4 - 2; i >= 0; --i) q = run[i] == m ? i : q;
+                uint4 k4 = *reinterpret_cast<const uint4 *>(mine + 4 * q);
+                const int v = k4.x == m ? 0 : k4.y == m ? 1 : k4.z == m ? 2 : 3;
+                mine[4 * q + v] = 0u;
+                k4.x = v == 0 ? 0u : k4.x, k4.y = v == 1 ? 0u : k4.y, k4.z = v == 2 ? 0u : k4.z, k4.w = v == 3 ? 0u : k4.w;
+                const uint32_t next = max(max(k4.x, k4.y), max(k4.z, k4.w));
+                best = 0;
+#pragma unroll
+                for (int i = 0; i < NV / 4; ++i) {
+                    run[i] = i == q ? next : run[i];
+                    best = max(best, run[i]);
+                }
+                e = first + 4 * q + v;
+            }
+            out[j] = e;
         }
     }
-    if (lane < A.k) {
-        A.idx[t * A.k + lane] = mine;
-        A.w[t * A.k + lane] = A.scale * w;
+    __syncwarp();
+
+    // weights: lane r of the row has the choices r, r + L, ...
+    constexpr int C = ROUTE_MAX_K / L;
+    int e[C];
+    float l[C], w[C];
+#pragma unroll
+    for (int p = 0; p < C; ++p) {
+        e[p] = (p * L + r < A.k) ? out[p * L + r] : -1;
+        l[p] = (e[p] >= 0) ? Io<T>::load1(row + e[p]) : -CUDART_INF_F;
+    }
+    float peak = l[0], sum = 0.f;
+    if (A.renorm && A.score != LAPSUM_ROUTE_GIVEN) {
+#pragma unroll
+        for (int p = 1; p < C; ++p) peak = fmaxf(peak, l[p]);
+        peak = row_max_f<L>(peak);
+    }
+    const float floor_ = fminf(0.f, peak), e_floor = A.renorm && A.score == LAPSUM_ROUTE_SIGMOID ? expf(floor_) : 0.f;
+#pragma unroll
+    for (int p = 0; p < C; ++p) {
+        if (p * L >= A.k) break;
+        float v = 0.f;
+        if (e[p] >= 0) {
+            if (A.score == LAPSUM_ROUTE_SOFTMAX)  // renormalised: the softmax of the chosen logits alone, never 0 / 0
+                v = A.renorm ? expf(l[p] - peak) : expf(l[p] - top) / total;
+            else if (A.score == LAPSUM_ROUTE_SIGMOID)  // s e^{-m} = 1 / (e^m + e^{m - l}), m = min(0, largest l): no underflow of the sum
+                v = A.renorm ? 1.f / (e_floor + expf(floor_ - l[p])) : sigmoid_f(l[p]);
+            else
+                v = l[p];
+        }
+        w[p] = v;
+        sum += v;
+    }
+    if (A.renorm) sum = row_sum_f<L>(sum);
+#pragma unroll
+    for (int p = 0; p < C; ++p) {
+        const int j = p * L + r;
+        if (j >= A.k) break;
+        if (A.renorm) w[p] = (e[p] >= 0 && sum != 0.f) ? w[p] / sum : 0.f;
+        if (live) {
+            A.idx[t * A.k + j] = e[p];
+            A.w[t * A.k + j] = A.scale * w[p];
+        }
     }
 }
 
@@ -234,96 +264,125 @@ struct RouteBackArgs {
     float scale;
 };
 
-// Gradient of one token's logits by one warp: lane j holds choice j.  With W = sum_j gw_j w_j / scale and
-// g_j = w_j (gw_j - W):  softmax renormalised: g_j;  sigmoid renormalised: g_j (1 - s_j);  sigmoid: gw_j scale s (1 - s);
-// softmax: p_i (scale [i chosen] gw - scale sum_j gw_j p_j), the one case that is dense in i;
+__device__ __forceinline__ float route_grad_w(const RouteBackArgs &A, int64_t at)
+{
+    return A.gw_dtype == LAPSUM_IO_F32   ? __ldg(reinterpret_cast<const float *>(A.grad_w) + at)
+           : A.gw_dtype == LAPSUM_IO_F16 ? Io<__half>::load1(reinterpret_cast<const __half *>(A.grad_w) + at)
+                                         : Io<__nv_bfloat16>::load1(reinterpret_cast<const __nv_bfloat16 *>(A.grad_w) + at);
+}
+
+// Gradient of the logits where only the chosen ones have one: with W = sum_j gw_j w_j / scale and g_j = w_j (gw_j - W),
+// softmax renormalised: g_j;  sigmoid renormalised: g_j (1 - s_j);  sigmoid: gw_j scale s_j (1 - s_j);
 // given: scale gw_j, renormalised (scale gw_j - sum gw w) / sum s.
-// The row is zeroed (or filled with the dense part) first and the chosen entries are written over it by the same warp.
-template <typename T, int NV, bool VEC>
+// A warp has 32 / L tokens, a lane per choice.  It writes zeros over its rows, which lie side by side, and then the chosen entries.
+template <typename T, int L, bool VEC>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_backward_kernel(const RouteBackArgs A)
 {
+    constexpr int R = 32 / L;
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t t = (int64_t)blockIdx.x * ROUTE_WARPS + warp;
-    if (t >= A.tokens) return;
-    const T *row = reinterpret_cast<const T *>(A.logits) + t * A.stride;
-    T *out = reinterpret_cast<T *>(A.grad) + t * A.E;
+    const int lane = threadIdx.x & 31, r = lane % L;
+    const int64_t t0 = ((int64_t)blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5)) * R, t = t0 + lane / L;
+    if (t0 >= A.tokens) return;
     int mine = -1;
-    float w = 0.f, gw = 0.f;
-    if (lane < A.k) {
-        const int64_t at = t * A.k + lane;
+    float w = 0.f, gw = 0.f, l = 0.f;
+    if (r < A.k && t < A.tokens) {
+        const int64_t at = t * A.k + r;
         mine = __ldg(A.idx + at);
-        if (mine >= A.E) mine = -1;
         w = __ldg(A.w + at);
-        gw = A.gw_dtype == LAPSUM_IO_F32   ? __ldg(reinterpret_cast<const float *>(A.grad_w) + at)
-             : A.gw_dtype == LAPSUM_IO_F16 ? Io<__half>::load1(reinterpret_cast<const __half *>(A.grad_w) + at)
-                                           : Io<__nv_bfloat16>::load1(reinterpret_cast<const __nv_bfloat16 *>(A.grad_w) + at);
+        gw = route_grad_w(A, at);
     }
-    const bool chosen = mine >= 0;
-    if (!chosen) w = 0.f, gw = 0.f;
-    const float gww = warp_sum_f(gw * w);  // = scale * W
-    float g = 0.f, dense = 0.f, top = 0.f, inv = 0.f;
-    float x[NV];
-    const bool full = A.score == LAPSUM_ROUTE_SOFTMAX && !A.renorm;
-    if (full) {
-        load_row<T, NV, VEC>(row, A.E, lane, x);
-        float m = -CUDART_INF_F;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) m = fmaxf(m, x[i]);
-        top = warp_max_f(m);
-        if (top == -CUDART_INF_F) top = 0.f;
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            x[i] = (x[i] > -CUDART_INF_F) ? expf(x[i] - top) : 0.f;
-            s += x[i];
-        }
-        s = warp_sum_f(s);
-        inv = s > 0.f ? 1.f / s : 0.f;
-        dense = -gww;
-        g = w * (gw - gww / A.scale);  // w = scale p
-    } else if (A.score == LAPSUM_ROUTE_SOFTMAX) {
-        g = w * (gw - gww / A.scale);
+    T *const out = reinterpret_cast<T *>(A.grad) + t0 * A.E;
+    const int n = (int)min((int64_t)R, A.tokens - t0) * A.E;
+    if constexpr (VEC) {
+        constexpr int V = 16 / sizeof(T);
+        for (int i = lane * V; i < n; i += 32 * V) *reinterpret_cast<uint4 *>(out + i) = make_uint4(0, 0, 0, 0);
     } else {
-        const float l = chosen ? Io<T>::load1(row + mine) : 0.f;
-        if (A.score == LAPSUM_ROUTE_SIGMOID) {
-            const float e = expf(-fabsf(l));  // 1 - s = 1 / (1 + e^l) without cancellation
-            const float rest = (l >= 0.f ? e : 1.f) / (1.f + e);
-            g = (A.renorm ? w * (gw - gww / A.scale) : w * gw) * rest;
-        } else if (A.renorm) {
-            const float s = warp_sum_f(l);
-            g = s != 0.f ? (A.scale * gw - gww) / s : 0.f;
-        } else {
-            g = A.scale * gw;
-        }
+        for (int i = lane; i < n; i += 32) Io<T>::store1(out + i, 0.f);
     }
+    const bool chosen = mine >= 0 && mine < A.E;
+    if (!chosen) w = 0.f, gw = 0.f;
+    if (chosen && A.score != LAPSUM_ROUTE_SOFTMAX) l = Io<T>::load1(reinterpret_cast<const T *>(A.logits) + t * A.stride + mine);
+    const float gww = row_sum_f<L>(gw * w);  // = scale W
+    float g;
+    if (A.score == LAPSUM_ROUTE_SOFTMAX) {
+        g = w * (gw - gww / A.scale);
+    } else if (A.score == LAPSUM_ROUTE_SIGMOID) {
+        const float e = expf(-fabsf(l));  // 1 - s = 1 / (1 + e^l) without cancellation
+        g = (A.renorm ? w * (gw - gww / A.scale) : w * gw) * ((l >= 0.f ? e : 1.f) / (1.f + e));
+    } else if (A.renorm) {
+        const float s = row_sum_f<L>(chosen ? l : 0.f);
+        g = s != 0.f ? (A.scale * gw - gww) / s : 0.f;
+    } else {
+        g = A.scale * gw;
+    }
+    __syncwarp();  // orders the zeros before the chosen entries
+    if (chosen) Io<T>::store1(out + (int64_t)(lane / L) * A.E + mine, g);
+}
+
+// Softmax without renormalisation: p_i (scale [i chosen] gw_i - scale sum_j gw_j p_j), dense in i.  L lanes per token.
+template <typename T, int L, int NV, bool VEC>
+__global__ void __launch_bounds__(32 * ROUTE_WARPS) route_backward_dense_kernel(const RouteBackArgs A)
+{
+    constexpr int ROWS = 32 / L * ROUTE_WARPS, C = ROUTE_MAX_K / L;
+    pdl_wait();
+    const int lane = threadIdx.x & 31, r = lane % L;
+    const int64_t t = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
+    const bool live = t < A.tokens;
+    const T *row = reinterpret_cast<const T *>(A.logits) + (live ? t : A.tokens - 1) * A.stride;
+    T *const out = reinterpret_cast<T *>(A.grad) + t * A.E;
+    const int first = r * NV;
+    float x[NV];
+    load_run<T, NV, VEC>(row, first, A.E, x);
+    int mine[C];
+    float w[C], gw[C], gww = 0.f;
 #pragma unroll
-    for (int q = 0; q < NV / 4; ++q) {
-        const int i = 128 * q + 4 * lane;
-        float y[4] = {0.f, 0.f, 0.f, 0.f};
-        if (full) {
-#pragma unroll
-            for (int v = 0; v < 4; ++v) y[v] = x[4 * q + v] * inv * dense;
+    for (int p = 0; p < C; ++p) {
+        const int j = p * L + r;
+        mine[p] = -1, w[p] = gw[p] = 0.f;
+        if (live && j < A.k) {
+            mine[p] = __ldg(A.idx + t * A.k + j);
+            if (mine[p] >= A.E) mine[p] = -1;
+            if (mine[p] >= 0) w[p] = __ldg(A.w + t * A.k + j), gw[p] = route_grad_w(A, t * A.k + j);
         }
-        if constexpr (VEC) {
-            if (i < A.E) {
-                if constexpr (sizeof(T) == 4) {
-                    *reinterpret_cast<float4 *>(out + i) = make_float4(y[0], y[1], y[2], y[3]);
-                } else {
-                    T h[4];
+        gww += gw[p] * w[p];
+    }
+    gww = row_sum_f<L>(gww);  // w = scale p
+    float m = -CUDART_INF_F, s = 0.f;
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) Io<T>::store1(h + v, y[v]);
-                    *reinterpret_cast<uint2 *>(out + i) = *reinterpret_cast<const uint2 *>(h);
+    for (int i = 0; i < NV; ++i) m = fmaxf(m, x[i]);
+    m = row_max_f<L>(m);
+    if (m == -CUDART_INF_F) m = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        x[i] = (x[i] > -CUDART_INF_F) ? expf(x[i] - m) : 0.f;
+        s += x[i];
+    }
+    s = row_sum_f<L>(s);
+    const float inv = s > 0.f ? 1.f / s : 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) x[i] = -x[i] * inv * gww;
+    if (live) {
+        if constexpr (VEC) {
+            constexpr int V = 16 / sizeof(T) < NV ? 16 / sizeof(T) : NV;
+#pragma unroll
+            for (int q = 0; q < NV / V; ++q)
+                if (first + q * V < A.E) {
+                    T h[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) Io<T>::store1(h + v, x[q * V + v]);
+                    if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4 *>(out + first + q * V) = *reinterpret_cast<const uint4 *>(h);
+                    else *reinterpret_cast<uint2 *>(out + first + q * V) = *reinterpret_cast<const uint2 *>(h);
                 }
-            }
         } else {
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
-                if (i + v < A.E) Io<T>::store1(out + i + v, y[v]);
+            for (int v = 0; v < NV; ++v)
+                if (first + v < A.E) Io<T>::store1(out + first + v, x[v]);
         }
     }
     __syncwarp();  // orders the row's stores before the chosen entries'
-    if (chosen) Io<T>::store1(out + mine, g);
+#pragma unroll
+    for (int p = 0; p < C; ++p)
+        if (mine[p] >= 0) Io<T>::store1(out + mine[p], w[p] * (gw[p] - gww / A.scale));
 }
 
 // ------------------------------------------------------------------ dispatch ----
