@@ -28,12 +28,11 @@ struct RouteArgs {
     float scale;
 };
 
-// 0 for an expert that cannot be chosen (-inf or NaN), else the order-preserving key; -0 counts as +0
-__device__ __forceinline__ uint32_t route_key(float x)
-{
-    return (x > -CUDART_INF_F) ? float_to_key(x + 0.f) : 0u;
-}
+// What experts are compared by: -inf for one that cannot be chosen (NaN, by fmaxf's rule), +0 for -0
+__device__ __forceinline__ float route_key(float x) { return fmaxf(x + 0.f, -CUDART_INF_F); }
 __device__ __forceinline__ float sigmoid_f(float x) { return 1.f / (1.f + expf(-x)); }
+// For the keys, which only order the experts: a few units of 2^-24 off, the same value for the same logit
+__device__ __forceinline__ float sigmoid_key(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 
 template <int L>
 __device__ __forceinline__ float row_sum_f(float v)
@@ -78,14 +77,32 @@ template <int L, typename Place>
 __device__ __forceinline__ uint32_t kept_groups(const float *c, float *strength, const RouteArgs &A, int r, int row_lane, Place place)
 {
     const int size = A.E / A.groups;
-    for (int g = r; g < A.groups; g += L) {
+    int lanes = 1;  // lanes that share a group's experts: a power of two
+    while (2 * lanes * A.groups <= L && 4 * lanes < size) lanes *= 2;
+    const int share = r % lanes;
+    for (int g0 = 0; g0 < A.groups; g0 += L / lanes) {
+        const int g = g0 + r / lanes;
         float a = -CUDART_INF_F, b = -CUDART_INF_F;  // best and second best
-        for (int i = g * size; i < (g + 1) * size; ++i) {
-            const float v = c[place(i)];
+        auto take = [&](float v) {
             b = fmaxf(b, fminf(a, v));
             a = fmaxf(a, v);
+        };
+        if (g < A.groups) {
+            if (size % 4 == 0) {  // whole runs of four
+                for (int i = g * size + 4 * share; i < (g + 1) * size; i += 4 * lanes) {
+                    const float4 v = *reinterpret_cast<const float4 *>(c + place(i));
+                    take(v.x), take(v.y), take(v.z), take(v.w);
+                }
+            } else {
+                for (int i = g * size + share; i < (g + 1) * size; i += lanes) take(c[place(i)]);
+            }
         }
-        strength[g] = (A.top > 1 && b > -CUDART_INF_F) ? a + b : a;  // a group with one expert left counts that one
+        for (int o = 1; o < lanes; o <<= 1) {
+            const float a2 = __shfl_xor_sync(FULL, a, o), b2 = __shfl_xor_sync(FULL, b, o);
+            b = fmaxf(fmaxf(b, b2), fminf(a, a2));
+            a = fmaxf(a, a2);
+        }
+        if (g < A.groups && share == 0) strength[g] = (A.top > 1 && b > -CUDART_INF_F) ? a + b : a;  // one expert left: that one
     }
     __syncwarp();
     uint32_t keep = 0;
@@ -104,18 +121,18 @@ __device__ __forceinline__ uint32_t kept_groups(const float *c, float *strength,
 }
 
 template <typename T, int L, int NV, bool VEC, bool GROUPS>
-__global__ void __launch_bounds__(32 * ROUTE_WARPS) route_forward_kernel(const RouteArgs A)
+__global__ void __launch_bounds__(32 * ROUTE_WARPS, 4) route_forward_kernel(const RouteArgs A)
 {
     constexpr int ROWS = 32 / L * ROUTE_WARPS, PITCH = NV + 4;  // a lane's keys: 16-byte pieces of eight lanes meet no bank twice
-    __shared__ __align__(16) uint32_t keys[32 * ROUTE_WARPS * PITCH];
-    __shared__ int choice[ROWS * ROUTE_MAX_K];
+    __shared__ __align__(16) float keys[32 * ROUTE_WARPS * PITCH];
+    __shared__ short choice[ROWS * ROUTE_MAX_K];
     __shared__ float strength[GROUPS ? ROWS * ROUTE_MAX_GROUPS : 1];
     pdl_wait();
     const int lane = threadIdx.x & 31, r = lane % L, row_lane = lane - r, row_in_block = threadIdx.x / L;
     const int64_t t = (int64_t)blockIdx.x * ROWS + row_in_block;
     const bool live = t < A.tokens;
     const T *row = reinterpret_cast<const T *>(A.logits) + (live ? t : A.tokens - 1) * A.stride;
-    uint32_t *const mine = keys + threadIdx.x * PITCH;
+    float *const mine = keys + threadIdx.x * PITCH;
     const int first = r * NV;
     float x[NV];
     load_run<T, NV, VEC>(row, first, A.E, x);
@@ -140,17 +157,15 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_forward_kernel(const R
         for (int i = 0; i < NV; ++i) {
             float s = x[i];
             if (A.score == LAPSUM_ROUTE_SOFTMAX) s = expf(s - top) / total;
-            else if (A.score == LAPSUM_ROUTE_SIGMOID) s = sigmoid_f(s);
+            else if (A.score == LAPSUM_ROUTE_SIGMOID) s = sigmoid_key(s);
             if (A.bias != nullptr && first + i < A.E) s += __ldg(A.bias + first + i);
             c[i] = (x[i] > -CUDART_INF_F && s > -CUDART_INF_F) ? s : -CUDART_INF_F;  // a NaN counts as unavailable
         }
         if constexpr (GROUPS) {
-            float *const f = reinterpret_cast<float *>(mine);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) f[i] = c[i];
+            for (int q = 0; q < NV / 4; ++q) *reinterpret_cast<float4 *>(mine + 4 * q) = make_float4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]);
             __syncwarp();
-            const float *const all = reinterpret_cast<const float *>(keys + (threadIdx.x - r) * PITCH);
-            const uint32_t keep = kept_groups<L>(all, strength + row_in_block * ROUTE_MAX_GROUPS, A, r, row_lane,
+            const uint32_t keep = kept_groups<L>(keys + (threadIdx.x - r) * PITCH, strength + row_in_block * ROUTE_MAX_GROUPS, A, r, row_lane,
                                                  [](int e) { return e / NV * PITCH + e % NV; });
             __syncwarp();
             const int size = A.E / A.groups;
@@ -169,42 +184,39 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_forward_kernel(const R
     }
 
     // maxima of the lane's runs of four keys
-    uint32_t run[NV / 4];
-    uint32_t best = 0;
+    float run[NV / 4], best = -CUDART_INF_F;
 #pragma unroll
     for (int q = 0; q < NV / 4; ++q) {
-        const uint4 k4 = make_uint4(route_key(x[4 * q]), route_key(x[4 * q + 1]), route_key(x[4 * q + 2]), route_key(x[4 * q + 3]));
-        *reinterpret_cast<uint4 *>(mine + 4 * q) = k4;
-        run[q] = max(max(k4.x, k4.y), max(k4.z, k4.w));
-        best = max(best, run[q]);
+        const float4 k4 = make_float4(route_key(x[4 * q]), route_key(x[4 * q + 1]), route_key(x[4 * q + 2]), route_key(x[4 * q + 3]));
+        *reinterpret_cast<float4 *>(mine + 4 * q) = k4;
+        run[q] = fmaxf(fmaxf(k4.x, k4.y), fmaxf(k4.z, k4.w));
+        best = fmaxf(best, run[q]);
     }
-    int *const out = choice + row_in_block * ROUTE_MAX_K;
+    short *const out = choice + row_in_block * ROUTE_MAX_K;
     for (int j = 0; j < A.k; ++j) {
-        uint32_t m = best;
-#pragma unroll
-        for (int o = L / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(FULL, m, o));
+        const float m = row_max_f<L>(best);
         const uint32_t bal = __ballot_sync(FULL, best == m);
         const uint32_t owners = (L == 32) ? bal : (bal >> row_lane) & ((1u << (L & 31)) - 1u);
         if (r == __ffs(owners) - 1) {
             int e = -1;
-            if (m != 0u) {
+            if (m > -CUDART_INF_F) {
                 int q = NV / 4 - 1;
 #pragma unroll
                 for (int i = NV / 4 - 2; i >= 0; --i) q = run[i] == m ? i : q;
-                uint4 k4 = *reinterpret_cast<const uint4 *>(mine + 4 * q);
+                const float4 k4 = *reinterpret_cast<const float4 *>(mine + 4 * q);
+                // the run's first largest goes: the largest of the others stays
+                const float lo = fmaxf(k4.z, k4.w), next = k4.x == m ? fmaxf(k4.y, lo) : k4.y == m ? fmaxf(k4.x, lo) : fmaxf(fmaxf(k4.x, k4.y), k4.z == m ? k4.w : k4.z);
                 const int v = k4.x == m ? 0 : k4.y == m ? 1 : k4.z == m ? 2 : 3;
-                mine[4 * q + v] = 0u;
-                k4.x = v == 0 ? 0u : k4.x, k4.y = v == 1 ? 0u : k4.y, k4.z = v == 2 ? 0u : k4.z, k4.w = v == 3 ? 0u : k4.w;
-                const uint32_t next = max(max(k4.x, k4.y), max(k4.z, k4.w));
-                best = 0;
+                mine[4 * q + v] = -CUDART_INF_F;
+                best = -CUDART_INF_F;
 #pragma unroll
                 for (int i = 0; i < NV / 4; ++i) {
                     run[i] = i == q ? next : run[i];
-                    best = max(best, run[i]);
+                    best = fmaxf(best, run[i]);
                 }
                 e = first + 4 * q + v;
             }
-            out[j] = e;
+            out[j] = (short)e;
         }
     }
     __syncwarp();
