@@ -35,6 +35,8 @@ struct ExpertsArgs {
     unsigned long long wait_ns;     // bound of every wait
     int E, D, F, k, tokens;
     int keep;                       // GATE_UP: store g and u
+    int row_tiles;                  // row tiles that the batch may need at most; those it does not need have tile_expert -1
+    int early;                      // the tables were complete before the previous kernel of the stream began
     int hold;                       // test hook: the producer brings nothing, so the waits run out
 };
 
@@ -256,12 +258,13 @@ struct ExpertsShape {
     static constexpr int A_BYTES = KS * A_SUB, B_BYTES = KS * B_SUB, STAGE = A_BYTES + B_BYTES;
     static constexpr int SLAB = 4096;                                        // 32 rows x 64 columns of results of one epilogue warp
     static constexpr int SLABS = MODE == GATE_UP ? 3 : MODE == DH ? 4 : 2;   // per warp
-    static constexpr int FIT = (229376 - 4 * SLABS * SLAB) / STAGE;
+    static constexpr int WARPS = ROWS < 32 ? 1 : ROWS / 32;                  // epilogue warps with rows
+    static constexpr int FIT = (229376 - WARPS * SLABS * SLAB) / STAGE;
     static constexpr int STAGES = FIT < 12 ? FIT : 12;
     static constexpr int ACC = 2;  // accumulators: one is finished while the next is computed
     static constexpr int TMEM = ACC * BN;
     static constexpr int NSTEP = MODE == GATE_UP ? BN / 2 : BN;  // output columns of a tile
-    static constexpr int SMEM = STAGES * STAGE + 4 * SLABS * SLAB + 1024 + 512;
+    static constexpr int SMEM = STAGES * STAGE + WARPS * SLABS * SLAB + 1024 + 512;
     // the A ring comes first: M = 128 rows read from its last stage stay inside the B ring behind it
     static_assert(STAGES >= 2 && STAGES * B_BYTES >= 16384 - A_SUB && TMEM <= 512 && NSTEP % 64 == 0, "tile does not fit");
 };
@@ -279,7 +282,7 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
     constexpr bool PAIR = S::PAIR;
     extern __shared__ uint8_t raw[];
     const uint32_t ring_a = (smem_u32(raw) + 1023) & ~1023u, ring_b = ring_a + S::STAGES * S::A_BYTES;
-    const uint32_t slabs = ring_b + S::STAGES * S::B_BYTES, bars = slabs + 4 * S::SLABS * S::SLAB;
+    const uint32_t slabs = ring_b + S::STAGES * S::B_BYTES, bars = slabs + S::WARPS * S::SLABS * S::SLAB;
     const uint32_t full = bars, empty = full + 8 * S::STAGES, acc_full = empty + 8 * S::STAGES, acc_empty = acc_full + 8 * S::ACC,
                    drain = acc_empty + 8 * S::ACC, loaded = drain + 8;  // loaded: DH, two per epilogue warp
     __shared__ uint32_t tmem_at;
@@ -297,6 +300,11 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
     }
+    if (tid == 96) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.out) : "memory");
+    }
     if (warp == 2) {
         if constexpr (PAIR) {
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_at)), "n"(S::TMEM) : "memory");
@@ -311,18 +319,22 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
     if constexpr (PAIR) cluster_barrier();
     tc_fence_after();
     const uint32_t tmem = tmem_at;
-    pdl_wait();
+    // Weights may be brought while the previous kernel still writes the other operand: the producer waits for that kernel
+    // behind its first copies of weights.  The next kernel may be scheduled from here on; it waits for this one in turn.
+    const bool early = !S::WGRAD && P.early && warp == 0;
+    if (!early) pdl_wait();
+    if (tid == 64) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     constexpr int MT = PAIR ? 256 : 128;                                           // output rows of a weight gradient's tile
     const int M = MODE == DW_DOWN ? P.D : 2 * P.F;                                 // weight gradients only
     const int N = (MODE == DOWN || MODE == DX || MODE == DW_GATE_UP) ? P.D : P.F;  // output columns
     const int K = (MODE == GATE_UP || MODE == DH) ? P.D : MODE == DOWN ? P.F : 2 * P.F;
-    const int nts = (N + S::NSTEP - 1) / S::NSTEP, mts = S::WGRAD ? (M + MT - 1) / MT : __ldg(P.offsets + P.E) / AR;
+    const int nts = (N + S::NSTEP - 1) / S::NSTEP, mts = S::WGRAD ? (M + MT - 1) / MT : P.row_tiles;
     const int64_t tiles = S::WGRAD ? (int64_t)P.E * mts * nts : (int64_t)mts * nts;
     const int64_t tile0 = PAIR ? blockIdx.x / 2 : blockIdx.x, tile_step = PAIR ? gridDim.x / 2 : gridDim.x;
 
     struct Tile {
-        int e, m0, n0, kb, nkb;  // expert, first slot (or output row), first output column, first slot of the contraction, stages
+        int e, m0, n0, kb, nkb;  // expert (-1: no tile from here on), first slot (or output row), first output column, first slot of the contraction, stages
     };
     auto tile_at = [&](int64_t i) {
         Tile t;
@@ -335,7 +347,7 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
             t.kb = __ldg(P.offsets + t.e);
             t.nkb = (__ldg(P.offsets + t.e + 1) - t.kb) / 64;
         } else {
-            t.e = __ldg(P.tile_expert + rest);
+            t.e = __ldcg(P.tile_expert + rest);  // past L1: it may be read before griddepcontrol.wait
             t.m0 = (int)rest * AR + (int)rank * 128;
             t.kb = 0;
             t.nkb = (K + 64 * KS - 1) / (64 * KS);  // columns beyond K read as zeros
@@ -357,59 +369,93 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
             else tma_load_3d(dst, map, x, y, z, bar);
         };
         // The next tile's expert and tokens are on their way while this tile's copies are issued.
-        Tile next = {};
+        Tile next;
+        next.e = -1;
         int4 entries = make_int4(0, 0, 0, 0);
         auto look_ahead = [&](int64_t i) {
-            if (i >= tiles) return;
-            next = tile_at(i);
+            if (i < tiles) next = tile_at(i);
+            else next.e = -1;
             if constexpr (S::A_GATHER)  // four neighbouring slots per lane
-                if (lane < AR / 4) entries = __ldg(reinterpret_cast<const int4 *>(P.entry_of + next.m0 + 4 * lane));
+                if (i < tiles && lane < AR / 4) entries = __ldg(reinterpret_cast<const int4 *>(P.entry_of + next.m0 + 4 * lane));
         };
         look_ahead(tile0);
+        int4 rows = make_int4(0, 0, 0, 0);  // the tile's tokens; holes give a row beyond the matrix, which reads as zeros
+        int fours = 0;                      // fours of slots with a token, from the tile's start; the others' rows keep what they hold
+        auto bring_a = [&](const Tile &t, int kb, uint32_t s, uint32_t bar) {
+            const uint32_t a = ring_a + s * S::A_BYTES;
+            if constexpr (S::WGRAD) {
+                if (lane < 2) load_2d(a + lane * 8192, &maps.a, t.m0 + lane * 64, t.kb + kb * 64, bar);
+            } else {
+#pragma unroll
+                for (int q = 0; q < KS; ++q) {
+                    const int k0 = (kb * KS + q) * 64;
+                    if constexpr (S::A_GATHER) {
+                        if (lane < fours) tma_gather4(a + q * S::A_SUB + lane * 512, &maps.a, k0, rows, bar);
+                    } else {
+                        if (lane == 0) load_2d(a + q * S::A_SUB, &maps.a, k0, t.m0, bar);
+                    }
+                }
+            }
+        };
+        auto bring_b = [&](const Tile &t, int kb, uint32_t s, uint32_t bar) {
+            const uint32_t b = ring_b + s * S::B_BYTES;
+            const int n0 = t.n0 + (int)rank * S::COLS;  // of this block; GATE_UP: see below
+            if constexpr (S::WGRAD) {
+                if (lane >= 2 && lane < 2 + S::COLS / 64)
+                    load_2d(b + (lane - 2) * 8192, &maps.b, n0 + (lane - 2) * 64, t.kb + kb * 64, bar);
+            } else {
+#pragma unroll
+                for (int q = 0; q < KS; ++q) {
+                    const int k0 = (kb * KS + q) * 64;
+                    const uint32_t bq = b + q * S::B_SUB;
+                    if constexpr (MODE == GATE_UP) {  // gate rows, then up rows; a pair's blocks bring one kind each
+                        if constexpr (PAIR) {
+                            if (lane == 0) load_3d(bq, &maps.b, k0, t.n0, 2 * t.e + (int)rank, bar);
+                        } else {
+                            if (lane < 2) load_3d(bq + lane * (S::B_SUB / 2), &maps.b, k0, t.n0, 2 * t.e + lane, bar);
+                        }
+                    } else if constexpr (MODE == DOWN) {
+                        if (lane == 0) load_3d(bq, &maps.b, k0, n0, t.e, bar);
+                    } else {
+                        if (lane < S::COLS / 64) load_3d(bq + lane * 8192, &maps.b, n0 + lane * 64, k0, t.e, bar);
+                    }
+                }
+            }
+        };
+        auto barrier_of = [&](uint32_t s) { return PAIR ? in_block(full + 8 * s, 0) : full + 8 * s; };  // a pair's first block counts for both
+        auto announce = [&](uint32_t s) {
+            const uint32_t bytes = S::A_GATHER ? KS * 512 * fours + S::B_BYTES : S::STAGE;
+            if (lane == 0 && rank == 0) mbar_expect_tx(full + 8 * s, PAIR ? 2 * bytes : bytes);
+            __syncwarp();
+        };
+        look_ahead(tile0);
+        int ahead = 0;  // stages of the first tile that have their weights already
+        if (early) {
+            if (next.e >= 0 && !P.hold)
+                for (; ahead < next.nkb && ahead < S::STAGES; ++ahead) {
+                    announce(ahead);
+                    bring_b(next, ahead, ahead, barrier_of(ahead));
+                }
+            pdl_wait();
+        }
         for (int64_t i = tile0; i < tiles && ok; i += tile_step) {
             const Tile t = next;
-            int4 rows = make_int4(0, 0, 0, 0);  // their tokens; holes give a row beyond the matrix, which reads as zeros
-            if constexpr (S::A_GATHER)
+            if (t.e < 0) break;
+            if constexpr (S::A_GATHER) {
                 rows = make_int4(entries.x < 0 ? P.tokens : entries.x / P.k, entries.y < 0 ? P.tokens : entries.y / P.k,
                                  entries.z < 0 ? P.tokens : entries.z / P.k, entries.w < 0 ? P.tokens : entries.w / P.k);
+                fours = __popc(__ballot_sync(FULL, lane < AR / 4 && entries.x >= 0));  // a tile's entries come before its holes
+            }
             look_ahead(i + tile_step);
             for (int kb = 0; kb < t.nkb; ++kb, ++fill) {
                 const uint32_t s = fill % S::STAGES, phase = (fill / S::STAGES) & 1;
                 ok = waits.wait(empty + 8 * s, phase ^ 1);
                 ok = __all_sync(FULL, ok);
                 if (!ok || P.hold) break;
-                const uint32_t a = ring_a + s * S::A_BYTES, b = ring_b + s * S::B_BYTES;
-                const uint32_t bar = PAIR ? in_block(full + 8 * s, 0) : full + 8 * s;  // the pair's first block counts for both
-                if (lane == 0 && rank == 0) mbar_expect_tx(full + 8 * s, PAIR ? 2 * S::STAGE : S::STAGE);
-                __syncwarp();
-                if constexpr (S::WGRAD) {
-                    const int slot = t.kb + kb * 64, n0 = t.n0 + (int)rank * S::COLS;
-                    if (lane < 2) load_2d(a + lane * 8192, &maps.a, t.m0 + lane * 64, slot, bar);
-                    if (lane >= 2 && lane < 2 + S::COLS / 64) load_2d(b + (lane - 2) * 8192, &maps.b, n0 + (lane - 2) * 64, slot, bar);
-                } else {
-#pragma unroll
-                    for (int q = 0; q < KS; ++q) {
-                        const int k0 = (kb * KS + q) * 64;
-                        const uint32_t aq = a + q * S::A_SUB, bq = b + q * S::B_SUB;
-                        if constexpr (S::A_GATHER) {
-                            if (lane < AR / 4) tma_gather4(aq + lane * 512, &maps.a, k0, rows, bar);
-                        } else {
-                            if (lane == 0) load_2d(aq, &maps.a, k0, t.m0, bar);
-                        }
-                        if constexpr (MODE == GATE_UP) {  // gate rows, then up rows; a pair's blocks bring one kind each
-                            if constexpr (PAIR) {
-                                if (lane == 0) load_3d(bq, &maps.b, k0, t.n0, 2 * t.e + (int)rank, bar);
-                            } else {
-                                if (lane < 2) load_3d(bq + lane * (S::B_SUB / 2), &maps.b, k0, t.n0, 2 * t.e + lane, bar);
-                            }
-                        } else if constexpr (MODE == DOWN) {
-                            if (lane == 0) load_3d(bq, &maps.b, k0, t.n0 + (int)rank * S::COLS, t.e, bar);
-                        } else {
-                            if (lane < S::COLS / 64)
-                                load_3d(bq + lane * 8192, &maps.b, t.n0 + (int)rank * S::COLS + lane * 64, k0, t.e, bar);
-                        }
-                    }
-                }
+                const bool there = (int)fill < ahead;
+                if (!there) announce(s);
+                bring_a(t, kb, s, barrier_of(s));
+                if (!there) bring_b(t, kb, s, barrier_of(s));
             }
             if (P.hold) break;
         }
@@ -431,6 +477,7 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
             bool ok = true, any = false;
             for (int64_t i = tile0; i < tiles && ok; i += tile_step) {
                 const Tile t = tile_at(i);
+                if (t.e < 0) break;
                 if (t.nkb == 0) continue;
                 const uint32_t buf = it % S::ACC, phase = (it / S::ACC) & 1;
                 ++it;
@@ -498,6 +545,7 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
         };
         for (int64_t i = tile0; i < tiles; i += tile_step) {
             const Tile t = tile_at(i);
+            if (t.e < 0) break;
             const uint32_t buf = it % S::ACC, phase = (it / S::ACC) & 1;
             int entry = -1;
             float w = 0.f, dot = 0.f;
@@ -642,6 +690,117 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
     }
 }
 
+// ------------------------------------------------------------- a few tokens ----
+// One or a few tokens: every weight is used once, so the products are streams of weights at memory speed and the tensor core
+// has nothing to add.  Each lane keeps eight or more 16-byte loads in flight; a token's choices are finished in one warp, so
+// there is neither a table of slots to combine nor a rounding per slot.
+template <typename T>
+__device__ __forceinline__ float dot8(const uint4 &a, const uint4 &b, float sum)
+{
+    float2 x[4], y[4], s = make_float2(sum, 0.f);
+    Io<T>::unpack2(a, x);
+    Io<T>::unpack2(b, y);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = fma2(x[i], y[i], s);
+    return s.x + s.y;
+}
+__device__ __forceinline__ float warp_total(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+    return v;
+}
+
+// hw[entry][f] = w silu(g) u.  A block has FEW_FEATURES features of one entry (so its expert is looked up once), a warp one
+// feature at a time: sixteen loads of its two rows at once, 16 warps per SM, 128 KB on their way.  (Three blocks per SM spill and
+// are no faster; 8, 32 or 64 features a block are within 5 %.)
+constexpr int FEW_FEATURES = 16;
+template <typename T>
+__global__ void __launch_bounds__(256, 2) experts_few_gate_up_kernel(const T *x, int64_t stride, const T *w_gate_up, const float *w,
+                                                                     const int32_t *slot_of, const int32_t *tile_expert, int shift, T *hw, int k,
+                                                                     int D, int F)
+{
+    pdl_wait();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x & 31, entry = blockIdx.y;
+    const int slot = __ldg(slot_of + entry);
+    if (slot < 0) return;  // dropped: the second product skips it too
+    const int64_t e = __ldg(tile_expert + (slot >> shift));
+    const T *const xt = x + entry / k * stride;
+    const float scale = __ldg(w + entry);
+    const int f1 = min(F, (int)(blockIdx.x + 1) * FEW_FEATURES);
+    for (int f = blockIdx.x * FEW_FEATURES + (threadIdx.x >> 5); f < f1; f += 8) {
+        const T *const gate = w_gate_up + (e * 2 * F + f) * D, *const up = gate + (int64_t)F * D;
+        float g = 0.f, u = 0.f;
+        for (int c = 8 * lane; c < D; c += 2048) {
+            uint4 a[8], b[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool in = c + 256 * i < D;
+                a[i] = in ? __ldcs(reinterpret_cast<const uint4 *>(gate + c + 256 * i)) : Io<T>::zero();
+                b[i] = in ? __ldcs(reinterpret_cast<const uint4 *>(up + c + 256 * i)) : Io<T>::zero();
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + 256 * i < D) {
+                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(xt + c + 256 * i));
+                    g = dot8<T>(a[i], v, g);
+                    u = dot8<T>(b[i], v, u);
+                }
+        }
+        g = warp_total(g), u = warp_total(u);
+        if (lane == 0) Io<T>::store1(hw + (int64_t)entry * F + f, scale * (g * sigmoid_fast(g) * u));
+    }
+}
+
+// y[t][d] = sum over the token's choices of <W_down[e][d], hw>.  A block has four values of d, a warp every eighth choice: four
+// rows in steps of 1024, sixteen loads at once, the first of them before the activations are there.  The warps' sums are added
+// in order.
+template <typename T>
+__global__ void __launch_bounds__(256, 3) experts_few_down_kernel(const T *w_down, const T *hw, const int32_t *slot_of, const int32_t *tile_expert,
+                                                                  int shift, T *y, int k, int D, int F)
+{
+    __shared__ float part[8][4];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = blockIdx.y, d = 4 * blockIdx.x;  // D is a multiple of 8
+    float sum[4] = {};
+    bool waited = false;
+    for (int j = warp; j < k; j += 8) {
+        const int slot = __ldcg(slot_of + (int64_t)t * k + j);
+        if (slot < 0) continue;
+        const int64_t e = __ldcg(tile_expert + (slot >> shift));
+        const T *const rows = w_down + (e * D + d) * F, *const v = hw + ((int64_t)t * k + j) * F;
+        for (int c = 8 * lane; c < F; c += 1024) {
+            uint4 a[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    a[r][i] = c + 256 * i < F ? __ldcs(reinterpret_cast<const uint4 *>(rows + (int64_t)r * F + c + 256 * i)) : Io<T>::zero();
+            if (!waited) pdl_wait(), waited = true;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (c + 256 * i < F) {
+                    const uint4 h = __ldg(reinterpret_cast<const uint4 *>(v + c + 256 * i));
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sum[r] = dot8<T>(a[r][i], h, sum[r]);
+                }
+        }
+    }
+    if (!waited) pdl_wait();
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        sum[r] = warp_total(sum[r]);
+        if (lane == 0) part[warp][r] = sum[r];
+    }
+    __syncthreads();
+    if (threadIdx.x < 4) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += part[i][threadIdx.x];
+        Io<T>::store1(y + (int64_t)t * D + d + threadIdx.x, s);
+    }
+}
+
 // Rows of a matrix in slot order, a warp per slot; holes become zeros.  Bound by memory: it writes 2 D bytes a slot and reads
 // every token's row once from HBM, k - 1 times from L2.
 template <typename T>
@@ -649,6 +808,7 @@ __global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t
                                                              int k, int D)
 {
     pdl_wait();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const int64_t slot = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (slot >= __ldg(used)) return;
@@ -673,6 +833,7 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(const T *slots, co
                                                               const float *partial, T *grad_w, int64_t tokens, int k, int D, int nts)
 {
     pdl_wait();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int per = D / 8;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t t = id / per;

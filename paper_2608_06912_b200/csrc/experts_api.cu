@@ -269,9 +269,15 @@ int begin_call(const lapsum_experts_dims *p, const void *dispatch, size_t dispat
     c.A.offsets = reinterpret_cast<const int32_t *>(d + c.X.d.off_offsets);
     c.A.status = reinterpret_cast<uint32_t *>(ws);
     c.A.wait_ns = 2000000000ull;
+    c.A.row_tiles = (int)c.X.d.tiles;
     c.A.E = (int)p->experts, c.A.D = (int)p->d, c.A.F = (int)p->f, c.A.k = p->k, c.A.tokens = (int)p->tokens;
     return LAPSUM_OK;
 }
+
+// Up to this many tokens the products run without the tensor core.  Measured (bf16, 8 of 64 experts, 2048 x 1024): one token 28 us
+// against 36 us on tiles, 2: 45 / 51, 4: 74 / 73, 6: 108 / 93 (tokens begin to share experts); 2 of 32 experts, 1024 x 1024:
+// 4: 22 / 27, 8: 35 / 35.
+constexpr int64_t FEW_TOKENS = 4;
 
 // One of the four products whose rows are slots
 template <int MODE, typename T>
@@ -326,6 +332,17 @@ int forward_t(Call &c, const void *x, int64_t x_stride, const void *w_gate_up, c
     const int dt = p.io_dtype, rows = p.tile_rows < 128 ? p.tile_rows : 128, out_rows = rows < 32 ? rows : 32;
     const int64_t cap = c.X.d.capacity;
     const bool pair = p.tile_rows == 256;
+    if (!saved && !hold && p.tokens <= FEW_TOKENS) {
+        const int32_t *slot_of = reinterpret_cast<const int32_t *>(dispatch + c.X.d.off_slot_of);
+        T *hw = reinterpret_cast<T *>(c.ws + c.X.off_hw);
+        int shift = 4;
+        while ((1 << shift) < p.tile_rows) ++shift;
+        RUN(launch_pdl(experts_few_gate_up_kernel<T>, dim3((unsigned)ceil_div(p.f, FEW_FEATURES), (unsigned)(p.tokens * p.k)), 256, 0, st,
+                       static_cast<const T *>(x), x_stride, static_cast<const T *>(w_gate_up), w, slot_of, c.A.tile_expert, shift, hw, (int)p.k,
+                       (int)p.d, (int)p.f));
+        return launch_pdl(experts_few_down_kernel<T>, dim3((unsigned)(p.d / 4), (unsigned)p.tokens), 256, 0, st, static_cast<const T *>(w_down),
+                          hw, slot_of, c.A.tile_expert, shift, static_cast<T *>(y), (int)p.k, (int)p.d, (int)p.f);
+    }
     uint8_t *rowbuf = c.ws + c.X.off_slots;  // in turn: x in slot order, the second product's results
     void *hw = saved ? saved + c.X.off_hw_saved : c.ws + c.X.off_hw;
     ExpertsMaps m;
@@ -344,6 +361,7 @@ int forward_t(Call &c, const void *x, int64_t x_stride, const void *w_gate_up, c
     A.w = w;
     A.keep = saved != nullptr;
     A.hold = hold;
+    A.early = rows > GATHER_ROWS && !hold;  // the gather came between
     RUN((run_rows<GATE_UP, T>(c, m, A, p.f, wide, st)));
     if (hold) return LAPSUM_OK;
 
@@ -351,7 +369,9 @@ int forward_t(Call &c, const void *x, int64_t x_stride, const void *w_gate_up, c
     RUN(map_2d(&m.a, dt, hw, p.f, cap, p.f, rows));
     RUN(map_3d(&m.b, dt, w_down, p.f, p.d, p.experts, wide && !pair ? 256 : 128));
     RUN(map_2d(&m.out, dt, rowbuf, p.d, cap, p.d, out_rows));
-    RUN((run_rows<DOWN, T>(c, m, c.A, p.d, wide, st)));
+    A = c.A;
+    A.early = 1;
+    RUN((run_rows<DOWN, T>(c, m, A, p.d, wide, st)));
     return combine<T>(c, dispatch, y, p.d, nullptr, nullptr, st);
 }
 
@@ -374,7 +394,7 @@ int backward_t(Call &c, const void *grad_y, int64_t gy_stride, const void *x, in
     RUN(map_gu(&m.out, dt, dgu, p.f, cap, 32));
     RUN(map_gu(&m.gu, dt, saved + c.X.off_gu_saved, p.f, cap, 32));
     ExpertsArgs A = c.A;
-    A.w = w, A.partial = partial;
+    A.w = w, A.partial = partial, A.early = 1;
     RUN((run_rows<DH, T>(c, m, A, p.f, c.X.wide_dh, st)));
 
     RUN(map_2d(&m.a, dt, rowbuf, p.d, cap, p.d, 64));
@@ -391,7 +411,9 @@ int backward_t(Call &c, const void *grad_y, int64_t gy_stride, const void *x, in
     RUN(map_2d(&m.a, dt, dgu, 2 * p.f, cap, 2 * p.f, rows));
     RUN(map_3d(&m.b, dt, w_gate_up, p.d, 2 * p.f, p.experts, 64));
     RUN(map_2d(&m.out, dt, rowbuf, p.d, cap, p.d, 32));
-    RUN((run_rows<DX, T>(c, m, c.A, p.d, wide_tiles(&p, c.X.d, p.d, false), st)));
+    A = c.A;
+    A.early = 1;
+    RUN((run_rows<DX, T>(c, m, A, p.d, wide_tiles(&p, c.X.d, p.d, false), st)));
     return combine<T>(c, dispatch, grad_x, p.d, partial, grad_w, st);
 }
 
@@ -462,8 +484,9 @@ int lapsum_dispatch(const int32_t *idx, int64_t tokens, int32_t k, int64_t exper
     A.E = (int)experts, A.rows = tile_rows;
     A.chunks = (int)ceil_div(A.entries, DISPATCH_CHUNK);
     if (A.chunks < 1) A.chunks = 1;
-    A.bits = 1;
-    while ((1 << A.bits) <= (int)experts) ++A.bits;  // values 0 .. experts
+    const auto place = experts <= 128 ? dispatch_place_kernel<7> : experts <= 256 ? dispatch_place_kernel<8> : dispatch_place_kernel<10>;
+    const size_t smem = dispatch_place_smem((int)experts);
+    if (smem > 48 * 1024) CU_OK(cudaFuncSetAttribute(place, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     A.counts = reinterpret_cast<int32_t *>(d + L.off_counts), A.offsets = reinterpret_cast<int32_t *>(d + L.off_offsets);
     A.slot_of = reinterpret_cast<int32_t *>(d + L.off_slot_of), A.entry_of = reinterpret_cast<int32_t *>(d + L.off_entry_of);
     A.tile_expert = reinterpret_cast<int32_t *>(d + L.off_tile_expert), A.partial = reinterpret_cast<int32_t *>(d + L.off_partial);
@@ -471,8 +494,7 @@ int lapsum_dispatch(const int32_t *idx, int64_t tokens, int32_t k, int64_t exper
     if (A.chunks > 1) RUN(launch_pdl(dispatch_count_kernel, (unsigned)A.chunks, DISPATCH_THREADS, 4 * (size_t)dispatch_stride((int)experts), st, A));
     A.shift = 4;
     while ((1 << A.shift) < tile_rows) ++A.shift;
-    const size_t smem = 4 * (size_t)(DISPATCH_THREADS / 32 + 3) * (size_t)dispatch_stride((int)experts) + 16;
-    return launch_pdl(dispatch_place_kernel, (unsigned)A.chunks, DISPATCH_THREADS, smem, st, A);
+    return launch_pdl(place, (unsigned)A.chunks, DISPATCH_THREADS, smem, st, A);
 }
 
 int lapsum_experts_describe(const lapsum_experts_dims *dims, lapsum_experts_layout *out)

@@ -11,10 +11,10 @@ int cuda_fail(cudaError_t e);  // remembers e for lapsum_last_cuda_error, return
 int post_launch();             // counts a launch and picks up its error
 
 template <typename... KArgs, typename... Args>
-int launch_clusters(unsigned cluster, void (*kernel)(KArgs...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, const Args &...args)
+int launch_clusters(unsigned cluster, void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, const Args &...args)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
@@ -34,7 +34,7 @@ int launch_clusters(unsigned cluster, void (*kernel)(KArgs...), unsigned grid, u
 }
 
 template <typename... KArgs, typename... Args>
-int launch_pdl(void (*kernel)(KArgs...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, const Args &...args)
+int launch_pdl(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, const Args &...args)
 {
     return launch_clusters(1, kernel, grid, block, smem, st, args...);
 }

@@ -398,91 +398,117 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_backward_dense_kernel(
 }
 
 // ------------------------------------------------------------------ dispatch ----
-constexpr int DISPATCH_THREADS = 256, DISPATCH_CHUNK = 4096;  // entries per block; a warp takes 512 neighbours
+// A block takes 4096 neighbouring entries, a warp 128 of them; a batch of up to 4096 entries needs one launch of one block.  The
+// kernel is bound by its instructions (one block per SM, IPC 2 to 2.5), so 65536 x 8 entries are spread over 128 blocks.
+constexpr int DISPATCH_THREADS = 1024, DISPATCH_WARPS = DISPATCH_THREADS / 32, DISPATCH_PER = 4, DISPATCH_CHUNK = DISPATCH_THREADS * DISPATCH_PER;
 __host__ __device__ constexpr int dispatch_stride(int E) { return (E + 3) & ~3; }  // words of one row of counts: 16-byte rows
+__host__ __device__ constexpr int dispatch_pitch(int E) { return (E / 2 * 2 + 2) | ((E / 2 + 1) % 2 ? 0 : 2); }  // 16-bit counts of a warp: an odd number of words
+constexpr size_t dispatch_place_smem(int E) { return 12 * (size_t)dispatch_stride(E) + 16 + 2 * (size_t)DISPATCH_WARPS * (size_t)dispatch_pitch(E); }
 
 struct DispatchArgs {
     const int32_t *idx;
     int64_t entries, capacity;
-    int E, rows, shift, chunks, bits;  // rows = 1 << shift
+    int E, rows, shift, chunks;  // rows = 1 << shift
     int32_t *counts, *offsets, *slot_of, *entry_of, *tile_expert, *partial;
 };
 
 // Entries per expert of one chunk (integer atomics in shared memory: the counts do not depend on their order)
 __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_count_kernel(const DispatchArgs A)
 {
-    extern __shared__ int32_t dispatch_sh[];
+    extern __shared__ __align__(16) int32_t dispatch_sh[];
     const int stride = dispatch_stride(A.E);
     for (int e = threadIdx.x; e < stride; e += DISPATCH_THREADS) dispatch_sh[e] = 0;
     pdl_wait();
     __syncthreads();
     const int64_t begin = (int64_t)blockIdx.x * DISPATCH_CHUNK;
-    const int n = (int)min((int64_t)DISPATCH_CHUNK, A.entries - begin);
-#pragma unroll 8
-    for (int i = threadIdx.x; i < n; i += DISPATCH_THREADS) {
-        const int e = __ldg(A.idx + begin + i);
-        if ((unsigned)e < (unsigned)A.E) atomicAdd(dispatch_sh + e, 1);
+    int e[DISPATCH_PER];
+#pragma unroll
+    for (int j = 0; j < DISPATCH_PER; ++j) {
+        const int64_t i = begin + j * DISPATCH_THREADS + threadIdx.x;
+        e[j] = i < A.entries ? __ldg(A.idx + i) : -1;
     }
+#pragma unroll
+    for (int j = 0; j < DISPATCH_PER; ++j)
+        if ((unsigned)e[j] < (unsigned)A.E) atomicAdd(dispatch_sh + e[j], 1);
     __syncthreads();
-    for (int e = threadIdx.x; e < stride; e += DISPATCH_THREADS) A.partial[(int64_t)blockIdx.x * stride + e] = dispatch_sh[e];
+    for (int i = threadIdx.x; i < stride; i += DISPATCH_THREADS) A.partial[(int64_t)blockIdx.x * stride + i] = dispatch_sh[i];
 }
 
-// Positions.  Every block sums the chunks' counts itself (chunks x E words from L2: less than another launch), scans the
-// experts' padded lengths, then gives its entries their slots in order: a warp's 32 entries find their equals by ballot.
+// Positions.  A warp numbers its entries per expert 32 at a time (equals are found by ballot), the block scans the warps'
+// counts of every expert and the experts' padded lengths; with several chunks every block sums the chunks' counts itself
+// (chunks x E words from L2: less than another launch).
+template <int BITS>  // of an expert's number
 __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_place_kernel(const DispatchArgs A)
 {
     extern __shared__ __align__(16) int32_t dispatch_sh[];
-    constexpr int W = DISPATCH_THREADS / 32;
-    const int E = A.E, stride = dispatch_stride(E);
-    int32_t *const hist = dispatch_sh;          // [W][stride]: a warp's entries per expert, then its next slot
-    int32_t *const before = hist + W * stride;  // [stride]: entries of the chunks before this one
-    int32_t *const count = before + stride;     // [stride]: entries of all chunks
-    int32_t *const offset = count + stride;     // [E + 1]
-    __shared__ int32_t scan[W];
+    const int E = A.E, stride = dispatch_stride(E), pitch = dispatch_pitch(E);
+    int32_t *const count = dispatch_sh;      // [stride]: entries of all chunks
+    int32_t *const next = count + stride;    // [stride]: entries of the chunks before this one, then this chunk's first slot
+    int32_t *const offset = next + stride;   // [E + 1]
+    uint16_t *const hist = reinterpret_cast<uint16_t *>(offset + stride + 4);  // [warps][pitch]: a warp's entries, then those of the warps before
+    __shared__ int32_t scan[DISPATCH_WARPS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    for (int i = tid; i < (W + 2) * stride; i += DISPATCH_THREADS) hist[i] = 0;
+    for (int i = tid; i < 2 * stride; i += DISPATCH_THREADS) count[i] = 0;
+    for (int i = tid; i < DISPATCH_WARPS * pitch / 2; i += DISPATCH_THREADS) reinterpret_cast<uint32_t *>(hist)[i] = 0;
     pdl_wait();
-    __syncthreads();
-    const int64_t begin = (int64_t)blockIdx.x * DISPATCH_CHUNK;
-    const int n = max(0, (int)min((int64_t)DISPATCH_CHUNK, A.entries - begin));
-    const int per = (n + 32 * W - 1) / (32 * W) * 32;  // entries of a warp: neighbours, so that the order is kept
-    const int w0 = min(n, warp * per), w1 = min(n, w0 + per);
-#pragma unroll 8
-    for (int i = w0 + lane; i < w1; i += 32) {
-        const int e = __ldg(A.idx + begin + i);
-        if ((unsigned)e < (unsigned)E) {
-            atomicAdd(hist + warp * stride + e, 1);
-            if (A.chunks == 1) atomicAdd(count + e, 1);
-        }
+    const int64_t chunk = (int64_t)blockIdx.x * DISPATCH_CHUNK;
+    const int n = (int)min((int64_t)DISPATCH_CHUNK, A.entries - chunk);
+    const int rounds = (n + DISPATCH_THREADS - 1) / DISPATCH_THREADS;  // of 32 entries per warp: few entries are spread over the warps
+    const int64_t begin = chunk + warp * 32 * rounds + lane;
+    int e[DISPATCH_PER], rank[DISPATCH_PER];
+#pragma unroll
+    for (int j = 0; j < DISPATCH_PER; ++j) {
+        const int v = j < rounds && begin + 32 * j < A.entries ? __ldg(A.idx + begin + 32 * j) : -1;
+        e[j] = (unsigned)v < (unsigned)E ? v : E;  // E: dropped
     }
-    if (A.chunks > 1) {  // four experts of one chunk per load
-        const int quads = stride / 4;
-        const int4 *const p = reinterpret_cast<const int4 *>(A.partial);
-#pragma unroll 8
-        for (int i = tid; i < A.chunks * quads; i += DISPATCH_THREADS) {
-            const int4 v = __ldg(p + i);
-            const int c = i / quads, q = 4 * (i - c * quads);
-            int32_t *const all = count + q, *const b = before + q;
-            if (v.x) atomicAdd(all, v.x);
-            if (v.y) atomicAdd(all + 1, v.y);
-            if (v.z) atomicAdd(all + 2, v.z);
-            if (v.w) atomicAdd(all + 3, v.w);
-            if (c < (int)blockIdx.x) {
-                if (v.x) atomicAdd(b, v.x);
-                if (v.y) atomicAdd(b + 1, v.y);
-                if (v.z) atomicAdd(b + 2, v.z);
-                if (v.w) atomicAdd(b + 3, v.w);
+    __syncthreads();
+    if (A.chunks > 1) {  // a thread has four experts of every `groups`-th chunk
+        const int quads = stride / 4, groups = DISPATCH_THREADS / quads, c0 = tid / quads, q = 4 * (tid - c0 * quads);
+        if (c0 < groups) {
+            int4 all = make_int4(0, 0, 0, 0), b = make_int4(0, 0, 0, 0);
+#pragma unroll 4
+            for (int c = c0; c < A.chunks; c += groups) {
+                const int4 v = __ldg(reinterpret_cast<const int4 *>(A.partial + (int64_t)c * stride + q));
+                all.x += v.x, all.y += v.y, all.z += v.z, all.w += v.w;
+                if (c < (int)blockIdx.x) b.x += v.x, b.y += v.y, b.z += v.z, b.w += v.w;
             }
+            atomicAdd(count + q, all.x), atomicAdd(count + q + 1, all.y), atomicAdd(count + q + 2, all.z), atomicAdd(count + q + 3, all.w);
+            atomicAdd(next + q, b.x), atomicAdd(next + q + 1, b.y), atomicAdd(next + q + 2, b.z), atomicAdd(next + q + 3, b.w);
         }
     }
+    uint16_t *const mine = hist + warp * pitch;
+#pragma unroll
+    for (int j = 0; j < DISPATCH_PER; ++j) {
+        unsigned peers = __ballot_sync(FULL, e[j] < E);
+        if (peers == 0) continue;
+#pragma unroll
+        for (int b = 0; b < BITS; ++b) {
+            const bool bit = (e[j] >> b) & 1;
+            const unsigned bal = __ballot_sync(FULL, bit);
+            peers &= bit ? bal : ~bal;
+        }
+        const int before = __popc(peers & ((1u << lane) - 1u));
+        rank[j] = e[j] < E ? mine[e[j]] + before : 0;
+        __syncwarp();
+        if (e[j] < E && before == 0) mine[e[j]] = (uint16_t)(mine[e[j]] + __popc(peers));
+        __syncwarp();
+    }
     __syncthreads();
-    // exclusive scan of the padded lengths: a thread takes `own` neighbouring experts
-    const int own = (E + DISPATCH_THREADS - 1) / DISPATCH_THREADS;
-    auto padded = [&](int e) { return (count[e] + A.rows - 1) >> A.shift << A.shift; };
-    int sum = 0;
-    for (int j = 0; j < own; ++j)
-        if (tid * own + j < E) sum += padded(tid * own + j);
-    int run = sum;
+    if (tid < E) {  // a thread per expert (E <= threads)
+        int v[DISPATCH_WARPS], run = 0;
+#pragma unroll
+        for (int w = 0; w < DISPATCH_WARPS; ++w) v[w] = hist[w * pitch + tid];
+#pragma unroll
+        for (int w = 0; w < DISPATCH_WARPS; ++w) {
+            hist[w * pitch + tid] = (uint16_t)run;
+            run += v[w];
+        }
+        if (A.chunks == 1) count[tid] = run;
+    }
+    __syncthreads();
+    // exclusive scan of the padded lengths, a thread per expert
+    const int padded = tid < E ? (count[tid] + A.rows - 1) >> A.shift << A.shift : 0;
+    int run = padded;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const int v = __shfl_up_sync(FULL, run, o);
@@ -490,51 +516,31 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_place_kernel(const 
     }
     if (lane == 31) scan[warp] = run;
     __syncthreads();
-    int base = run - sum;
-    for (int w = 0; w < warp; ++w) base += scan[w];
-    for (int j = 0; j < own; ++j) {
-        const int e = tid * own + j;
-        if (e >= E) break;
-        offset[e] = base;
-        int next = base + before[e];
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const int v = hist[w * stride + e];
-            hist[w * stride + e] = next;
-            next += v;
-        }
-        base += padded(e);
-        if (e == E - 1) offset[E] = base;
+    if (tid < E) {
+        int base = run - padded;
+        for (int w = 0; w < warp; ++w) base += scan[w];
+        offset[tid] = base;
+        next[tid] += base;
+        if (tid == E - 1) offset[E] = base + padded;
     }
     __syncthreads();
-    for (int i = w0; i < w1; i += 32) {
-        const int at = i + lane;
-        const int e = at < w1 ? __ldg(A.idx + begin + at) : -1;
-        const bool there = (unsigned)e < (unsigned)E;
-        const uint32_t id = there ? (uint32_t)e : (uint32_t)E;
-        unsigned peers = FULL;
-        for (int b = 0; b < A.bits; ++b) {
-            const bool bit = (id >> b) & 1u;
-            const unsigned bal = __ballot_sync(FULL, bit);
-            peers &= bit ? bal : ~bal;
-        }
-        const int rank = __popc(peers & ((1u << lane) - 1u));
-        int slot = -1;
-        if (there) slot = hist[warp * stride + e] + rank;
-        __syncwarp();
-        if (there && rank == 0) hist[warp * stride + e] += __popc(peers);
-        __syncwarp();
-        if (at < w1) {
-            A.slot_of[begin + at] = slot;
-            if (there) A.entry_of[slot] = (int32_t)(begin + at);
+#pragma unroll
+    for (int j = 0; j < DISPATCH_PER; ++j) {
+        if (j < rounds && begin + 32 * j < A.entries) {
+            int slot = -1;
+            if (e[j] < E) {
+                slot = next[e[j]] + mine[e[j]] + rank[j];
+                A.entry_of[slot] = (int32_t)(begin + 32 * j);
+            }
+            A.slot_of[begin + 32 * j] = slot;
         }
     }
     // the tables' rest: holes of the slots, experts of the row tiles, counts and offsets; a warp per expert
-    for (int e = blockIdx.x * W + warp; e < E; e += gridDim.x * W) {
-        const int lo = offset[e], hi = offset[e + 1], c = count[e];
+    for (int i = blockIdx.x * DISPATCH_WARPS + warp; i < E; i += gridDim.x * DISPATCH_WARPS) {
+        const int lo = offset[i], hi = offset[i + 1], c = count[i];
         for (int s = lo + c + lane; s < hi; s += 32) A.entry_of[s] = -1;
-        for (int r = (lo >> A.shift) + lane; r < (hi >> A.shift); r += 32) A.tile_expert[r] = e;
-        if (lane == 0) A.counts[e] = c, A.offsets[e] = lo;
+        for (int r = (lo >> A.shift) + lane; r < (hi >> A.shift); r += 32) A.tile_expert[r] = i;
+        if (lane == 0) A.counts[i] = c, A.offsets[i] = lo;
     }
     const int all = offset[E];
     if (blockIdx.x == 0 && tid == 0) A.offsets[E] = all;
