@@ -28,7 +28,7 @@ namespace lapsum {
 enum ExpertsMode { GATE_UP = 0, DOWN = 1, DH = 2, DX = 3, DW_DOWN = 4, DW_GATE_UP = 5 };
 
 struct ExpertsArgs {
-    const int32_t *entry_of, *tile_expert, *offsets;
+    const int32_t *entry_of, *tile_expert, *offsets, *counts;
     const float *w;                 // per entry (token, choice)
     float *partial;                 // DH: per slot and column tile, <dh, h>
     uint32_t *status;
@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
             t.e = (int)(rest / mts);
             t.m0 = (int)(rest % mts) * MT + (int)rank * 128;
             t.kb = __ldg(P.offsets + t.e);
-            t.nkb = (__ldg(P.offsets + t.e + 1) - t.kb) / 64;
+            t.nkb = (__ldg(P.counts + t.e) + 63) / 64;  // the last stage's holes are zeros
         } else {
             t.e = __ldcg(P.tile_expert + rest);  // past L1: it may be read before griddepcontrol.wait
             t.m0 = (int)rest * AR + (int)rank * 128;
@@ -801,28 +801,45 @@ __global__ void __launch_bounds__(256, 3) experts_few_down_kernel(const T *w_dow
     }
 }
 
-// Rows of a matrix in slot order, a warp per slot; holes become zeros.  Bound by memory: it writes 2 D bytes a slot and reads
-// every token's row once from HBM, k - 1 times from L2.
+// Rows of a matrix in slot order.  The first blocks have a warp per token and 1024 columns, which reads them once and writes them
+// to the token's slots; the others (backward only: the sums over slots must not meet what a hole's row held) fill the holes below
+// the last used slot with zeros, a warp per four slots.  Bound by the bytes written.
 template <typename T>
-__global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t stride, const int32_t *entry_of, const int32_t *used, T *out,
-                                                             int k, int D)
+__global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t stride, const int32_t *slot_of, const int32_t *entry_of,
+                                                             const int32_t *used, T *out, int64_t tokens, int token_blocks, int k, int D)
 {
     pdl_wait();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31;
-    const int64_t slot = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (slot >= __ldg(used)) return;
-    const int entry = __ldg(entry_of + slot);
-    const uint4 *const from = reinterpret_cast<const uint4 *>(x + (int64_t)(entry < 0 ? 0 : entry / k) * stride);
-    uint4 *const to = reinterpret_cast<uint4 *>(out + slot * D);
-    const int n = D / 8;
-    for (int i = lane; i < n; i += 256) {
-        uint4 v[8];
+    const int lane = threadIdx.x & 31, n = D / 8, parts = (D + 1023) / 1024;
+    const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if ((int)blockIdx.x < token_blocks) {
+        const int64_t t = unit / parts;
+        if (t >= tokens) return;
+        const int i = (int)(unit - t * parts) * 128 + lane;
+        const int mine = lane < k ? __ldg(slot_of + t * k + lane) : -1;
+        const uint4 *const from = reinterpret_cast<const uint4 *>(x + t * stride);
+        uint4 v[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = (entry >= 0 && i + 32 * j < n) ? __ldg(from + i + 32 * j) : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < 4; ++j)
+            if (i + 32 * j < n) v[j] = __ldg(from + i + 32 * j);
+        for (int c = 0; c < k; ++c) {
+            const int slot = __shfl_sync(FULL, mine, c);
+            if (slot < 0) continue;
+            uint4 *const to = reinterpret_cast<uint4 *>(out + (int64_t)slot * D);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (i + 32 * j < n) to[i + 32 * j] = v[j];
+            for (int j = 0; j < 4; ++j)
+                if (i + 32 * j < n) to[i + 32 * j] = v[j];
+        }
+    } else {
+        const int64_t slot0 = (unit - 8 * (int64_t)token_blocks) * 4;
+        if (slot0 >= __ldg(used)) return;  // a multiple of 64
+        const int4 e = __ldg(reinterpret_cast<const int4 *>(entry_of + slot0));
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            if ((s == 0 ? e.x : s == 1 ? e.y : s == 2 ? e.z : e.w) >= 0) continue;
+            uint4 *const to = reinterpret_cast<uint4 *>(out + (slot0 + s) * D);
+            for (int i = lane; i < n; i += 32) to[i] = make_uint4(0, 0, 0, 0);
+        }
     }
 }
 

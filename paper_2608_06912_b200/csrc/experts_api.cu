@@ -267,6 +267,7 @@ int begin_call(const lapsum_experts_dims *p, const void *dispatch, size_t dispat
     c.A.entry_of = reinterpret_cast<const int32_t *>(d + c.X.d.off_entry_of);
     c.A.tile_expert = reinterpret_cast<const int32_t *>(d + c.X.d.off_tile_expert);
     c.A.offsets = reinterpret_cast<const int32_t *>(d + c.X.d.off_offsets);
+    c.A.counts = reinterpret_cast<const int32_t *>(d + c.X.d.off_counts);
     c.A.status = reinterpret_cast<uint32_t *>(ws);
     c.A.wait_ns = 2000000000ull;
     c.A.row_tiles = (int)c.X.d.tiles;
@@ -309,10 +310,12 @@ int run_weights(const Call &c, const ExpertsMaps &maps, int64_t m, int64_t n, cu
 }
 
 template <typename T>
-int gather(const Call &c, const void *x, int64_t stride, cudaStream_t st)
+int gather(const Call &c, const uint8_t *dispatch, const void *x, int64_t stride, bool holes, cudaStream_t st)
 {
-    return launch_pdl(experts_gather_kernel<T>, (unsigned)ceil_div(c.X.d.capacity, 8), 256, 0, st, static_cast<const T *>(x), stride,
-                      c.A.entry_of, c.A.offsets + c.A.E, reinterpret_cast<T *>(c.ws + c.X.off_slots), (int)c.p->k, (int)c.p->d);
+    const int64_t token_blocks = ceil_div(c.p->tokens * ceil_div(c.p->d, 1024), 8), hole_blocks = holes ? ceil_div(c.X.d.capacity, 32) : 0;
+    return launch_pdl(experts_gather_kernel<T>, (unsigned)(token_blocks + hole_blocks), 256, 0, st, static_cast<const T *>(x), stride,
+                      reinterpret_cast<const int32_t *>(dispatch + c.X.d.off_slot_of), c.A.entry_of, c.A.offsets + c.A.E,
+                      reinterpret_cast<T *>(c.ws + c.X.off_slots), c.p->tokens, (int)token_blocks, (int)c.p->k, (int)c.p->d);
 }
 
 template <typename T>
@@ -347,7 +350,7 @@ int forward_t(Call &c, const void *x, int64_t x_stride, const void *w_gate_up, c
     void *hw = saved ? saved + c.X.off_hw_saved : c.ws + c.X.off_hw;
     ExpertsMaps m;
     if (rows > GATHER_ROWS) {
-        if (!hold) RUN(gather<T>(c, x, x_stride, st));
+        if (!hold) RUN(gather<T>(c, dispatch, x, x_stride, false, st));
         RUN(map_2d(&m.a, dt, rowbuf, p.d, cap, p.d, rows));
     } else {
         RUN(map_2d(&m.a, dt, x, p.d, p.tokens, x_stride, 1));
@@ -388,7 +391,7 @@ int backward_t(Call &c, const void *grad_y, int64_t gy_stride, const void *x, in
     float *partial = reinterpret_cast<float *>(c.ws + c.X.off_partial);
     void *rowbuf = c.ws + c.X.off_slots;  // in turn: grad_y in slot order, x in slot order, grad_x per slot
     ExpertsMaps m;
-    RUN(gather<T>(c, grad_y, gy_stride, st));
+    RUN(gather<T>(c, dispatch, grad_y, gy_stride, true, st));
     RUN(map_2d(&m.a, dt, rowbuf, p.d, cap, p.d, rows));
     RUN(map_3d(&m.b, dt, w_down, p.f, p.d, p.experts, 64));
     RUN(map_gu(&m.out, dt, dgu, p.f, cap, 32));
@@ -402,7 +405,7 @@ int backward_t(Call &c, const void *grad_y, int64_t gy_stride, const void *x, in
     RUN(map_3d(&m.out, dt, grad_w_down, p.f, p.d, p.experts, 32));
     RUN((run_weights<DW_DOWN, T>(c, m, p.d, p.f, st)));
 
-    RUN(gather<T>(c, x, x_stride, st));
+    RUN(gather<T>(c, dispatch, x, x_stride, true, st));
     RUN(map_2d(&m.a, dt, dgu, 2 * p.f, cap, 2 * p.f, 64));
     RUN(map_2d(&m.b, dt, rowbuf, p.d, cap, p.d, 64));
     RUN(map_3d(&m.out, dt, grad_w_gate_up, p.d, 2 * p.f, p.experts, 32));
