@@ -257,7 +257,7 @@ struct ExpertsShape {
     static constexpr int A_SUB = ROWS * 128, B_SUB = COLS * 128;             // bytes of one step
     static constexpr int A_BYTES = KS * A_SUB, B_BYTES = KS * B_SUB, STAGE = A_BYTES + B_BYTES;
     static constexpr int SLAB = 4096;                                        // 32 rows x 64 columns of results of one epilogue warp
-    static constexpr int SLABS = MODE == GATE_UP ? 3 : MODE == DH ? 4 : 2;   // per warp
+    static constexpr int SLABS = MODE == DH ? 4 : 2;                         // per warp: one is filled while the other is stored
     static constexpr int WARPS = ROWS < 32 ? 1 : ROWS / 32;                  // epilogue warps with rows
     static constexpr int FIT = (229376 - WARPS * SLABS * SLAB) / STAGE;
     static constexpr int STAGES = FIT < 12 ? FIT : 12;
@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = x[i];
         };
-        uint32_t it = 0, chunk = 0;  // chunk: slabs used so far (DH: pairs)
+        uint32_t it = 0, chunk = 0, used = 0;  // chunk: DH: pairs of slabs used so far; used: slabs
         bool ok = true;
         auto bring = [&](const Tile &t, int c, uint32_t q) {  // DH: g and u of 64 columns into pair q & 1
             const uint32_t at = slab + (q & 1) * 2 * S::SLAB, bar = loaded + 8 * (2 * ew + (q & 1));
@@ -574,35 +574,34 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
 #pragma unroll 1
                 for (int c = 0; c < S::NSTEP && t.n0 + c < N; c += 64, ++chunk) {
                     if constexpr (MODE == GATE_UP) {
-                        // slabs: w h, g, u
-                        if (lane == 0) tma_store_wait_read<0>();
-                        __syncwarp();
+                        // w h, and for the backward g and u, one after the other
+                        for (int what = 0; what < (P.keep ? 3 : 1); ++what) {
+                            const uint32_t at = slab + (used++ & 1) * S::SLAB;
+                            if (lane == 0) tma_store_wait_read<1>();
+                            __syncwarp();
 #pragma unroll
-                        for (int j = 0; j < 64 && c + j < S::NSTEP; j += 16) {
-                            float g[16], u[16], h[16];
-                            tmem_ld16(d + c + j, g);
-                            tmem_ld16(d + BN / 2 + c + j, u);
-                            tmem_wait_ld(g);
-                            tmem_pin(u);
+                            for (int j = 0; j < 64; j += 16) {
+                                float g[16], u[16];
+                                if (what != 2) tmem_ld16(d + c + j, g);
+                                if (what != 1) tmem_ld16(d + BN / 2 + c + j, u);
+                                tmem_wait_ld(g);
+                                tmem_pin(u);
+                                if (what == 0) {
 #pragma unroll
-                            for (int v = 0; v < 16; ++v) h[v] = entry >= 0 ? w * (g[v] * sigmoid_fast(g[v]) * u[v]) : 0.f;
-                            if (mine) {
-                                put(slab, j / 8, h), put(slab, j / 8 + 1, h + 8);
-                                if (P.keep) {
-                                    put(slab + S::SLAB, j / 8, g), put(slab + S::SLAB, j / 8 + 1, g + 8);
-                                    put(slab + 2 * S::SLAB, j / 8, u), put(slab + 2 * S::SLAB, j / 8 + 1, u + 8);
+                                    for (int v = 0; v < 16; ++v) g[v] = entry >= 0 ? w * (g[v] * sigmoid_fast(g[v]) * u[v]) : 0.f;
+                                } else if (what == 2) {
+#pragma unroll
+                                    for (int v = 0; v < 16; ++v) g[v] = u[v];
                                 }
+                                if (mine) put(at, j / 8, g), put(at, j / 8 + 1, g + 8);
                             }
-                        }
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) {
-                            tma_store_2d(&maps.out, slab, t.n0 + c, t.m0 + 32 * ew);
-                            if (P.keep) {
-                                tma_store_3d(&maps.gu, slab + S::SLAB, t.n0 + c, 0, t.m0 + 32 * ew);
-                                tma_store_3d(&maps.gu, slab + 2 * S::SLAB, t.n0 + c, 1, t.m0 + 32 * ew);
+                            fence_async_smem();
+                            __syncwarp();
+                            if (lane == 0) {
+                                if (what == 0) tma_store_2d(&maps.out, at, t.n0 + c, t.m0 + 32 * ew);
+                                else tma_store_3d(&maps.gu, at, t.n0 + c, what - 1, t.m0 + 32 * ew);
+                                tma_store_commit();
                             }
-                            tma_store_commit();
                         }
                     } else if constexpr (MODE == DH) {
                         // the pair of slabs holds g and u and takes dg and du in their place; the other pair is filled meanwhile
@@ -644,7 +643,7 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
                             tma_store_commit();
                         }
                     } else {
-                        const uint32_t at = slab + (chunk & 1) * S::SLAB;
+                        const uint32_t at = slab + (used++ & 1) * S::SLAB;
                         if (lane == 0) tma_store_wait_read<1>();
                         __syncwarp();
 #pragma unroll

@@ -97,6 +97,17 @@ int route_backward_t(const RouteBackArgs &A, cudaStream_t st)
 }
 
 // ---------------------------------------------------------------- dispatch ----
+// chunks of neighbouring entries that one block works off, and the blocks that need
+inline int64_t dispatch_chunks(int64_t entries)
+{
+    const int64_t chunks = (entries + DISPATCH_CHUNK - 1) / DISPATCH_CHUNK;
+    return chunks <= DISPATCH_BLOCKS ? 1 : (chunks + DISPATCH_BLOCKS - 1) / DISPATCH_BLOCKS;
+}
+inline int64_t dispatch_blocks(int64_t entries)
+{
+    const int64_t per = dispatch_chunks(entries) * DISPATCH_CHUNK;
+    return entries <= per ? 1 : (entries + per - 1) / per;
+}
 int dispatch_layout(int64_t tokens, int32_t k, int64_t experts, int32_t rows, lapsum_dispatch_layout *L)
 {
     if (tokens < 0 || k < 1 || k > ROUTE_MAX_K || experts < 1 || experts > ROUTE_MAX_E) return LAPSUM_ERR_SHAPE;
@@ -117,7 +128,7 @@ int dispatch_layout(int64_t tokens, int32_t k, int64_t experts, int32_t rows, la
     L->off_slot_of = take((size_t)entries);
     L->off_entry_of = take((size_t)L->capacity);
     L->off_tile_expert = take((size_t)L->tiles);
-    L->off_partial = take((size_t)((entries + DISPATCH_CHUNK - 1) / DISPATCH_CHUNK * dispatch_stride((int)experts)));
+    L->off_partial = take((size_t)(dispatch_blocks(entries) * dispatch_stride((int)experts)));
     L->bytes = at;
     return LAPSUM_OK;
 }
@@ -137,13 +148,13 @@ constexpr int MIN_TILES = 2 * 148;
 inline bool wide_tiles(const lapsum_experts_dims *p, const lapsum_dispatch_layout &d, int64_t cols, bool gate_up)
 {
     const int step = gate_up ? 128 : 256;
-    return p->tile_rows >= 128 || d.tiles * ((cols + step - 1) / step) >= MIN_TILES;
+    return p->tile_rows == 256 || d.tiles * ((cols + step - 1) / step) >= MIN_TILES;
 }
 
 int experts_layout(const lapsum_experts_dims *p, ExpertsLayout &X, lapsum_experts_layout *out)
 {
     if (!p) return LAPSUM_ERR_NULL;
-    if (p->d < 8 || p->f < 8 || p->d % 8 || p->f % 8 || p->d > 1 << 20 || p->f > 1 << 20) return LAPSUM_ERR_SHAPE;
+    if (p->d < 8 || p->f < 8 || p->d % 8 || p->f % 8 || p->d > 1 << 16 || p->f > 1 << 16) return LAPSUM_ERR_SHAPE;
     if (p->io_dtype != LAPSUM_IO_F16 && p->io_dtype != LAPSUM_IO_BF16) return LAPSUM_ERR_UNSUPPORTED;
     if (p->training != 0 && p->training != 1) return LAPSUM_ERR_PARAM;
     RUN(dispatch_layout(p->tokens, p->k, p->experts, p->tile_rows, &X.d));
@@ -289,7 +300,7 @@ int run_rows(const Call &c, const ExpertsMaps &maps, const ExpertsArgs &P, int64
     const int64_t tiles = c.X.d.tiles * ceil_div(cols, step);
     switch (c.p->tile_rows) {
     case 256: return run_experts<MODE, 256, 256, 1, T>(maps, P, tiles, st);
-    case 128: return run_experts<MODE, 128, 256, 1, T>(maps, P, tiles, st);
+    case 128: return wide ? run_experts<MODE, 128, 256, 1, T>(maps, P, tiles, st) : run_experts<MODE, 128, 128, 1, T>(maps, P, tiles, st);
     case 64: return wide ? run_experts<MODE, 64, 256, 1, T>(maps, P, tiles, st) : run_experts<MODE, 64, 128, 2, T>(maps, P, tiles, st);
     default: break;
     }
@@ -485,8 +496,7 @@ int lapsum_dispatch(const int32_t *idx, int64_t tokens, int32_t k, int64_t exper
     A.idx = idx;
     A.entries = tokens * k, A.capacity = L.capacity;
     A.E = (int)experts, A.rows = tile_rows;
-    A.chunks = (int)ceil_div(A.entries, DISPATCH_CHUNK);
-    if (A.chunks < 1) A.chunks = 1;
+    A.chunks = (int)dispatch_chunks(A.entries), A.blocks = (int)dispatch_blocks(A.entries);
     const auto place = experts <= 128 ? dispatch_place_kernel<7> : experts <= 256 ? dispatch_place_kernel<8> : dispatch_place_kernel<10>;
     const size_t smem = dispatch_place_smem((int)experts);
     if (smem > 48 * 1024) CU_OK(cudaFuncSetAttribute(place, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
@@ -494,10 +504,10 @@ int lapsum_dispatch(const int32_t *idx, int64_t tokens, int32_t k, int64_t exper
     A.slot_of = reinterpret_cast<int32_t *>(d + L.off_slot_of), A.entry_of = reinterpret_cast<int32_t *>(d + L.off_entry_of);
     A.tile_expert = reinterpret_cast<int32_t *>(d + L.off_tile_expert), A.partial = reinterpret_cast<int32_t *>(d + L.off_partial);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (A.chunks > 1) RUN(launch_pdl(dispatch_count_kernel, (unsigned)A.chunks, DISPATCH_THREADS, 4 * (size_t)dispatch_stride((int)experts), st, A));
+    if (A.blocks > 1) RUN(launch_pdl(dispatch_count_kernel, (unsigned)A.blocks, DISPATCH_THREADS, 4 * (size_t)dispatch_stride((int)experts), st, A));
     A.shift = 4;
     while ((1 << A.shift) < tile_rows) ++A.shift;
-    return launch_pdl(place, (unsigned)A.chunks, DISPATCH_THREADS, smem, st, A);
+    return launch_pdl(place, (unsigned)A.blocks, DISPATCH_THREADS, smem, st, A);
 }
 
 int lapsum_experts_describe(const lapsum_experts_dims *dims, lapsum_experts_layout *out)

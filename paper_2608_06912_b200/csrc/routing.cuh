@@ -400,6 +400,8 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_backward_dense_kernel(
 // ------------------------------------------------------------------ dispatch ----
 // A block takes 4096 neighbouring entries, a warp 128 of them; a batch of up to 4096 entries needs one launch of one block.  The
 // kernel is bound by its instructions (one block per SM, IPC 2 to 2.5), so 65536 x 8 entries are spread over 128 blocks.
+// More than DISPATCH_BLOCKS of them are worked off one after the other, so that the blocks' counts stay a small table.
+constexpr int DISPATCH_BLOCKS = 512;
 constexpr int DISPATCH_THREADS = 1024, DISPATCH_WARPS = DISPATCH_THREADS / 32, DISPATCH_PER = 4, DISPATCH_CHUNK = DISPATCH_THREADS * DISPATCH_PER;
 __host__ __device__ constexpr int dispatch_stride(int E) { return (E + 3) & ~3; }  // words of one row of counts: 16-byte rows
 __host__ __device__ constexpr int dispatch_pitch(int E) { return (E / 2 * 2 + 2) | ((E / 2 + 1) % 2 ? 0 : 2); }  // 16-bit counts of a warp: an odd number of words
@@ -408,11 +410,11 @@ constexpr size_t dispatch_place_smem(int E) { return 12 * (size_t)dispatch_strid
 struct DispatchArgs {
     const int32_t *idx;
     int64_t entries, capacity;
-    int E, rows, shift, chunks;  // rows = 1 << shift
+    int E, rows, shift, blocks, chunks;  // rows = 1 << shift; blocks: of `chunks` neighbouring chunks each
     int32_t *counts, *offsets, *slot_of, *entry_of, *tile_expert, *partial;
 };
 
-// Entries per expert of one chunk (integer atomics in shared memory: the counts do not depend on their order)
+// Entries per expert of one block's chunks (integer atomics in shared memory: the counts do not depend on their order)
 __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_count_kernel(const DispatchArgs A)
 {
     extern __shared__ __align__(16) int32_t dispatch_sh[];
@@ -420,54 +422,47 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_count_kernel(const 
     for (int e = threadIdx.x; e < stride; e += DISPATCH_THREADS) dispatch_sh[e] = 0;
     pdl_wait();
     __syncthreads();
-    const int64_t begin = (int64_t)blockIdx.x * DISPATCH_CHUNK;
-    int e[DISPATCH_PER];
+    for (int c = 0; c < A.chunks; ++c) {
+        const int64_t begin = ((int64_t)blockIdx.x * A.chunks + c) * DISPATCH_CHUNK;
+        int e[DISPATCH_PER];
 #pragma unroll
-    for (int j = 0; j < DISPATCH_PER; ++j) {
-        const int64_t i = begin + j * DISPATCH_THREADS + threadIdx.x;
-        e[j] = i < A.entries ? __ldg(A.idx + i) : -1;
+        for (int j = 0; j < DISPATCH_PER; ++j) {
+            const int64_t i = begin + j * DISPATCH_THREADS + threadIdx.x;
+            e[j] = i < A.entries ? __ldg(A.idx + i) : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < DISPATCH_PER; ++j)
+            if ((unsigned)e[j] < (unsigned)A.E) atomicAdd(dispatch_sh + e[j], 1);
     }
-#pragma unroll
-    for (int j = 0; j < DISPATCH_PER; ++j)
-        if ((unsigned)e[j] < (unsigned)A.E) atomicAdd(dispatch_sh + e[j], 1);
     __syncthreads();
     for (int i = threadIdx.x; i < stride; i += DISPATCH_THREADS) A.partial[(int64_t)blockIdx.x * stride + i] = dispatch_sh[i];
 }
 
 // Positions.  A warp numbers its entries per expert 32 at a time (equals are found by ballot), the block scans the warps'
-// counts of every expert and the experts' padded lengths; with several chunks every block sums the chunks' counts itself
-// (chunks x E words from L2: less than another launch).
+// counts of every expert and, once, the experts' padded lengths; with several blocks every one of them sums the blocks' counts
+// itself (blocks x E words from L2: less than another launch).
 template <int BITS>  // of an expert's number
 __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_place_kernel(const DispatchArgs A)
 {
     extern __shared__ __align__(16) int32_t dispatch_sh[];
     const int E = A.E, stride = dispatch_stride(E), pitch = dispatch_pitch(E);
-    int32_t *const count = dispatch_sh;      // [stride]: entries of all chunks
-    int32_t *const next = count + stride;    // [stride]: entries of the chunks before this one, then this chunk's first slot
+    int32_t *const count = dispatch_sh;      // [stride]: entries of all blocks
+    int32_t *const next = count + stride;    // [stride]: entries of the blocks before this one, then the next slot
     int32_t *const offset = next + stride;   // [E + 1]
     uint16_t *const hist = reinterpret_cast<uint16_t *>(offset + stride + 4);  // [warps][pitch]: a warp's entries, then those of the warps before
     __shared__ int32_t scan[DISPATCH_WARPS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint16_t *const mine = hist + warp * pitch;
     for (int i = tid; i < 2 * stride; i += DISPATCH_THREADS) count[i] = 0;
     for (int i = tid; i < DISPATCH_WARPS * pitch / 2; i += DISPATCH_THREADS) reinterpret_cast<uint32_t *>(hist)[i] = 0;
     pdl_wait();
-    const int64_t chunk = (int64_t)blockIdx.x * DISPATCH_CHUNK;
-    const int n = (int)min((int64_t)DISPATCH_CHUNK, A.entries - chunk);
-    const int rounds = (n + DISPATCH_THREADS - 1) / DISPATCH_THREADS;  // of 32 entries per warp: few entries are spread over the warps
-    const int64_t begin = chunk + warp * 32 * rounds + lane;
-    int e[DISPATCH_PER], rank[DISPATCH_PER];
-#pragma unroll
-    for (int j = 0; j < DISPATCH_PER; ++j) {
-        const int v = j < rounds && begin + 32 * j < A.entries ? __ldg(A.idx + begin + 32 * j) : -1;
-        e[j] = (unsigned)v < (unsigned)E ? v : E;  // E: dropped
-    }
     __syncthreads();
-    if (A.chunks > 1) {  // a thread has four experts of every `groups`-th chunk
+    if (A.blocks > 1) {  // a thread has four experts of every `groups`-th block
         const int quads = stride / 4, groups = DISPATCH_THREADS / quads, c0 = tid / quads, q = 4 * (tid - c0 * quads);
         if (c0 < groups) {
             int4 all = make_int4(0, 0, 0, 0), b = make_int4(0, 0, 0, 0);
 #pragma unroll 4
-            for (int c = c0; c < A.chunks; c += groups) {
+            for (int c = c0; c < A.blocks; c += groups) {
                 const int4 v = __ldg(reinterpret_cast<const int4 *>(A.partial + (int64_t)c * stride + q));
                 all.x += v.x, all.y += v.y, all.z += v.z, all.w += v.w;
                 if (c < (int)blockIdx.x) b.x += v.x, b.y += v.y, b.z += v.z, b.w += v.w;
@@ -476,63 +471,82 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_place_kernel(const 
             atomicAdd(next + q, b.x), atomicAdd(next + q + 1, b.y), atomicAdd(next + q + 2, b.z), atomicAdd(next + q + 3, b.w);
         }
     }
-    uint16_t *const mine = hist + warp * pitch;
+    for (int chunk = 0; chunk < A.chunks; ++chunk) {
+        const int64_t from = ((int64_t)blockIdx.x * A.chunks + chunk) * DISPATCH_CHUNK;
+        if (from >= A.entries && chunk > 0) break;  // uniform in the block
+        const int n = (int)min((int64_t)DISPATCH_CHUNK, A.entries - from);
+        const int rounds = (n + DISPATCH_THREADS - 1) / DISPATCH_THREADS;  // of 32 entries per warp: few entries are spread over the warps
+        const int64_t begin = from + warp * 32 * rounds + lane;
+        int e[DISPATCH_PER], rank[DISPATCH_PER];
 #pragma unroll
-    for (int j = 0; j < DISPATCH_PER; ++j) {
-        unsigned peers = __ballot_sync(FULL, e[j] < E);
-        if (peers == 0) continue;
-#pragma unroll
-        for (int b = 0; b < BITS; ++b) {
-            const bool bit = (e[j] >> b) & 1;
-            const unsigned bal = __ballot_sync(FULL, bit);
-            peers &= bit ? bal : ~bal;
+        for (int j = 0; j < DISPATCH_PER; ++j) {
+            const int v = j < rounds && begin + 32 * j < A.entries ? __ldg(A.idx + begin + 32 * j) : -1;
+            e[j] = (unsigned)v < (unsigned)E ? v : E;  // E: dropped
         }
-        const int before = __popc(peers & ((1u << lane) - 1u));
-        rank[j] = e[j] < E ? mine[e[j]] + before : 0;
-        __syncwarp();
-        if (e[j] < E && before == 0) mine[e[j]] = (uint16_t)(mine[e[j]] + __popc(peers));
-        __syncwarp();
-    }
-    __syncthreads();
-    if (tid < E) {  // a thread per expert (E <= threads)
-        int v[DISPATCH_WARPS], run = 0;
 #pragma unroll
-        for (int w = 0; w < DISPATCH_WARPS; ++w) v[w] = hist[w * pitch + tid];
+        for (int j = 0; j < DISPATCH_PER; ++j) {
+            unsigned peers = __ballot_sync(FULL, e[j] < E);
+            if (peers == 0) continue;
 #pragma unroll
-        for (int w = 0; w < DISPATCH_WARPS; ++w) {
-            hist[w * pitch + tid] = (uint16_t)run;
-            run += v[w];
-        }
-        if (A.chunks == 1) count[tid] = run;
-    }
-    __syncthreads();
-    // exclusive scan of the padded lengths, a thread per expert
-    const int padded = tid < E ? (count[tid] + A.rows - 1) >> A.shift << A.shift : 0;
-    int run = padded;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(FULL, run, o);
-        if (lane >= o) run += v;
-    }
-    if (lane == 31) scan[warp] = run;
-    __syncthreads();
-    if (tid < E) {
-        int base = run - padded;
-        for (int w = 0; w < warp; ++w) base += scan[w];
-        offset[tid] = base;
-        next[tid] += base;
-        if (tid == E - 1) offset[E] = base + padded;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < DISPATCH_PER; ++j) {
-        if (j < rounds && begin + 32 * j < A.entries) {
-            int slot = -1;
-            if (e[j] < E) {
-                slot = next[e[j]] + mine[e[j]] + rank[j];
-                A.entry_of[slot] = (int32_t)(begin + 32 * j);
+            for (int b = 0; b < BITS; ++b) {
+                const bool bit = (e[j] >> b) & 1;
+                const unsigned bal = __ballot_sync(FULL, bit);
+                peers &= bit ? bal : ~bal;
             }
-            A.slot_of[begin + 32 * j] = slot;
+            const int before = __popc(peers & ((1u << lane) - 1u));
+            rank[j] = e[j] < E ? mine[e[j]] + before : 0;
+            __syncwarp();
+            if (e[j] < E && before == 0) mine[e[j]] = (uint16_t)(mine[e[j]] + __popc(peers));
+            __syncwarp();
+        }
+        __syncthreads();
+        int total = 0;  // of expert `tid` in this chunk (E <= threads)
+        if (tid < E) {
+            int v[DISPATCH_WARPS];
+#pragma unroll
+            for (int w = 0; w < DISPATCH_WARPS; ++w) v[w] = hist[w * pitch + tid];
+#pragma unroll
+            for (int w = 0; w < DISPATCH_WARPS; ++w) {
+                hist[w * pitch + tid] = (uint16_t)total;
+                total += v[w];
+            }
+        }
+        if (chunk == 0) {  // exclusive scan of the padded lengths, a thread per expert
+            if (tid < E && A.blocks == 1) count[tid] = total;  // then there is one chunk too
+            const int padded = tid < E ? (count[tid] + A.rows - 1) >> A.shift << A.shift : 0;
+            int run = padded;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(FULL, run, o);
+                if (lane >= o) run += v;
+            }
+            if (lane == 31) scan[warp] = run;
+            __syncthreads();
+            if (tid < E) {
+                int base = run - padded;
+                for (int w = 0; w < warp; ++w) base += scan[w];
+                offset[tid] = base;
+                next[tid] += base;
+                if (tid == E - 1) offset[E] = base + padded;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < DISPATCH_PER; ++j) {
+            if (j < rounds && begin + 32 * j < A.entries) {
+                int slot = -1;
+                if (e[j] < E) {
+                    slot = next[e[j]] + mine[e[j]] + rank[j];
+                    A.entry_of[slot] = (int32_t)(begin + 32 * j);
+                }
+                A.slot_of[begin + 32 * j] = slot;
+            }
+        }
+        if (chunk + 1 < A.chunks) {
+            __syncthreads();
+            if (tid < E) next[tid] += total;
+            for (int i = tid; i < DISPATCH_WARPS * pitch / 2; i += DISPATCH_THREADS) reinterpret_cast<uint32_t *>(hist)[i] = 0;
+            __syncthreads();
         }
     }
     // the tables' rest: holes of the slots, experts of the row tiles, counts and offsets; a warp per expert

@@ -187,6 +187,19 @@ def test_gradients_against_differences():
         assert abs(got - want) <= bound, (name, got, want, bound)
 
 
+def test_offsets_beyond_32_bits():
+    """1.12 million slots of 2048 columns: more than 2^31 elements per slot buffer; a sample of the tokens is checked"""
+    T, E, k, d, f = 140_000, 16, 8, 2048, 64
+    r = Run(T, E, k, d, f, seed=14, tile_rows=128)
+    assert r.disp.capacity * d > 2 ** 31
+    out = r()
+    torch.cuda.synchronize()
+    assert r.ws.status() == 0
+    late = torch.cat([torch.arange(64), torch.randint(0, T, (128,)), torch.arange(T - 64, T)]).cuda()
+    want, bound = experts_reference(r.x[late], r.a, r.b, r.idx[late], r.w[late])["y"]
+    assert ((out["y"][late].double() - want).abs() <= bound).all()
+
+
 def test_cuda_graph_replay():
     r = Run(64, 8, 2, 128, 64, training=True, seed=12)
     side = torch.cuda.Stream()

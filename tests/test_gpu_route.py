@@ -210,6 +210,30 @@ def test_dispatch_tables(T, E, k, rows):
     check_dispatch(chosen(T, E, k, gen, drop=0.1 if T > 30 else 0.0, device="cpu"), E, rows)
 
 
+def test_dispatch_with_several_chunks_per_block():
+    """more than 512 chunks of 4096 entries; checked against a stable sort (integers: any difference is an error)"""
+    T, k, E, rows = 700_001, 5, 37, 64
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    idx = torch.randint(-1, E, (T, k), generator=gen, device="cuda", dtype=torch.int32)
+    d = L.Dispatch(T, k, E, tile_rows=rows)
+    d.buf.fill_(119)
+    L.lapsum_dispatch(idx, d)
+    flat = idx.reshape(-1).long()
+    key = torch.where(flat < 0, E, flat)
+    order = key.sort(dim=0, stable=True).indices
+    counts = torch.bincount(key, minlength=E + 1)[:E]
+    offsets = torch.cat([counts.new_zeros(1), ((counts + rows - 1) // rows * rows).cumsum(0)])
+    n = int(counts.sum())
+    e = key[order[:n]]
+    slots = torch.arange(n, device="cuda") - (counts.cumsum(0) - counts)[e] + offsets[e]
+    slot_of = torch.full_like(flat, -1)
+    slot_of[order[:n]] = slots
+    entry_of = torch.full((d.capacity,), -1, dtype=torch.int64, device="cuda")
+    entry_of[slots] = order[:n]
+    assert torch.equal(d.counts.long(), counts) and torch.equal(d.offsets.long(), offsets)
+    assert torch.equal(d.slot_of.reshape(-1).long(), slot_of) and torch.equal(d.entry_of.long(), entry_of)
+
+
 def test_dispatch_of_odd_batches():
     check_dispatch(torch.full((300, 4), -1, dtype=torch.int32), 8, 16)                  # nothing
     check_dispatch(torch.full((3000, 3), 7, dtype=torch.int32), 8, 64)                  # one expert takes all
