@@ -28,7 +28,10 @@ namespace lapsum {
 enum ExpertsMode { GATE_UP = 0, DOWN = 1, DH = 2, DX = 3, DW_DOWN = 4, DW_GATE_UP = 5 };
 
 struct ExpertsArgs {
+    // The tables are the caller's memory: whatever they hold (a dispatch that was never run, a race of the caller's), no index
+    // read from them is used unchecked; an entry, slot or expert out of range counts as a hole.
     const int32_t *entry_of, *tile_expert, *offsets, *counts;
+    int entries, capacity;          // tokens k, slots
     const float *w;                 // per entry (token, choice)
     float *partial;                 // DH: per slot and column tile, <dh, h>
     uint32_t *status;
@@ -344,10 +347,11 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
         if constexpr (S::WGRAD) {
             t.e = (int)(rest / mts);
             t.m0 = (int)(rest % mts) * MT + (int)rank * 128;
-            t.kb = __ldg(P.offsets + t.e);
-            t.nkb = (__ldg(P.counts + t.e) + 63) / 64;  // the last stage's holes are zeros
+            t.kb = min(max(__ldg(P.offsets + t.e), 0), P.capacity);
+            t.nkb = (min(max(__ldg(P.counts + t.e), 0), P.capacity) + 63) / 64;  // the last stage's holes are zeros
         } else {
             t.e = __ldcg(P.tile_expert + rest);  // past L1: it may be read before griddepcontrol.wait
+            if ((unsigned)t.e >= (unsigned)P.E) t.e = -1;
             t.m0 = (int)rest * AR + (int)rank * 128;
             t.kb = 0;
             t.nkb = (K + 64 * KS - 1) / (64 * KS);  // columns beyond K read as zeros
@@ -551,6 +555,7 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
             float w = 0.f, dot = 0.f;
             if constexpr (MODE == GATE_UP || MODE == DH) {
                 if (mine) entry = __ldg(P.entry_of + t.m0 + row);
+                if ((unsigned)entry >= (unsigned)P.entries) entry = -1;
                 if (entry >= 0) w = __ldg(P.w + entry);
             }
             if constexpr (MODE == DH) {
@@ -716,15 +721,16 @@ __device__ __forceinline__ float warp_total(float v)
 constexpr int FEW_FEATURES = 16;
 template <typename T>
 __global__ void __launch_bounds__(256, 2) experts_few_gate_up_kernel(const T *x, int64_t stride, const T *w_gate_up, const float *w,
-                                                                     const int32_t *slot_of, const int32_t *tile_expert, int shift, T *hw, int k,
-                                                                     int D, int F)
+                                                                     const int32_t *slot_of, const int32_t *tile_expert, int shift, int capacity,
+                                                                     int E, T *hw, int k, int D, int F)
 {
     pdl_wait();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, entry = blockIdx.y;
     const int slot = __ldg(slot_of + entry);
-    if (slot < 0) return;  // dropped: the second product skips it too
+    if ((unsigned)slot >= (unsigned)capacity) return;  // dropped: the second product skips it too
     const int64_t e = __ldg(tile_expert + (slot >> shift));
+    if (e < 0 || e >= E) return;
     const T *const xt = x + entry / k * stride;
     const float scale = __ldg(w + entry);
     const int f1 = min(F, (int)(blockIdx.x + 1) * FEW_FEATURES);
@@ -757,7 +763,7 @@ __global__ void __launch_bounds__(256, 2) experts_few_gate_up_kernel(const T *x,
 // in order.
 template <typename T>
 __global__ void __launch_bounds__(256, 3) experts_few_down_kernel(const T *w_down, const T *hw, const int32_t *slot_of, const int32_t *tile_expert,
-                                                                  int shift, T *y, int k, int D, int F)
+                                                                  int shift, int capacity, int E, T *y, int k, int D, int F)
 {
     __shared__ float part[8][4];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = blockIdx.y, d = 4 * blockIdx.x;  // D is a multiple of 8
@@ -765,8 +771,9 @@ __global__ void __launch_bounds__(256, 3) experts_few_down_kernel(const T *w_dow
     bool waited = false;
     for (int j = warp; j < k; j += 8) {
         const int slot = __ldcg(slot_of + (int64_t)t * k + j);
-        if (slot < 0) continue;
+        if ((unsigned)slot >= (unsigned)capacity) continue;
         const int64_t e = __ldcg(tile_expert + (slot >> shift));
+        if (e < 0 || e >= E) continue;
         const T *const rows = w_down + (e * D + d) * F, *const v = hw + ((int64_t)t * k + j) * F;
         for (int c = 8 * lane; c < F; c += 1024) {
             uint4 a[4][4];
@@ -805,7 +812,7 @@ __global__ void __launch_bounds__(256, 3) experts_few_down_kernel(const T *w_dow
 // the last used slot with zeros, a warp per four slots.  Bound by the bytes written.
 template <typename T>
 __global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t stride, const int32_t *slot_of, const int32_t *entry_of,
-                                                             const int32_t *used, T *out, int64_t tokens, int token_blocks, int k, int D)
+                                                             const int32_t *used, T *out, int64_t tokens, int token_blocks, int capacity, int k, int D)
 {
     pdl_wait();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -823,7 +830,7 @@ __global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t
             if (i + 32 * j < n) v[j] = __ldg(from + i + 32 * j);
         for (int c = 0; c < k; ++c) {
             const int slot = __shfl_sync(FULL, mine, c);
-            if (slot < 0) continue;
+            if ((unsigned)slot >= (unsigned)capacity) continue;
             uint4 *const to = reinterpret_cast<uint4 *>(out + (int64_t)slot * D);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -831,7 +838,7 @@ __global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t
         }
     } else {
         const int64_t slot0 = (unit - 8 * (int64_t)token_blocks) * 4;
-        if (slot0 >= __ldg(used)) return;  // a multiple of 64
+        if (slot0 >= min(__ldg(used), capacity)) return;  // both multiples of 64
         const int4 e = __ldg(reinterpret_cast<const int4 *>(entry_of + slot0));
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
@@ -846,7 +853,7 @@ __global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t
 // With `partial` also grad_w of the token's entries: the column tiles' sums in order.
 template <typename T>
 __global__ void __launch_bounds__(256) experts_combine_kernel(const T *slots, const int32_t *slot_of, T *out, int64_t out_stride,
-                                                              const float *partial, T *grad_w, int64_t tokens, int k, int D, int nts)
+                                                              const float *partial, T *grad_w, int64_t tokens, int capacity, int k, int D, int nts)
 {
     pdl_wait();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -863,7 +870,7 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(const T *slots, co
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[j] = j0 + j < k ? __ldg(at + j0 + j) : -1;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = s[j] >= 0 ? __ldg(reinterpret_cast<const uint4 *>(slots + (int64_t)s[j] * D + 8 * c)) : Io<T>::zero();
+        for (int j = 0; j < 8; ++j) q[j] = (unsigned)s[j] < (unsigned)capacity ? __ldg(reinterpret_cast<const uint4 *>(slots + (int64_t)s[j] * D + 8 * c)) : Io<T>::zero();
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float v[8];
@@ -877,7 +884,7 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(const T *slots, co
         for (int j = c; j < k; j += per) {
             const int s = __ldg(at + j);
             float g = 0.f;
-            if (s >= 0)
+            if ((unsigned)s < (unsigned)capacity)
                 for (int n = 0; n < nts; ++n) g += partial[(int64_t)s * nts + n];
             Io<T>::store1(grad_w + t * k + j, g);
         }

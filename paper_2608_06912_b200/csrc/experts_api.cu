@@ -282,6 +282,7 @@ int begin_call(const lapsum_experts_dims *p, const void *dispatch, size_t dispat
     c.A.status = reinterpret_cast<uint32_t *>(ws);
     c.A.wait_ns = 2000000000ull;
     c.A.row_tiles = (int)c.X.d.tiles;
+    c.A.entries = (int)(p->tokens * p->k), c.A.capacity = (int)c.X.d.capacity;
     c.A.E = (int)p->experts, c.A.D = (int)p->d, c.A.F = (int)p->f, c.A.k = p->k, c.A.tokens = (int)p->tokens;
     return LAPSUM_OK;
 }
@@ -326,7 +327,7 @@ int gather(const Call &c, const uint8_t *dispatch, const void *x, int64_t stride
     const int64_t token_blocks = ceil_div(c.p->tokens * ceil_div(c.p->d, 1024), 8), hole_blocks = holes ? ceil_div(c.X.d.capacity, 32) : 0;
     return launch_pdl(experts_gather_kernel<T>, (unsigned)(token_blocks + hole_blocks), 256, 0, st, static_cast<const T *>(x), stride,
                       reinterpret_cast<const int32_t *>(dispatch + c.X.d.off_slot_of), c.A.entry_of, c.A.offsets + c.A.E,
-                      reinterpret_cast<T *>(c.ws + c.X.off_slots), c.p->tokens, (int)token_blocks, (int)c.p->k, (int)c.p->d);
+                      reinterpret_cast<T *>(c.ws + c.X.off_slots), c.p->tokens, (int)token_blocks, c.A.capacity, (int)c.p->k, (int)c.p->d);
 }
 
 template <typename T>
@@ -335,7 +336,7 @@ int combine(const Call &c, const uint8_t *dispatch, void *out, int64_t stride, c
     const int64_t work = c.p->tokens * (c.p->d / 8);
     return launch_pdl(experts_combine_kernel<T>, (unsigned)ceil_div(work, 256), 256, 0, st, reinterpret_cast<const T *>(c.ws + c.X.off_slots),
                       reinterpret_cast<const int32_t *>(dispatch + c.X.d.off_slot_of), static_cast<T *>(out), stride, partial,
-                      static_cast<T *>(grad_w), c.p->tokens, (int)c.p->k, (int)c.p->d, c.X.nts_dh);
+                      static_cast<T *>(grad_w), c.p->tokens, c.A.capacity, (int)c.p->k, (int)c.p->d, c.X.nts_dh);
 }
 
 template <typename T>
@@ -352,10 +353,10 @@ int forward_t(Call &c, const void *x, int64_t x_stride, const void *w_gate_up, c
         int shift = 4;
         while ((1 << shift) < p.tile_rows) ++shift;
         RUN(launch_pdl(experts_few_gate_up_kernel<T>, dim3((unsigned)ceil_div(p.f, FEW_FEATURES), (unsigned)(p.tokens * p.k)), 256, 0, st,
-                       static_cast<const T *>(x), x_stride, static_cast<const T *>(w_gate_up), w, slot_of, c.A.tile_expert, shift, hw, (int)p.k,
+                       static_cast<const T *>(x), x_stride, static_cast<const T *>(w_gate_up), w, slot_of, c.A.tile_expert, shift, c.A.capacity, c.A.E, hw, (int)p.k,
                        (int)p.d, (int)p.f));
         return launch_pdl(experts_few_down_kernel<T>, dim3((unsigned)(p.d / 4), (unsigned)p.tokens), 256, 0, st, static_cast<const T *>(w_down),
-                          hw, slot_of, c.A.tile_expert, shift, static_cast<T *>(y), (int)p.k, (int)p.d, (int)p.f);
+                          hw, slot_of, c.A.tile_expert, shift, c.A.capacity, c.A.E, static_cast<T *>(y), (int)p.k, (int)p.d, (int)p.f);
     }
     uint8_t *rowbuf = c.ws + c.X.off_slots;  // in turn: x in slot order, the second product's results
     void *hw = saved ? saved + c.X.off_hw_saved : c.ws + c.X.off_hw;

@@ -537,7 +537,8 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_place_kernel(const 
                 int slot = -1;
                 if (e[j] < E) {
                     slot = next[e[j]] + mine[e[j]] + rank[j];
-                    A.entry_of[slot] = (int32_t)(begin + 32 * j);
+                    if ((unsigned)slot < (unsigned)A.capacity) A.entry_of[slot] = (int32_t)(begin + 32 * j);
+                    else slot = -1;  // only if the caller changes idx between the two kernels
                 }
                 A.slot_of[begin + 32 * j] = slot;
             }

@@ -203,6 +203,7 @@ def test_offsets_beyond_32_bits():
 def test_cuda_graph_replay():
     r = Run(64, 8, 2, 128, 64, training=True, seed=12)
     side = torch.cuda.Stream()
+    torch.cuda.synchronize()
     with torch.cuda.stream(side):
         r()
     side.synchronize()
@@ -232,6 +233,25 @@ def test_a_wait_that_runs_out_is_reported():
     torch.cuda.synchronize()
     want, bound = experts_reference(r.x, r.a, r.b, r.idx, r.w)["y"]
     assert ((out["y"].double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("T,training", [(3, False), (40, False), (300, True)])
+def test_tables_of_another_batch_s_bytes_do_no_harm(T, training):
+    """Tables that hold anything (a dispatch that was forgotten): the results mean nothing, but every index is checked, so the call
+    ends and the workspace serves the next batch"""
+    r = Run(T, 6, 2, 72, 80, training=training, seed=15)
+    dispatch = L.lapsum_dispatch
+    gen = torch.Generator(device="cuda").manual_seed(16)
+    for low, high in ((-2 ** 31, 2 ** 31 - 1), (-5, 4000), (0, 7)):
+        words = r.disp.buf.view(torch.int32)
+        words.copy_(torch.randint(low, high, words.shape, generator=gen, device="cuda", dtype=torch.int64).to(torch.int32))
+        try:
+            L.lapsum_dispatch = lambda *a: None
+            r()
+        finally:
+            L.lapsum_dispatch = dispatch
+        torch.cuda.synchronize()
+    r.check()
 
 
 def test_refusals():
