@@ -260,8 +260,12 @@ struct ExpertsShape {
     static constexpr int A_SUB = ROWS * 128, B_SUB = COLS * 128;             // bytes of one step
     static constexpr int A_BYTES = KS * A_SUB, B_BYTES = KS * B_SUB, STAGE = A_BYTES + B_BYTES;
     static constexpr int SLAB = 4096;                                        // 32 rows x 64 columns of results of one epilogue warp
-    static constexpr int SLABS = MODE == DH ? 4 : 2;                         // per warp: one is filled while the other is stored
-    static constexpr int WARPS = ROWS < 32 ? 1 : ROWS / 32;                  // epilogue warps with rows
+    // Epilogue warps come in sets of four (a set reads the 128 lanes of TMEM); two sets share a tile's columns.  DH has one set and
+    // four slabs per warp, two of which are loaded while the others are used.  Elsewhere a warp has two slabs where the ring keeps
+    // four stages beside them (a prompt of 1021 tokens on 128 x 256 tiles: 262 us with one and four stages, 275 us with two and three).
+    static constexpr int SETS = MODE == DH ? 1 : 2, SLABS = MODE == DH ? 4 : AR >= 128 && BN == 256 ? 1 : 2;
+    static constexpr int THREADS = 128 + 128 * SETS;
+    static constexpr int WARPS = SETS * (ROWS < 32 ? 1 : ROWS / 32);         // epilogue warps with rows
     static constexpr int FIT = (229376 - WARPS * SLABS * SLAB) / STAGE;
     static constexpr int STAGES = FIT < 12 ? FIT : 12;
     static constexpr int ACC = 2;  // accumulators: one is finished while the next is computed
@@ -279,7 +283,7 @@ struct ExpertsMaps {
 };
 
 template <int MODE, int AR, int BN, int KS, typename T>
-__global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__ ExpertsMaps maps, const ExpertsArgs P)
+__global__ void __launch_bounds__((ExpertsShape<MODE, AR, BN, KS>::THREADS), 1) experts_kernel(const __grid_constant__ ExpertsMaps maps, const ExpertsArgs P)
 {
     using S = ExpertsShape<MODE, AR, BN, KS>;
     constexpr bool PAIR = S::PAIR;
@@ -296,7 +300,7 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
     if (tid == 0) {
         abort_flag = 0;
         for (int s = 0; s < S::STAGES; ++s) mbar_init(full + 8 * s, 1), mbar_init(empty + 8 * s, 1);
-        for (int a = 0; a < S::ACC; ++a) mbar_init(acc_full + 8 * a, 1), mbar_init(acc_empty + 8 * a, PAIR ? 8 : 4);
+        for (int a = 0; a < S::ACC; ++a) mbar_init(acc_full + 8 * a, 1), mbar_init(acc_empty + 8 * a, (PAIR ? 8 : 4) * S::SETS);
         mbar_init(drain, 1);
         if constexpr (MODE == DH)
             for (int i = 0; i < 8; ++i) mbar_init(loaded + 8 * i, 1);
@@ -341,12 +345,18 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
     };
     auto tile_at = [&](int64_t i) {
         Tile t;
-        const int nt = (int)(i % nts);
-        const int64_t rest = i / nts;
+        int nt;
+        int64_t rest;
+        if (tiles >> 31) {
+            nt = (int)(i % nts), rest = i / nts;
+        } else {  // divisions of 64 bits cost hundreds of cycles
+            const uint32_t q = (uint32_t)i / (uint32_t)nts;
+            nt = (int)((uint32_t)i - q * (uint32_t)nts), rest = q;
+        }
         t.n0 = nt * S::NSTEP;
         if constexpr (S::WGRAD) {
-            t.e = (int)(rest / mts);
-            t.m0 = (int)(rest % mts) * MT + (int)rank * 128;
+            t.e = (int)((uint32_t)rest / (uint32_t)mts);  // experts x row tiles stay below 2^31
+            t.m0 = (int)((uint32_t)rest - (uint32_t)t.e * (uint32_t)mts) * MT + (int)rank * 128;
             t.kb = min(max(__ldg(P.offsets + t.e), 0), P.capacity);
             t.nkb = (min(max(__ldg(P.counts + t.e), 0), P.capacity) + 63) / 64;  // the last stage's holes are zeros
         } else {
@@ -517,9 +527,9 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
         // A warp puts its 32 rows x 64 columns as 16-bit values into a slab of its own (rows of 128 bytes, 16-byte pieces
         // exchanged by the row's low three bits, as TMA's 128-byte swizzle has it) and stores it with one TMA instruction:
         // a row per thread written directly costs the load / store unit 32 lines per instruction.
-        const int ew = warp - 4, row = tid - 128;
+        const int ew = warp & 3, set = (warp - 4) >> 2, row = 32 * ew + lane;
         const uint32_t lanes = (uint32_t)ew << 21;  // 32 TMEM lanes per warp, lane index in the upper half
-        const uint32_t slab = slabs + ew * S::SLABS * S::SLAB;
+        const uint32_t slab = slabs + (set * (S::WARPS / S::SETS) + ew) * S::SLABS * S::SLAB;  // of live warps only
         const bool live = ew * 32 < S::ROWS, mine = row < S::ROWS;  // live: uniform in the warp
         auto piece = [&](uint32_t base, int j) { return base + lane * 128 + ((j ^ (lane & 7)) << 4); };  // 8 columns of my row
         auto put = [&](uint32_t base, int j, const float *v) {
@@ -577,28 +587,35 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
             const uint32_t d = tmem + buf * BN + lanes;
             if (live && (!S::WGRAD || t.m0 + 32 * ew < M)) {
 #pragma unroll 1
-                for (int c = 0; c < S::NSTEP && t.n0 + c < N; c += 64, ++chunk) {
+                for (int c = 64 * set; c < S::NSTEP && t.n0 + c < N; c += 64 * S::SETS, ++chunk) {
                     if constexpr (MODE == GATE_UP) {
                         // w h, and for the backward g and u, one after the other
                         for (int what = 0; what < (P.keep ? 3 : 1); ++what) {
-                            const uint32_t at = slab + (used++ & 1) * S::SLAB;
-                            if (lane == 0) tma_store_wait_read<1>();
+                            const uint32_t at = slab + (used++ % S::SLABS) * S::SLAB;
+                            if (lane == 0) tma_store_wait_read<S::SLABS - 1>();
                             __syncwarp();
 #pragma unroll
-                            for (int j = 0; j < 64; j += 16) {
-                                float g[16], u[16];
-                                if (what != 2) tmem_ld16(d + c + j, g);
-                                if (what != 1) tmem_ld16(d + BN / 2 + c + j, u);
-                                tmem_wait_ld(g);
-                                tmem_pin(u);
-                                if (what == 0) {
+                            for (int j = 0; j < 64; j += 32) {
+                                float g[2][16], u[2][16];
 #pragma unroll
-                                    for (int v = 0; v < 16; ++v) g[v] = entry >= 0 ? w * (g[v] * sigmoid_fast(g[v]) * u[v]) : 0.f;
-                                } else if (what == 2) {
-#pragma unroll
-                                    for (int v = 0; v < 16; ++v) g[v] = u[v];
+                                for (int h = 0; h < 2; ++h) {
+                                    if (what != 2) tmem_ld16(d + c + j + 16 * h, g[h]);
+                                    if (what != 1) tmem_ld16(d + BN / 2 + c + j + 16 * h, u[h]);
                                 }
-                                if (mine) put(at, j / 8, g), put(at, j / 8 + 1, g + 8);
+                                tmem_wait_ld(g[0]);
+                                tmem_pin(g[1]), tmem_pin(u[0]), tmem_pin(u[1]);
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+                                    if (what == 0) {
+#pragma unroll
+                                        for (int v = 0; v < 16; ++v)
+                                            g[h][v] = entry >= 0 ? w * (g[h][v] * sigmoid_fast(g[h][v]) * u[h][v]) : 0.f;
+                                    } else if (what == 2) {
+#pragma unroll
+                                        for (int v = 0; v < 16; ++v) g[h][v] = u[h][v];
+                                    }
+                                    if (mine) put(at, j / 8 + 2 * h, g[h]), put(at, j / 8 + 2 * h + 1, g[h] + 8);
+                                }
                             }
                             fence_async_smem();
                             __syncwarp();
@@ -648,20 +665,22 @@ __global__ void __launch_bounds__(256, 1) experts_kernel(const __grid_constant__
                             tma_store_commit();
                         }
                     } else {
-                        const uint32_t at = slab + (used++ & 1) * S::SLAB;
-                        if (lane == 0) tma_store_wait_read<1>();
+                        const uint32_t at = slab + (used++ % S::SLABS) * S::SLAB;
+                        float v[4][16];  // all 64 columns are asked for before the first is used
+                        if (t.nkb > 0) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) tmem_ld16(d + c + 16 * j, v[j]);
+                            tmem_wait_ld(v[0]);
+                            tmem_pin(v[1]), tmem_pin(v[2]), tmem_pin(v[3]);
+                        } else {  // an expert without tokens
+#pragma unroll
+                            for (int j = 0; j < 64; ++j) v[j / 16][j % 16] = 0.f;
+                        }
+                        if (lane == 0) tma_store_wait_read<S::SLABS - 1>();
                         __syncwarp();
+                        if (mine) {
 #pragma unroll
-                        for (int j = 0; j < 64; j += 16) {
-                            float v[16];
-                            if (t.nkb > 0) {
-                                tmem_ld16(d + c + j, v);
-                                tmem_wait_ld(v);
-                            } else {  // an expert without tokens
-#pragma unroll
-                                for (int q = 0; q < 16; ++q) v[q] = 0.f;
-                            }
-                            if (mine) put(at, j / 8, v), put(at, j / 8 + 1, v + 8);
+                            for (int j = 0; j < 8; ++j) put(at, j, v[j / 2] + 8 * (j % 2));
                         }
                         fence_async_smem();
                         __syncwarp();

@@ -252,7 +252,7 @@ int run_experts(const ExpertsMaps &maps, const ExpertsArgs &P, int64_t tiles_max
         dev_ready = dev;
     }
     const int64_t units = S::PAIR ? sms / 2 : sms, n = tiles_max < 1 ? 1 : tiles_max < units ? tiles_max : units;
-    return launch_clusters(S::PAIR ? 2 : 1, kernel, (unsigned)(S::PAIR ? 2 * n : n), 256, S::SMEM, st, maps, P);
+    return launch_clusters(S::PAIR ? 2 : 1, kernel, (unsigned)(S::PAIR ? 2 * n : n), S::THREADS, S::SMEM, st, maps, P);
 }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
