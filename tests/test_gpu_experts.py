@@ -61,6 +61,14 @@ def test_forward(T, dtype):
     Run(T, 12, 3, 200, 136, dtype, seed=T).check()
 
 
+@pytest.mark.parametrize("T,k", [(1, 1), (1, 8), (2, 3), (4, 32)])
+@pytest.mark.parametrize("d,f", [(8, 8), (1000, 520), (2048, 1024), (2056, 2056), (4104, 4104), (72, 5000)])
+def test_few_tokens(T, k, d, f):
+    """no tensor core: rows shorter and longer than a stage, several choices' rows in a stage, dropped entries"""
+    Run(T, 33, k, d, f, seed=T + d).check()
+    Run(T, 33, k, d, f, torch.float16, seed=T + d, drop=0.5).check()
+
+
 @pytest.mark.parametrize("rows", [16, 32, 64, 128, 256])
 @pytest.mark.parametrize("d,f", [(8, 8), (64, 64), (72, 40), (256, 128), (520, 264), (1000, 1032)])
 def test_forward_on_every_row_tile(rows, d, f):
