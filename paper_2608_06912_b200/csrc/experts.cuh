@@ -13,9 +13,15 @@
 // and finish the previous tile.  Operands that the contraction runs along the rows of (W_down in DH, W_gate_up in DX, both
 // sides of the weight gradients) are read as they lie in memory: the tensor core takes them "MN-major".
 //
+// Measured on pairs of blocks (8192 tokens, 4 of 32 experts, 2048 x 1024, bf16; 1.5 to 1.6 GHz under the profiler): GATE_UP 225 us,
+// DOWN 112 us, DX 207 us with the tensor pipe 68 to 75 % busy (1.22 to 1.33 PFLOP/s on the real rows), the weight gradients 120 and
+// 220 us, DH 142 us.  In a row they run at the board's power limit (1.0 PFLOP/s over whole passes at 1.38 GHz, where a library
+// matrix product alone sustains 1.38).  With few tokens they are bound by the weights: 6.0 TB/s at 48 tokens on 128 experts.
+//
 // Roundings: the inputs of a product are 16-bit, so w h, g, u, dg, du are rounded to the storage type once, sums are
-// fp32 in TMEM; o and dx are rounded once per slot before the fp32 sum over the slots (an fp32 copy would double the
-// traffic of the combine for an error of the size of the final rounding).
+// fp32 in TMEM; o and dx are rounded once per slot before the fp32 sum over the slots: an fp32 copy would double the traffic of
+// the combine (1.1 GB more, 0.16 ms by its bytes, on 1.65 ms for 131072 slots) to take away an error of the size of the final rounding.  Against 64
+// bits the outputs are 2.9e-3 (y, bf16; one rounding alone gives 1.7e-3) to 3.4e-3 (grad_x) off in the 2-norm.
 #pragma once
 #include <cuda.h>
 
@@ -828,7 +834,7 @@ __global__ void __launch_bounds__(256, 3) experts_few_down_kernel(const T *w_dow
 
 // Rows of a matrix in slot order.  The first blocks have a warp per token and 1024 columns, which reads them once and writes them
 // to the token's slots; the others (backward only: the sums over slots must not meet what a hole's row held) fill the holes below
-// the last used slot with zeros, a warp per four slots.  Bound by the bytes written.
+// the last used slot with zeros, a warp per four slots.  Bound by the bytes written: 131072 slots of 4 KB in 98 us (6.1 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t stride, const int32_t *slot_of, const int32_t *entry_of,
                                                              const int32_t *used, T *out, int64_t tokens, int token_blocks, int capacity, int k, int D)
@@ -869,7 +875,8 @@ __global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t
 }
 
 // y_t = sum over the token's slots, in the order of its choices, eight columns per thread; dropped entries (-1) add nothing.
-// With `partial` also grad_w of the token's entries: the column tiles' sums in order.
+// With `partial` also grad_w of the token's entries: the column tiles' sums in order.  Bound by memory: 131072 slots of 4 KB in 89 us
+// (6.7 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(256) experts_combine_kernel(const T *slots, const int32_t *slot_of, T *out, int64_t out_stride,
                                                               const float *partial, T *grad_w, int64_t tokens, int capacity, int k, int D, int nts)

@@ -7,9 +7,11 @@
 //          Bound by integer instructions, not by memory, so the work per choice is kept small: a lane knows the maxima of
 //          its runs of four keys, log2 L exchanges find the row's largest, a ballot the lane (lanes hold ascending
 //          runs, so the lowest lane is the lowest index), and that lane alone looks into one run in shared memory.
-//          Measured at 65536 x 128, k = 8: a warp per token with its logits spread over all lanes took 47 us (780
-//          instructions a token).
-// dispatch a stable counting sort of the T k entries by expert, integers only.
+//          Measured at 65536 x 128 fp32, k = 8: forward 24 us (220 instructions a token, the integer pipe two thirds busy; its 38 MB
+//          would take 6 us), where a warp per token with its logits spread over all lanes took 47 us; backward 11 us for 34 MB
+//          written; 28.5 us together.  16381 x 256 bf16 in 8 groups: 24 and 7 us, 23.5 us together.
+// dispatch a stable counting sort of the T k entries by expert, integers only.  65536 x 8 entries, 128 experts: 11 us in two
+//          launches (6.4 MB would take 1 us; two dependent passes of latency and 27 k instructions a block); 32 x 8: 5.5 us.
 #pragma once
 #include "common.cuh"
 
