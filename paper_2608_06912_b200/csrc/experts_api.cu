@@ -455,7 +455,7 @@ int lapsum_route_forward(const void *logits, int64_t tokens, int64_t experts, in
     if (tokens == 0) return LAPSUM_OK;
     if (!logits || !idx || !w) return LAPSUM_ERR_NULL;
     const RouteArgs A{logits, bias, idx, w, tokens, stride, (int)experts, prm->k, prm->groups, prm->groups_kept, prm->group_top,
-                      prm->score, prm->renormalise != 0, (float)prm->scale};
+                      prm->score, prm->renormalise != 0, experts % 4 == 0 && aligned(bias, 16), (float)prm->scale};
     return BY_TYPE(route_forward_t, prm->io_dtype, A, static_cast<cudaStream_t>(stream));
 }
 

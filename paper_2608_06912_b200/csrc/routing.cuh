@@ -27,6 +27,7 @@ struct RouteArgs {
     float *w;
     int64_t tokens, stride;
     int E, k, groups, kept, top, score, renorm;
+    int bias_vec;  // four experts' bias per load
     float scale;
 };
 
@@ -123,7 +124,7 @@ __device__ __forceinline__ uint32_t kept_groups(const float *c, float *strength,
 }
 
 template <typename T, int L, int NV, bool VEC, bool GROUPS>
-__global__ void __launch_bounds__(32 * ROUTE_WARPS, 4) route_forward_kernel(const RouteArgs A)
+__global__ void __launch_bounds__(32 * ROUTE_WARPS, NV > 16 ? 2 : 4) route_forward_kernel(const RouteArgs A)
 {
     constexpr int ROWS = 32 / L * ROUTE_WARPS, PITCH = NV + 4;  // a lane's keys: 16-byte pieces of eight lanes meet no bank twice
     __shared__ __align__(16) float keys[32 * ROUTE_WARPS * PITCH];
@@ -154,13 +155,29 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, 4) route_forward_kernel(cons
         total = row_sum_f<L>(s);
     }
     if (by_score) {
-        float c[NV];
+        float c[NV], offset[NV];  // the bias of my experts
+#pragma unroll
+        for (int q = 0; q < NV / 4; ++q) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            const int i = first + 4 * q;
+            if (A.bias != nullptr) {
+                if (A.bias_vec) {
+                    if (i < A.E) v = __ldg(reinterpret_cast<const float4 *>(A.bias + i));
+                } else {
+                    if (i < A.E) v.x = __ldg(A.bias + i);
+                    if (i + 1 < A.E) v.y = __ldg(A.bias + i + 1);
+                    if (i + 2 < A.E) v.z = __ldg(A.bias + i + 2);
+                    if (i + 3 < A.E) v.w = __ldg(A.bias + i + 3);
+                }
+            }
+            offset[4 * q] = v.x, offset[4 * q + 1] = v.y, offset[4 * q + 2] = v.z, offset[4 * q + 3] = v.w;
+        }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float s = x[i];
             if (A.score == LAPSUM_ROUTE_SOFTMAX) s = expf(s - top) / total;
             else if (A.score == LAPSUM_ROUTE_SIGMOID) s = sigmoid_key(s);
-            if (A.bias != nullptr && first + i < A.E) s += __ldg(A.bias + first + i);
+            s += offset[i];
             c[i] = (x[i] > -CUDART_INF_F && s > -CUDART_INF_F) ? s : -CUDART_INF_F;  // a NaN counts as unavailable
         }
         if constexpr (GROUPS) {
@@ -171,11 +188,18 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, 4) route_forward_kernel(cons
                                                  [](int e) { return e / NV * PITCH + e % NV; });
             __syncwarp();
             const int size = A.E / A.groups;
-            int g = first / size, left = (g + 1) * size - first;  // experts until the next group
+            int g = first / size;
+            if (size % NV == 0) {  // all of the lane's experts are of one group
+                const bool in = (keep >> (g & 31)) & 1u;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                if (!((keep >> (g & 31)) & 1u)) c[i] = x[i] = -CUDART_INF_F;
-                if (--left == 0) ++g, left = size;
+                for (int i = 0; i < NV; ++i) c[i] = in ? c[i] : -CUDART_INF_F, x[i] = in ? x[i] : -CUDART_INF_F;
+            } else {
+                int left = (g + 1) * size - first;  // experts until the next group
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (!((keep >> (g & 31)) & 1u)) c[i] = x[i] = -CUDART_INF_F;
+                    if (--left == 0) ++g, left = size;
+                }
             }
         }
         // without a bias the experts of the kept groups are compared by their logits, which the score rises with
