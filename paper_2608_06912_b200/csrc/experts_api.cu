@@ -44,16 +44,21 @@ inline unsigned route_grid(int64_t tokens, int lanes) { return (unsigned)((token
 
 template <typename T, int L, int NV>
 struct RouteShape {
-    static constexpr int V = 16 / (int)sizeof(T) < NV ? 16 / (int)sizeof(T) : NV;  // elements of a vector access
+    [[maybe_unused]] static constexpr int V = 16 / (int)sizeof(T) < NV ? 16 / (int)sizeof(T) : NV;  // elements of a vector access
     // whole vectors at aligned addresses in every row
     static bool vec(const void *p, int64_t stride, int E) { return E % V == 0 && stride % V == 0 && aligned(p, V * sizeof(T)); }
 
     static int forward(const RouteArgs &A, cudaStream_t st)
     {
         const bool v = vec(A.logits, A.stride, A.E);
-        const auto kernel = A.groups > 1 ? (v ? route_forward_kernel<T, L, NV, true, true> : route_forward_kernel<T, L, NV, false, true>)
-                                         : (v ? route_forward_kernel<T, L, NV, true, false> : route_forward_kernel<T, L, NV, false, false>);
+        const auto kernel = A.groups > 1
+                                ? (v ? route_forward_kernel<T, L, NV, true, true, false> : route_forward_kernel<T, L, NV, false, true, false>)
+                                : (v ? route_forward_kernel<T, L, NV, true, false, false> : route_forward_kernel<T, L, NV, false, false, false>);
         return launch_pdl(kernel, route_grid(A.tokens, L), 32 * ROUTE_WARPS, 0, st, A);
+    }
+    static int plain(const RouteArgs &A, cudaStream_t st)
+    {
+        return launch_pdl(route_forward_kernel<T, L, NV, true, false, true>, route_grid(A.tokens, L), 32 * ROUTE_WARPS, 0, st, A);
     }
     static int dense(const RouteBackArgs &A, cudaStream_t st)
     {
@@ -62,8 +67,8 @@ struct RouteShape {
                           route_grid(A.tokens, L), 32 * ROUTE_WARPS, 0, st, A);
     }
 };
-// Lanes per token: eight with up to 16 logits each, more only where a row is longer (a choice costs a warp the same
-// instructions however many tokens it holds).
+// Lanes per token where scores, biases and groups are held in registers: eight with up to 16 logits each, more only where a row is
+// longer.
 #define BY_WIDTH(T, what, E, ...)                                 \
     ((E) <= 32    ? RouteShape<T, 8, 4>::what(__VA_ARGS__)        \
      : (E) <= 64  ? RouteShape<T, 8, 8>::what(__VA_ARGS__)        \
@@ -79,6 +84,14 @@ struct RouteShape {
 template <typename T>
 int route_forward_t(const RouteArgs &A, cudaStream_t st)
 {
+    // Four lanes per token and more where a lane would have over 32 logits; whole vectors of four.
+    if (A.bias == nullptr && A.groups == 1 && A.E % 4 == 0 && A.stride % 4 == 0 && aligned(A.logits, 4 * sizeof(T)))
+        return A.E <= 32    ? RouteShape<T, 4, 8>::plain(A, st)
+               : A.E <= 64  ? RouteShape<T, 4, 16>::plain(A, st)
+               : A.E <= 128 ? RouteShape<T, 4, 32>::plain(A, st)
+               : A.E <= 256 ? RouteShape<T, 8, 32>::plain(A, st)
+               : A.E <= 512 ? RouteShape<T, 16, 32>::plain(A, st)
+                            : RouteShape<T, 32, 32>::plain(A, st);
     return BY_WIDTH(T, forward, A.E, A, st);
 }
 template <typename T, int L>

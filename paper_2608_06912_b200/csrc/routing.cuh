@@ -1,15 +1,16 @@
 // Routing of tokens to experts and the dispatch tables that bring every expert's tokens side by side.
 //
-// route    L lanes per token (8, 16 or 32), NV neighbouring logits in each lane's registers.
+// route    L lanes per token (4 to 32), each with a run of NV neighbouring logits.
 //          keys   c_i = l_i (softmax or sigmoid without a bias: both rise with the logit), else s_i + bias_i
 //          groups the `kept` groups with the largest sum of their best `group_top` keys keep their experts
 //          choice k largest keys, ties to the lower index; weights from the scores s, never from the bias
 //          Bound by integer instructions, not by memory, so the work per choice is kept small: a lane knows the maxima of
 //          its runs of four keys, log2 L exchanges find the row's largest, a ballot the lane (lanes hold ascending
 //          runs, so the lowest lane is the lowest index), and that lane alone looks into one run in shared memory.
-//          Measured at 65536 x 128 fp32, k = 8: forward 24 us (220 instructions a token, the integer pipe two thirds busy; its 38 MB
-//          would take 6 us), where a warp per token with its logits spread over all lanes took 47 us; backward 11 us for 34 MB
-//          written; 28.5 us together.  16381 x 256 bf16 in 8 groups: 24 and 7 us, 23.5 us together.
+//          A choice costs a warp the same instructions however many tokens it holds, so few lanes per token are better:
+//          65536 x 128 fp32, k = 8, forward: 47 us with 32 lanes, 24 us with 8, 20 us with 4 (160 instructions a token, the
+//          integer pipe 60 % busy; its 38 MB would take 6 us); the backward takes 11 us for 34 MB written, both together
+//          25.9 us.  16381 x 256 bf16 with a bias and 8 groups (16 lanes): 23 and 7 us, 21.9 us together.
 // dispatch a stable counting sort of the T k entries by expert, integers only.  65536 x 8 entries, 128 experts: 11 us in two
 //          launches (6.4 MB would take 1 us; two dependent passes of latency and 27 k instructions a block); 32 x 8: 5.5 us.
 #pragma once
@@ -123,8 +124,10 @@ __device__ __forceinline__ uint32_t kept_groups(const float *c, float *strength,
     return keep;
 }
 
-template <typename T, int L, int NV, bool VEC, bool GROUPS>
-__global__ void __launch_bounds__(32 * ROUTE_WARPS, NV > 16 ? 2 : 4) route_forward_kernel(const RouteArgs A)
+// PLAIN: no bias and no groups, so the logits are the keys and nothing else of the row is kept: the warp brings its rows in whole
+// lines and hands each lane its run through shared memory, and four lanes hold a token of up to 128 logits.
+template <typename T, int L, int NV, bool VEC, bool GROUPS, bool PLAIN>
+__global__ void __launch_bounds__(32 * ROUTE_WARPS, NV > 16 && !PLAIN ? 2 : 4) route_forward_kernel(const RouteArgs A)
 {
     constexpr int ROWS = 32 / L * ROUTE_WARPS, PITCH = NV + 4;  // a lane's keys: 16-byte pieces of eight lanes meet no bank twice
     __shared__ __align__(16) float keys[32 * ROUTE_WARPS * PITCH];
@@ -137,86 +140,121 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, NV > 16 ? 2 : 4) route_forwa
     const T *row = reinterpret_cast<const T *>(A.logits) + (live ? t : A.tokens - 1) * A.stride;
     float *const mine = keys + threadIdx.x * PITCH;
     const int first = r * NV;
-    float x[NV];
-    load_run<T, NV, VEC>(row, first, A.E, x);
-
-    // softmax over the whole row, where the scores themselves are needed
-    const bool by_score = A.bias != nullptr || GROUPS;
-    float top = 0.f, total = 1.f;
-    if (A.score == LAPSUM_ROUTE_SOFTMAX && (by_score || !A.renorm)) {
-        float m = -CUDART_INF_F;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) m = fmaxf(m, x[i]);  // fmaxf skips NaN
-        top = row_max_f<L>(m);
-        if (top == -CUDART_INF_F) top = 0.f;
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) s += (x[i] > -CUDART_INF_F) ? expf(x[i] - top) : 0.f;
-        total = row_sum_f<L>(s);
-    }
-    if (by_score) {
-        float c[NV], offset[NV];  // the bias of my experts
+    float top = 0.f, total = 1.f;                       // softmax: the row's largest logit and sum
+    float run[NV / 4], best = -CUDART_INF_F;            // maxima of the lane's runs of four keys
+    if constexpr (PLAIN) {
+        constexpr int EP = L * NV;  // a row, padded
+        const int64_t t0 = (int64_t)blockIdx.x * ROWS + (threadIdx.x >> 5) * (32 / L);
+        float *const all = keys + (threadIdx.x - lane) * PITCH;
 #pragma unroll
         for (int q = 0; q < NV / 4; ++q) {
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            const int i = first + 4 * q;
-            if (A.bias != nullptr) {
-                if (A.bias_vec) {
-                    if (i < A.E) v = __ldg(reinterpret_cast<const float4 *>(A.bias + i));
+            const int f = (32 * q + lane) * 4, rr = f / EP, e = f % EP;
+            float4 k4 = make_float4(-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F);
+            if (t0 + rr < A.tokens && e < A.E) {
+                T h[4];
+                const T *const from = reinterpret_cast<const T *>(A.logits) + (t0 + rr) * A.stride + e;
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4 *>(h) = __ldg(reinterpret_cast<const uint4 *>(from));
+                else *reinterpret_cast<uint2 *>(h) = __ldg(reinterpret_cast<const uint2 *>(from));
+                k4 = make_float4(route_key(Io<T>::from_storage(h[0])), route_key(Io<T>::from_storage(h[1])), route_key(Io<T>::from_storage(h[2])),
+                                 route_key(Io<T>::from_storage(h[3])));
+            }
+            *reinterpret_cast<float4 *>(all + (rr * L + e / NV) * PITCH + e % NV) = k4;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < NV / 4; ++q) {
+            const float4 k4 = *reinterpret_cast<const float4 *>(mine + 4 * q);
+            run[q] = fmaxf(fmaxf(k4.x, k4.y), fmaxf(k4.z, k4.w));
+            best = fmaxf(best, run[q]);
+        }
+        if (A.score == LAPSUM_ROUTE_SOFTMAX && !A.renorm) {
+            top = row_max_f<L>(best);
+            if (top == -CUDART_INF_F) top = 0.f;
+            float s = 0.f;
+#pragma unroll
+            for (int q = 0; q < NV / 4; ++q) {
+                const float4 k4 = *reinterpret_cast<const float4 *>(mine + 4 * q);
+                s += (expf(k4.x - top) + expf(k4.y - top)) + (expf(k4.z - top) + expf(k4.w - top));  // 0 for -inf
+            }
+            total = row_sum_f<L>(s);
+        }
+    } else {
+        float x[NV];
+        load_run<T, NV, VEC>(row, first, A.E, x);
+        // softmax over the whole row, where the scores themselves are needed
+        const bool by_score = A.bias != nullptr || GROUPS;
+        if (A.score == LAPSUM_ROUTE_SOFTMAX && (by_score || !A.renorm)) {
+            float m = -CUDART_INF_F;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) m = fmaxf(m, x[i]);  // fmaxf skips NaN
+            top = row_max_f<L>(m);
+            if (top == -CUDART_INF_F) top = 0.f;
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) s += (x[i] > -CUDART_INF_F) ? expf(x[i] - top) : 0.f;
+            total = row_sum_f<L>(s);
+        }
+        if (by_score) {
+            float c[NV], offset[NV];  // the bias of my experts
+#pragma unroll
+            for (int q = 0; q < NV / 4; ++q) {
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                const int i = first + 4 * q;
+                if (A.bias != nullptr) {
+                    if (A.bias_vec) {
+                        if (i < A.E) v = __ldg(reinterpret_cast<const float4 *>(A.bias + i));
+                    } else {
+                        if (i < A.E) v.x = __ldg(A.bias + i);
+                        if (i + 1 < A.E) v.y = __ldg(A.bias + i + 1);
+                        if (i + 2 < A.E) v.z = __ldg(A.bias + i + 2);
+                        if (i + 3 < A.E) v.w = __ldg(A.bias + i + 3);
+                    }
+                }
+                offset[4 * q] = v.x, offset[4 * q + 1] = v.y, offset[4 * q + 2] = v.z, offset[4 * q + 3] = v.w;
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float s = x[i];
+                if (A.score == LAPSUM_ROUTE_SOFTMAX) s = expf(s - top) / total;
+                else if (A.score == LAPSUM_ROUTE_SIGMOID) s = sigmoid_key(s);
+                s += offset[i];
+                c[i] = (x[i] > -CUDART_INF_F && s > -CUDART_INF_F) ? s : -CUDART_INF_F;  // a NaN counts as unavailable
+            }
+            if constexpr (GROUPS) {
+#pragma unroll
+                for (int q = 0; q < NV / 4; ++q) *reinterpret_cast<float4 *>(mine + 4 * q) = make_float4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]);
+                __syncwarp();
+                const uint32_t keep = kept_groups<L>(keys + (threadIdx.x - r) * PITCH, strength + row_in_block * ROUTE_MAX_GROUPS, A, r, row_lane,
+                                                     [](int e) { return e / NV * PITCH + e % NV; });
+                __syncwarp();
+                const int size = A.E / A.groups;
+                int g = first / size;
+                if (size % NV == 0) {  // all of the lane's experts are of one group
+                    const bool in = (keep >> (g & 31)) & 1u;
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) c[i] = in ? c[i] : -CUDART_INF_F, x[i] = in ? x[i] : -CUDART_INF_F;
                 } else {
-                    if (i < A.E) v.x = __ldg(A.bias + i);
-                    if (i + 1 < A.E) v.y = __ldg(A.bias + i + 1);
-                    if (i + 2 < A.E) v.z = __ldg(A.bias + i + 2);
-                    if (i + 3 < A.E) v.w = __ldg(A.bias + i + 3);
+                    int left = (g + 1) * size - first;  // experts until the next group
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
+                        if (!((keep >> (g & 31)) & 1u)) c[i] = x[i] = -CUDART_INF_F;
+                        if (--left == 0) ++g, left = size;
+                    }
                 }
             }
-            offset[4 * q] = v.x, offset[4 * q + 1] = v.y, offset[4 * q + 2] = v.z, offset[4 * q + 3] = v.w;
-        }
+            // without a bias the experts of the kept groups are compared by their logits, which the score rises with
+            if (A.bias != nullptr) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float s = x[i];
-            if (A.score == LAPSUM_ROUTE_SOFTMAX) s = expf(s - top) / total;
-            else if (A.score == LAPSUM_ROUTE_SIGMOID) s = sigmoid_key(s);
-            s += offset[i];
-            c[i] = (x[i] > -CUDART_INF_F && s > -CUDART_INF_F) ? s : -CUDART_INF_F;  // a NaN counts as unavailable
-        }
-        if constexpr (GROUPS) {
-#pragma unroll
-            for (int q = 0; q < NV / 4; ++q) *reinterpret_cast<float4 *>(mine + 4 * q) = make_float4(c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]);
-            __syncwarp();
-            const uint32_t keep = kept_groups<L>(keys + (threadIdx.x - r) * PITCH, strength + row_in_block * ROUTE_MAX_GROUPS, A, r, row_lane,
-                                                 [](int e) { return e / NV * PITCH + e % NV; });
-            __syncwarp();
-            const int size = A.E / A.groups;
-            int g = first / size;
-            if (size % NV == 0) {  // all of the lane's experts are of one group
-                const bool in = (keep >> (g & 31)) & 1u;
-#pragma unroll
-                for (int i = 0; i < NV; ++i) c[i] = in ? c[i] : -CUDART_INF_F, x[i] = in ? x[i] : -CUDART_INF_F;
-            } else {
-                int left = (g + 1) * size - first;  // experts until the next group
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    if (!((keep >> (g & 31)) & 1u)) c[i] = x[i] = -CUDART_INF_F;
-                    if (--left == 0) ++g, left = size;
-                }
+                for (int i = 0; i < NV; ++i) x[i] = c[i];
             }
         }
-        // without a bias the experts of the kept groups are compared by their logits, which the score rises with
-        if (A.bias != nullptr) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) x[i] = c[i];
+        for (int q = 0; q < NV / 4; ++q) {
+            const float4 k4 = make_float4(route_key(x[4 * q]), route_key(x[4 * q + 1]), route_key(x[4 * q + 2]), route_key(x[4 * q + 3]));
+            *reinterpret_cast<float4 *>(mine + 4 * q) = k4;
+            run[q] = fmaxf(fmaxf(k4.x, k4.y), fmaxf(k4.z, k4.w));
+            best = fmaxf(best, run[q]);
         }
-    }
-
-    // maxima of the lane's runs of four keys
-    float run[NV / 4], best = -CUDART_INF_F;
-#pragma unroll
-    for (int q = 0; q < NV / 4; ++q) {
-        const float4 k4 = make_float4(route_key(x[4 * q]), route_key(x[4 * q + 1]), route_key(x[4 * q + 2]), route_key(x[4 * q + 3]));
-        *reinterpret_cast<float4 *>(mine + 4 * q) = k4;
-        run[q] = fmaxf(fmaxf(k4.x, k4.y), fmaxf(k4.z, k4.w));
-        best = fmaxf(best, run[q]);
     }
     short *const out = choice + row_in_block * ROUTE_MAX_K;
     for (int j = 0; j < A.k; ++j) {
