@@ -44,9 +44,12 @@ inline unsigned route_grid(int64_t tokens, int lanes) { return (unsigned)((token
 
 template <typename T, int L, int NV>
 struct RouteShape {
-    [[maybe_unused]] static constexpr int V = 16 / (int)sizeof(T) < NV ? 16 / (int)sizeof(T) : NV;  // elements of a vector access
     // whole vectors at aligned addresses in every row
-    static bool vec(const void *p, int64_t stride, int E) { return E % V == 0 && stride % V == 0 && aligned(p, V * sizeof(T)); }
+    static bool vec(const void *p, int64_t stride, int E)
+    {
+        constexpr int V = 16 / (int)sizeof(T) < NV ? 16 / (int)sizeof(T) : NV;  // elements of a vector access
+        return E % V == 0 && stride % V == 0 && aligned(p, V * sizeof(T));
+    }
 
     static int forward(const RouteArgs &A, cudaStream_t st)
     {
