@@ -9,8 +9,8 @@
 //   DW_GATE_UP    dW_gate_up = [dg; du]^T x
 //
 // A block per SM walks over output tiles.  Warp 0 brings operand tiles of 64 along the contraction into a ring of
-// shared-memory stages by TMA, one thread of warp 1 issues tcgen05.mma into one of two accumulators in TMEM, warps 4-7 read the other one
-// and finish the previous tile.  Operands that the contraction runs along the rows of (W_down in DH, W_gate_up in DX, both
+// shared-memory stages by TMA, one thread of warp 1 issues tcgen05.mma into one of two accumulators in TMEM, warps 4 to 11 (4 to 7
+// in DH) read the other one and finish the previous tile.  Operands that the contraction runs along the rows of (W_down in DH, W_gate_up in DX, both
 // sides of the weight gradients) are read as they lie in memory: the tensor core takes them "MN-major".
 //
 // Measured on pairs of blocks (8192 tokens, 4 of 32 experts, 2048 x 1024, bf16; 1.5 to 1.6 GHz under the profiler): GATE_UP 225 us,
@@ -20,8 +20,8 @@
 //
 // Roundings: the inputs of a product are 16-bit, so w h, g, u, dg, du are rounded to the storage type once, sums are
 // fp32 in TMEM; o and dx are rounded once per slot before the fp32 sum over the slots: an fp32 copy would double the traffic of
-// the combine (1.1 GB more, 0.16 ms by its bytes, on 1.65 ms for 131072 slots) to take away an error of the size of the final rounding.  Against 64
-// bits the outputs are 2.9e-3 (y, bf16; one rounding alone gives 1.7e-3) to 3.4e-3 (grad_x) off in the 2-norm.
+// the combine (1.1 GB more, 0.16 ms by its bytes, on 1.65 ms for 131072 slots) to take away an error of the size of the final
+// rounding.  Against 64 bits the outputs are 2.9e-3 (y, bf16; one rounding alone gives 1.7e-3) to 3.4e-3 (grad_x) off in the 2-norm.
 #pragma once
 #include <cuda.h>
 

@@ -157,9 +157,9 @@ struct ExpertsLayout {
     bool wide_dh;  // of 256 columns
 };
 
-// Columns of an output tile: 256, the most that two accumulators in TMEM allow; 128 for narrow row tiles where 256 would leave
-// SMs without work (fewer than two tiles for each).  Measured, bf16 / fp16: 48 tokens on 128 experts 210 us with 256 columns and
-// 215 us with 128, one token on 8 experts 43 us and 35 us.
+// Columns of an output tile: 256, the most that two accumulators in TMEM allow; 128 where 256 would leave SMs without work (fewer
+// than two tiles for each; pairs of blocks always take 256).  Measured: 48 tokens on 128 experts 210 us with 256 columns and 215 us with
+// 128, eight experts' first product for one row tile each 43 us and 35 us, DH of 777 tokens on 24 experts 26 us and 19 us.
 constexpr int MIN_TILES = 2 * 148;
 inline bool wide_tiles(const lapsum_experts_dims *p, const lapsum_dispatch_layout &d, int64_t cols, bool gate_up)
 {
