@@ -17,6 +17,10 @@ constexpr unsigned FULL = 0xffffffffu;
 // completed and its writes are visible.  (A no-op for kernels launched the ordinary way.)  Every
 // kernel must execute it, early-exit paths included, so that completion stays transitive.
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// A load of data that the previous kernel may have written, for kernels that can overlap with it: the coherent path.  (ld.global.nc
+// promises data that stays constant for the kernel's life, so the compiler may move such a load above the wait.)
+template <typename T>
+__device__ __forceinline__ T ld(const T *p) { return *p; }
 
 // ---------------------------------------------------------------- keys ----
 // Ascending total order on fp32 bit patterns: flip all bits of negatives, set

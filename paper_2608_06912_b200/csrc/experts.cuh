@@ -364,8 +364,8 @@ __global__ void __launch_bounds__((ExpertsShape<MODE, AR, BN, KS>::THREADS), 1) 
         if constexpr (S::WGRAD) {
             t.e = (int)((uint32_t)rest / (uint32_t)mts);  // experts x row tiles stay below 2^31
             t.m0 = (int)((uint32_t)rest - (uint32_t)t.e * (uint32_t)mts) * MT + (int)rank * 128;
-            t.kb = min(max(__ldg(P.offsets + t.e), 0), P.capacity);
-            t.nkb = (min(max(__ldg(P.counts + t.e), 0), P.capacity) + 63) / 64;  // the last stage's holes are zeros
+            t.kb = min(max(ld(P.offsets + t.e), 0), P.capacity);
+            t.nkb = (min(max(ld(P.counts + t.e), 0), P.capacity) + 63) / 64;  // the last stage's holes are zeros
         } else {
             t.e = __ldcg(P.tile_expert + rest);  // past L1: it may be read before griddepcontrol.wait
             if ((unsigned)t.e >= (unsigned)P.E) t.e = -1;
@@ -397,7 +397,7 @@ __global__ void __launch_bounds__((ExpertsShape<MODE, AR, BN, KS>::THREADS), 1) 
             if (i < tiles) next = tile_at(i);
             else next.e = -1;
             if constexpr (S::A_GATHER)  // four neighbouring slots per lane
-                if (i < tiles && lane < AR / 4) entries = __ldg(reinterpret_cast<const int4 *>(P.entry_of + next.m0 + 4 * lane));
+                if (i < tiles && lane < AR / 4) entries = ld(reinterpret_cast<const int4 *>(P.entry_of + next.m0 + 4 * lane));
         };
         look_ahead(tile0);
         int4 rows = make_int4(0, 0, 0, 0);  // the tile's tokens; holes give a row beyond the matrix, which reads as zeros
@@ -571,9 +571,9 @@ __global__ void __launch_bounds__((ExpertsShape<MODE, AR, BN, KS>::THREADS), 1) 
             int entry = -1;
             float w = 0.f, dot = 0.f;
             if constexpr (MODE == GATE_UP || MODE == DH) {
-                if (mine) entry = __ldg(P.entry_of + t.m0 + row);
+                if (mine) entry = ld(P.entry_of + t.m0 + row);
                 if ((unsigned)entry >= (unsigned)P.entries) entry = -1;
-                if (entry >= 0) w = __ldg(P.w + entry);
+                if (entry >= 0) w = ld(P.w + entry);
             }
             if constexpr (MODE == DH) {
                 if (live) {
@@ -753,12 +753,12 @@ __global__ void __launch_bounds__(256, 2) experts_few_gate_up_kernel(const T *x,
     pdl_wait();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, entry = blockIdx.y;
-    const int slot = __ldg(slot_of + entry);
+    const int slot = ld(slot_of + entry);
     if ((unsigned)slot >= (unsigned)capacity) return;  // dropped: the second product skips it too
-    const int64_t e = __ldg(tile_expert + (slot >> shift));
+    const int64_t e = ld(tile_expert + (slot >> shift));
     if (e < 0 || e >= E) return;
     const T *const xt = x + entry / k * stride;
-    const float scale = __ldg(w + entry);
+    const float scale = ld(w + entry);
     const int f1 = min(F, (int)(blockIdx.x + 1) * FEW_FEATURES);
     for (int f = blockIdx.x * FEW_FEATURES + (threadIdx.x >> 5); f < f1; f += 8) {
         const T *const gate = w_gate_up + (e * 2 * F + f) * D, *const up = gate + (int64_t)F * D;
@@ -774,7 +774,7 @@ __global__ void __launch_bounds__(256, 2) experts_few_gate_up_kernel(const T *x,
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (c + 256 * i < D) {
-                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(xt + c + 256 * i));
+                    const uint4 v = ld(reinterpret_cast<const uint4 *>(xt + c + 256 * i));
                     g = dot8<T>(a[i], v, g);
                     u = dot8<T>(b[i], v, u);
                 }
@@ -812,7 +812,7 @@ __global__ void __launch_bounds__(256, 3) experts_few_down_kernel(const T *w_dow
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (c + 256 * i < F) {
-                    const uint4 h = __ldg(reinterpret_cast<const uint4 *>(v + c + 256 * i));
+                    const uint4 h = ld(reinterpret_cast<const uint4 *>(v + c + 256 * i));
 #pragma unroll
                     for (int r = 0; r < 4; ++r) sum[r] = dot8<T>(a[r][i], h, sum[r]);
                 }
@@ -848,12 +848,12 @@ __global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t
         const int64_t t = unit / parts;
         if (t >= tokens) return;
         const int i = (int)(unit - t * parts) * 128 + lane;
-        const int mine = lane < k ? __ldg(slot_of + t * k + lane) : -1;
+        const int mine = lane < k ? ld(slot_of + t * k + lane) : -1;
         const uint4 *const from = reinterpret_cast<const uint4 *>(x + t * stride);
         uint4 v[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (i + 32 * j < n) v[j] = __ldg(from + i + 32 * j);
+            if (i + 32 * j < n) v[j] = ld(from + i + 32 * j);
         for (int c = 0; c < k; ++c) {
             const int slot = __shfl_sync(FULL, mine, c);
             if ((unsigned)slot >= (unsigned)capacity) continue;
@@ -864,8 +864,8 @@ __global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t
         }
     } else {
         const int64_t slot0 = (unit - 8 * (int64_t)token_blocks) * 4;
-        if (slot0 >= min(__ldg(used), capacity)) return;  // both multiples of 64
-        const int4 e = __ldg(reinterpret_cast<const int4 *>(entry_of + slot0));
+        if (slot0 >= min(ld(used), capacity)) return;  // both multiples of 64
+        const int4 e = ld(reinterpret_cast<const int4 *>(entry_of + slot0));
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             if ((s == 0 ? e.x : s == 1 ? e.y : s == 2 ? e.z : e.w) >= 0) continue;
@@ -877,13 +877,12 @@ __global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t
 
 // y_t = sum over the token's slots, in the order of its choices, eight columns per thread; dropped entries (-1) add nothing.
 // With `partial` also grad_w of the token's entries: the column tiles' sums in order.  Bound by memory: 131072 slots of 4 KB in 89 us
-// (6.7 TB/s).
+// (6.7 TB/s).  The last kernel of a call lets no other start early: its results may go to kernels that read through the non-coherent path.
 template <typename T>
 __global__ void __launch_bounds__(256) experts_combine_kernel(const T *slots, const int32_t *slot_of, T *out, int64_t out_stride,
                                                               const float *partial, T *grad_w, int64_t tokens, int capacity, int k, int D, int nts)
 {
     pdl_wait();
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int per = D / 8;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t t = id / per;
@@ -895,9 +894,9 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(const T *slots, co
         int s[8];
         uint4 q[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] = j0 + j < k ? __ldg(at + j0 + j) : -1;
+        for (int j = 0; j < 8; ++j) s[j] = j0 + j < k ? ld(at + j0 + j) : -1;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = (unsigned)s[j] < (unsigned)capacity ? __ldg(reinterpret_cast<const uint4 *>(slots + (int64_t)s[j] * D + 8 * c)) : Io<T>::zero();
+        for (int j = 0; j < 8; ++j) q[j] = (unsigned)s[j] < (unsigned)capacity ? ld(reinterpret_cast<const uint4 *>(slots + (int64_t)s[j] * D + 8 * c)) : Io<T>::zero();
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float v[8];
@@ -909,7 +908,7 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(const T *slots, co
     store8(out + t * out_stride + 8 * c, sum);
     if (partial != nullptr)
         for (int j = c; j < k; j += per) {
-            const int s = __ldg(at + j);
+            const int s = ld(at + j);
             float g = 0.f;
             if ((unsigned)s < (unsigned)capacity)
                 for (int n = 0; n < nts; ++n) g += partial[(int64_t)s * nts + n];

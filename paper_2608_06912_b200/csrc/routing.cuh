@@ -63,15 +63,15 @@ __device__ __forceinline__ void load_run(const T *row, int first, int E, float (
         for (int q = 0; q < NV / V; ++q) {
             T h[V];
             if (first + q * V < E) {
-                if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4 *>(h) = __ldg(reinterpret_cast<const uint4 *>(row + first + q * V));
-                else *reinterpret_cast<uint2 *>(h) = __ldg(reinterpret_cast<const uint2 *>(row + first + q * V));
+                if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4 *>(h) = ld(reinterpret_cast<const uint4 *>(row + first + q * V));
+                else *reinterpret_cast<uint2 *>(h) = ld(reinterpret_cast<const uint2 *>(row + first + q * V));
             }
 #pragma unroll
             for (int v = 0; v < V; ++v) x[q * V + v] = (first + q * V < E) ? Io<T>::from_storage(h[v]) : -CUDART_INF_F;
         }
     } else {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) x[v] = (first + v < E) ? Io<T>::load1(row + first + v) : -CUDART_INF_F;
+        for (int v = 0; v < NV; ++v) x[v] = (first + v < E) ? Io<T>::from_storage(ld(row + first + v)) : -CUDART_INF_F;
     }
 }
 
@@ -153,8 +153,8 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, NV > 16 && !PLAIN ? 2 : 4) r
             if (t0 + rr < A.tokens && e < A.E) {
                 T h[4];
                 const T *const from = reinterpret_cast<const T *>(A.logits) + (t0 + rr) * A.stride + e;
-                if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4 *>(h) = __ldg(reinterpret_cast<const uint4 *>(from));
-                else *reinterpret_cast<uint2 *>(h) = __ldg(reinterpret_cast<const uint2 *>(from));
+                if constexpr (sizeof(T) == 4) *reinterpret_cast<uint4 *>(h) = ld(reinterpret_cast<const uint4 *>(from));
+                else *reinterpret_cast<uint2 *>(h) = ld(reinterpret_cast<const uint2 *>(from));
                 k4 = make_float4(route_key(Io<T>::from_storage(h[0])), route_key(Io<T>::from_storage(h[1])), route_key(Io<T>::from_storage(h[2])),
                                  route_key(Io<T>::from_storage(h[3])));
             }
@@ -202,12 +202,12 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, NV > 16 && !PLAIN ? 2 : 4) r
                 const int i = first + 4 * q;
                 if (A.bias != nullptr) {
                     if (A.bias_vec) {
-                        if (i < A.E) v = __ldg(reinterpret_cast<const float4 *>(A.bias + i));
+                        if (i < A.E) v = ld(reinterpret_cast<const float4 *>(A.bias + i));
                     } else {
-                        if (i < A.E) v.x = __ldg(A.bias + i);
-                        if (i + 1 < A.E) v.y = __ldg(A.bias + i + 1);
-                        if (i + 2 < A.E) v.z = __ldg(A.bias + i + 2);
-                        if (i + 3 < A.E) v.w = __ldg(A.bias + i + 3);
+                        if (i < A.E) v.x = ld(A.bias + i);
+                        if (i + 1 < A.E) v.y = ld(A.bias + i + 1);
+                        if (i + 2 < A.E) v.z = ld(A.bias + i + 2);
+                        if (i + 3 < A.E) v.w = ld(A.bias + i + 3);
                     }
                 }
                 offset[4 * q] = v.x, offset[4 * q + 1] = v.y, offset[4 * q + 2] = v.z, offset[4 * q + 3] = v.w;
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, NV > 16 && !PLAIN ? 2 : 4) r
 #pragma unroll
     for (int p = 0; p < C; ++p) {
         e[p] = (p * L + r < A.k) ? out[p * L + r] : -1;
-        l[p] = (e[p] >= 0) ? Io<T>::load1(row + e[p]) : -CUDART_INF_F;
+        l[p] = (e[p] >= 0) ? Io<T>::from_storage(ld(row + e[p])) : -CUDART_INF_F;
     }
     float peak = l[0], sum = 0.f;
     if (A.renorm && A.score != LAPSUM_ROUTE_GIVEN) {
@@ -342,9 +342,9 @@ struct RouteBackArgs {
 
 __device__ __forceinline__ float route_grad_w(const RouteBackArgs &A, int64_t at)
 {
-    return A.gw_dtype == LAPSUM_IO_F32   ? __ldg(reinterpret_cast<const float *>(A.grad_w) + at)
-           : A.gw_dtype == LAPSUM_IO_F16 ? Io<__half>::load1(reinterpret_cast<const __half *>(A.grad_w) + at)
-                                         : Io<__nv_bfloat16>::load1(reinterpret_cast<const __nv_bfloat16 *>(A.grad_w) + at);
+    return A.gw_dtype == LAPSUM_IO_F32   ? ld(reinterpret_cast<const float *>(A.grad_w) + at)
+           : A.gw_dtype == LAPSUM_IO_F16 ? Io<__half>::from_storage(ld(reinterpret_cast<const __half *>(A.grad_w) + at))
+                                         : Io<__nv_bfloat16>::from_storage(ld(reinterpret_cast<const __nv_bfloat16 *>(A.grad_w) + at));
 }
 
 // Gradient of the logits where only the chosen ones have one: with W = sum_j gw_j w_j / scale and g_j = w_j (gw_j - W),
@@ -363,8 +363,8 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_backward_kernel(const 
     float w = 0.f, gw = 0.f, l = 0.f;
     if (r < A.k && t < A.tokens) {
         const int64_t at = t * A.k + r;
-        mine = __ldg(A.idx + at);
-        w = __ldg(A.w + at);
+        mine = ld(A.idx + at);
+        w = ld(A.w + at);
         gw = route_grad_w(A, at);
     }
     T *const out = reinterpret_cast<T *>(A.grad) + t0 * A.E;
@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_backward_kernel(const 
     }
     const bool chosen = mine >= 0 && mine < A.E;
     if (!chosen) w = 0.f, gw = 0.f;
-    if (chosen && A.score != LAPSUM_ROUTE_SOFTMAX) l = Io<T>::load1(reinterpret_cast<const T *>(A.logits) + t * A.stride + mine);
+    if (chosen && A.score != LAPSUM_ROUTE_SOFTMAX) l = Io<T>::from_storage(ld(reinterpret_cast<const T *>(A.logits) + t * A.stride + mine));
     const float gww = row_sum_f<L>(gw * w);  // = scale W
     float g;
     if (A.score == LAPSUM_ROUTE_SOFTMAX) {
@@ -416,9 +416,9 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_backward_dense_kernel(
         const int j = p * L + r;
         mine[p] = -1, w[p] = gw[p] = 0.f;
         if (live && j < A.k) {
-            mine[p] = __ldg(A.idx + t * A.k + j);
+            mine[p] = ld(A.idx + t * A.k + j);
             if (mine[p] >= A.E) mine[p] = -1;
-            if (mine[p] >= 0) w[p] = __ldg(A.w + t * A.k + j), gw[p] = route_grad_w(A, t * A.k + j);
+            if (mine[p] >= 0) w[p] = ld(A.w + t * A.k + j), gw[p] = route_grad_w(A, t * A.k + j);
         }
         gww += gw[p] * w[p];
     }
@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_count_kernel(const 
 #pragma unroll
         for (int j = 0; j < DISPATCH_PER; ++j) {
             const int64_t i = begin + j * DISPATCH_THREADS + threadIdx.x;
-            e[j] = i < A.entries ? __ldg(A.idx + i) : -1;
+            e[j] = i < A.entries ? ld(A.idx + i) : -1;
         }
 #pragma unroll
         for (int j = 0; j < DISPATCH_PER; ++j)
@@ -527,7 +527,7 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_place_kernel(const 
             int4 all = make_int4(0, 0, 0, 0), b = make_int4(0, 0, 0, 0);
 #pragma unroll 4
             for (int c = c0; c < A.blocks; c += groups) {
-                const int4 v = __ldg(reinterpret_cast<const int4 *>(A.partial + (int64_t)c * stride + q));
+                const int4 v = ld(reinterpret_cast<const int4 *>(A.partial + (int64_t)c * stride + q));
                 all.x += v.x, all.y += v.y, all.z += v.z, all.w += v.w;
                 if (c < (int)blockIdx.x) b.x += v.x, b.y += v.y, b.z += v.z, b.w += v.w;
             }
@@ -544,7 +544,7 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_place_kernel(const 
         int e[DISPATCH_PER], rank[DISPATCH_PER];
 #pragma unroll
         for (int j = 0; j < DISPATCH_PER; ++j) {
-            const int v = j < rounds && begin + 32 * j < A.entries ? __ldg(A.idx + begin + 32 * j) : -1;
+            const int v = j < rounds && begin + 32 * j < A.entries ? ld(A.idx + begin + 32 * j) : -1;
             e[j] = (unsigned)v < (unsigned)E ? v : E;  // E: dropped
         }
 #pragma unroll
