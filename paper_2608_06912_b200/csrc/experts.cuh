@@ -199,7 +199,8 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn_major)
     return (uint64_t)((addr & 0x3ffff) >> 4) | (lbo << 16) | (sbo << 32) | (1ull << 46) | (2ull << 61);
 }
 
-// Waits of one block: bounded; the first that runs out raises the block's flag, on which all others give up.
+// Waits of one block: bounded; the first that runs out raises the block's flag, on which all others give up, except those
+// for copies into the block's own memory, which must land before it ends.
 struct Waits {
     volatile int *abort;
     uint32_t *status;
@@ -640,7 +641,7 @@ __global__ void __launch_bounds__((ExpertsShape<MODE, AR, BN, KS>::THREADS), 1) 
                             __syncwarp();
                             bring(t, c + 64, chunk + 1);
                         }
-                        ok = waits.wait(loaded + 8 * (2 * ew + (chunk & 1)), (chunk >> 1) & 1);
+                        waits.plain(loaded + 8 * (2 * ew + (chunk & 1)), (chunk >> 1) & 1, false);  // whatever the others do: the copy must land
 #pragma unroll
                         for (int j = 0; j < 64; j += 16) {
                             float dh[16];

@@ -40,3 +40,12 @@ def test_the_last_kernel_of_a_call_lets_no_other_start_early():
     for kernel in ("experts_combine_kernel", "experts_few_down_kernel"):
         assert "launch_dependents" not in body(text, kernel), kernel
     assert "launch_dependents" not in code("routing.cuh")
+
+
+def test_copies_into_a_block_s_memory_are_waited_for_though_the_block_gave_up():
+    """A wait that heeds the block's give-up flag returns while the copy is on its way, and the block could end before the copy lands
+    in its shared memory.  Waits for copies (of the ring on the way out, and of the epilogue's own) are bounded by time alone."""
+    text = code("experts.cuh")
+    assert not re.search(r"waits\.wait\(loaded\b", text)
+    assert len(re.findall(r"waits\.plain\(loaded\b[^;]*, false\)", text)) == 2
+    assert re.search(r"waits\.plain\(full \+ 8 \* s, phase, false\)", text)
