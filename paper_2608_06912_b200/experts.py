@@ -5,12 +5,14 @@
     experts   ExpertsWorkspace, lapsum_experts_forward / lapsum_experts_backward
 
 Argument marshalling only, like binding.py.  Outputs are the caller's tensors.  A call made on another stream than the
-one its tensors were made on follows PyTorch's rules: the caller orders the streams; buffers that Dispatch and
-ExpertsWorkspace own are recorded on the stream of every call, so dropping the object early is safe.
+one its tensors were made on follows PyTorch's rules: the caller orders the streams, and records tensors of its own (`saved` among
+them).  Buffers that Dispatch and ExpertsWorkspace own are recorded on the stream of every call, given or current, so
+dropping the object early is safe.
 """
 from __future__ import annotations
 
 import ctypes as C
+from contextlib import nullcontext
 from typing import Optional
 
 import torch
@@ -109,7 +111,24 @@ def _cuda(device) -> torch.device:
     return torch.device(device) if device is not None else torch.device("cuda", torch.cuda.current_device())
 
 
-class Dispatch:
+class _Memory:
+    """A buffer of the library's and the streams that use it."""
+
+    def _allocate(self, n: int, device: torch.device) -> None:
+        self.buf = _buffer(n, device)
+        self.ptr, self.device = self.buf.data_ptr(), self.buf.device
+        self._streams = {_stream(None, self.device)}  # the allocator's memory belongs to the stream that is current
+
+    def _use(self, stream: Optional[torch.cuda.Stream]) -> int:
+        """The handle of a call's stream; when the buffer is freed, its memory waits for every stream that was seen here."""
+        handle = _stream(stream, self.device)
+        if handle not in self._streams:
+            self.buf.record_stream(stream if stream is not None else torch.cuda.current_stream(self.device))
+            self._streams.add(handle)
+        return handle
+
+
+class Dispatch(_Memory):
     """The tables of one batch (lapsum_dispatch_describe): counts, offsets, slot_of (tokens x k), entry_of, tile_expert are
     int32 views of one buffer that lapsum_dispatch fills."""
 
@@ -120,8 +139,7 @@ class Dispatch:
         self.tile_rows = int(tile_rows) if tile_rows is not None else dispatch_tile_rows(tokens, k, experts, training)
         self.layout = L = lapsum_dispatch_describe(self.tokens, self.k, self.experts, self.tile_rows)
         self.capacity, self.bytes = L.capacity, L.bytes
-        self.buf = _buffer(L.bytes, dev)
-        self.ptr, self.device = self.buf.data_ptr(), self.buf.device
+        self._allocate(L.bytes, dev)
 
         def words(off, n):
             return self.buf[off:off + 4 * n].view(torch.int32)
@@ -136,15 +154,13 @@ class Dispatch:
 def lapsum_dispatch(idx: torch.Tensor, dispatch: Dispatch, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Fill the tables from idx (int32, tokens x k; entries outside [0, experts) are dropped)."""
     d = dispatch
-    if stream is not None:
-        d.buf.record_stream(stream)
     rc = lib().lapsum_dispatch(_dense(idx, torch.int32, (d.tokens, d.k), "idx"), d.tokens, d.k, d.experts, d.tile_rows, d.ptr,
-                               d.bytes, _stream(stream, d.device))
+                               d.bytes, d._use(stream))
     if rc:
         _check(rc, "lapsum_dispatch")
 
 
-class ExpertsWorkspace:
+class ExpertsWorkspace(_Memory):
     """Scratch of the experts' products for one shape (lapsum_experts_describe); new_saved() makes the buffer that a
     training forward leaves its activations in, one per forward whose backward is still to come."""
 
@@ -158,11 +174,10 @@ class ExpertsWorkspace:
         _check(lib().lapsum_experts_describe(C.byref(self.dims), C.byref(out)), "lapsum_experts_describe")
         self.bytes, self.saved_bytes = out.workspace_bytes, out.saved_bytes
         self.shape = (p.tokens, p.k, p.experts, p.tile_rows)
-        self.buf = _buffer(self.bytes, p.device)
-        self.ptr, self.device = self.buf.data_ptr(), self.buf.device
-        if stream is not None:
-            self.buf.record_stream(stream)
-        _check(lib().lapsum_experts_workspace_init(self.ptr, self.bytes, C.byref(self.dims), _stream(stream, self.device)),
+        # on the stream that clears it: memory asked for on another one may still be written by what is queued there
+        with torch.cuda.stream(stream) if stream is not None else nullcontext():
+            self._allocate(self.bytes, p.device)
+        _check(lib().lapsum_experts_workspace_init(self.ptr, self.bytes, C.byref(self.dims), self._use(stream)),
                "lapsum_experts_workspace_init")
         self._x = (p.tokens, int(d))
         self._gate_up, self._down = (p.experts, 2 * int(f), int(d)), (p.experts, int(d), int(f))
@@ -176,7 +191,7 @@ class ExpertsWorkspace:
     def status(self, stream: Optional[torch.cuda.Stream] = None) -> int:
         """Status bits (ST_EXPERTS_TIMEOUT); synchronises the stream."""
         out = C.c_uint32()
-        _check(lib().lapsum_experts_status(self.ptr, _stream(stream, self.device), C.byref(out)), "lapsum_experts_status")
+        _check(lib().lapsum_experts_status(self.ptr, self._use(stream), C.byref(out)), "lapsum_experts_status")
         return out.value
 
 
@@ -200,14 +215,12 @@ def lapsum_experts_forward(x: torch.Tensor, w_gate_up: torch.Tensor, w_down: tor
     stride = _rows(x, ws.dtype, "x")
     if x.shape != ws._x:
         raise ValueError(f"x must have shape {ws._x}")
-    if stream is not None:
-        dispatch.buf.record_stream(stream)
-        ws.buf.record_stream(stream)
+    dispatch._use(stream)
     rc = lib().lapsum_experts_forward(
         x.data_ptr(), stride, _dense(w_gate_up, ws.dtype, ws._gate_up, "w_gate_up"), _dense(w_down, ws.dtype, ws._down, "w_down"),
         _dense(w, torch.float32, ws._w, "w"), dispatch.ptr, dispatch.bytes, None if saved is None else _saved(saved, ws),
         0 if saved is None else saved.numel(), _dense(y, ws.dtype, ws._x, "y"), C.byref(ws.dims), ws.ptr, ws.bytes,
-        _stream(stream, ws.device))
+        ws._use(stream))
     if rc:
         _check(rc, "lapsum_experts_forward")
 
@@ -221,14 +234,12 @@ def lapsum_experts_backward(grad_y: torch.Tensor, x: torch.Tensor, w_gate_up: to
     gy_stride, x_stride = _rows(grad_y, ws.dtype, "grad_y"), _rows(x, ws.dtype, "x")
     if x.shape != ws._x or grad_y.shape != ws._x:
         raise ValueError(f"x and grad_y must have shape {ws._x}")
-    if stream is not None:
-        dispatch.buf.record_stream(stream)
-        ws.buf.record_stream(stream)
+    dispatch._use(stream)
     rc = lib().lapsum_experts_backward(
         grad_y.data_ptr(), gy_stride, x.data_ptr(), x_stride, _dense(w_gate_up, ws.dtype, ws._gate_up, "w_gate_up"),
         _dense(w_down, ws.dtype, ws._down, "w_down"), _dense(w, torch.float32, ws._w, "w"), dispatch.ptr, dispatch.bytes,
         _saved(saved, ws), saved.numel(), _dense(grad_x, ws.dtype, ws._x, "grad_x"),
         _dense(grad_w_gate_up, ws.dtype, ws._gate_up, "grad_w_gate_up"), _dense(grad_w_down, ws.dtype, ws._down, "grad_w_down"),
-        _dense(grad_w, ws.dtype, ws._w, "grad_w"), C.byref(ws.dims), ws.ptr, ws.bytes, _stream(stream, ws.device))
+        _dense(grad_w, ws.dtype, ws._w, "grad_w"), C.byref(ws.dims), ws.ptr, ws.bytes, ws._use(stream))
     if rc:
         _check(rc, "lapsum_experts_backward")
