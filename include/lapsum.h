@@ -456,7 +456,8 @@ const char *lapsum_kernel_name(int kernel_id);
 /*
  * Mixture-of-experts operators: what follows a routing score in a model.  route -> dispatch -> experts; the scores may be
  * a router's logits or the soft mask that lapsum_forward returns.  None of these calls allocates, synchronises or keeps
- * anything from one call for the next; every buffer is the caller's.
+ * anything from one call for the next; every buffer is the caller's.  Buffers and stream belong to the calling thread's current
+ * device, where the kernels are launched.
  *
  * lapsum_route_forward: per token, from `experts` logits l (rows `stride` elements apart, io_dtype):
  *   scores   s = softmax(l) | sigmoid(l) | l itself ("given": a soft mask)

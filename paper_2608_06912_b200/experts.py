@@ -7,7 +7,7 @@
 Argument marshalling only, like binding.py.  Outputs are the caller's tensors.  A call made on another stream than the
 one its tensors were made on follows PyTorch's rules: the caller orders the streams, and records tensors of its own (`saved` among
 them).  Buffers that Dispatch and ExpertsWorkspace own are recorded on the stream of every call, given or current, so
-dropping the object early is safe.
+dropping the object early is safe.  A call's tensors are all on the current device, and so is its stream; anything else is refused.
 """
 from __future__ import annotations
 
@@ -36,23 +36,37 @@ def route_params(**overrides) -> RouteParams:
     return p
 
 
-def _stream(stream: Optional[torch.cuda.Stream], device: torch.device) -> int:
-    # the current stream's handle alone: building a Stream object costs 2 us a call
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
+def _stream(stream: Optional[torch.cuda.Stream], gpu: int) -> int:
+    """The handle of a call's stream on the GPU of its tensors, which has to be the current one: the library launches there."""
+    if torch._C._cuda_getDevice() != gpu:
+        raise ValueError(f"the tensors are on cuda:{gpu}, but cuda:{torch._C._cuda_getDevice()} is the current device")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(gpu)  # the handle alone: building a Stream object costs 2 us a call
+    if stream.device_index != gpu:
+        raise ValueError(f"the tensors are on cuda:{gpu}, the stream on cuda:{stream.device_index}")
+    return stream.cuda_stream
 
 
-def _rows(t: torch.Tensor, dtype: torch.dtype, name: str) -> int:
+def _on(t: torch.Tensor, gpu: int, name: str) -> None:
+    if t.get_device() != gpu:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the call's other tensors on cuda:{gpu}")
+
+
+def _rows(t: torch.Tensor, dtype: torch.dtype, name: str, gpu: Optional[int] = None) -> int:
     """Row stride of a matrix whose rows are contiguous."""
     if not (t.is_cuda and t.dtype == dtype and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)):
         raise TypeError(f"{name} must be a {dtype} CUDA matrix with contiguous rows")
+    if gpu is not None:
+        _on(t, gpu, name)
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def _dense(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str) -> int:
+def _dense(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str, gpu: int) -> int:
     if not (t.is_cuda and t.dtype == dtype and t.is_contiguous()):
         raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    _on(t, gpu, name)
     return t.data_ptr()
 
 
@@ -62,10 +76,10 @@ def lapsum_route_forward(logits: torch.Tensor, bias: Optional[torch.Tensor], par
     params' io_dtype with contiguous rows (any row stride); bias: float32, one per expert, or None."""
     stride = _rows(logits, IO_TORCH[params.io_dtype], "logits")
     tokens, experts = logits.shape
-    out = (tokens, params.k)
+    out, gpu = (tokens, params.k), logits.get_device()
     rc = lib().lapsum_route_forward(
-        logits.data_ptr(), tokens, experts, stride, None if bias is None else _dense(bias, torch.float32, (experts,), "bias"),
-        C.byref(params), _dense(idx, torch.int32, out, "idx"), _dense(w, torch.float32, out, "w"), _stream(stream, logits.device))
+        logits.data_ptr(), tokens, experts, stride, None if bias is None else _dense(bias, torch.float32, (experts,), "bias", gpu),
+        C.byref(params), _dense(idx, torch.int32, out, "idx", gpu), _dense(w, torch.float32, out, "w", gpu), _stream(stream, gpu))
     if rc:
         _check(rc, "lapsum_route_forward")
 
@@ -76,11 +90,11 @@ def lapsum_route_backward(grad_w: torch.Tensor, logits: torch.Tensor, idx: torch
     dtype = IO_TORCH[params.io_dtype]
     stride = _rows(logits, dtype, "logits")
     tokens, experts = logits.shape
-    ch = (tokens, params.k)
+    ch, gpu = (tokens, params.k), logits.get_device()
     rc = lib().lapsum_route_backward(
-        _dense(grad_w, IO_TORCH[params.grad_w_dtype], ch, "grad_w"), logits.data_ptr(), tokens, experts, stride,
-        _dense(idx, torch.int32, ch, "idx"), _dense(w, torch.float32, ch, "w"), C.byref(params),
-        _dense(grad_logits, dtype, (tokens, experts), "grad_logits"), _stream(stream, logits.device))
+        _dense(grad_w, IO_TORCH[params.grad_w_dtype], ch, "grad_w", gpu), logits.data_ptr(), tokens, experts, stride,
+        _dense(idx, torch.int32, ch, "idx", gpu), _dense(w, torch.float32, ch, "w", gpu), C.byref(params),
+        _dense(grad_logits, dtype, (tokens, experts), "grad_logits", gpu), _stream(stream, gpu))
     if rc:
         _check(rc, "lapsum_route_backward")
 
@@ -116,12 +130,12 @@ class _Memory:
 
     def _allocate(self, n: int, device: torch.device) -> None:
         self.buf = _buffer(n, device)
-        self.ptr, self.device = self.buf.data_ptr(), self.buf.device
-        self._streams = {_stream(None, self.device)}  # the allocator's memory belongs to the stream that is current
+        self.ptr, self.device, self.gpu = self.buf.data_ptr(), self.buf.device, self.buf.get_device()
+        self._streams = {torch._C._cuda_getCurrentRawStream(self.gpu)}  # the allocator's memory belongs to the stream that is current
 
     def _use(self, stream: Optional[torch.cuda.Stream]) -> int:
         """The handle of a call's stream; when the buffer is freed, its memory waits for every stream that was seen here."""
-        handle = _stream(stream, self.device)
+        handle = _stream(stream, self.gpu)
         if handle not in self._streams:
             self.buf.record_stream(stream if stream is not None else torch.cuda.current_stream(self.device))
             self._streams.add(handle)
@@ -154,7 +168,7 @@ class Dispatch(_Memory):
 def lapsum_dispatch(idx: torch.Tensor, dispatch: Dispatch, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Fill the tables from idx (int32, tokens x k; entries outside [0, experts) are dropped)."""
     d = dispatch
-    rc = lib().lapsum_dispatch(_dense(idx, torch.int32, (d.tokens, d.k), "idx"), d.tokens, d.k, d.experts, d.tile_rows, d.ptr,
+    rc = lib().lapsum_dispatch(_dense(idx, torch.int32, (d.tokens, d.k), "idx", d.gpu), d.tokens, d.k, d.experts, d.tile_rows, d.ptr,
                                d.bytes, d._use(stream))
     if rc:
         _check(rc, "lapsum_dispatch")
@@ -174,6 +188,7 @@ class ExpertsWorkspace(_Memory):
         _check(lib().lapsum_experts_describe(C.byref(self.dims), C.byref(out)), "lapsum_experts_describe")
         self.bytes, self.saved_bytes = out.workspace_bytes, out.saved_bytes
         self.shape = (p.tokens, p.k, p.experts, p.tile_rows)
+        _stream(stream, p.gpu)  # the checks
         # on the stream that clears it: memory asked for on another one may still be written by what is queued there
         with torch.cuda.stream(stream) if stream is not None else nullcontext():
             self._allocate(self.bytes, p.device)
@@ -198,11 +213,14 @@ class ExpertsWorkspace(_Memory):
 def _same_shape(dispatch: Dispatch, ws: ExpertsWorkspace) -> None:
     if (dispatch.tokens, dispatch.k, dispatch.experts, dispatch.tile_rows) != ws.shape:
         raise ValueError("the dispatch tables and the workspace were made for different shapes")
+    if dispatch.gpu != ws.gpu:
+        raise ValueError(f"the dispatch tables are on cuda:{dispatch.gpu}, the workspace on cuda:{ws.gpu}")
 
 
 def _saved(saved: Optional[torch.Tensor], ws: ExpertsWorkspace) -> int:
     if saved is None or not (saved.is_cuda and saved.dtype == torch.uint8 and saved.is_contiguous()):
         raise TypeError("saved must be a buffer of ExpertsWorkspace.new_saved()")
+    _on(saved, ws.gpu, "saved")
     return saved.data_ptr()
 
 
@@ -212,14 +230,15 @@ def lapsum_experts_forward(x: torch.Tensor, w_gate_up: torch.Tensor, w_down: tor
     """y (tokens x d) <- the weighted sum of every token's experts.  x: tokens x d with contiguous rows; w_gate_up: experts x
     2f x d; w_down: experts x d x f; w: tokens x k float32.  `saved` for a training workspace only."""
     _same_shape(dispatch, ws)
-    stride = _rows(x, ws.dtype, "x")
+    gpu = ws.gpu
+    stride = _rows(x, ws.dtype, "x", gpu)
     if x.shape != ws._x:
         raise ValueError(f"x must have shape {ws._x}")
     dispatch._use(stream)
     rc = lib().lapsum_experts_forward(
-        x.data_ptr(), stride, _dense(w_gate_up, ws.dtype, ws._gate_up, "w_gate_up"), _dense(w_down, ws.dtype, ws._down, "w_down"),
-        _dense(w, torch.float32, ws._w, "w"), dispatch.ptr, dispatch.bytes, None if saved is None else _saved(saved, ws),
-        0 if saved is None else saved.numel(), _dense(y, ws.dtype, ws._x, "y"), C.byref(ws.dims), ws.ptr, ws.bytes,
+        x.data_ptr(), stride, _dense(w_gate_up, ws.dtype, ws._gate_up, "w_gate_up", gpu), _dense(w_down, ws.dtype, ws._down, "w_down", gpu),
+        _dense(w, torch.float32, ws._w, "w", gpu), dispatch.ptr, dispatch.bytes, None if saved is None else _saved(saved, ws),
+        0 if saved is None else saved.numel(), _dense(y, ws.dtype, ws._x, "y", gpu), C.byref(ws.dims), ws.ptr, ws.bytes,
         ws._use(stream))
     if rc:
         _check(rc, "lapsum_experts_forward")
@@ -231,15 +250,16 @@ def lapsum_experts_backward(grad_y: torch.Tensor, x: torch.Tensor, w_gate_up: to
                             stream: Optional[torch.cuda.Stream] = None) -> None:
     """Every gradient of lapsum_experts_forward; grad_w has the workspace's 16-bit type."""
     _same_shape(dispatch, ws)
-    gy_stride, x_stride = _rows(grad_y, ws.dtype, "grad_y"), _rows(x, ws.dtype, "x")
+    gpu = ws.gpu
+    gy_stride, x_stride = _rows(grad_y, ws.dtype, "grad_y", gpu), _rows(x, ws.dtype, "x", gpu)
     if x.shape != ws._x or grad_y.shape != ws._x:
         raise ValueError(f"x and grad_y must have shape {ws._x}")
     dispatch._use(stream)
     rc = lib().lapsum_experts_backward(
-        grad_y.data_ptr(), gy_stride, x.data_ptr(), x_stride, _dense(w_gate_up, ws.dtype, ws._gate_up, "w_gate_up"),
-        _dense(w_down, ws.dtype, ws._down, "w_down"), _dense(w, torch.float32, ws._w, "w"), dispatch.ptr, dispatch.bytes,
-        _saved(saved, ws), saved.numel(), _dense(grad_x, ws.dtype, ws._x, "grad_x"),
-        _dense(grad_w_gate_up, ws.dtype, ws._gate_up, "grad_w_gate_up"), _dense(grad_w_down, ws.dtype, ws._down, "grad_w_down"),
-        _dense(grad_w, ws.dtype, ws._w, "grad_w"), C.byref(ws.dims), ws.ptr, ws.bytes, ws._use(stream))
+        grad_y.data_ptr(), gy_stride, x.data_ptr(), x_stride, _dense(w_gate_up, ws.dtype, ws._gate_up, "w_gate_up", gpu),
+        _dense(w_down, ws.dtype, ws._down, "w_down", gpu), _dense(w, torch.float32, ws._w, "w", gpu), dispatch.ptr, dispatch.bytes,
+        _saved(saved, ws), saved.numel(), _dense(grad_x, ws.dtype, ws._x, "grad_x", gpu),
+        _dense(grad_w_gate_up, ws.dtype, ws._gate_up, "grad_w_gate_up", gpu), _dense(grad_w_down, ws.dtype, ws._down, "grad_w_down", gpu),
+        _dense(grad_w, ws.dtype, ws._w, "grad_w", gpu), C.byref(ws.dims), ws.ptr, ws.bytes, ws._use(stream))
     if rc:
         _check(rc, "lapsum_experts_backward")

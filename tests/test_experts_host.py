@@ -138,3 +138,86 @@ def test_a_workspace_s_memory_belongs_to_the_stream_that_clears_it(world):
     world.streams[0] = 55
     ws = L.ExpertsWorkspace(disp, D, F, training=True)
     assert world.made[-1] == 55 and ws.buf.notes == []
+
+
+def route_operands(gpu=0):
+    z = lambda *s, dt=torch.float32: fake(torch.zeros(*s, dtype=dt), gpu)  # noqa: E731
+    return [z(T, E), z(E), L.route_params(k=K), z(T, K, dt=torch.int32), z(T, K)]
+
+
+def back_operands(gpu=0):
+    z = lambda *s, dt=torch.float32: fake(torch.zeros(*s, dtype=dt), gpu)  # noqa: E731
+    return [z(T, K), z(T, E), z(T, K, dt=torch.int32), z(T, K), L.route_params(k=K), z(T, E)]
+
+
+def refused(world, call):
+    before = list(world.calls)
+    with pytest.raises(ValueError, match="cuda:"):
+        call()
+    assert world.calls == before  # nothing reached the library
+
+
+def test_tensors_of_several_devices_are_refused(world):
+    disp = L.Dispatch(T, K, E, training=True)
+    ws = L.ExpertsWorkspace(disp, D, F, training=True)
+    saved, o = ws.new_saved(), batch()
+    L.lapsum_route_forward(*route_operands())
+    L.lapsum_route_backward(*back_operands())
+    step(o, disp, ws, saved)
+    for i in (1, 3, 4):
+        args = route_operands()
+        args[i] = route_operands(1)[i]
+        refused(world, lambda: L.lapsum_route_forward(*args))
+    for i in (0, 2, 3, 5):
+        args = back_operands()
+        args[i] = back_operands(1)[i]
+        refused(world, lambda: L.lapsum_route_backward(*args))
+    other = batch(1)
+    refused(world, lambda: L.lapsum_dispatch(other["idx"], disp))
+    fwd = dict(x=o["x"], w_gate_up=o["a"], w_down=o["b"], w=o["w"], dispatch=disp, y=o["y"], ws=ws, saved=saved)
+    elsewhere = fake(torch.zeros(ws.saved_bytes, dtype=torch.uint8), 1)
+    for name, key in (("x", "x"), ("w_gate_up", "a"), ("w_down", "b"), ("w", "w"), ("y", "y")):
+        refused(world, lambda: L.lapsum_experts_forward(**{**fwd, name: other[key]}))
+    refused(world, lambda: L.lapsum_experts_forward(**{**fwd, "saved": elsewhere}))
+    back = dict(grad_y=o["gy"], x=o["x"], w_gate_up=o["a"], w_down=o["b"], w=o["w"], dispatch=disp, saved=saved, grad_x=o["gx"], grad_w_gate_up=o["ga"],
+                grad_w_down=o["gb"], grad_w=o["gw"], ws=ws)
+    L.lapsum_experts_backward(**back)
+    for name, key in (("grad_y", "gy"), ("x", "x"), ("w_gate_up", "a"), ("w_down", "b"), ("w", "w"), ("grad_x", "gx"), ("grad_w_gate_up", "ga"),
+                      ("grad_w_down", "gb"), ("grad_w", "gw")):
+        refused(world, lambda: L.lapsum_experts_backward(**{**back, name: other[key]}))
+    refused(world, lambda: L.lapsum_experts_backward(**{**back, "saved": elsewhere}))
+    far = L.Dispatch(T, K, E, training=True, device="cuda:1")
+    refused(world, lambda: L.lapsum_experts_forward(**{**fwd, "dispatch": far}))
+    refused(world, lambda: L.lapsum_experts_backward(**{**back, "dispatch": far}))
+
+
+def test_a_device_that_is_not_current_is_refused(world):
+    """the launches go to the current device; another one's tensors would be foreign memory there"""
+    disp = L.Dispatch(T, K, E, training=True, device="cuda:1")  # tables may be made for any device
+    assert disp.device == torch.device("cuda", 1)
+    refused(world, lambda: L.ExpertsWorkspace(disp, D, F, training=True))
+    world.device = 1
+    ws = L.ExpertsWorkspace(disp, D, F, training=True)
+    saved, o = ws.new_saved(), batch(1)
+    step(o, disp, ws, saved)
+    ws.status()
+    L.lapsum_route_forward(*route_operands(1))
+    L.lapsum_route_backward(*back_operands(1))
+    world.device = 0
+    refused(world, lambda: L.lapsum_route_forward(*route_operands(1)))
+    refused(world, lambda: L.lapsum_route_backward(*back_operands(1)))
+    refused(world, lambda: L.lapsum_dispatch(o["idx"], disp))
+    refused(world, lambda: L.lapsum_experts_forward(o["x"], o["a"], o["b"], o["w"], disp, o["y"], ws, saved=saved))
+    refused(world, lambda: L.lapsum_experts_backward(o["gy"], o["x"], o["a"], o["b"], o["w"], disp, saved, o["gx"], o["ga"], o["gb"], o["gw"], ws))
+    refused(world, lambda: ws.status())
+
+
+def test_a_stream_of_another_device_is_refused(world):
+    disp = L.Dispatch(T, K, E)
+    ws = L.ExpertsWorkspace(disp, D, F)
+    o, far = batch(), Stream(7, gpu=1)
+    refused(world, lambda: L.lapsum_route_forward(*route_operands(), stream=far))
+    refused(world, lambda: L.lapsum_dispatch(o["idx"], disp, far))
+    refused(world, lambda: L.lapsum_experts_forward(o["x"], o["a"], o["b"], o["w"], disp, o["y"], ws, stream=far))
+    refused(world, lambda: L.ExpertsWorkspace(disp, D, F, stream=far))
+    refused(world, lambda: ws.status(far))
