@@ -124,6 +124,20 @@ inline int64_t dispatch_blocks(int64_t entries)
     const int64_t per = dispatch_chunks(entries) * DISPATCH_CHUNK;
     return entries <= per ? 1 : (entries + per - 1) / per;
 }
+// More than 48 KB of a block's shared memory, its static part included, has to be asked for.  The kernel for over 256 experts asks for
+// what 1024 of them need: the same value from every call, so that threads with different widths do not take it from one another.
+int dispatch_allow_widest()
+{
+    static_assert(dispatch_place_smem(256) + 1024 <= 48 * 1024, "the narrower kernels' memory is given without asking");
+    static thread_local int dev_ready = -1;  // the attribute belongs to the device's context
+    int dev = 0;
+    CU_OK(cudaGetDevice(&dev));
+    if (dev != dev_ready) {
+        CU_OK(cudaFuncSetAttribute(dispatch_place_kernel<10>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dispatch_place_smem(ROUTE_MAX_E)));
+        dev_ready = dev;
+    }
+    return LAPSUM_OK;
+}
 int dispatch_layout(int64_t tokens, int32_t k, int64_t experts, int32_t rows, lapsum_dispatch_layout *L)
 {
     if (tokens < 0 || k < 1 || k > ROUTE_MAX_K || experts < 1 || experts > ROUTE_MAX_E) return LAPSUM_ERR_SHAPE;
@@ -516,7 +530,7 @@ int lapsum_dispatch(const int32_t *idx, int64_t tokens, int32_t k, int64_t exper
     A.chunks = (int)dispatch_chunks(A.entries), A.blocks = (int)dispatch_blocks(A.entries);
     const auto place = experts <= 128 ? dispatch_place_kernel<7> : experts <= 256 ? dispatch_place_kernel<8> : dispatch_place_kernel<10>;
     const size_t smem = dispatch_place_smem((int)experts);
-    if (smem > 48 * 1024) CU_OK(cudaFuncSetAttribute(place, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (experts > 256) RUN(dispatch_allow_widest());
     A.counts = reinterpret_cast<int32_t *>(d + L.off_counts), A.offsets = reinterpret_cast<int32_t *>(d + L.off_offsets);
     A.slot_of = reinterpret_cast<int32_t *>(d + L.off_slot_of), A.entry_of = reinterpret_cast<int32_t *>(d + L.off_entry_of);
     A.tile_expert = reinterpret_cast<int32_t *>(d + L.off_tile_expert), A.partial = reinterpret_cast<int32_t *>(d + L.off_partial);
