@@ -10,7 +10,7 @@
 //          A choice costs a warp the same instructions however many tokens it holds, so few lanes per token are better:
 //          65536 x 128 fp32, k = 8, forward: 47 us with 32 lanes, 24 us with 8, 20 us with 4 (160 instructions a token, the
 //          integer pipe 60 % busy; its 38 MB would take 6 us); the backward takes 11 us for 34 MB written, both together
-//          25.9 us.  16381 x 256 bf16 with a bias and 8 groups (16 lanes): 23 and 7 us, 21.9 us together.
+//          25.9 us.  16381 x 256 bf16 sigmoid with a bias and 8 groups (16 lanes): 24.0 us together.
 // dispatch a stable counting sort of the T k entries by expert, integers only.  65536 x 8 entries, 128 experts: 11 us in two
 //          launches (6.4 MB would take 1 us; two dependent passes of latency and 27 k instructions a block); 32 x 8: 5.5 us.
 #pragma once
@@ -34,9 +34,9 @@ struct RouteArgs {
 
 // What experts are compared by: -inf for one that cannot be chosen (NaN, by fmaxf's rule), +0 for -0
 __device__ __forceinline__ float route_key(float x) { return fmaxf(x + 0.f, -CUDART_INF_F); }
+// For weights and keys alike.  (Keys of the fast exponential and quotient, several units of 2^-23 off, took a sixth of neighbouring logits
+// between -60 and -8 in the wrong order.)
 __device__ __forceinline__ float sigmoid_f(float x) { return 1.f / (1.f + expf(-x)); }
-// For the keys, which only order the experts: a few units of 2^-24 off, the same value for the same logit
-__device__ __forceinline__ float sigmoid_key(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 
 template <int L>
 __device__ __forceinline__ float row_sum_f(float v)
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS, NV > 16 && !PLAIN ? 2 : 4) r
             for (int i = 0; i < NV; ++i) {
                 float s = x[i];
                 if (A.score == LAPSUM_ROUTE_SOFTMAX) s = expf(s - top) / total;
-                else if (A.score == LAPSUM_ROUTE_SIGMOID) s = sigmoid_key(s);
+                else if (A.score == LAPSUM_ROUTE_SIGMOID) s = sigmoid_f(s);
                 s += offset[i];
                 c[i] = (x[i] > -CUDART_INF_F && s > -CUDART_INF_F) ? s : -CUDART_INF_F;  // a NaN counts as unavailable
             }
