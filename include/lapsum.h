@@ -530,7 +530,8 @@ int lapsum_dispatch(const int32_t *idx, int64_t tokens, int32_t k, int64_t exper
  * x: tokens rows of d, x_stride elements apart (a multiple of 8); w_gate_up: experts x 2f x d (f gate rows, then f up
  * rows); w_down: experts x d x f; w: tokens x k floats; dispatch: the tables of the same idx; y: tokens x d.  d and f are
  * multiples of 8 up to 65536; every tensor starts at a multiple of 16 bytes.  A token without an entry gets y = 0.
- * A value beyond the storage type's range (fp16: 65504) becomes infinity, in the activations as in the results.
+ * A value beyond the storage type's range (fp16: 65504) becomes infinity, in the activations as in the results.  The slope of
+ * silu is 0 at a gate of -infinity and 1 at +infinity, so a gate below the range alone leaves every gradient finite.
  * With dims.training the call leaves g, u and the weighted activations in `saved` (256-byte aligned, `saved_bytes` as
  * described) for lapsum_experts_backward; otherwise saved is NULL.
  *

@@ -241,6 +241,19 @@ __device__ __forceinline__ void load8(const T *p, float *v)
 }
 __device__ __forceinline__ float sigmoid_fast(float g) { return __fdividef(1.f, 1.f + __expf(-g)); }
 
+// The backward's silu(g) and slope s + silu(g) (1 - s), s = sigmoid(g), from a g that was kept in 16 bits.  fp16 keeps a g beyond 65504 as an
+// infinity: there silu(-inf) is 0, not -inf x 0, and the slopes are 0 and 1, not an infinity times 0.  A NaN stays one through s.
+template <typename T>
+__device__ __forceinline__ float silu_of(float g, float s)
+{
+    return std::is_same<T, __half>::value ? fmaxf(g, -65504.f) * s : g * s;
+}
+template <typename T>
+__device__ __forceinline__ float below_infinity(float a)
+{
+    return std::is_same<T, __half>::value ? fminf(a, 65504.f) : a;
+}
+
 // ---------------------------------------------------------------- the kernel ----
 // Row tiles up to GATHER_ROWS take their tokens' rows from x by TMA gather, four rows per instruction.  A gather takes about 40
 // cycles whatever the reuse (measured: 32 of them per step of 64 made the first product of 131072 slots 2.43 ms instead of
@@ -656,9 +669,9 @@ __global__ void __launch_bounds__((ExpertsShape<MODE, AR, BN, KS>::THREADS), 1) 
                                 const bool real = entry >= 0 && t.n0 + c + j + 8 * p < N;
 #pragma unroll
                                 for (int v = 0; v < 8; ++v) {
-                                    const float s = sigmoid_fast(g[v]), a = g[v] * s, x = dh[8 * p + v], xw = x * w, uv = u[v];
+                                    const float s = sigmoid_fast(g[v]), a = silu_of<T>(g[v], s), x = dh[8 * p + v], xw = x * w, uv = u[v];
                                     dot += real ? x * a * uv : 0.f;
-                                    g[v] = real ? xw * uv * (s + a * (1.f - s)) : 0.f;
+                                    g[v] = real ? xw * uv * (s + below_infinity<T>(a) * (1.f - s)) : 0.f;
                                     u[v] = real ? xw * a : 0.f;
                                 }
                                 put(at, j / 8 + p, g);
