@@ -536,7 +536,8 @@ int lapsum_dispatch(const int32_t *idx, int64_t tokens, int32_t k, int64_t exper
  * described) for lapsum_experts_backward; otherwise saved is NULL.
  *
  * lapsum_experts_backward: every gradient: grad_x (tokens x d), grad_w_gate_up, grad_w_down (written in full, zeros for an
- * expert without tokens), grad_w (tokens x k, in io_dtype, 0 for dropped entries: it is a sum over 16-bit activations).
+ * expert without tokens), grad_w (tokens x k, 0 for dropped entries).  grad_w has io_dtype or, with dims.grad_w_f32, fp32: a
+ * sum over 16-bit activations has no more digits than those, but it is a sum over d as well and may pass fp16's range.
  * Results do not depend on scheduling: no sum is formed by atomics.
  *
  * One workspace serves one stream at a time.  lapsum_experts_workspace_init clears its status word (enqueued on `stream`);
@@ -547,6 +548,7 @@ typedef struct lapsum_experts_dims {
     int32_t k, tile_rows; /* as given to lapsum_dispatch */
     int32_t io_dtype;     /* LAPSUM_IO_F16 or LAPSUM_IO_BF16 */
     int32_t training;     /* 1: a forward is followed by a backward */
+    int32_t grad_w_f32;   /* 1: grad_w is fp32 like w, 0 (default): it has io_dtype */
 } lapsum_experts_dims;
 
 typedef struct lapsum_experts_layout {

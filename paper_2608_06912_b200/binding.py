@@ -104,7 +104,7 @@ class DispatchLayout(C.Structure):
 class ExpertsDims(C.Structure):
     _fields_ = [
         ("tokens", C.c_int64), ("experts", C.c_int64), ("d", C.c_int64), ("f", C.c_int64), ("k", C.c_int32),
-        ("tile_rows", C.c_int32), ("io_dtype", C.c_int32), ("training", C.c_int32),
+        ("tile_rows", C.c_int32), ("io_dtype", C.c_int32), ("training", C.c_int32), ("grad_w_f32", C.c_int32),
     ]
 
 

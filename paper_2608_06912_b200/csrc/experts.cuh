@@ -894,7 +894,8 @@ __global__ void __launch_bounds__(256) experts_gather_kernel(const T *x, int64_t
 // (6.7 TB/s).  The last kernel of a call lets no other start early: its results may go to kernels that read through the non-coherent path.
 template <typename T>
 __global__ void __launch_bounds__(256) experts_combine_kernel(const T *slots, const int32_t *slot_of, T *out, int64_t out_stride,
-                                                              const float *partial, T *grad_w, int64_t tokens, int capacity, int k, int D, int nts)
+                                                              const float *partial, void *grad_w, int grad_w_f32, int64_t tokens, int capacity, int k, int D,
+                                                              int nts)
 {
     pdl_wait();
     const int per = D / 8;
@@ -926,7 +927,8 @@ __global__ void __launch_bounds__(256) experts_combine_kernel(const T *slots, co
             float g = 0.f;
             if ((unsigned)s < (unsigned)capacity)
                 for (int n = 0; n < nts; ++n) g += partial[(int64_t)s * nts + n];
-            Io<T>::store1(grad_w + t * k + j, g);
+            if (grad_w_f32) static_cast<float *>(grad_w)[t * k + j] = g;
+            else Io<T>::store1(static_cast<T *>(grad_w) + t * k + j, g);
         }
 }
 

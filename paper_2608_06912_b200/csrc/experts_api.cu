@@ -186,7 +186,7 @@ int experts_layout(const lapsum_experts_dims *p, ExpertsLayout &X, lapsum_expert
     if (!p) return LAPSUM_ERR_NULL;
     if (p->d < 8 || p->f < 8 || p->d % 8 || p->f % 8 || p->d > 1 << 16 || p->f > 1 << 16) return LAPSUM_ERR_SHAPE;
     if (p->io_dtype != LAPSUM_IO_F16 && p->io_dtype != LAPSUM_IO_BF16) return LAPSUM_ERR_UNSUPPORTED;
-    if (p->training != 0 && p->training != 1) return LAPSUM_ERR_PARAM;
+    if ((p->training != 0 && p->training != 1) || (p->grad_w_f32 != 0 && p->grad_w_f32 != 1)) return LAPSUM_ERR_PARAM;
     RUN(dispatch_layout(p->tokens, p->k, p->experts, p->tile_rows, &X.d));
     if (p->training && p->tile_rows < 64) return LAPSUM_ERR_PARAM;
     const size_t cap = (size_t)X.d.capacity, D = (size_t)p->d, F = (size_t)p->f;
@@ -366,7 +366,7 @@ int combine(const Call &c, const uint8_t *dispatch, void *out, int64_t stride, c
     const int64_t work = c.p->tokens * (c.p->d / 8);
     return launch_pdl(experts_combine_kernel<T>, (unsigned)ceil_div(work, 256), 256, 0, st, reinterpret_cast<const T *>(c.ws + c.X.off_slots),
                       reinterpret_cast<const int32_t *>(dispatch + c.X.d.off_slot_of), static_cast<T *>(out), stride, partial,
-                      static_cast<T *>(grad_w), c.p->tokens, c.A.capacity, (int)c.p->k, (int)c.p->d, c.X.nts_dh);
+                      grad_w, (int)c.p->grad_w_f32, c.p->tokens, c.A.capacity, (int)c.p->k, (int)c.p->d, c.X.nts_dh);
 }
 
 template <typename T>

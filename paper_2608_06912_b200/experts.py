@@ -197,6 +197,10 @@ class ExpertsWorkspace(_Memory):
         self._x = (p.tokens, int(d))
         self._gate_up, self._down = (p.experts, 2 * int(f), int(d)), (p.experts, int(d), int(f))
         self._w = (p.tokens, p.k)
+        self._grad_w = {self.dtype: self.dims}  # the dims by grad_w's type
+        if self.training:
+            self._grad_w[torch.float32] = wide = ExpertsDims.from_buffer_copy(self.dims)
+            wide.grad_w_f32 = 1
 
     def new_saved(self) -> torch.Tensor:
         if not self.training:
@@ -248,18 +252,21 @@ def lapsum_experts_backward(grad_y: torch.Tensor, x: torch.Tensor, w_gate_up: to
                             dispatch: Dispatch, saved: torch.Tensor, grad_x: torch.Tensor, grad_w_gate_up: torch.Tensor,
                             grad_w_down: torch.Tensor, grad_w: torch.Tensor, ws: ExpertsWorkspace,
                             stream: Optional[torch.cuda.Stream] = None) -> None:
-    """Every gradient of lapsum_experts_forward; grad_w has the workspace's 16-bit type."""
+    """Every gradient of lapsum_experts_forward; grad_w has the workspace's 16-bit type or, like w, float32."""
     _same_shape(dispatch, ws)
     gpu = ws.gpu
     gy_stride, x_stride = _rows(grad_y, ws.dtype, "grad_y", gpu), _rows(x, ws.dtype, "x", gpu)
     if x.shape != ws._x or grad_y.shape != ws._x:
         raise ValueError(f"x and grad_y must have shape {ws._x}")
+    dims = ws._grad_w.get(grad_w.dtype)
+    if dims is None:
+        raise TypeError(f"grad_w must be {ws.dtype} or torch.float32")
     dispatch._use(stream)
     rc = lib().lapsum_experts_backward(
         grad_y.data_ptr(), gy_stride, x.data_ptr(), x_stride, _dense(w_gate_up, ws.dtype, ws._gate_up, "w_gate_up", gpu),
         _dense(w_down, ws.dtype, ws._down, "w_down", gpu), _dense(w, torch.float32, ws._w, "w", gpu), dispatch.ptr, dispatch.bytes,
         _saved(saved, ws), saved.numel(), _dense(grad_x, ws.dtype, ws._x, "grad_x", gpu),
         _dense(grad_w_gate_up, ws.dtype, ws._gate_up, "grad_w_gate_up", gpu), _dense(grad_w_down, ws.dtype, ws._down, "grad_w_down", gpu),
-        _dense(grad_w, ws.dtype, ws._w, "grad_w", gpu), C.byref(ws.dims), ws.ptr, ws.bytes, ws._use(stream))
+        _dense(grad_w, grad_w.dtype, ws._w, "grad_w", gpu), C.byref(dims), ws.ptr, ws.bytes, ws._use(stream))
     if rc:
         _check(rc, "lapsum_experts_backward")

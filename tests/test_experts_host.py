@@ -221,3 +221,19 @@ def test_a_stream_of_another_device_is_refused(world):
     refused(world, lambda: L.lapsum_experts_forward(o["x"], o["a"], o["b"], o["w"], disp, o["y"], ws, stream=far))
     refused(world, lambda: L.ExpertsWorkspace(disp, D, F, stream=far))
     refused(world, lambda: ws.status(far))
+
+
+def test_the_weights_gradient_may_be_fp32(world):
+    disp = L.Dispatch(T, K, E, training=True)
+    ws = L.ExpertsWorkspace(disp, D, F, training=True)
+    saved, o = ws.new_saved(), batch()
+    wide = fake(torch.zeros(T, K), 0)
+    L.lapsum_experts_backward(o["gy"], o["x"], o["a"], o["b"], o["w"], disp, saved, o["gx"], o["ga"], o["gb"], wide, ws)
+    assert world.calls[-1] == "lapsum_experts_backward"
+    import ctypes as C
+
+    from paper_2608_06912_b200 import binding as B
+    out, real = B.ExpertsLayout(), L.lib()
+    for flag, rc in ((0, 0), (1, 0), (2, -7), (-1, -7)):
+        d = B.ExpertsDims(tokens=T, experts=E, d=D, f=F, k=K, tile_rows=64, io_dtype=L.IO_BF16, training=1, grad_w_f32=flag)
+        assert real.lapsum_experts_describe(C.byref(d), C.byref(out)) == rc, flag
