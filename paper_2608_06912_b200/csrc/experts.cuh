@@ -413,7 +413,6 @@ __global__ void __launch_bounds__((ExpertsShape<MODE, AR, BN, KS>::THREADS), 1) 
             if constexpr (S::A_GATHER)  // four neighbouring slots per lane
                 if (i < tiles && lane < AR / 4) entries = ld(reinterpret_cast<const int4 *>(P.entry_of + next.m0 + 4 * lane));
         };
-        look_ahead(tile0);
         int4 rows = make_int4(0, 0, 0, 0);  // the tile's tokens; holes give a row beyond the matrix, which reads as zeros
         int fours = 0;                      // fours of slots with a token, from the tile's start; the others' rows keep what they hold
         auto bring_a = [&](const Tile &t, int kb, uint32_t s, uint32_t bar) {

@@ -290,16 +290,16 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 struct Call {
     const lapsum_experts_dims *p;
     ExpertsLayout X;
+    lapsum_experts_layout out;
     ExpertsArgs A;
     uint8_t *ws;
 };
 
 int begin_call(const lapsum_experts_dims *p, const void *dispatch, size_t dispatch_bytes, void *ws, size_t ws_bytes, Call &c)
 {
-    lapsum_experts_layout out;
-    RUN(experts_layout(p, c.X, &out));
+    RUN(experts_layout(p, c.X, &c.out));
     if (!dispatch || !ws) return LAPSUM_ERR_NULL;
-    if (!aligned(ws, 256) || ws_bytes < out.workspace_bytes || !aligned(dispatch, 256) || dispatch_bytes < c.X.d.bytes)
+    if (!aligned(ws, 256) || ws_bytes < c.out.workspace_bytes || !aligned(dispatch, 256) || dispatch_bytes < c.X.d.bytes)
         return LAPSUM_ERR_WORKSPACE;
     c.p = p;
     c.ws = static_cast<uint8_t *>(ws);
@@ -577,9 +577,7 @@ int lapsum_experts_forward(const void *x, int64_t x_stride, const void *w_gate_u
     if (dims->tokens == 0) return LAPSUM_OK;
     if (dims->training && !saved) return LAPSUM_ERR_NULL;
     if (!dims->training && saved) return LAPSUM_ERR_PARAM;
-    lapsum_experts_layout out;
-    RUN(experts_layout(dims, c.X, &out));
-    if (saved && (!aligned(saved, 256) || saved_bytes < out.saved_bytes)) return LAPSUM_ERR_WORKSPACE;
+    if (saved && (!aligned(saved, 256) || saved_bytes < c.out.saved_bytes)) return LAPSUM_ERR_WORKSPACE;
     if (x_stride < dims->d || x_stride % 8) return LAPSUM_ERR_SHAPE;
     if (!x || !w_gate_up || !w_down || !w || !y) return LAPSUM_ERR_NULL;
     if (!aligned(x, 16) || !aligned(w_gate_up, 16) || !aligned(w_down, 16) || !aligned(y, 16)) return LAPSUM_ERR_ALIGN;
@@ -607,10 +605,8 @@ int lapsum_experts_backward(const void *grad_y, int64_t grad_y_stride, const voi
         CU_OK(cudaMemsetAsync(grad_w_down, 0, bytes, st));
         return LAPSUM_OK;
     }
-    lapsum_experts_layout out;
-    RUN(experts_layout(dims, c.X, &out));
     if (!saved) return LAPSUM_ERR_NULL;
-    if (!aligned(saved, 256) || saved_bytes < out.saved_bytes) return LAPSUM_ERR_WORKSPACE;
+    if (!aligned(saved, 256) || saved_bytes < c.out.saved_bytes) return LAPSUM_ERR_WORKSPACE;
     if (x_stride < dims->d || x_stride % 8 || grad_y_stride < dims->d || grad_y_stride % 8) return LAPSUM_ERR_SHAPE;
     if (!grad_y || !x || !w_gate_up || !w_down || !w || !grad_x || !grad_w) return LAPSUM_ERR_NULL;
     if (!aligned(grad_y, 16) || !aligned(x, 16) || !aligned(w_gate_up, 16) || !aligned(w_down, 16) || !aligned(grad_x, 16))

@@ -549,14 +549,9 @@ __global__ void __launch_bounds__(DISPATCH_THREADS) dispatch_place_kernel(const 
         }
 #pragma unroll
         for (int j = 0; j < DISPATCH_PER; ++j) {
-            unsigned peers = __ballot_sync(FULL, e[j] < E);
-            if (peers == 0) continue;
-#pragma unroll
-            for (int b = 0; b < BITS; ++b) {
-                const bool bit = (e[j] >> b) & 1;
-                const unsigned bal = __ballot_sync(FULL, bit);
-                peers &= bit ? bal : ~bal;
-            }
+            const unsigned valid = __ballot_sync(FULL, e[j] < E);
+            if (valid == 0) continue;
+            const unsigned peers = valid & match_bits<BITS>((uint32_t)e[j]);
             const int before = __popc(peers & ((1u << lane) - 1u));
             rank[j] = e[j] < E ? mine[e[j]] + before : 0;
             __syncwarp();

@@ -47,17 +47,16 @@ def _stream(stream: Optional[torch.cuda.Stream], gpu: int) -> int:
     return stream.cuda_stream
 
 
-def _on(t: torch.Tensor, gpu: int, name: str) -> None:
-    if t.get_device() != gpu:
-        raise ValueError(f"{name} is on cuda:{t.get_device()}, the call's other tensors on cuda:{gpu}")
+def _elsewhere(t: torch.Tensor, gpu: int, name: str) -> None:
+    raise ValueError(f"{name} is on cuda:{t.get_device()}, the call's other tensors on cuda:{gpu}")
 
 
 def _rows(t: torch.Tensor, dtype: torch.dtype, name: str, gpu: Optional[int] = None) -> int:
     """Row stride of a matrix whose rows are contiguous."""
     if not (t.is_cuda and t.dtype == dtype and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)):
         raise TypeError(f"{name} must be a {dtype} CUDA matrix with contiguous rows")
-    if gpu is not None:
-        _on(t, gpu, name)
+    if gpu is not None and t.get_device() != gpu:
+        _elsewhere(t, gpu, name)
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
@@ -66,7 +65,8 @@ def _dense(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str, gpu: in
         raise TypeError(f"{name} must be a contiguous {dtype} CUDA tensor")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    _on(t, gpu, name)
+    if t.get_device() != gpu:
+        _elsewhere(t, gpu, name)
     return t.data_ptr()
 
 
@@ -224,7 +224,8 @@ def _same_shape(dispatch: Dispatch, ws: ExpertsWorkspace) -> None:
 def _saved(saved: Optional[torch.Tensor], ws: ExpertsWorkspace) -> int:
     if saved is None or not (saved.is_cuda and saved.dtype == torch.uint8 and saved.is_contiguous()):
         raise TypeError("saved must be a buffer of ExpertsWorkspace.new_saved()")
-    _on(saved, ws.gpu, "saved")
+    if saved.get_device() != ws.gpu:
+        _elsewhere(saved, ws.gpu, "saved")
     return saved.data_ptr()
 
 
