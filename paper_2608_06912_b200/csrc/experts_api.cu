@@ -317,10 +317,19 @@ int begin_call(const lapsum_experts_dims *p, const void *dispatch, size_t dispat
     return LAPSUM_OK;
 }
 
-// Up to this many tokens the products run without the tensor core.  Measured (bf16, 8 of 64 experts, 2048 x 1024): one token 28 us
-// against 36 us on tiles, 2: 45 / 51, 4: 74 / 73, 6: 108 / 93 (tokens begin to share experts); 2 of 32 experts, 1024 x 1024:
-// 4: 22 / 27, 8: 35 / 35.
-constexpr int64_t FEW_TOKENS = 4;
+// Up to four tokens the products run without the tensor core, which saves a launch and the tiles' prologue (some 9 us) but reads an
+// expert's weights once for every token that chose it.  So only where that reads at most 48 MiB again, by the experts that so many
+// tokens choose on average.  Measured, without / on tiles, us: one token on 8 of 64 experts of 2048 x 1024 27 / 37, 2: 44 / 52, 4: 74 / 75,
+// 6: 105 / 88; on 8 of 8 one token 27 / 36, 2: 39 / 36, 4: 62 / 37; on 8 of 16 2: 42 / 48, 3: 55 / 49; 4 tokens on 2 of 4 experts of 1000 x 520
+// 15 / 24.
+constexpr int64_t FEW_TOKENS = 4, FEW_AGAIN = 48 << 20;
+inline bool few_tokens(const lapsum_experts_dims &p)
+{
+    if (p.tokens > FEW_TOKENS) return false;
+    const double entries = (double)p.tokens * p.k, E = (double)p.experts;
+    const double chosen = E * (1.0 - std::pow(std::fmax(0.0, 1.0 - p.k / E), (double)p.tokens));
+    return (entries - chosen) * 6.0 * (double)p.d * (double)p.f <= (double)FEW_AGAIN;
+}
 
 // One of the four products whose rows are slots
 template <int MODE, typename T>
@@ -377,7 +386,7 @@ int forward_t(Call &c, const void *x, int64_t x_stride, const void *w_gate_up, c
     const int dt = p.io_dtype, rows = p.tile_rows < 128 ? p.tile_rows : 128, out_rows = rows < 32 ? rows : 32;
     const int64_t cap = c.X.d.capacity;
     const bool pair = p.tile_rows == 256;
-    if (!saved && !hold && p.tokens <= FEW_TOKENS) {
+    if (!saved && !hold && few_tokens(p)) {
         const int32_t *slot_of = reinterpret_cast<const int32_t *>(dispatch + c.X.d.off_slot_of);
         T *hw = reinterpret_cast<T *>(c.ws + c.X.off_hw);
         int shift = 4;
