@@ -468,7 +468,8 @@ const char *lapsum_kernel_name(int kernel_id);
  *   choice   idx: the k largest keys, largest first; equal keys (and equal groups) by the lower index
  *   weights  w_j = scale s_j, with renormalise = 1 scale s_j / sum over the chosen s
  * An expert whose logit is -inf or NaN (or whose key is) is never chosen.  Where fewer than k are left, the remaining
- * idx are -1 with weight 0.  A logit of +inf makes the row's softmax weights NaN.  "given" scores that sum to 0 give weights 0.
+ * idx are -1 with weight 0.  A logit of +inf makes the row's softmax weights NaN
+ * (with a bias or groups the keys, so that none is chosen).  "given" scores that sum to 0 give weights 0.
  * k <= 32, experts <= 1024, groups <= 32.
  *
  * lapsum_route_backward: the gradient of the logits (tokens x experts, io_dtype, written in full) from grad_w (type

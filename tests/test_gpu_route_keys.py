@@ -31,3 +31,25 @@ def test_sigmoid_keys_of_neighbouring_logits(low, high, by, E):
     L.lapsum_route_forward(x.cuda(), torch.zeros(E, device="cuda") if by == "bias" else None, p, idx, w)
     wrong = (idx.cpu()[:, 0] != b).sum().item()
     assert wrong == 0, f"{wrong} of {T}"
+
+
+@pytest.mark.parametrize("by", ["logits", "bias", "groups"])
+def test_an_infinite_logit_under_softmax(by):
+    """its weights are NaN; where the scores themselves are the keys, a NaN key is never chosen.  Other rows do not notice."""
+    gen = torch.Generator().manual_seed(1)
+    x = torch.randn(5, 16, generator=gen).cuda()
+    clean = x.clone()
+    x[2, 3] = float("inf")
+    bias = torch.zeros(16, device="cuda") if by == "bias" else None
+    p = L.route_params(k=4, groups=4 if by == "groups" else 1, groups_kept=2 if by == "groups" else 1)
+    got = []
+    for v in (x, clean):
+        idx, w = torch.empty(5, 4, dtype=torch.int32, device="cuda"), torch.empty(5, 4, device="cuda")
+        L.lapsum_route_forward(v, bias, p, idx, w)
+        got.append((idx.cpu(), w.cpu()))
+    others = [0, 1, 3, 4]
+    assert torch.equal(got[0][0][others], got[1][0][others]) and torch.equal(got[0][1][others], got[1][1][others])
+    if by == "logits":
+        assert got[0][0][2, 0] == 3 and torch.isnan(got[0][1][2]).all()
+    else:
+        assert (got[0][0][2] == -1).all() and (got[0][1][2] == 0).all()
