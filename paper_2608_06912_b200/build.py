@@ -8,7 +8,7 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-# LAPSUM_B200_CHECK_BUILD=1 selects the check build (every computed store index compared with its limit, see
+# LAPSUM_B200_CHECK_BUILD=1 selects the check build (every store index that the soft top-k's kernels compute is compared with its limit, see
 # LAPSUM_IN_BOUNDS in csrc/common.cuh): a separate library, built with build(check_bounds=True)
 CHECK = os.environ.get("LAPSUM_B200_CHECK_BUILD", "0") not in ("", "0")
 LIB = os.path.join(HERE, "liblapsum_b200_check.so" if CHECK else "liblapsum_b200.so")

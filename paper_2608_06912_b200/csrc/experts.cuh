@@ -13,10 +13,11 @@
 // in DH) read the other one and finish the previous tile.  Operands that the contraction runs along the rows of (W_down in DH, W_gate_up in DX, both
 // sides of the weight gradients) are read as they lie in memory: the tensor core takes them "MN-major".
 //
-// Measured on pairs of blocks (8192 tokens, 4 of 32 experts, 2048 x 1024, bf16; 1.5 to 1.6 GHz under the profiler): GATE_UP 225 us,
-// DOWN 112 us, DX 207 us with the tensor pipe 68 to 75 % busy (1.22 to 1.33 PFLOP/s on the real rows), the weight gradients 120 and
-// 220 us, DH 142 us.  In a row they run at the board's power limit (1.0 PFLOP/s over whole passes at 1.38 GHz, where a library
-// matrix product alone sustains 1.38).  With few tokens they are bound by the weights: 6.0 TB/s at 48 tokens on 128 experts.
+// Measured on pairs of blocks (8192 tokens, 4 of 32 experts, 2048 x 1024, bf16; each kernel alone under the profiler): GATE_UP 225 us, DOWN
+// 116 us, DX 219 us with the tensor pipe 68 to 75 % busy (1.18 to 1.26 PFLOP/s on the real rows), the weight gradients 126 and 232 us
+// (57 and 64 % busy), DH 142 us (55 %: one set of warps does the heaviest epilogue).  Whole passes reach 0.85 to 0.99 PFLOP/s at 990 W and 1.34
+// to 1.43 GHz; a library matrix product alone reaches 1.39 at 1.32 GHz under the same power limit, so the rest is pipe time: the shares above,
+// 6 to 8 % padded rows and 15 % in tables, copies and sums.  With few tokens they are bound by the weights: 6.0 TB/s at 48 tokens on 128 experts.
 //
 // Roundings: the inputs of a product are 16-bit, so w h, g, u, dg, du are rounded to the storage type once, sums are
 // fp32 in TMEM; o and dx are rounded once per slot before the fp32 sum over the slots: an fp32 copy would double the traffic of
@@ -257,7 +258,7 @@ __device__ __forceinline__ float below_infinity(float a)
 // ---------------------------------------------------------------- the kernel ----
 // Row tiles up to GATHER_ROWS take their tokens' rows from x by TMA gather, four rows per instruction.  A gather takes about 40
 // cycles whatever the reuse (measured: 32 of them per step of 64 made the first product of 131072 slots 2.43 ms instead of
-// 0.97), so wider tiles read a copy of x in slot order that experts_gather_kernel writes at memory speed (8 of 64 experts,
+// 0.84 and 0.10 for the copy), so wider tiles read a copy of x in slot order that experts_gather_kernel writes at memory speed (8 of 64 experts,
 // 2048 x 1024: 64-row tiles at 384 tokens 175 us with the copy, 198 us gathered; 128-row tiles at 512 tokens 177 and 223).
 constexpr int GATHER_ROWS = 32;
 
@@ -735,7 +736,7 @@ __global__ void __launch_bounds__((ExpertsShape<MODE, AR, BN, KS>::THREADS), 1) 
 
 // ------------------------------------------------------------- a few tokens ----
 // One or a few tokens: every weight is used once, so the products are streams of weights at memory speed and the tensor core
-// has nothing to add.  Each lane keeps eight or more 16-byte loads in flight; a token's choices are finished in one warp, so
+// has nothing to add, as long as tokens hardly share experts (few_tokens, experts_api.cu).  Each lane keeps eight or more 16-byte loads in flight; a token's choices are finished in one warp, so
 // there is neither a table of slots to combine nor a rounding per slot.
 template <typename T>
 __device__ __forceinline__ float dot8(const uint4 &a, const uint4 &b, float sum)
@@ -798,7 +799,7 @@ __global__ void __launch_bounds__(256, 2) experts_few_gate_up_kernel(const T *x,
 }
 
 // y[t][d] = sum over the token's choices of <W_down[e][d], hw>.  A block has four values of d, a warp every eighth choice: four
-// rows in steps of 1024, sixteen loads at once, the first of them before the activations are there.  The warps' sums are added
+// rows in steps of 1024, sixteen loads at once (three blocks per SM, though that spills some 60 bytes), the first of them before the activations are there.  The warps' sums are added
 // in order.
 template <typename T>
 __global__ void __launch_bounds__(256, 3) experts_few_down_kernel(const T *w_down, const T *hw, const int32_t *slot_of, const int32_t *tile_expert,
