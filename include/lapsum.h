@@ -119,6 +119,7 @@ typedef struct lapsum_params {
 #define LAPSUM_ST_BAD_ALPHA 0x100u       /* a row's own temperature (alpha_rows) was zero, not finite or outside
                                             fp32's normal range: that row is void                                */
 
+#define LAPSUM_ST_LINEAR_TIMEOUT 0x800u  /* a bounded wait of a linear kernel gave up: results invalid        */
 #define LAPSUM_ST_EXPERTS_TIMEOUT 0x400u /* a bounded wait of an experts kernel gave up: results invalid
                                             (lapsum_experts_status)                                              */
 
@@ -575,6 +576,112 @@ int lapsum_experts_backward(const void *grad_y, int64_t grad_y_stride, const voi
 int lapsum_debug_experts_timeout(int64_t wait_us, void *ws, size_t ws_bytes, const void *dispatch, size_t dispatch_bytes,
                                  const void *x, const void *w_gate_up, const float *w, const lapsum_experts_dims *dims,
                                  void *stream);
+
+/*
+ * Dense operators on both sides of the experts: embed (token ids -> rows), linear (rows -> router logits, dense layers, vocabulary
+ * logits), sample (logits -> token ids).  As above: nothing is allocated, synchronised or kept from one call for the next, every
+ * buffer is the caller's and belongs, like the stream, to the calling thread's current device.
+ *
+ * lapsum_linear_forward (fp16 or bf16 operands, sums in fp32):   P = x W^T + bias,   y = act(P) + residual
+ * x: rows x k, rows x_stride elements apart; w: n x k; bias: n values of bias_dtype (io_dtype or fp32) or NULL; residual and y: rows x n
+ * of out_dtype (io_dtype or fp32), any row strides >= n (elements); residual may be NULL, or y itself.  k and x_stride are multiples
+ * of 8, x and w start at multiples of 16 bytes; n is free.
+ *   act   none | relu | silu P s(P) | gelu P Phi(P) | gelu_tanh P s(2 u), u = sqrt(2 / pi) (P + 0.044715 P^3), s = sigmoid
+ * `pre` (pre_bytes as described, 256-byte aligned) keeps P in io_dtype for the backward, rows pre_stride elements apart.  It belongs to
+ * dims.training with an activation; otherwise it is NULL.
+ *
+ * lapsum_linear_backward:  dP = grad_y act'(P),  grad_x = dP W,  grad_w = dP^T x,  grad_bias = sum over rows of dP.
+ * grad_y: rows x n of out_dtype, any row stride >= n; grad_x: rows x k of io_dtype, any row stride >= k; grad_w: n x k of grad_w_dtype
+ * (io_dtype or fp32); grad_bias: n of bias_dtype.  Each result may be NULL.  The residual's gradient is grad_y.  dP is rounded to
+ * io_dtype for the products (the tensor core's operands); grad_bias sums it unrounded.  With rows = 0 grad_w and grad_bias are zeros.
+ * Results do not depend on scheduling.
+ *
+ * A workspace made for some rows serves calls of fewer.  It serves one stream at a time.  lapsum_linear_workspace_init clears its status
+ * word; lapsum_linear_status synchronises and reads it (LAPSUM_ST_LINEAR_TIMEOUT: a bounded wait inside a kernel gave up).
+ */
+typedef enum lapsum_activation {
+    LAPSUM_ACT_NONE = 0,
+    LAPSUM_ACT_RELU = 1,
+    LAPSUM_ACT_SILU = 2,
+    LAPSUM_ACT_GELU = 3,
+    LAPSUM_ACT_GELU_TANH = 4
+} lapsum_activation;
+
+typedef struct lapsum_linear_dims {
+    int64_t rows, n, k;   /* rows <= 2^30, n <= 2^23, k <= 2^20                             */
+    int32_t activation;   /* lapsum_activation                                              */
+    int32_t io_dtype;     /* LAPSUM_IO_F16 or LAPSUM_IO_BF16: x, w, pre, grad_x             */
+    int32_t out_dtype;    /* io_dtype or LAPSUM_IO_F32: y, residual, grad_y                 */
+    int32_t bias_dtype;   /* io_dtype or LAPSUM_IO_F32: bias, grad_bias                     */
+    int32_t grad_w_dtype; /* io_dtype or LAPSUM_IO_F32                                      */
+    int32_t training;     /* 1: a forward is followed by a backward                         */
+} lapsum_linear_dims;
+
+typedef struct lapsum_linear_layout {
+    size_t workspace_bytes, pre_bytes;
+    int64_t pre_stride; /* elements */
+} lapsum_linear_layout;
+
+int lapsum_linear_describe(const lapsum_linear_dims *dims, lapsum_linear_layout *out);
+int lapsum_linear_workspace_init(void *ws, size_t bytes, const lapsum_linear_dims *dims, void *stream);
+int lapsum_linear_status(void *ws, void *stream, uint32_t *status_bits);
+int lapsum_linear_forward(const void *x, int64_t x_stride, const void *w, const void *bias, const void *residual,
+                          int64_t residual_stride, void *y, int64_t y_stride, void *pre, size_t pre_bytes,
+                          const lapsum_linear_dims *dims, void *ws, size_t ws_bytes, void *stream);
+int lapsum_linear_backward(const void *grad_y, int64_t grad_y_stride, const void *x, int64_t x_stride, const void *w, const void *pre,
+                           size_t pre_bytes, void *grad_x, int64_t grad_x_stride, void *grad_w, void *grad_bias,
+                           const lapsum_linear_dims *dims, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Test hook for the bounded waits of the linear kernels: runs the forward's product with a producer that brings nothing and a bound of
+ * wait_us (1 .. 100000) microseconds, so that every wait runs out and LAPSUM_ST_LINEAR_TIMEOUT is raised.  y: as in the forward (what it
+ * holds is invalid afterwards); more than 4 rows, no bias, residual or pre.
+ */
+int lapsum_debug_linear_timeout(int64_t wait_us, const void *x, const void *w, void *y, const lapsum_linear_dims *dims, void *ws,
+                                size_t ws_bytes, void *stream);
+
+/*
+ * lapsum_sample: one token per row of logits (rows `stride` elements apart, io_dtype), from one random number u in [0, 1) per row.
+ *   weights  e_i = exp((x_i - max) / temperature); tokens are ranked by x_i, largest first, equal ones by the lower index
+ *   top_k    the first top_k of the rank (0 or less, or vocab and more: all)      min_p  those with e_i >= min_p (0: all)
+ *   top_p    of what both leave, the least number of first tokens whose weights reach top_p of the sum (1 and more: all)
+ *   token    the first i, by index, at which the weights of the kept tokens up to i sum to more than u times the sum of all kept
+ * Each setting is one value for all rows (params) or, where a pointer is given, one per row (fp32, top_k int32).  temperature 0 keeps the first
+ * largest logit alone.  A logit of -inf or NaN is never kept; beside +inf nothing else is.
+ *   token: int32; logprob (nullable): log of the probability with which it was drawn, fp32; kept (nullable): number of kept tokens, int32
+ * A row without a usable logit gets token -1, logprob -inf, kept 0; a row with a setting out of range (temperature negative or not
+ * finite, top_p <= 0, min_p outside [0, 1], u outside [0, 1), any of them NaN) token -1, logprob NaN, kept 0.
+ * Sums are exact integers of weights with 45 fractional bits (fewer beyond 2^17 tokens): the result does not depend on scheduling,
+ * and it is the definition's unless u or top_p meets a border to within about 2^-37.  rows <= 2^27, vocab <= 2^30.
+ */
+typedef struct lapsum_sample_params {
+    double temperature; /* default 1                                    */
+    double top_p;       /* default 1                                    */
+    double min_p;       /* default 0                                    */
+    int32_t top_k;      /* default 0                                    */
+    int32_t io_dtype;   /* lapsum_io_dtype of the logits; default fp32  */
+} lapsum_sample_params;
+
+void lapsum_sample_default_params(lapsum_sample_params *prm);
+int lapsum_sample(const void *logits, int64_t rows, int64_t vocab, int64_t stride, const float *u, const lapsum_sample_params *prm,
+                  const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token,
+                  float *logprob, int32_t *kept, void *stream);
+
+/*
+ * lapsum_embed_forward: out_i = scale table[ids_i]   (table: vocab x d, out: tokens x d, any row strides >= d, both io_dtype: fp32, fp16, bf16).
+ * ids: int32, or int64 with id_bytes = 8.  An id outside [0, vocab) gives a row of zeros.
+ * lapsum_embed_backward: grad_table (vocab x d, contiguous, written in full) with rows scale * sum of grad_out_i over ids_i = row, zeros for
+ * tokens that do not occur; ids outside [0, vocab) and those equal to `skip` (padding; -1: none) add nothing.  grad_out: io_dtype, any row
+ * stride >= d; grad_table: grad_dtype (io_dtype or fp32).  Sums are fp32 in an order that depends on the ids alone.
+ * Workspace: 256-byte aligned, bytes as described for at least as many tokens and the same vocab and d; needs no initialisation, serves one stream at a time.
+ * tokens <= 2^30, vocab <= 2^30, d <= 2^20.
+ */
+int lapsum_embed_forward(const void *ids, int32_t id_bytes, int64_t tokens, const void *table, int64_t table_stride, int64_t vocab,
+                         int64_t d, double scale, int32_t io_dtype, void *out, int64_t out_stride, void *stream);
+int lapsum_embed_workspace_bytes(int64_t tokens, int64_t vocab, int64_t d, size_t *bytes);
+int lapsum_embed_backward(const void *grad_out, int64_t grad_stride, const void *ids, int32_t id_bytes, int64_t tokens, int64_t vocab,
+                          int64_t d, double scale, int64_t skip, int32_t io_dtype, int32_t grad_dtype, void *grad_table, void *ws,
+                          size_t ws_bytes, void *stream);
 
 /* Number of kernel launches this library has enqueued since it was loaded. */
 int64_t lapsum_launch_count(void);

@@ -34,6 +34,7 @@ ST_BAD_BUDGET = 0x80
 ST_BAD_ALPHA = 0x100
 ST_BOUNDS = 0x200
 ST_EXPERTS_TIMEOUT = 0x400
+ST_LINEAR_TIMEOUT = 0x800
 
 EXPORTS = (
     "lapsum_default_params", "lapsum_workspace_bytes", "lapsum_workspace_init", "lapsum_workspace_release",
@@ -49,6 +50,9 @@ EXPORTS = (
     "lapsum_dispatch_tile_rows", "lapsum_dispatch_describe", "lapsum_dispatch",
     "lapsum_experts_describe", "lapsum_experts_workspace_init", "lapsum_experts_status", "lapsum_experts_forward",
     "lapsum_experts_backward", "lapsum_debug_experts_timeout",
+    "lapsum_linear_describe", "lapsum_linear_workspace_init", "lapsum_linear_status", "lapsum_linear_forward",
+    "lapsum_linear_backward", "lapsum_debug_linear_timeout", "lapsum_sample_default_params", "lapsum_sample",
+    "lapsum_embed_forward", "lapsum_embed_workspace_bytes", "lapsum_embed_backward",
 )
 
 KERNELS = ("row_block_forward", "row_block_backward", "rs_histogram", "rs_onesweep", "tile_aggregate", "solve_global",
@@ -110,6 +114,23 @@ class ExpertsDims(C.Structure):
 
 class ExpertsLayout(C.Structure):
     _fields_ = [("workspace_bytes", C.c_size_t), ("saved_bytes", C.c_size_t)]
+
+
+class LinearDims(C.Structure):
+    _fields_ = [
+        ("rows", C.c_int64), ("n", C.c_int64), ("k", C.c_int64), ("activation", C.c_int32), ("io_dtype", C.c_int32),
+        ("out_dtype", C.c_int32), ("bias_dtype", C.c_int32), ("grad_w_dtype", C.c_int32), ("training", C.c_int32),
+    ]
+
+
+class LinearLayout(C.Structure):
+    _fields_ = [("workspace_bytes", C.c_size_t), ("pre_bytes", C.c_size_t), ("pre_stride", C.c_int64)]
+
+
+class SampleParams(C.Structure):
+    _fields_ = [
+        ("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int32), ("io_dtype", C.c_int32),
+    ]
 
 
 class Stats(C.Structure):
@@ -180,6 +201,18 @@ def lib():
         L.lapsum_experts_status.argtypes = [vp, vp, C.POINTER(C.c_uint32)]
         L.lapsum_experts_forward.argtypes = [vp, i64, vp, vp, vp, vp, sz, vp, sz, vp, vp, vp, sz, vp]
         L.lapsum_experts_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, sz, vp, sz, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.lapsum_linear_describe.argtypes = [vp, C.POINTER(LinearLayout)]
+        L.lapsum_linear_workspace_init.argtypes = [vp, sz, vp, vp]
+        L.lapsum_linear_status.argtypes = [vp, vp, C.POINTER(C.c_uint32)]
+        L.lapsum_linear_forward.argtypes = [vp, i64, vp, vp, vp, i64, vp, i64, vp, sz, vp, vp, sz, vp]
+        L.lapsum_linear_backward.argtypes = [vp, i64, vp, i64, vp, vp, sz, vp, i64, vp, vp, vp, vp, sz, vp]
+        L.lapsum_debug_linear_timeout.argtypes = [i64, vp, vp, vp, vp, vp, sz, vp]
+        L.lapsum_sample_default_params.argtypes = [C.POINTER(SampleParams)]
+        L.lapsum_sample_default_params.restype = None
+        L.lapsum_sample.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.lapsum_embed_forward.argtypes = [vp, i32, i64, vp, i64, i64, i64, dbl, i32, vp, i64, vp]
+        L.lapsum_embed_workspace_bytes.argtypes = [i64, i64, i64, C.POINTER(sz)]
+        L.lapsum_embed_backward.argtypes = [vp, i64, vp, i32, i64, i64, i64, dbl, i64, i32, i32, vp, vp, sz, vp]
         L.lapsum_debug_experts_timeout.argtypes = [i64, vp, sz, vp, sz, vp, vp, vp, vp, vp]
         L.lapsum_launch_count.argtypes = []
         L.lapsum_launch_count.restype = i64

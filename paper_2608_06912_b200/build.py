@@ -12,9 +12,9 @@ CSRC = os.path.join(HERE, "csrc")
 # LAPSUM_IN_BOUNDS in csrc/common.cuh): a separate library, built with build(check_bounds=True)
 CHECK = os.environ.get("LAPSUM_B200_CHECK_BUILD", "0") not in ("", "0")
 LIB = os.path.join(HERE, "liblapsum_b200_check.so" if CHECK else "liblapsum_b200.so")
-SOURCES = ["lapsum_api.cu", "experts_api.cu"]
+SOURCES = ["lapsum_api.cu", "experts_api.cu", "linear_api.cu", "token_api.cu"]
 HEADERS = ["common.cuh", "solve.cuh", "radix_sort.cuh", "row_block.cuh", "global_path.cuh", "bracket_select.cuh",
-           "host.h", "routing.cuh", "experts.cuh",
+           "host.h", "routing.cuh", "experts.cuh", "tensor_core.cuh", "api.h", "linear.cuh", "sample.cuh", "embed.cuh",
            os.path.join("..", "..", "include", "lapsum.h")]
 
 

@@ -207,6 +207,24 @@ __device__ __forceinline__ typename Io<T>::Vec io_ldcs(const typename Io<T>::Vec
 template <typename T>
 __device__ __forceinline__ void io_stcs(typename Io<T>::Vec *p, const typename Io<T>::Vec &v) { __stcs(p, v); }
 
+// sum + <a, b> of eight 16-bit values each; a warp's total of one float per lane, in every lane
+template <typename T>
+__device__ __forceinline__ float dot8(const uint4 &a, const uint4 &b, float sum)
+{
+    float2 x[4], y[4], s = make_float2(sum, 0.f);
+    Io<T>::unpack2(a, x);
+    Io<T>::unpack2(b, y);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = fma2(x[i], y[i], s);
+    return s.x + s.y;
+}
+__device__ __forceinline__ float warp_total(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
+    return v;
+}
+
 // ------------------------------------------------------------- monoid ----
 // Stabilised exponential prefix (App. A: the affine recurrence
 // x_i = w_i x_{i-1} + 1 is associative): an aggregate is the sum of

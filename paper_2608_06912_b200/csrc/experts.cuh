@@ -24,11 +24,11 @@
 // the combine (1.1 GB more, 0.16 ms by its bytes, on 1.65 ms for 131072 slots) to take away an error of the size of the final
 // rounding.  Against 64 bits the outputs are 2.9e-3 (y, bf16; one rounding alone gives 1.7e-3) to 3.4e-3 (grad_x) off in the 2-norm.
 #pragma once
-#include <cuda.h>
 
 #include <type_traits>
 
 #include "common.cuh"
+#include "tensor_core.cuh"
 
 namespace lapsum {
 
@@ -48,180 +48,6 @@ struct ExpertsArgs {
     int row_tiles;                  // row tiles that the batch may need at most; those it does not need have tile_expert -1
     int early;                      // the tables were complete before the previous kernel of the stream began
     int hold;                       // test hook: the producer brings nothing, so the waits run out
-};
-
-// ------------------------------------------------------------------- PTX ----
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)  // a shared::cluster address
-{
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-                 : "=r"(ok)
-                 : "r"(bar), "r"(parity)
-                 : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ unsigned long long global_ns()
-{
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-                 "l"(map), "r"(x), "r"(y), "r"(bar)
-                 : "memory");
-}
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
-{
-    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
-                 : "memory");
-}
-// The same by one block of a pair: the bytes are counted by a barrier of the pair's first block (a shared::cluster address).
-__device__ __forceinline__ void tma_pair_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(bar)
-        : "memory");
-}
-__device__ __forceinline__ void tma_pair_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
-        : "memory");
-}
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int x, int y)
-{
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
-}
-__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, uint32_t src, int x, int y, int z)
-{
-    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z)
-                 : "memory");
-}
-__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void tma_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank)  // the address of another block's copy of a shared variable
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ void cluster_barrier()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// four rows of a matrix, 64 columns each; a row index beyond the matrix reads as zeros
-__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map, int x, int4 r, uint32_t bar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
-        "l"(map), "r"(x), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w), "r"(bar)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&v)[16])
-{
-    uint32_t r[16];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(addr));
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-// The wait names the loaded registers as its operands, so that no use of theirs can be scheduled before it.
-__device__ __forceinline__ void tmem_pin(float (&v)[16])
-{
-    asm volatile("" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]), "+f"(v[8]), "+f"(v[9]),
-                 "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]));
-}
-__device__ __forceinline__ void tmem_wait_ld(float (&v)[16])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-    tmem_pin(v);
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-template <bool PAIR>
-__device__ __forceinline__ void tc_commit(uint32_t bar)  // PAIR: on the barrier of this name in both blocks
-{
-    if constexpr (PAIR)
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                     "h"((uint16_t)3)
-                     : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-template <bool PAIR>
-__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
-{
-    if constexpr (PAIR)
-        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-                     "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-                     : "memory");
-    else
-        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-                     "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
-                     : "memory");
-}
-
-// Shared-memory matrix descriptor, 128-byte swizzle.  K-major: rows of 64 elements along the contraction, groups of 8 rows
-// 1024 bytes apart.  MN-major: rows of 64 elements along M or N, one per index of the contraction; groups of 8 such rows
-// 1024 bytes apart, the next 64 of M or N 8192 bytes (64 rows) further on.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn_major)
-{
-    const uint64_t lbo = mn_major ? 8192 >> 4 : 1, sbo = 1024 >> 4;
-    return (uint64_t)((addr & 0x3ffff) >> 4) | (lbo << 16) | (sbo << 32) | (1ull << 46) | (2ull << 61);
-}
-
-// Waits of one block: bounded; the first that runs out raises the block's flag, on which all others give up, except those
-// for copies into the block's own memory, which must land before it ends.
-struct Waits {
-    volatile int *abort;
-    uint32_t *status;
-    unsigned long long limit;
-    __device__ __forceinline__ bool plain(uint32_t bar, uint32_t parity, bool heed)
-    {
-        if (mbar_try(bar, parity)) return true;
-        const unsigned long long t0 = global_ns();
-        for (;;) {
-            for (int i = 0; i < 32; ++i)
-                if (mbar_try(bar, parity)) return true;
-            if (heed && *abort) return false;
-            if (global_ns() - t0 > limit) {
-                *abort = 1;
-                atomicOr(status, LAPSUM_ST_EXPERTS_TIMEOUT);
-                return false;
-            }
-        }
-    }
-    __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) { return plain(bar, parity, true); }
 };
 
 template <typename T>
@@ -390,7 +216,7 @@ __global__ void __launch_bounds__((ExpertsShape<MODE, AR, BN, KS>::THREADS), 1) 
         }
         return t;
     };
-    Waits waits{&abort_flag, P.status, P.wait_ns};
+    Waits waits{&abort_flag, P.status, P.wait_ns, LAPSUM_ST_EXPERTS_TIMEOUT};
 
     if (warp == 0) {
         // ------------------------------------------------ producer
@@ -738,23 +564,6 @@ __global__ void __launch_bounds__((ExpertsShape<MODE, AR, BN, KS>::THREADS), 1) 
 // One or a few tokens: every weight is used once, so the products are streams of weights at memory speed and the tensor core
 // has nothing to add, as long as tokens hardly share experts (few_tokens, experts_api.cu).  Each lane keeps eight or more 16-byte loads in flight; a token's choices are finished in one warp, so
 // there is neither a table of slots to combine nor a rounding per slot.
-template <typename T>
-__device__ __forceinline__ float dot8(const uint4 &a, const uint4 &b, float sum)
-{
-    float2 x[4], y[4], s = make_float2(sum, 0.f);
-    Io<T>::unpack2(a, x);
-    Io<T>::unpack2(b, y);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s = fma2(x[i], y[i], s);
-    return s.x + s.y;
-}
-__device__ __forceinline__ float warp_total(float v)
-{
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL, v, o);
-    return v;
-}
-
 // hw[entry][f] = w silu(g) u.  A block has FEW_FEATURES features of one entry (so its expert is looked up once), a warp one
 // feature at a time: sixteen loads of its two rows at once, 16 warps per SM, 128 KB on their way.  (Three blocks per SM spill and
 // are no faster; 8, 32 or 64 features a block are within 5 %.)

@@ -4,6 +4,7 @@
 #include <cstring>
 
 #include "../../include/lapsum.h"
+#include "api.h"
 #include "experts.cuh"
 #include "host.h"
 #include "routing.cuh"
@@ -11,20 +12,6 @@
 using namespace lapsum;
 
 namespace {
-
-inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
-inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-#define CU_OK(x)                                      \
-    do {                                              \
-        const cudaError_t e__ = (x);                  \
-        if (e__ != cudaSuccess) return cuda_fail(e__); \
-    } while (0)
-#define RUN(x)                    \
-    do {                          \
-        const int rc__ = (x);     \
-        if (rc__ != 0) return rc__; \
-    } while (0)
 
 // ------------------------------------------------------------------- route ----
 int route_check(int64_t tokens, int64_t experts, int64_t stride, const lapsum_route_params *p)
@@ -79,10 +66,6 @@ struct RouteShape {
      : (E) <= 256 ? RouteShape<T, 16, 16>::what(__VA_ARGS__)      \
      : (E) <= 512 ? RouteShape<T, 32, 16>::what(__VA_ARGS__)      \
                   : RouteShape<T, 32, 32>::what(__VA_ARGS__))
-#define BY_TYPE(fn, dtype, ...)                                  \
-    ((dtype) == LAPSUM_IO_F32   ? fn<float>(__VA_ARGS__)          \
-     : (dtype) == LAPSUM_IO_F16 ? fn<__half>(__VA_ARGS__)         \
-                                : fn<__nv_bfloat16>(__VA_ARGS__))
 
 template <typename T>
 int route_forward_t(const RouteArgs &A, cudaStream_t st)
@@ -204,42 +187,6 @@ int experts_layout(const lapsum_experts_dims *p, ExpertsLayout &X, lapsum_expert
     return LAPSUM_OK;
 }
 
-using EncodeFn = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                              const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                              CUtensorMapFloatOOBfill);
-EncodeFn encode_fn()
-{
-    static const EncodeFn fn = [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeFn>(p);
-    }();
-    return fn;
-}
-
-// dims from the innermost; strides in elements for dimensions 1..; 128-byte swizzle; reads beyond the tensor give zeros
-int tensor_map(CUtensorMap *map, int dtype, const void *base, int rank, const int64_t *dims, const int64_t *strides, const int *box)
-{
-    const EncodeFn fn = encode_fn();
-    if (!fn) return cuda_fail(cudaErrorNotSupported);
-    cuuint64_t d[3], s[2];
-    cuuint32_t b[3], one[3] = {1, 1, 1};
-    for (int i = 0; i < rank; ++i) d[i] = (cuuint64_t)dims[i], b[i] = (cuuint32_t)box[i];
-    for (int i = 0; i + 1 < rank; ++i) s[i] = (cuuint64_t)strides[i] * 2;
-    const CUresult r = fn(map, dtype == LAPSUM_IO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank,
-                          const_cast<void *>(base), d, s, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? LAPSUM_OK : cuda_fail(cudaErrorInvalidValue);
-}
-int map_2d(CUtensorMap *m, int dtype, const void *base, int64_t cols, int64_t rows, int64_t stride, int box_rows)
-{
-    const int64_t d[2] = {cols, rows}, s[1] = {stride};
-    const int b[2] = {64, box_rows};
-    return tensor_map(m, dtype, base, 2, d, s, b);
-}
 int map_3d(CUtensorMap *m, int dtype, const void *base, int64_t cols, int64_t rows, int64_t depth, int box_rows)
 {
     const int64_t d[3] = {cols, rows, depth}, s[2] = {cols, cols * rows};
@@ -253,19 +200,6 @@ int map_gu(CUtensorMap *m, int dtype, const void *base, int64_t f, int64_t slots
     const int64_t d[3] = {f, 2, slots}, s[2] = {f, 2 * f};
     const int b[3] = {64, 1, box_rows};
     return tensor_map(m, dtype, base, 3, d, s, b);
-}
-
-int sm_count(int *n)
-{
-    static thread_local int dev_known = -1, sms = 0;
-    int dev = 0;
-    CU_OK(cudaGetDevice(&dev));
-    if (dev != dev_known) {
-        CU_OK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-        dev_known = dev;
-    }
-    *n = sms;
-    return LAPSUM_OK;
 }
 
 template <int MODE, int AR, int BN, int KS, typename T>
@@ -284,8 +218,6 @@ int run_experts(const ExpertsMaps &maps, const ExpertsArgs &P, int64_t tiles_max
     const int64_t units = S::PAIR ? sms / 2 : sms, n = tiles_max < 1 ? 1 : tiles_max < units ? tiles_max : units;
     return launch_clusters(S::PAIR ? 2 : 1, kernel, (unsigned)(S::PAIR ? 2 * n : n), S::THREADS, S::SMEM, st, maps, P);
 }
-
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct Call {
     const lapsum_experts_dims *p;

@@ -1,0 +1,187 @@
+// C entries between token ids and rows: lapsum_sample, lapsum_embed_*.  Argument checks, buffer layout and launches; nothing is allocated
+// and the host never waits.
+#include <cmath>
+#include <cstring>
+
+#include "../../include/lapsum.h"
+#include "api.h"
+#include "embed.cuh"
+#include "host.h"
+#include "sample.cuh"
+
+using namespace lapsum;
+
+namespace {
+
+// ------------------------------------------------------------------ sample ----
+constexpr int SAMPLE_BLOCK_BYTES = 64 << 10, SAMPLE_MOST_BYTES = 190 << 10;
+
+// Blocks per row: as many as keep a block's run at 64 KB (two blocks per SM), and more, down to runs of 4096 tokens, while the rows
+// leave SMs without work.
+template <typename T>
+int sample_t(SampleArgs A, int64_t rows, cudaStream_t st)
+{
+    int sms = 0, dev = 0;
+    RUN(sm_count(&sms));
+    int cluster = 1;
+    while (cluster < 8 && ((int64_t)A.vocab * (int)sizeof(T) > (int64_t)cluster * SAMPLE_BLOCK_BYTES ||
+                           (rows * cluster < 2 * sms && A.vocab >= 2 * 4096 * cluster)))
+        cluster *= 2;
+    A.cluster = cluster;
+    A.chunk = (int)(ceil_div(ceil_div(A.vocab, cluster), 128) * 128);
+    const size_t run = (size_t)A.chunk * sizeof(T);
+    A.resident = run <= SAMPLE_MOST_BYTES;
+    const size_t smem = sizeof(SampleShared) + (A.resident ? run : 0);
+    static thread_local int dev_ready = -1;  // the attribute belongs to the device's context
+    CU_OK(cudaGetDevice(&dev));
+    if (dev != dev_ready) {
+        CU_OK(cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SampleShared) + SAMPLE_MOST_BYTES));
+        dev_ready = dev;
+    }
+    return launch_clusters((unsigned)cluster, sample_kernel<T>, (unsigned)(rows * cluster), SAMPLE_THREADS, smem, st, A);
+}
+
+// ------------------------------------------------------------------- embed ----
+int embed_check(const void *ids, int32_t id_bytes, int64_t tokens, int64_t vocab, int64_t d, double scale, int32_t io_dtype)
+{
+    if (tokens < 0 || tokens > (int64_t)1 << 30 || vocab < 1 || vocab > (int64_t)1 << 30 || d < 1 || d > (int64_t)1 << 20) return LAPSUM_ERR_SHAPE;
+    if ((id_bytes != 4 && id_bytes != 8) || !std::isfinite(scale) || !std::isfinite((float)scale)) return LAPSUM_ERR_PARAM;
+    if (io_dtype < LAPSUM_IO_F32 || io_dtype > LAPSUM_IO_BF16) return LAPSUM_ERR_UNSUPPORTED;
+    if (tokens > 0 && !ids) return LAPSUM_ERR_NULL;
+    return LAPSUM_OK;
+}
+struct EmbedLayout {
+    size_t off_start, off_order, off_long, off_partial, bytes;
+};
+EmbedLayout embed_layout(int64_t tokens, int64_t vocab, int64_t d)
+{
+    EmbedLayout X;
+    size_t at = 256;  // the long rows' counter
+    X.off_start = at, at += align_up((size_t)(vocab + 1) * 4);
+    X.off_order = at, at += align_up((size_t)tokens * 4);
+    X.off_long = at, at += align_up((size_t)(tokens / EMBED_LONG + 1) * 4);
+    X.off_partial = at, at += align_up((size_t)ceil_div(tokens, EMBED_LONG) * 2 * (size_t)d * 4);
+    X.bytes = at;
+    return X;
+}
+template <typename T, bool VEC>
+int64_t embed_parts(int64_t d) { return ceil_div(d, EmbedShape<T, VEC>::SPAN); }
+
+template <typename T>
+int embed_forward_t(const EmbedArgs &A, cudaStream_t st)
+{
+    constexpr int V = Io<T>::V;
+    const bool vec = A.d % V == 0 && A.table_stride % V == 0 && A.out_stride % V == 0 && aligned(A.table, 16) && aligned(A.out, 16);
+    const int64_t units = A.tokens * (vec ? embed_parts<T, true>(A.d) : embed_parts<T, false>(A.d));
+    if (units > (int64_t)8 << 31) return LAPSUM_ERR_SHAPE;
+    return launch_pdl(vec ? embed_forward_kernel<T, true> : embed_forward_kernel<T, false>, (unsigned)ceil_div(units, 8), 256, 0, st, A);
+}
+
+template <typename T>
+int embed_backward_t(EmbedArgs A, cudaStream_t st)
+{
+    constexpr int V = Io<T>::V, smem = EMBED_WARPS * EMBED_RANGE * 4;
+    const bool vec = A.d % V == 0 && A.grad_stride % V == 0 && aligned(A.grad_out, 16) && aligned(A.grad, 16);
+    const int64_t parts = vec ? embed_parts<T, true>(A.d) : embed_parts<T, false>(A.d);
+    A.chunk_blocks = ceil_div(ceil_div(A.tokens, EMBED_LONG) * parts, 8);
+    const int64_t blocks = A.chunk_blocks + ceil_div(A.vocab * parts, 8);
+    if (blocks >= (int64_t)1 << 31) return LAPSUM_ERR_SHAPE;
+    int sms = 0, dev = 0;
+    RUN(sm_count(&sms));
+    static thread_local int dev_ready = -1;  // the attribute belongs to the device's context
+    CU_OK(cudaGetDevice(&dev));
+    if (dev != dev_ready) {
+        CU_OK(cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        dev_ready = dev;
+    }
+    RUN(launch_pdl(embed_sort_kernel, (unsigned)ceil_div(A.vocab, EMBED_RANGE), 32 * EMBED_WARPS, smem, st, A));
+    RUN(launch_pdl(vec ? embed_grad_kernel<T, true> : embed_grad_kernel<T, false>, (unsigned)blocks, 256, 0, st, A));
+    if (A.tokens <= EMBED_LONG) return LAPSUM_OK;  // no row can be long
+    return launch_pdl(embed_join_kernel<T>, (unsigned)(4 * sms), 256, 0, st, A);
+}
+
+
+}  // namespace
+
+extern "C" {
+
+void lapsum_sample_default_params(lapsum_sample_params *p)
+{
+    if (!p) return;
+    std::memset(p, 0, sizeof(*p));
+    p->temperature = p->top_p = 1.0;
+    p->io_dtype = LAPSUM_IO_F32;
+}
+
+int lapsum_sample(const void *logits, int64_t rows, int64_t vocab, int64_t stride, const float *u, const lapsum_sample_params *prm,
+                  const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token, float *logprob,
+                  int32_t *kept, void *stream)
+{
+    if (!prm) return LAPSUM_ERR_NULL;
+    if (rows < 0 || rows > (int64_t)1 << 27 || vocab < 1 || vocab > (int64_t)1 << 30 || stride < vocab) return LAPSUM_ERR_SHAPE;
+    // a setting for all rows has to be in range (one per row voids its row instead)
+    if (prm->io_dtype < LAPSUM_IO_F32 || prm->io_dtype > LAPSUM_IO_BF16 || (!temperature && !(prm->temperature >= 0 && std::isfinite(prm->temperature))) ||
+        (!top_p && !(prm->top_p > 0)) || (!min_p && !(prm->min_p >= 0 && prm->min_p <= 1)))
+        return LAPSUM_ERR_PARAM;
+    if (rows == 0) return LAPSUM_OK;
+    if (!logits || !u || !token) return LAPSUM_ERR_NULL;
+    SampleArgs A;
+    std::memset(&A, 0, sizeof(A));
+    A.logits = logits, A.stride = stride, A.u = u;
+    A.temperature_row = temperature, A.top_k_row = top_k, A.top_p_row = top_p, A.min_p_row = min_p;
+    A.temperature = prm->temperature, A.top_p = prm->top_p, A.min_p = prm->min_p, A.top_k = prm->top_k;
+    A.token = token, A.logprob = logprob, A.kept = kept;
+    A.vocab = (int)vocab;
+    A.bits = 45;
+    while (A.bits > 0 && vocab > (int64_t)1 << (62 - A.bits)) --A.bits;
+    return BY_TYPE(sample_t, prm->io_dtype, A, rows, static_cast<cudaStream_t>(stream));
+}
+
+int lapsum_embed_forward(const void *ids, int32_t id_bytes, int64_t tokens, const void *table, int64_t table_stride, int64_t vocab, int64_t d,
+                         double scale, int32_t io_dtype, void *out, int64_t out_stride, void *stream)
+{
+    RUN(embed_check(ids, id_bytes, tokens, vocab, d, scale, io_dtype));
+    if (table_stride < d || out_stride < d) return LAPSUM_ERR_SHAPE;
+    if (tokens == 0) return LAPSUM_OK;
+    if (!table || !out) return LAPSUM_ERR_NULL;
+    EmbedArgs A;
+    std::memset(&A, 0, sizeof(A));
+    A.ids = ids, A.wide_ids = id_bytes == 8, A.tokens = tokens, A.vocab = vocab, A.d = d, A.skip = -1, A.scale = (float)scale;
+    A.table = table, A.table_stride = table_stride, A.out = out, A.out_stride = out_stride;
+    return BY_TYPE(embed_forward_t, io_dtype, A, static_cast<cudaStream_t>(stream));
+}
+
+int lapsum_embed_workspace_bytes(int64_t tokens, int64_t vocab, int64_t d, size_t *bytes)
+{
+    if (!bytes) return LAPSUM_ERR_NULL;
+    if (tokens < 0 || tokens > (int64_t)1 << 30 || vocab < 1 || vocab > (int64_t)1 << 30 || d < 1 || d > (int64_t)1 << 20) return LAPSUM_ERR_SHAPE;
+    *bytes = embed_layout(tokens, vocab, d).bytes;
+    return LAPSUM_OK;
+}
+
+int lapsum_embed_backward(const void *grad_out, int64_t grad_stride, const void *ids, int32_t id_bytes, int64_t tokens, int64_t vocab, int64_t d,
+                          double scale, int64_t skip, int32_t io_dtype, int32_t grad_dtype, void *grad_table, void *ws, size_t ws_bytes, void *stream)
+{
+    RUN(embed_check(ids, id_bytes, tokens, vocab, d, scale, io_dtype));
+    if (grad_stride < d) return LAPSUM_ERR_SHAPE;
+    if (grad_dtype != io_dtype && grad_dtype != LAPSUM_IO_F32) return LAPSUM_ERR_UNSUPPORTED;
+    if (!grad_table || !ws || (tokens > 0 && !grad_out)) return LAPSUM_ERR_NULL;
+    const EmbedLayout X = embed_layout(tokens, vocab, d);
+    if (!aligned(ws, 256) || ws_bytes < X.bytes) return LAPSUM_ERR_WORKSPACE;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (tokens == 0) {
+        CU_OK(cudaMemsetAsync(grad_table, 0, (size_t)vocab * (size_t)d * (grad_dtype == LAPSUM_IO_F32 ? 4 : 2), st));
+        return LAPSUM_OK;
+    }
+    uint8_t *const at = static_cast<uint8_t *>(ws);
+    EmbedArgs A;
+    std::memset(&A, 0, sizeof(A));
+    A.ids = ids, A.wide_ids = id_bytes == 8, A.tokens = tokens, A.vocab = vocab, A.d = d, A.skip = skip, A.scale = (float)scale;
+    A.grad_out = grad_out, A.grad_stride = grad_stride, A.grad = grad_table, A.grad_f32 = grad_dtype == LAPSUM_IO_F32;
+    A.long_count = reinterpret_cast<uint32_t *>(at);
+    A.row_start = reinterpret_cast<int32_t *>(at + X.off_start), A.order = reinterpret_cast<int32_t *>(at + X.off_order);
+    A.long_rows = reinterpret_cast<int32_t *>(at + X.off_long), A.partial = reinterpret_cast<float *>(at + X.off_partial);
+    return BY_TYPE(embed_backward_t, io_dtype, A, st);
+}
+
+}  // extern "C"
