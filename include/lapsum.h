@@ -587,13 +587,14 @@ int lapsum_debug_experts_timeout(int64_t wait_us, void *ws, size_t ws_bytes, con
  * of out_dtype (io_dtype or fp32), any row strides >= n (elements); residual may be NULL, or y itself.  k and x_stride are multiples
  * of 8, x and w start at multiples of 16 bytes; n is free.
  *   act   none | relu | silu P s(P) | gelu P Phi(P) | gelu_tanh P s(2 u), u = sqrt(2 / pi) (P + 0.044715 P^3), s = sigmoid
- * `pre` (pre_bytes as described, 256-byte aligned) keeps P in io_dtype for the backward, rows pre_stride elements apart.  It belongs to
- * dims.training with an activation; otherwise it is NULL.
+ * `pre` (pre_bytes as described, 256-byte aligned) keeps P in pre_dtype for the backward, rows pre_stride elements apart.  It belongs to
+ * dims.training with an activation; otherwise it is NULL.  fp32 keeps the slope's digits; 16 bits take half the memory and leave an
+ * error of the size of a 16-bit rounding in the gradients.
  *
  * lapsum_linear_backward:  dP = grad_y act'(P),  grad_x = dP W,  grad_w = dP^T x,  grad_bias = sum over rows of dP.
  * grad_y: rows x n of out_dtype, any row stride >= n; grad_x: rows x k of io_dtype, any row stride >= k; grad_w: n x k of grad_w_dtype
  * (io_dtype or fp32); grad_bias: n of bias_dtype.  Each result may be NULL.  The residual's gradient is grad_y.  dP is rounded to
- * io_dtype for the products (the tensor core's operands); grad_bias sums it unrounded.  With rows = 0 grad_w and grad_bias are zeros.
+ * io_dtype for the products (the tensor core's operands); for an fp32 grad_w the remainder takes part as well, and grad_bias sums it unrounded.  With rows = 0 grad_w and grad_bias are zeros.
  * Results do not depend on scheduling.
  *
  * A workspace made for some rows serves calls of fewer.  It serves one stream at a time.  lapsum_linear_workspace_init clears its status
@@ -614,6 +615,7 @@ typedef struct lapsum_linear_dims {
     int32_t out_dtype;    /* io_dtype or LAPSUM_IO_F32: y, residual, grad_y                 */
     int32_t bias_dtype;   /* io_dtype or LAPSUM_IO_F32: bias, grad_bias                     */
     int32_t grad_w_dtype; /* io_dtype or LAPSUM_IO_F32                                      */
+    int32_t pre_dtype;    /* io_dtype or LAPSUM_IO_F32: what `pre` keeps                    */
     int32_t training;     /* 1: a forward is followed by a backward                         */
 } lapsum_linear_dims;
 

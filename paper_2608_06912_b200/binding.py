@@ -119,7 +119,8 @@ class ExpertsLayout(C.Structure):
 class LinearDims(C.Structure):
     _fields_ = [
         ("rows", C.c_int64), ("n", C.c_int64), ("k", C.c_int64), ("activation", C.c_int32), ("io_dtype", C.c_int32),
-        ("out_dtype", C.c_int32), ("bias_dtype", C.c_int32), ("grad_w_dtype", C.c_int32), ("training", C.c_int32),
+        ("out_dtype", C.c_int32), ("bias_dtype", C.c_int32), ("grad_w_dtype", C.c_int32), ("pre_dtype", C.c_int32),
+        ("training", C.c_int32),
     ]
 
 

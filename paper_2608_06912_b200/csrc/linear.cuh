@@ -22,18 +22,19 @@
 namespace lapsum {
 
 struct LinearMaps {
-    CUtensorMap a, b;
+    CUtensorMap a, b, b_low;  // b_low: what the rounding of b to 16 bits left, where the contraction runs over both
 };
 
 struct LinearArgs {
     void *out;             // fp32 (out_f32) or T, rows out_stride elements apart
     const void *residual;  // like out, or null
     const void *bias;      // fp32 (bias_f32) or T, or null
-    void *pre;             // T, rows pre_stride elements apart, or null
+    void *pre;             // fp32 (pre_f32) or T, rows pre_stride elements apart, or null
     int64_t out_stride, residual_stride, pre_stride;
     int L, C, K;           // lanes, columns, contraction
     int lane_tiles, col_tiles;
-    int act, out_f32, bias_f32;
+    int act, out_f32, bias_f32, pre_f32;
+    int twice;             // the contraction runs over (a, b), then over (a, b_low)
     int split;             // blocks of a cluster that share the contraction of one tile
     int hold;              // test hook: the producer brings nothing, so the waits run out
     uint32_t *status;
@@ -41,38 +42,64 @@ struct LinearArgs {
 };
 
 // ---------------------------------------------------------------- activations ----
-// e^x to about 2 ulp: the product with log2(e) split in two
-__device__ __forceinline__ float exp_of(float x) { return exp2f(fmaf(x, 1.44269502f, x * 1.92596299e-8f)); }
-__device__ __forceinline__ float sigmoid_of(float x) { return __fdividef(1.f, 1.f + exp_of(-x)); }
+// 1 / (1 + e^-x) to about 3 ulp: the product with log2(e) split in two, the hardware's 2^x and reciprocal.  (Subnormal e^-x are 0 beside the 1.)
+__device__ __forceinline__ float exp_of(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaf(x, 1.44269502f, x * 1.92596299e-8f)));
+    return y;
+}
+__device__ __forceinline__ float sigmoid_of(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(1.f + exp_of(-x)));
+    return y;
+}
 constexpr float GELU_A = 0.797884561f, GELU_B = 0.044715f;  // sqrt(2 / pi), the tanh form's cubic term
 
-__device__ __forceinline__ float activate(float x, int act)
+template <int ACT>
+__device__ __forceinline__ float activate(float x)
+{
+    if constexpr (ACT == LAPSUM_ACT_RELU) return x > 0.f ? x : x == x ? 0.f : x;
+    else if constexpr (ACT == LAPSUM_ACT_SILU) return x * sigmoid_of(x);
+    else if constexpr (ACT == LAPSUM_ACT_GELU) return 0.5f * x * (1.f + erff(0.707106781f * x));
+    else if constexpr (ACT == LAPSUM_ACT_GELU_TANH)
+        return x * sigmoid_of(2.f * GELU_A * x * fmaf(GELU_B * x, x, 1.f));  // (1 + tanh u) / 2 = sigmoid(2 u)
+    else return x;
+}
+template <int ACT>
+struct Act {
+    static constexpr int value = ACT;
+};
+template <typename F>
+__device__ __forceinline__ void by_activation(int act, F f)
 {
     switch (act) {
-    case LAPSUM_ACT_RELU: return x > 0.f ? x : x == x ? 0.f : x;
-    case LAPSUM_ACT_SILU: return x * sigmoid_of(x);
-    case LAPSUM_ACT_GELU: return 0.5f * x * (1.f + erff(0.707106781f * x));
-    case LAPSUM_ACT_GELU_TANH: return x * sigmoid_of(2.f * GELU_A * x * fmaf(GELU_B * x, x, 1.f));  // (1 + tanh u) / 2 = sigmoid(2 u)
-    default: return x;
+    case LAPSUM_ACT_RELU: f(Act<LAPSUM_ACT_RELU>()); break;
+    case LAPSUM_ACT_SILU: f(Act<LAPSUM_ACT_SILU>()); break;
+    case LAPSUM_ACT_GELU: f(Act<LAPSUM_ACT_GELU>()); break;
+    case LAPSUM_ACT_GELU_TANH: f(Act<LAPSUM_ACT_GELU_TANH>()); break;
+    default: f(Act<LAPSUM_ACT_NONE>()); break;
     }
 }
 // The slope at a pre-activation that was kept in 16 bits; beyond +-1000 every activation's slope is its limit (an infinity kept by
 // fp16 included, where the formulas would give infinity times 0).
-__device__ __forceinline__ float slope_of(float x, int act)
+template <int ACT>
+__device__ __forceinline__ float slope_of(float x)
 {
     x = x > 1000.f ? 1000.f : x < -1000.f ? -1000.f : x;  // NaN stays
-    switch (act) {
-    case LAPSUM_ACT_RELU: return x > 0.f ? 1.f : x == x ? 0.f : x;
-    case LAPSUM_ACT_SILU: {
+    if constexpr (ACT == LAPSUM_ACT_RELU) {
+        return x > 0.f ? 1.f : x == x ? 0.f : x;
+    } else if constexpr (ACT == LAPSUM_ACT_SILU) {
         const float s = sigmoid_of(x);
         return s * fmaf(x, 1.f - s, 1.f);
-    }
-    case LAPSUM_ACT_GELU: return fmaf(0.398942280f * x, exp_of(-0.5f * x * x), 0.5f + 0.5f * erff(0.707106781f * x));
-    case LAPSUM_ACT_GELU_TANH: {
+    } else if constexpr (ACT == LAPSUM_ACT_GELU) {
+        return fmaf(0.398942280f * x, exp_of(-0.5f * x * x), 0.5f + 0.5f * erff(0.707106781f * x));
+    } else if constexpr (ACT == LAPSUM_ACT_GELU_TANH) {
         const float s = sigmoid_of(2.f * GELU_A * x * fmaf(GELU_B * x, x, 1.f));
         return fmaf(2.f * GELU_A * x * s, (1.f - s) * fmaf(3.f * GELU_B * x, x, 1.f), s);
-    }
-    default: return 1.f;
+    } else {
+        return 1.f;
     }
 }
 
@@ -88,35 +115,65 @@ __device__ __forceinline__ void store_either(void *p, int64_t i, bool f32, float
     else Io<T>::store1(static_cast<T *>(p) + i, v);
 }
 
+// n of N values, `stride` apart
+template <typename S, int N>
+__device__ __forceinline__ void load_rows(const void *base, int64_t at, int64_t stride, int n, float (&v)[N])
+{
+    const S *p = static_cast<const S *>(base) + at;
+    S q[N];
+    if (n >= N) {
+#pragma unroll
+        for (int j = 0; j < N; ++j, p += stride) q[j] = ld(p);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = Io<S>::from_storage(q[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j, p += stride) v[j] = j < n ? Io<S>::from_storage(ld(p)) : 0.f;
+    }
+}
+template <typename S, int N>
+__device__ __forceinline__ void store_rows(void *base, int64_t at, int64_t stride, int n, const float (&v)[N])
+{
+    S *p = static_cast<S *>(base) + at;
+    if (n >= N) {
+#pragma unroll
+        for (int j = 0; j < N; ++j, p += stride) Io<S>::store1(p, v[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j, p += stride)
+            if (j < n) Io<S>::store1(p, v[j]);
+    }
+}
 // N values of lane l, rows r0 .. : bias, pre-activation, activation, residual, result
 template <typename T, int N>
 __device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N], int l, int r0, float bias)
 {
-    const int n = min(N, P.C - r0);
+    const int n = P.C - r0;
     float res[N];
     if (P.residual != nullptr) {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (j < n) res[j] = load_either<T>(P.residual, (int64_t)(r0 + j) * P.residual_stride + l, P.out_f32);
+        const int64_t at = (int64_t)r0 * P.residual_stride + l;
+        if (P.out_f32) load_rows<float>(P.residual, at, P.residual_stride, n, res);
+        else load_rows<T>(P.residual, at, P.residual_stride, n, res);
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] += bias;
     if (P.pre != nullptr) {
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (j < n) Io<T>::store1(static_cast<T *>(P.pre) + (int64_t)(r0 + j) * P.pre_stride + l, v[j]);
+        const int64_t at = (int64_t)r0 * P.pre_stride + l;
+        if (P.pre_f32) store_rows<float>(P.pre, at, P.pre_stride, n, v);
+        else store_rows<T>(P.pre, at, P.pre_stride, n, v);
     }
-    if (P.act != LAPSUM_ACT_NONE) {
+    if (P.act != LAPSUM_ACT_NONE)
+        by_activation(P.act, [&](auto act) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = activate(v[j], P.act);
-    }
+            for (int j = 0; j < N; ++j) v[j] = activate<decltype(act)::value>(v[j]);
+        });
     if (P.residual != nullptr) {
 #pragma unroll
         for (int j = 0; j < N; ++j) v[j] += res[j];
     }
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-        if (j < n) store_either<T>(P.out, (int64_t)(r0 + j) * P.out_stride + l, P.out_f32, v[j]);
+    const int64_t at = (int64_t)r0 * P.out_stride + l;
+    if (P.out_f32) store_rows<float>(P.out, at, P.out_stride, n, v);
+    else store_rows<T>(P.out, at, P.out_stride, n, v);
 }
 
 // ---------------------------------------------------------------- the kernel ----
@@ -124,6 +181,9 @@ __device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N]
 // into one of two accumulators in TMEM, warps 4 to 11 (two sets of four; a set reads the 128 lanes) finish the previous tile.
 //   PAIR   a cluster of two blocks works on one 256 x 256 tile (cta_group::2): each block brings 128 rows of A and half of B, 64 bytes per
 //          clock of tensor work instead of the 96 that a 128 x 256 tile of one block needs.
+//   WIDE   the tensor core's own additions truncate: an error of about 2^-25 of the sum each, all towards zero, 2e-6 at K = 2048 and 2e-5 at 16384.
+//          That is nothing to a 16-bit result.  For an fp32 result an accumulator takes ROUND steps (512 of the contraction), and the epilogue adds
+//          the rounds' sums in fp32 registers, rounded to nearest, while the next round is computed in the other accumulator: 5e-7.
 //   split  a cluster of `split` blocks shares the contraction of one tile, for shapes with few tiles: each leaves its sums in its shared
 //          memory, and after a cluster barrier adds its share of the columns over the blocks, in their order.
 template <int BN, bool PAIR_>
@@ -133,12 +193,14 @@ struct LinearShape {
     static constexpr int A_BYTES = 128 * 128, B_BYTES = COLS * 128, STAGE = A_BYTES + B_BYTES;
     static constexpr int FIT = 229376 / STAGE, STAGES = FIT < 12 ? FIT : 12;
     static constexpr int ACC = 2, TMEM = ACC * BN;
+    static constexpr int ROUND = 8;                // steps of 64 that one accumulator of a WIDE result takes
+    static constexpr int CHUNKS = (BN + 31) / 32;  // runs of 16 columns of one set of epilogue warps
     static constexpr int THREADS = 384;
     static constexpr int SMEM = STAGES * STAGE + 1024 + 512;
     static_assert(STAGES >= 2 && TMEM >= 32 && TMEM <= 512 && BN * 512 <= STAGES * STAGE, "tile does not fit");
 };
 
-template <bool A_MN, bool B_MN, int BN, bool PAIR, typename T>
+template <bool A_MN, bool B_MN, int BN, bool PAIR, bool WIDE, typename T>
 __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ LinearMaps maps, const LinearArgs P)
 {
     using S = LinearShape<BN, PAIR>;
@@ -181,9 +243,10 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
     const uint32_t tmem = tmem_at;
     pdl_wait();
 
-    const int steps = (P.K + 63) / 64;
+    const int half = (P.K + 63) / 64, steps = P.twice ? 2 * half : half;
     const int share = split ? (steps + P.split - 1) / P.split : steps;
     const int k_first = split ? min((int)rank * share, steps) : 0, nkb = min(share, steps - k_first);  // 0: a block without a part
+    const int round = WIDE ? S::ROUND : nkb;
     const int64_t tiles = (int64_t)P.lane_tiles * P.col_tiles;
     const int64_t group = PAIR ? 2 : split ? P.split : 1, tile0 = blockIdx.x / group, tile_step = gridDim.x / group;
 
@@ -218,7 +281,9 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
                 const uint32_t bar = PAIR ? in_block(full + 8 * s, 0) : full + 8 * s;  // a pair's first block counts for both
                 if (lane == 0 && (!PAIR || rank == 0)) mbar_expect_tx(full + 8 * s, PAIR ? 2 * S::STAGE : S::STAGE);
                 __syncwarp();
-                const int k0 = (k_first + kb) * 64;
+                const bool low = k_first + kb >= half;
+                const int k0 = (k_first + kb - (low ? half : 0)) * 64;
+                const CUtensorMap *const map_b = low ? &maps.b_low : &maps.b;
                 const uint32_t a = ring_a + s * S::A_BYTES, b = ring_b + s * S::B_BYTES;
                 if constexpr (A_MN) {
                     if (lane < 2) load(a + lane * 8192, &maps.a, t.l0 + lane * 64, k0, bar);
@@ -226,9 +291,9 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
                     if (lane == 0) load(a, &maps.a, k0, t.l0, bar);
                 }
                 if constexpr (B_MN) {
-                    if (lane >= 2 && lane < 2 + S::COLS / 64) load(b + (lane - 2) * 8192, &maps.b, c0 + (lane - 2) * 64, k0, bar);
+                    if (lane >= 2 && lane < 2 + S::COLS / 64) load(b + (lane - 2) * 8192, map_b, c0 + (lane - 2) * 64, k0, bar);
                 } else {
-                    if (lane == 2) load(b, &maps.b, k0, c0, bar);
+                    if (lane == 2) load(b, map_b, k0, c0, bar);
                 }
             }
             if (P.hold) break;
@@ -249,25 +314,26 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
             constexpr uint32_t step_a = A_MN ? 2048 : 32, step_b = B_MN ? 2048 : 32;  // 16 along the contraction
             uint32_t fill = 0, it = 0;
             bool ok = true, any = false;
-            for (int64_t i = tile0; i < tiles && ok && nkb > 0; i += tile_step, ++it) {
-                const uint32_t buf = it % S::ACC, phase = (it / S::ACC) & 1;
-                ok = waits.wait(acc_empty + 8 * buf, phase ^ 1);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t d = tmem + buf * BN;
-                for (int kb = 0; kb < nkb; ++kb, ++fill) {
-                    const uint32_t s = fill % S::STAGES;
-                    ok = waits.wait(full + 8 * s, (fill / S::STAGES) & 1);
+            for (int64_t i = tile0; i < tiles && ok; i += tile_step)
+                for (int k0 = 0; k0 < nkb && ok; k0 += round, ++it) {
+                    const uint32_t buf = it % S::ACC, phase = (it / S::ACC) & 1;
+                    ok = waits.wait(acc_empty + 8 * buf, phase ^ 1);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint64_t a = smem_desc(ring_a + s * S::A_BYTES, A_MN), b = smem_desc(ring_b + s * S::B_BYTES, B_MN);
+                    const uint32_t d = tmem + buf * BN;
+                    for (int kb = k0; kb < min(nkb, k0 + round); ++kb, ++fill) {
+                        const uint32_t s = fill % S::STAGES;
+                        ok = waits.wait(full + 8 * s, (fill / S::STAGES) & 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t a = smem_desc(ring_a + s * S::A_BYTES, A_MN), b = smem_desc(ring_b + s * S::B_BYTES, B_MN);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) tc_mma<PAIR>(d, a + q * (step_a >> 4), b + q * (step_b >> 4), idesc, (kb | q) != 0);
-                    any = true;
-                    tc_commit<PAIR>(empty + 8 * s);
+                        for (int q = 0; q < 4; ++q) tc_mma<PAIR>(d, a + q * (step_a >> 4), b + q * (step_b >> 4), idesc, (kb - k0) | q ? 1 : 0);
+                        any = true;
+                        tc_commit<PAIR>(empty + 8 * s);
+                    }
+                    if (ok) tc_commit<PAIR>(acc_full + 8 * buf);
                 }
-                if (ok) tc_commit<PAIR>(acc_full + 8 * buf);
-            }
             if (!ok && any) {  // a wait ran out: the products already issued end before the block does
                 tc_commit<PAIR>(drain);
                 waits.plain(drain, 0, false);
@@ -278,41 +344,69 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
         const int ew = warp & 3, set = (warp - 4) >> 2;
         const uint32_t lanes = (uint32_t)ew << 21;  // 32 TMEM lanes per warp, lane index in the upper half
         uint32_t it = 0;
-        for (int64_t i = tile0; i < tiles; i += tile_step, ++it) {
+        bool ok = true;
+        for (int64_t i = tile0; i < tiles && ok; i += tile_step) {
             const Tile t = tile_at(i);
-            const uint32_t buf = it % S::ACC, phase = (it / S::ACC) & 1;
             const int l = t.l0 + 32 * ew + lane;
             float bias = 0.f;
             if (P.bias != nullptr && l < P.L && !split) bias = load_either<T>(P.bias, l, P.bias_f32);
-            if (nkb > 0) {
-                const bool ok = waits.wait(acc_full + 8 * buf, phase);
-                if (!__all_sync(FULL, ok)) break;
-                tc_fence_after();
-            }
-            const uint32_t d = tmem + buf * BN + lanes;
-#pragma unroll 1
-            for (int c = 16 * set; c < BN && t.c0 + c < P.C; c += 32) {
-                float v[16];
-                if (nkb > 0) {
-                    tmem_ld16(d + c, v);
-                    tmem_wait_ld(v);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] = 0.f;
-                }
+            const auto finish = [&](float (&v)[16], int c0) {  // columns c0 .. of the tile
                 if (split) {
                     // the ring is free: all products of this block's only tile have ended.  [column][lane]
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(ring_a + 4 * ((c + j) * 128 + 32 * ew + lane)), "f"(v[j]) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(ring_a + 4 * ((c0 + j) * 128 + 32 * ew + lane)), "f"(v[j]) : "memory");
                 } else if (l < P.L) {
-                    linear_finish<T>(P, v, l, t.c0 + c, bias);
+                    linear_finish<T>(P, v, l, t.c0 + c0, bias);
                 }
+            };
+            float sum[WIDE ? S::CHUNKS : 1][16];
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int c = 0; c < S::CHUNKS; ++c)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[c][j] = 0.f;
             }
-            if (nkb > 0) {
+            for (int k0 = 0; k0 < nkb; k0 += round, ++it) {
+                const uint32_t buf = it % S::ACC, phase = (it / S::ACC) & 1;
+                ok = waits.wait(acc_full + 8 * buf, phase);
+                ok = __all_sync(FULL, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t d = tmem + buf * BN + lanes + 16 * set;
+                if constexpr (WIDE) {
+#pragma unroll
+                    for (int c = 0; c < S::CHUNKS; ++c) {
+                        if (16 * set + 32 * c >= BN) continue;
+                        float v[16];
+                        tmem_ld16(d + 32 * c, v);
+                        tmem_wait_ld(v);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[c][j] += v[j];
+                    }
+                } else {
+#pragma unroll 1
+                    for (int c = 0; 16 * set + c < BN && t.c0 + 16 * set + c < P.C; c += 32) {
+                        tmem_ld16(d + c, sum[0]);
+                        tmem_wait_ld(sum[0]);
+                        finish(sum[0], 16 * set + c);
+                    }
+                }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(PAIR ? in_block(acc_empty + 8 * buf, 0) : acc_empty + 8 * buf);
+            }
+            if (!ok) break;
+            if constexpr (WIDE) {
+                // a loop that is not unrolled, over sums that move up: unrolled, it is 80 KB of code, and instruction fetches bound the kernel
+#pragma unroll 1
+                for (int c = 16 * set; c < BN && t.c0 + c < P.C; c += 32) {
+                    finish(sum[0], c);
+#pragma unroll
+                    for (int i = 0; i + 1 < S::CHUNKS; ++i)
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[i][j] = sum[i + 1][j];
+                }
             }
         }
     }
@@ -323,20 +417,31 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
         if (split) {
             cluster_barrier();
             const Tile t = tile_at(tile0);
-            const int l = tid & 127, per = (BN + P.split - 1) / P.split;
-            const int c1 = min(min(((int)rank + 1) * per, BN), P.C - t.c0);
+            const int l = tid & 127, per = BN / P.split;  // columns of one block: two or more, for BN >= 16 and up to eight blocks
+            const int c1 = ((int)rank + 1) * per;
             if (t.l0 + l < P.L) {
                 const float bias = P.bias != nullptr ? load_either<T>(P.bias, t.l0 + l, P.bias_f32) : 0.f;
-                for (int c = (int)rank * per + (tid >> 7); c < c1; c += 3) {
-                    float part[8], v[1] = {0.f};
+#pragma unroll 1
+                for (int c = (int)rank * per + 8 * (tid >> 7); c < c1 && t.c0 + c < P.C; c += 24) {
+                    float v[8] = {};
 #pragma unroll
                     for (int s = 0; s < 8; ++s)
-                        if (s < P.split)
-                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[s]) : "r"(in_block(ring_a + 4 * (c * 128 + l), s)) : "memory");
+                        if (s < P.split) {
+                            const uint32_t from = in_block(ring_a + 4 * (c * 128 + l), s);
+                            float part[8];
 #pragma unroll
-                    for (int s = 0; s < 8; ++s)
-                        if (s < P.split) v[0] += part[s];
-                    linear_finish<T>(P, v, t.l0 + l, t.c0 + c, bias);
+                            for (int j = 0; j < 8; ++j)
+                                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[j]) : "r"(from + 512 * j) : "memory");
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[j] += part[j];
+                        }
+                    if (per >= 8) {
+                        linear_finish<T>(P, v, t.l0 + l, t.c0 + c, bias);
+                    } else {
+                        LinearArgs Q = P;  // the next columns are another block's
+                        Q.C = min(P.C, t.c0 + c1);
+                        linear_finish<T>(Q, v, t.l0 + l, t.c0 + c, bias);
+                    }
                 }
             }
             __syncwarp();
@@ -393,22 +498,33 @@ __global__ void __launch_bounds__(256) linear_few_kernel(const T *x, int64_t x_s
         for (int r = 0; r < R; ++r)
             if (lane == 2 * r + f) mine[0] = sum[f][r];
     const int l = f0 + (lane & 1), r = lane >> 1;
-    if (r < R && l < P.L) linear_finish<T>(P, mine, l, r, P.bias != nullptr ? load_either<T>(P.bias, l, P.bias_f32) : 0.f);
+    if (r < R && l < P.L) {
+        const float bias = P.bias != nullptr ? load_either<T>(P.bias, l, P.bias_f32) : 0.f;
+        linear_finish<T>(P, mine, l, r, bias);
+    }
 }
 
 // ---------------------------------------------------------- dP and its column sums ----
-// dP = dy act'(P) in 16 bits, the operand of both products (one rounding; the bias' gradient sums the values before it), and the sums over
-// GRAD_ROWS rows, which linear_bias_kernel adds in order.  A warp has 256 columns, eight per lane, and every eighth row of the block.
+// dP = dy act'(P) in 16 bits, the operand of both products, and the sums over GRAD_ROWS rows of the values before that rounding, which linear_bias_kernel adds in order.  A warp has 256 columns, eight per lane, and every eighth row of the block.
+// One rounding of dP is of the size of a 16-bit result's own.  Where grad_w is fp32 it would be the largest error by far (2^-9 against
+// 2^-20), so there what the rounding left is kept in 16 bits as well, and the contraction of dW runs over both: twice the products for
+// gradients with the digits of an fp32 sum (3e-6).
 constexpr int GRAD_ROWS = 64;
 struct LinearGradArgs {
     const void *grad_y;  // fp32 (y_f32) or T
-    const void *pre;     // T, null without an activation
+    const void *pre;     // fp32 (pre_f32) or T, null without an activation
     void *dp;            // T, null where grad_y itself serves
+    void *dp_low;        // T, dP less its rounding, null where grad_w is 16-bit
     float *partial;      // [blocks of rows][n], null without a bias
     int64_t y_stride, pre_stride, dp_stride, rows;
-    int n, act, y_f32;
+    int n, y_f32, pre_f32;
 };
-template <typename T, bool VEC>
+__device__ __forceinline__ void load8f(const float *p, float (&x)[8])
+{
+    const float4 a = ld(reinterpret_cast<const float4 *>(p)), b = ld(reinterpret_cast<const float4 *>(p) + 1);
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+template <typename T, int ACT, bool VEC>
 __global__ void __launch_bounds__(256) linear_grad_kernel(const LinearGradArgs P)
 {
     pdl_wait();
@@ -422,26 +538,32 @@ __global__ void __launch_bounds__(256) linear_grad_kernel(const LinearGradArgs P
         for (int64_t r = row0 + warp; r < row1; r += 8) {
             float g[8];
             if (VEC) {
-                if (P.y_f32) {
-                    const float4 *const q = reinterpret_cast<const float4 *>(static_cast<const float *>(P.grad_y) + r * P.y_stride + c);
-                    const float4 a = ld(q), b = ld(q + 1);
-                    g[0] = a.x, g[1] = a.y, g[2] = a.z, g[3] = a.w, g[4] = b.x, g[5] = b.y, g[6] = b.z, g[7] = b.w;
-                } else {
-                    Io<T>::unpack(ld(reinterpret_cast<const uint4 *>(static_cast<const T *>(P.grad_y) + r * P.y_stride + c)), g);
-                }
+                if (P.y_f32) load8f(static_cast<const float *>(P.grad_y) + r * P.y_stride + c, g);
+                else Io<T>::unpack(ld(reinterpret_cast<const uint4 *>(static_cast<const T *>(P.grad_y) + r * P.y_stride + c)), g);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) g[i] = c + i < P.n ? load_either<T>(P.grad_y, r * P.y_stride + c + i, P.y_f32) : 0.f;
             }
-            if (P.pre != nullptr) {
+            if constexpr (ACT != LAPSUM_ACT_NONE) {
                 float p[8];  // rows of pre are whole vectors
-                Io<T>::unpack(ld(reinterpret_cast<const uint4 *>(static_cast<const T *>(P.pre) + r * P.pre_stride + c)), p);
+                if (P.pre_f32) load8f(static_cast<const float *>(P.pre) + r * P.pre_stride + c, p);
+                else Io<T>::unpack(ld(reinterpret_cast<const uint4 *>(static_cast<const T *>(P.pre) + r * P.pre_stride + c)), p);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = c + i < P.n ? g[i] * slope_of(p[i], P.act) : 0.f;  // the padding is nobody's
+                for (int i = 0; i < 8; ++i) g[i] = c + i < P.n ? g[i] * slope_of<ACT>(p[i]) : 0.f;  // the padding is nobody's
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += g[i];
-            if (P.dp != nullptr) *reinterpret_cast<uint4 *>(static_cast<T *>(P.dp) + r * P.dp_stride + c) = Io<T>::pack(g);
+            if (P.dp != nullptr) {
+                const uint4 q = Io<T>::pack(g);
+                *reinterpret_cast<uint4 *>(static_cast<T *>(P.dp) + r * P.dp_stride + c) = q;
+                if (P.dp_low != nullptr) {
+                    float h[8];
+                    Io<T>::unpack(q, h);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[i] = isfinite(h[i]) ? g[i] - h[i] : 0.f;  // beyond the range the rounding stands
+                    *reinterpret_cast<uint4 *>(static_cast<T *>(P.dp_low) + r * P.dp_stride + c) = Io<T>::pack(h);
+                }
+            }
         }
     }
     if (P.partial == nullptr) return;

@@ -12,7 +12,7 @@ using namespace lapsum;
 namespace {
 
 struct LinearLayout {
-    size_t off_dp, off_partial;
+    size_t off_dp, off_low, off_partial;
     int64_t ld, parts;  // row stride of pre and dP, blocks of rows of the bias' partial sums
 };
 
@@ -22,16 +22,17 @@ int linear_layout(const lapsum_linear_dims *p, LinearLayout &X, lapsum_linear_la
     if (p->rows < 0 || p->rows > (int64_t)1 << 30 || p->n < 1 || p->n > (int64_t)1 << 23 || p->k < 8 || p->k > (int64_t)1 << 20 || p->k % 8)
         return LAPSUM_ERR_SHAPE;
     if (p->io_dtype != LAPSUM_IO_F16 && p->io_dtype != LAPSUM_IO_BF16) return LAPSUM_ERR_UNSUPPORTED;
-    for (const int32_t t : {p->out_dtype, p->bias_dtype, p->grad_w_dtype})
+    for (const int32_t t : {p->out_dtype, p->bias_dtype, p->grad_w_dtype, p->pre_dtype})
         if (t != p->io_dtype && t != LAPSUM_IO_F32) return LAPSUM_ERR_UNSUPPORTED;
     if (p->activation < LAPSUM_ACT_NONE || p->activation > LAPSUM_ACT_GELU_TANH || (p->training != 0 && p->training != 1)) return LAPSUM_ERR_PARAM;
     X.ld = (p->n + 7) / 8 * 8;
     X.parts = ceil_div(p->rows, GRAD_ROWS);
     size_t at = 256;  // control block: the status word
     X.off_dp = at, at += p->training ? align_up((size_t)p->rows * (size_t)X.ld * 2) : 0;
+    X.off_low = at, at += p->training ? align_up((size_t)p->rows * (size_t)X.ld * 2) : 0;
     X.off_partial = at, at += p->training ? align_up((size_t)X.parts * (size_t)p->n * 4) : 0;
     out->workspace_bytes = at;
-    out->pre_bytes = p->training && p->activation != LAPSUM_ACT_NONE ? (size_t)p->rows * (size_t)X.ld * 2 : 0;
+    out->pre_bytes = p->training && p->activation != LAPSUM_ACT_NONE ? (size_t)p->rows * (size_t)X.ld * (p->pre_dtype == LAPSUM_IO_F32 ? 4 : 2) : 0;
     out->pre_stride = X.ld;
     return LAPSUM_OK;
 }
@@ -54,6 +55,7 @@ Choice choose(int64_t L, int64_t C, int64_t K, bool b_mn, int sms)
         const double bytes = 128 * (128 + bn) / 65.0, step = bytes > 2.0 * bn ? bytes : 2.0 * bn;
         for (int split = 1; split <= 8; split *= 2) {
             if (split > 1 && (steps < 2 * split || tiles * split > sms)) break;
+            if ((split - 1) * ceil_div(steps, split) >= steps) continue;  // a block without a part
             const int64_t rounds = ceil_div(tiles * split, sms);
             const double t = (double)rounds * ((double)ceil_div(steps, split) * step + 10.0 * bn) + (split > 1 ? 2500.0 : 0.0);
             if (t < least) least = t, best = Choice{bn, split, false};
@@ -65,14 +67,14 @@ Choice choose(int64_t L, int64_t C, int64_t K, bool b_mn, int sms)
     return best;
 }
 
-template <bool A_MN, bool B_MN, int BN, bool PAIR, typename T>
+template <bool A_MN, bool B_MN, int BN, bool PAIR, bool WIDE, typename T>
 int run_tiles(const LinearMaps &maps, const LinearArgs &A, int sms, cudaStream_t st)
 {
     using S = LinearShape<BN, PAIR>;
     static thread_local int dev_ready = -1;  // the attribute belongs to the device's context
     int dev = 0;
     CU_OK(cudaGetDevice(&dev));
-    const auto kernel = linear_kernel<A_MN, B_MN, BN, PAIR, T>;
+    const auto kernel = linear_kernel<A_MN, B_MN, BN, PAIR, WIDE, T>;
     if (dev != dev_ready) {
         CU_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
         dev_ready = dev;
@@ -80,6 +82,22 @@ int run_tiles(const LinearMaps &maps, const LinearArgs &A, int sms, cudaStream_t
     const int64_t tiles = (int64_t)A.lane_tiles * A.col_tiles, units = PAIR ? sms / 2 : A.split > 1 ? tiles : sms;
     const int cluster = PAIR ? 2 : A.split;
     return launch_clusters((unsigned)cluster, kernel, (unsigned)((tiles < units ? tiles : units) * cluster), S::THREADS, S::SMEM, st, maps, A);
+}
+template <bool A_MN, bool B_MN, bool WIDE, typename T>
+int run_choice(const LinearMaps &m, const LinearArgs &A, const Choice &ch, int sms, cudaStream_t st)
+{
+    if (ch.pair) return run_tiles<A_MN, B_MN, 256, true, WIDE, T>(m, A, sms, st);
+    switch (ch.bn) {
+    case 256: return run_tiles<A_MN, B_MN, 256, false, WIDE, T>(m, A, sms, st);
+    case 128: return run_tiles<A_MN, B_MN, 128, false, WIDE, T>(m, A, sms, st);
+    case 64: return run_tiles<A_MN, B_MN, 64, false, WIDE, T>(m, A, sms, st);
+    default: break;
+    }
+    if constexpr (!B_MN) {
+        if (ch.bn == 32) return run_tiles<A_MN, B_MN, 32, false, WIDE, T>(m, A, sms, st);
+        return run_tiles<A_MN, B_MN, 16, false, WIDE, T>(m, A, sms, st);
+    }
+    return LAPSUM_ERR_PARAM;
 }
 
 struct Operand {
@@ -89,28 +107,21 @@ struct Operand {
 
 // One product.  A: [L][K] or, A_MN, [K][L]; B: [C][K] or, B_MN, [K][C].
 template <bool A_MN, bool B_MN, typename T>
-int product(const Operand &a, const Operand &b, LinearArgs A, int dtype, cudaStream_t st)
+int product(const Operand &a, const Operand &b, LinearArgs A, int dtype, cudaStream_t st, const void *low = nullptr)
 {
     int sms = 0;
     RUN(sm_count(&sms));
-    const Choice ch = choose(A.L, A.C, A.K, B_MN, sms);
+    A.twice = low != nullptr;
+    const Choice ch = choose(A.L, A.C, A.K * (low ? 2ll : 1ll), B_MN, sms);
     A.split = ch.split;
     A.lane_tiles = (int)ceil_div(A.L, ch.pair ? 256 : 128), A.col_tiles = (int)ceil_div(A.C, ch.bn);
     LinearMaps m;
     RUN(map_2d(&m.a, dtype, a.base, a.cols, a.rows, a.stride, A_MN ? 64 : 128));
     RUN(map_2d(&m.b, dtype, b.base, b.cols, b.rows, b.stride, B_MN ? 64 : ch.pair ? 128 : ch.bn));
-    if (ch.pair) return run_tiles<A_MN, B_MN, 256, true, T>(m, A, sms, st);
-    switch (ch.bn) {
-    case 256: return run_tiles<A_MN, B_MN, 256, false, T>(m, A, sms, st);
-    case 128: return run_tiles<A_MN, B_MN, 128, false, T>(m, A, sms, st);
-    case 64: return run_tiles<A_MN, B_MN, 64, false, T>(m, A, sms, st);
-    default: break;
-    }
-    if constexpr (!B_MN) {
-        if (ch.bn == 32) return run_tiles<A_MN, B_MN, 32, false, T>(m, A, sms, st);
-        return run_tiles<A_MN, B_MN, 16, false, T>(m, A, sms, st);
-    }
-    return LAPSUM_ERR_PARAM;
+    m.b_low = m.b;
+    if (low) RUN(map_2d(&m.b_low, dtype, low, b.cols, b.rows, b.stride, B_MN ? 64 : ch.pair ? 128 : ch.bn));
+    if constexpr (A_MN && !B_MN) return run_choice<A_MN, B_MN, false, T>(m, A, ch, sms, st);  // grad_x is 16-bit
+    else return A.out_f32 ? run_choice<A_MN, B_MN, true, T>(m, A, ch, sms, st) : run_choice<A_MN, B_MN, false, T>(m, A, ch, sms, st);
 }
 
 constexpr int64_t FEW_ROWS = 4;
@@ -145,6 +156,12 @@ LinearArgs base_args(void *ws)
     return A;
 }
 
+template <typename T, int ACT>
+int grad(bool vec, dim3 grid, const LinearGradArgs &G, cudaStream_t st)
+{
+    return launch_pdl(vec ? linear_grad_kernel<T, ACT, true> : linear_grad_kernel<T, ACT, false>, grid, 256, 0, st, G);
+}
+
 template <typename T>
 int backward_t(const lapsum_linear_dims &p, const LinearLayout &X, const void *grad_y, int64_t gy_stride, const void *x, int64_t x_stride,
                const void *w, const void *pre, void *grad_x, int64_t gx_stride, void *grad_w, void *grad_bias, uint8_t *ws, cudaStream_t st)
@@ -152,16 +169,24 @@ int backward_t(const lapsum_linear_dims &p, const LinearLayout &X, const void *g
     const bool y_f32 = p.out_dtype == LAPSUM_IO_F32;
     // grad_y is dP itself where there is no activation and the tensor maps can take it as it lies
     const bool direct = p.activation == LAPSUM_ACT_NONE && !y_f32 && gy_stride % 8 == 0 && aligned(grad_y, 16);
-    const bool products = grad_x || grad_w;
+    const bool products = grad_x || grad_w, keep_low = grad_w && !direct && p.grad_w_dtype == LAPSUM_IO_F32;
     if (grad_bias || (products && !direct)) {
         LinearGradArgs G;
         std::memset(&G, 0, sizeof(G));
         G.grad_y = grad_y, G.pre = pre, G.dp = products && !direct ? ws + X.off_dp : nullptr;
         G.partial = grad_bias ? reinterpret_cast<float *>(ws + X.off_partial) : nullptr;
-        G.y_stride = gy_stride, G.pre_stride = G.dp_stride = X.ld, G.rows = p.rows, G.n = (int)p.n, G.act = p.activation, G.y_f32 = y_f32;
+        if (G.dp && keep_low) G.dp_low = ws + X.off_low;
+        G.pre_f32 = p.pre_dtype == LAPSUM_IO_F32;
+        G.y_stride = gy_stride, G.pre_stride = G.dp_stride = X.ld, G.rows = p.rows, G.n = (int)p.n, G.y_f32 = y_f32;
         const bool vec = gy_stride % 8 == 0 && p.n % 8 == 0 && aligned(grad_y, 16);
-        RUN(launch_pdl(vec ? linear_grad_kernel<T, true> : linear_grad_kernel<T, false>, dim3((unsigned)X.parts, (unsigned)ceil_div(p.n, 256)), 256,
-                       0, st, G));
+        const dim3 grid((unsigned)X.parts, (unsigned)ceil_div(p.n, 256));
+        switch (p.activation) {
+        case LAPSUM_ACT_RELU: RUN((grad<T, LAPSUM_ACT_RELU>(vec, grid, G, st))); break;
+        case LAPSUM_ACT_SILU: RUN((grad<T, LAPSUM_ACT_SILU>(vec, grid, G, st))); break;
+        case LAPSUM_ACT_GELU: RUN((grad<T, LAPSUM_ACT_GELU>(vec, grid, G, st))); break;
+        case LAPSUM_ACT_GELU_TANH: RUN((grad<T, LAPSUM_ACT_GELU_TANH>(vec, grid, G, st))); break;
+        default: RUN((grad<T, LAPSUM_ACT_NONE>(vec, grid, G, st))); break;
+        }
         if (grad_bias)
             RUN(launch_pdl(linear_bias_kernel<T>, (unsigned)ceil_div(p.n, 32), 1024, 0, st, G.partial, X.parts, (int)p.n, grad_bias,
                            p.bias_dtype == LAPSUM_IO_F32 ? 1 : 0));
@@ -176,7 +201,7 @@ int backward_t(const lapsum_linear_dims &p, const LinearLayout &X, const void *g
     if (grad_w) {
         A.out = grad_w, A.out_stride = p.k, A.out_f32 = p.grad_w_dtype == LAPSUM_IO_F32;
         A.L = (int)p.k, A.C = (int)p.n, A.K = (int)p.rows;
-        RUN((product<true, true, T>(Operand{x, p.k, p.rows, x_stride}, dp, A, p.io_dtype, st)));
+        RUN((product<true, true, T>(Operand{x, p.k, p.rows, x_stride}, dp, A, p.io_dtype, st, keep_low ? ws + X.off_low : nullptr)));
     }
     return LAPSUM_OK;
 }
@@ -224,7 +249,7 @@ int lapsum_linear_forward(const void *x, int64_t x_stride, const void *w, const 
     A.out = y, A.residual = residual, A.bias = bias, A.pre = pre;
     A.out_stride = y_stride, A.residual_stride = residual_stride, A.pre_stride = X.ld;
     A.L = (int)dims->n, A.C = (int)dims->rows, A.K = (int)dims->k, A.act = dims->activation;
-    A.out_f32 = dims->out_dtype == LAPSUM_IO_F32, A.bias_f32 = dims->bias_dtype == LAPSUM_IO_F32;
+    A.out_f32 = dims->out_dtype == LAPSUM_IO_F32, A.bias_f32 = dims->bias_dtype == LAPSUM_IO_F32, A.pre_f32 = dims->pre_dtype == LAPSUM_IO_F32;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return dims->io_dtype == LAPSUM_IO_BF16 ? forward_t<__nv_bfloat16>(*dims, x, x_stride, w, A, st) : forward_t<__half>(*dims, x, x_stride, w, A, st);
 }

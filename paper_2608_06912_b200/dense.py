@@ -33,18 +33,19 @@ def _matrix(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str, gpu: i
 # ------------------------------------------------------------------------------------------------------------ linear
 class LinearWorkspace(_Memory):
     """Scratch of act(x W^T + bias) + residual for up to `rows` rows (lapsum_linear_describe).  new_pre() makes the buffer that a training
-    forward keeps its pre-activation in, one per forward whose backward is still to come; without an activation there is none."""
+    forward keeps its pre-activation in (pre_dtype: fp32, or the 16-bit type for half the memory and fewer digits of the slope), one per forward
+    whose backward is still to come; without an activation there is none."""
 
     def __init__(self, rows: int, n: int, k: int, activation: int = ACT_NONE, io_dtype: int = IO_BF16, out_dtype: Optional[int] = None,
-                 training: bool = False, device=None, stream: Optional[torch.cuda.Stream] = None):
+                 training: bool = False, pre_dtype: int = IO_F32, device=None, stream: Optional[torch.cuda.Stream] = None):
         dev = _cuda(device)
         out_dtype = io_dtype if out_dtype is None else out_dtype
         self.dims = LinearDims(int(rows), int(n), int(k), int(activation), int(io_dtype), int(out_dtype), int(io_dtype), int(io_dtype),
-                               int(bool(training)))
+                               int(pre_dtype), int(bool(training)))
         out = LinearLayout()
         _check(lib().lapsum_linear_describe(C.byref(self.dims), C.byref(out)), "lapsum_linear_describe")
         self.rows, self.n, self.k, self.training = int(rows), int(n), int(k), bool(training)
-        self.dtype, self.out_dtype = IO_TORCH[io_dtype], IO_TORCH[out_dtype]
+        self.dtype, self.out_dtype, self.pre_dtype = IO_TORCH[io_dtype], IO_TORCH[out_dtype], IO_TORCH[pre_dtype]
         self.bytes, self.pre_bytes, self.pre_stride = out.workspace_bytes, out.pre_bytes, out.pre_stride
         with torch.cuda.device(dev), torch.cuda.stream(stream) if stream is not None else nullcontext():
             self._allocate(self.bytes, dev)
@@ -56,7 +57,7 @@ class LinearWorkspace(_Memory):
             raise ValueError("a kept pre-activation belongs to a training workspace")
         if not self.pre_bytes:
             return None
-        return torch.empty(self.rows, self.pre_stride, dtype=self.dtype, device=self.device)[:, :self.n]
+        return torch.empty(self.rows, self.pre_stride, dtype=self.pre_dtype, device=self.device)[:, :self.n]
 
     def status(self, stream: Optional[torch.cuda.Stream] = None) -> int:
         """Status bits (ST_LINEAR_TIMEOUT); synchronises the stream."""
@@ -81,7 +82,7 @@ class LinearWorkspace(_Memory):
             return None, 0
         if pre is None:
             raise TypeError("pre must be a buffer of LinearWorkspace.new_pre()")
-        stride = _rows(pre, self.dtype, "pre", self.gpu)
+        stride = _rows(pre, self.pre_dtype, "pre", self.gpu)
         if pre.shape[1] != self.n or pre.shape[0] < rows or (stride != self.pre_stride and pre.shape[0] > 1):
             raise ValueError("pre must be a buffer of LinearWorkspace.new_pre()")
         room = pre.untyped_storage().nbytes() - pre.storage_offset() * pre.element_size()

@@ -4,7 +4,8 @@ Linear.  U is the largest relative error of one rounding to the 16-bit type (hal
 fp32; the tensor core adds them sixteen at a time, each addition off by at most 2^-22 of the partial sum, and the partial sums of terms t
 with random signs stay below 3 sqrt(sum t^2):  |dP| <= B(P) = 3 (K / 16 + 2) 2^-22 sqrt(sum t^2).
     y       1.13 B(P) (the largest slope) + 2^-19 (|act| + 1) (its evaluation) + one rounding of y
-    dP      is rounded (U |dP|) and its slope is taken at a rounded P: |act''| <= 1.2, so E = U |dP| + 1.2 |dy| (U |P| + B(P))
+    dP      is rounded (U |dP|, or U^2 |dP| where grad_w is fp32) and its slope is taken at a P rounded to pre's type (U_P):
+            |act''| <= 1.2, so E = U |dP| + 1.2 |dy| (U_P |P| + B(P)) + 2^-19 |dy| (the slope's evaluation)
     grad_x, grad_w: sums of many terms with independent errors of at most E |w| (E |x|): 6 sqrt(sum of squares), plus the sum's own error B
             and one rounding.    grad_bias sums the unrounded dP: E without U |dP|, additions off by 2^-24 of partial sums below 3 sqrt(sum dP^2)
 relu's slope jumps at 0, where P's own error decides the side: there |dP| <= |dy| is off by as much, so E = |dy| where |P| <= B(P).
@@ -25,7 +26,7 @@ def one_rounding(v, dtype):
     return (U[dtype] * v.abs()).clamp(min=torch.finfo(dtype).smallest_normal * U[dtype])
 
 
-def linear_reference(x, w, bias, residual, act, out_dtype, grad_y=None, grad_w_dtype=None, grad_bias_dtype=None):
+def linear_reference(x, w, bias, residual, act, out_dtype, grad_y=None, grad_w_dtype=None, grad_bias_dtype=None, pre_dtype=torch.float32):
     """{name: (value, error bound)} in 64 bits"""
     u = U[x.dtype]
     x64, w64 = x.double(), w.double()
@@ -48,14 +49,15 @@ def linear_reference(x, w, bias, residual, act, out_dtype, grad_y=None, grad_w_d
     gy = grad_y.double()
     (slope,) = torch.autograd.grad(a.sum(), leaf) if act != "none" else (torch.ones_like(p),)
     gp = gy * slope
-    off = torch.zeros_like(gp) if act == "none" else 1.2 * gy.abs() * (u * p.abs() + bp) + 2.0 ** -19 * gy.abs()
+    off = torch.zeros_like(gp) if act == "none" else 1.2 * gy.abs() * (U[pre_dtype] * p.abs() + bp) + 2.0 ** -19 * gy.abs()
     if act == "relu":
         off = torch.where(p.abs() <= bp, gy.abs(), torch.zeros_like(gp))
     e = off + u * gp.abs()
+    wide = off + (u * u if grad_w_dtype == torch.float32 else u) * gp.abs()  # the remainder of the rounding is rounded in its turn
     gx, bx = sums(gp, w64, n)
     out["grad_x"] = (gx, 6 * (e ** 2 @ w64 ** 2).sqrt() + bx + one_rounding(gx, x.dtype))
     gw, bw = sums(gp.t(), x64, rows)
-    out["grad_w"] = (gw, 6 * ((e ** 2).t() @ x64 ** 2).sqrt() + bw + one_rounding(gw, grad_w_dtype or x.dtype))
+    out["grad_w"] = (gw, 6 * ((wide ** 2).t() @ x64 ** 2).sqrt() + bw + one_rounding(gw, grad_w_dtype or x.dtype))
     if bias is not None:
         gb = gp.sum(0)
         out["grad_bias"] = (gb, 6 * (off ** 2).sum(0).sqrt() + 3 * (rows + 2) * 2.0 ** -24 * (gp ** 2).sum(0).sqrt()

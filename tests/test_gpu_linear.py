@@ -17,7 +17,7 @@ def strided(rows, cols, dtype, extra, gen, scale=1.0):
 
 
 def run(rows, n, k, dtype="bf16", act="none", bias=None, residual=False, out="same", backward=False, grad_w="same", extra=0, seed=0, ws_rows=None,
-        in_place=False):
+        in_place=False, pre_dtype=torch.float32):
     gen = torch.Generator(device="cuda").manual_seed(seed)
     dt = DT[dtype]
     odt = dt if out == "same" else DT[out]
@@ -29,7 +29,8 @@ def run(rows, n, k, dtype="bf16", act="none", bias=None, residual=False, out="sa
     r_in = res.clone() if residual else None
     if in_place:
         y = res
-    ws = L.LinearWorkspace(ws_rows or rows, n, k, activation=L.ACTIVATIONS[act], io_dtype=L.IO_OF[dt], out_dtype=L.IO_OF[odt], training=backward)
+    ws = L.LinearWorkspace(ws_rows or rows, n, k, activation=L.ACTIVATIONS[act], io_dtype=L.IO_OF[dt], out_dtype=L.IO_OF[odt], training=backward,
+                           pre_dtype=L.IO_OF[pre_dtype])
     pre = ws.new_pre() if backward else None
     y_base = y._base if y._base is not None else y
     gap = y_base[:, n:].clone()
@@ -45,7 +46,7 @@ def run(rows, n, k, dtype="bf16", act="none", bias=None, residual=False, out="sa
         L.lapsum_linear_backward(gy, x, w, pre, got["grad_x"], got["grad_w"], got.get("grad_bias"), ws)
     assert ws.status() == 0
     assert torch.equal(torch.isnan(y_base[:, n:]), torch.isnan(gap))  # what lies between the rows stays as it was
-    ref = linear_reference(x, w, b, r_in, act, odt, gy, got["grad_w"].dtype if backward else None, b.dtype if b is not None else None)
+    ref = linear_reference(x, w, b, r_in, act, odt, gy, got["grad_w"].dtype if backward else None, b.dtype if b is not None else None, pre_dtype)
     for name, t in got.items():
         value, bound = ref[name]
         err = (t.double() - value).abs()
@@ -89,6 +90,27 @@ def test_fewer_rows_than_the_workspace_and_the_residual_in_place():
     run(100, 264, 136, ws_rows=512, residual=True, in_place=True)
     run(3, 264, 136, ws_rows=512, act="silu", bias="same", backward=True)
     run(70, 264, 136, ws_rows=512, act="silu", bias="same", backward=True)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu_tanh"])
+def test_a_pre_activation_kept_in_16_bits(act):
+    run(200, 515, 136, act=act, bias="same", backward=True, grad_w="f32", pre_dtype=torch.bfloat16)
+    run(3, 40, 136, act=act, bias="f32", backward=True, pre_dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("rows,n,k", [(1000, 136, 16384), (20000, 264, 256)])
+def test_fp32_results_keep_fp32_digits_over_a_long_contraction(rows, n, k):
+    """in the 2-norm: the rounds of 512 keep the truncated additions' error below 32 x 2^-25, with dW's rounding remainder 2^-18"""
+    got = run(rows, n, k, act="silu", bias="f32", out="f32", backward=True, grad_w="f32")
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x = strided(rows, k, torch.bfloat16, 0, gen)
+    w = (torch.randn(n, k, device="cuda", generator=gen) * k ** -0.5).bfloat16()
+    b = 0.3 * torch.randn(n, device="cuda", generator=gen)
+    strided(rows, n, torch.float32, 0, gen)
+    ref = linear_reference(x, w, b, None, "silu", torch.float32, strided(rows, n, torch.float32, 0, gen))
+    for name in ("y", "grad_w", "grad_bias"):
+        value = ref[name][0]
+        assert (got[name].double() - value).norm() <= 2.0 ** -17 * value.norm(), name
 
 
 def test_no_rows():
@@ -153,7 +175,7 @@ def test_infinite_and_nan_inputs_reach_their_own_rows_alone():
     gen = torch.Generator(device="cuda").manual_seed(1)
     x = torch.randn(rows, k, device="cuda", generator=gen).half()
     w = (torch.randn(n, k, device="cuda", generator=gen) / 8).half()
-    ws = L.LinearWorkspace(rows, n, k, activation=L.ACT_GELU_TANH, io_dtype=L.IO_F16, training=True)
+    ws = L.LinearWorkspace(rows, n, k, activation=L.ACT_GELU_TANH, io_dtype=L.IO_F16, training=True, pre_dtype=L.IO_F16)
     clean, y = torch.empty(rows, n, device="cuda", dtype=torch.float16), torch.empty(rows, n, device="cuda", dtype=torch.float16)
     pre = ws.new_pre()
     L.lapsum_linear_forward(x, w, None, None, clean, ws, pre=pre)
