@@ -14,31 +14,65 @@ using namespace lapsum;
 namespace {
 
 // ------------------------------------------------------------------ sample ----
-constexpr int SAMPLE_BLOCK_BYTES = 64 << 10, SAMPLE_MOST_BYTES = 190 << 10;
+constexpr int SAMPLE_BLOCK_BYTES = 64 << 10, SMEM_MOST = 226 << 10;
 
-// Blocks per row: as many as keep a block's run at 64 KB (two blocks per SM), and more, down to runs of 4096 tokens, while the rows
-// leave SMs without work.
-template <typename T>
-int sample_t(SampleArgs A, int64_t rows, cudaStream_t st)
+// Clusters of a kernel that the device holds at once; more would wait for a whole turn of the others.  The answer is kept for the last question.
+template <typename K>
+int clusters_at_once(K kernel, int cluster, int threads, size_t smem, int dev, int *out)
 {
-    int sms = 0, dev = 0;
-    RUN(sm_count(&sms));
-    int cluster = 1;
-    while (cluster < 8 && ((int64_t)A.vocab * (int)sizeof(T) > (int64_t)cluster * SAMPLE_BLOCK_BYTES ||
-                           (rows * cluster < 2 * sms && A.vocab >= 2 * 4096 * cluster)))
-        cluster *= 2;
+    static thread_local int last[3] = {-1, -1, -1}, answer = 0;
+    if (last[0] != dev || last[1] != cluster || last[2] != (int)smem) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(cluster * 1024));
+        cfg.blockDim = dim3((unsigned)threads);
+        cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)cluster;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        CU_OK(cudaOccupancyMaxActiveClusters(&answer, kernel, &cfg));
+        if (answer < 1) answer = 1;
+        last[0] = dev, last[1] = cluster, last[2] = (int)smem;
+    }
+    *out = answer;
+    return LAPSUM_OK;
+}
+
+template <typename T, int THREADS>
+int sample_launch(SampleArgs &A, int cluster, cudaStream_t st)
+{
+    constexpr int FIXED = (int)sizeof(SampleShared<THREADS>);
     A.cluster = cluster;
     A.chunk = (int)(ceil_div(ceil_div(A.vocab, cluster), 128) * 128);
     const size_t run = (size_t)A.chunk * sizeof(T);
-    A.resident = run <= SAMPLE_MOST_BYTES;
-    const size_t smem = sizeof(SampleShared) + (A.resident ? run : 0);
+    A.resident = run + FIXED <= SMEM_MOST;
+    const size_t smem = FIXED + (A.resident ? run : 0);
     static thread_local int dev_ready = -1;  // the attribute belongs to the device's context
+    int dev = 0, fit = 0;
     CU_OK(cudaGetDevice(&dev));
     if (dev != dev_ready) {
-        CU_OK(cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SampleShared) + SAMPLE_MOST_BYTES));
+        CU_OK(cudaFuncSetAttribute(sample_kernel<T, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST));
         dev_ready = dev;
     }
-    return launch_clusters((unsigned)cluster, sample_kernel<T>, (unsigned)(rows * cluster), SAMPLE_THREADS, smem, st, A);
+    RUN(clusters_at_once(sample_kernel<T, THREADS>, cluster, THREADS, smem, dev, &fit));
+    const int64_t clusters = A.rows < fit ? A.rows : fit;
+    return launch_clusters((unsigned)cluster, sample_kernel<T, THREADS>, (unsigned)(clusters * cluster), THREADS, smem, st, A);
+}
+// A block per row where the rows occupy two thirds of the SMs; otherwise blocks as many as keep a block's run at 64 KB (two blocks per SM), and more, down
+// to runs of 4096 tokens, while SMs are without work.
+template <typename T>
+int sample_t(SampleArgs A, cudaStream_t st)
+{
+    int sms = 0;
+    RUN(sm_count(&sms));
+    if (3 * A.rows >= 2 * sms) return sample_launch<T, 1024>(A, 1, st);
+    int cluster = 1;
+    while (cluster < 8 && ((int64_t)A.vocab * (int)sizeof(T) > (int64_t)cluster * SAMPLE_BLOCK_BYTES ||
+                           (A.rows * cluster < 2 * sms && A.vocab >= 2 * 4096 * cluster)))
+        cluster *= 2;
+    return sample_launch<T, 512>(A, cluster, st);
 }
 
 // ------------------------------------------------------------------- embed ----
@@ -127,14 +161,14 @@ int lapsum_sample(const void *logits, int64_t rows, int64_t vocab, int64_t strid
     if (!logits || !u || !token) return LAPSUM_ERR_NULL;
     SampleArgs A;
     std::memset(&A, 0, sizeof(A));
-    A.logits = logits, A.stride = stride, A.u = u;
+    A.logits = logits, A.stride = stride, A.rows = rows, A.u = u;
     A.temperature_row = temperature, A.top_k_row = top_k, A.top_p_row = top_p, A.min_p_row = min_p;
     A.temperature = prm->temperature, A.top_p = prm->top_p, A.min_p = prm->min_p, A.top_k = prm->top_k;
     A.token = token, A.logprob = logprob, A.kept = kept;
     A.vocab = (int)vocab;
     A.bits = 45;
     while (A.bits > 0 && vocab > (int64_t)1 << (62 - A.bits)) --A.bits;
-    return BY_TYPE(sample_t, prm->io_dtype, A, rows, static_cast<cudaStream_t>(stream));
+    return BY_TYPE(sample_t, prm->io_dtype, A, static_cast<cudaStream_t>(stream));
 }
 
 int lapsum_embed_forward(const void *ids, int32_t id_bytes, int64_t tokens, const void *table, int64_t table_stride, int64_t vocab, int64_t d,
