@@ -4,9 +4,13 @@
 //   kept: the first min(top_k, #{e_i >= min_p}) of the rank, and of those the least number whose sum reaches top_p of theirs
 //   token: the first i, by index, at which the kept e sum to more than u times the sum of all kept
 //
-// A few rows: a cluster of up to 8 blocks of 512 threads has one; each block brings its run of the row into shared memory once, every later pass reads
-// it there.  A row for every SM: one block of 1024 threads has one, and what does not fit into shared memory is read again, from L2: cluster
-// barriers and loads from other blocks' memory take 2000 clocks and more, so with clusters 256 rows of 128000 took 157 us.
+// A cluster of up to 8 blocks of 512 threads has one row; each block brings its run of the row into shared memory once, every later pass reads it there.
+// Or, for many long rows without top-p, one block of 1024 threads has one and reads it again, from L2: no cluster barriers and no loads from other
+// blocks' memory, which take 2000 clocks and more.
+//
+// What bounds it.  One row (50021 tokens, 15 us with the call): a chain of three to nine cluster barriers and the fetch of code that runs once.
+// 256 x 128000 (131 MB, 20 us by its bytes): without filters 109 us, the exponentials, 9 operations in 64 bits and some 14 others per token, of which an SM
+// does 2.6 tokens a clock; with top-k, where only listed tokens are weighed, 82 us; rows of all kinds 193 us.
 //
 // Weights are integers, e_i 2^S rounded (S = 45 up to 2^17 tokens), from an exponential in 64 bits: their sums are exact in any order, so the
 // result depends neither on the cluster nor on atomics, and it is the definition's unless u or top_p falls within about 2^-37 of a border.
@@ -34,7 +38,7 @@ namespace lapsum {
 
 struct SampleArgs {
     const void *logits;
-    int64_t stride, rows;
+    int64_t stride;
     const float *u, *temperature_row, *top_p_row, *min_p_row;  // the last three may be null: one value for all rows
     const int32_t *top_k_row;
     double temperature, top_p, min_p;
@@ -42,7 +46,7 @@ struct SampleArgs {
     int32_t *token, *kept;  // kept and logprob may be null
     float *logprob;
     int vocab, chunk;  // chunk: tokens of a block, a multiple of 128
-    int cluster, resident;
+    int cluster;
     int bits;  // S
 };
 
@@ -52,14 +56,14 @@ constexpr int SAMPLE_SHORT_K = 96;
 
 template <int THREADS>
 struct alignas(16) SampleShared {
-    static constexpr int NEAR = THREADS == 1024 ? 32768 : 6144;  // tokens of the near list
-    double power[512];  // 2^(j / 512 + S)
+    static constexpr int NEAR = THREADS == 1024 ? 1024 : 128;  // tokens of a warp's near list: with 64 KB of the row two blocks of 512 threads fit an SM
+    double power[64 * 16];  // 2^(j / 64 + S), sixteen of each: a lane reads its own, so that no two meet in a bank
     unsigned long long mass[SAMPLE_BUCKETS];
     uint32_t count[SAMPLE_BUCKETS];
     unsigned long long slice_mass[SAMPLE_BUCKETS];  // this block's share of the buckets, summed over the cluster
     uint32_t slice_count[SAMPLE_BUCKETS];
     unsigned long long list[SAMPLE_LIST], sorted[SAMPLE_LIST];
-    uint32_t near[NEAR];  // where in this block's run the tokens from a bound on are, for top-p
+    uint32_t near[THREADS / 32][NEAR], near_of[THREADS / 32];  // where in this block's run the tokens from a bound on are, for top-p
     uint32_t groups[SAMPLE_GROUPS], ranked[SAMPLE_GROUPS];  // this block's groups' largest keys; those of all blocks, largest first
     unsigned long long warp_mass[THREADS / 32];
     uint32_t warp_count[THREADS / 32];
@@ -70,7 +74,7 @@ struct alignas(16) SampleShared {
     int index;
     // results of one block's search, for its own threads
     unsigned long long above;
-    uint32_t bucket, members, near_count;
+    uint32_t bucket, members;
     unsigned long long cut;
 };
 
@@ -115,7 +119,7 @@ __device__ __forceinline__ void far_all(const uint32_t *p, int cluster, uint32_t
 }
 
 // One row as one block sees it
-template <typename T, int THREADS>
+template <typename T, int THREADS, bool RESIDENT>
 struct SampleRow {
     static constexpr int V = Io<T>::V, WARPS = THREADS / 32;
     const SampleArgs &P;
@@ -126,16 +130,16 @@ struct SampleRow {
     uint32_t rank, home;     // home: the block that holds the row's list and finishes it
     int tid, lane, warp;
     float top;               // the largest logit
-    double factor;           // 512 log2(e) / T
+    double factor;           // 64 log2(e) / T
     float none_x;            // logits up to here weigh less than half of the last digit: nothing
     float cut_x;             // kept: x > cut_x, or x == cut_x and index <= cut_i
     int cut_i;
 
     // A NaN passes no comparison, so it is never kept.
-    __device__ __forceinline__ float at(int i) const { return P.resident ? Io<T>::from_storage(mine[i]) : Io<T>::from_storage(ld(row + begin + i)); }
+    __device__ __forceinline__ float at(int i) const { return RESIDENT ? Io<T>::from_storage(mine[i]) : Io<T>::from_storage(ld(row + begin + i)); }
     __device__ __forceinline__ void get(int i, float (&x)[V]) const  // V tokens from position i of the run on; -inf beyond the row
     {
-        if (P.resident) {
+        if constexpr (RESIDENT) {
             Io<T>::unpack(*reinterpret_cast<const typename Io<T>::Vec *>(mine + i), x);
         } else if (whole && i + V <= len) {
             Io<T>::unpack(ld(reinterpret_cast<const typename Io<T>::Vec *>(row + begin + i)), x);
@@ -144,10 +148,40 @@ struct SampleRow {
             for (int j = 0; j < V; ++j) x[j] = i + j < len ? Io<T>::from_storage(ld(row + begin + i + j)) : -CUDART_INF_F;
         }
     }
-    __device__ __forceinline__ float largest_at(int i) const  // of V tokens
+    // f(x, i) for vectors from position b on, one per lane, up to b1: Q loads at once where a warp's are all whole.  All lanes call f, with -inf beyond b1.
+    template <int Q, typename F>
+    __device__ __forceinline__ void stream(int b, int b1, int step, F f) const
     {
-        float x[V];
-        get(i, x);
+        for (; b < b1; b += Q * step) {
+            const int end = b + (Q - 1) * step + 32 * V, i = b + lane * V;
+            if (RESIDENT ? end <= b1 : whole && end <= min(b1, len)) {
+                typename Io<T>::Vec q[Q];
+                const typename Io<T>::Vec *const from = reinterpret_cast<const typename Io<T>::Vec *>((RESIDENT ? mine : row + begin) + i);
+#pragma unroll
+                for (int j = 0; j < Q; ++j) q[j] = ld(from + j * (step / V));
+#pragma unroll
+                for (int j = 0; j < Q; ++j) {
+                    float x[V];
+                    Io<T>::unpack(q[j], x);
+                    f(x, i + j * step);
+                }
+            } else {
+#pragma unroll 1
+                for (int j = 0; j < Q; ++j) {
+                    float x[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) x[v] = -CUDART_INF_F;
+                    if (i + j * step < b1) get(i + j * step, x);
+                    __syncwarp();
+                    f(x, i + j * step);
+                }
+            }
+        }
+    }
+    template <int Q, typename F>
+    __device__ __forceinline__ void stream_all(F f) const { stream<Q>(warp * 32 * V, padded, THREADS * V, f); }
+    __device__ __forceinline__ static float largest(const float (&x)[V])
+    {
         float m = x[0];
 #pragma unroll
         for (int j = 1; j < V; ++j) m = fmaxf(m, x[j]);
@@ -160,21 +194,23 @@ struct SampleRow {
         const int b = __float_as_int(x);
         return __hiloint2double(((b >> 3) & 0x8fffffff) + 0x38000000, b << 29);
     }
-    // 2^52 + e^((x - top) / T) 2^S, rounded, for an x from none_x on: exponent and one of 512 fractions by table, the rest by a polynomial (P. T. P. Tang,
-    // Table-driven implementation of the exponential function, 1989).  The remainder is below ln 2 / 1024, so four terms leave 2^-46 of the
-    // weight, the same way for all.  Eight operations in 64 bits and as many others; a library exponential and its conversions took 45.
+    // 2^52 + e^((x - top) / T) 2^S, rounded, for an x from none_x on: exponent and one of 64 fractions by table, the rest by a polynomial (P. T. P. Tang,
+    // Table-driven implementation of the exponential function, 1989).  The remainder is below ln 2 / 128, so five terms leave 2^-44 of the
+    // weight at its ends.  Nine operations in 64 bits and a dozen others; a library exponential and its conversions took 45 in all.  (512 fractions, read from
+    // one copy, save one of the nine, but their bank conflicts took as long as all the rest: 50000 clocks for 128000 tokens on one SM.)
     __device__ __forceinline__ unsigned long long raised(float x) const
     {
         const double d = widened(x) - widened(top);
         const double shifted = fma(d, factor, 6755399441055744.0);  // 1.5 2^52: rounds to whole numbers
         const int n = __double2loint(shifted);
         const double f = fma(d, factor, 6755399441055744.0 - shifted);
-        constexpr double C = 0.69314718055994530942 / 512;
-        double p = fma(f, C * C * C / 6, C * C / 2);
+        constexpr double C = 0.69314718055994530942 / 64;
+        double p = fma(f, C * C * C * C / 24, C * C * C / 6);
+        p = fma(f, p, C * C / 2);
         p = fma(f, p, C);
         p = fma(f, p, 1.0);
-        const double t = S.power[n & 511];
-        const double scale = __hiloint2double(__double2hiint(t) + (int)((uint32_t)(n & ~511) << 11), __double2loint(t));
+        const double t = S.power[(n & 63) * 16 + (lane & 15)];
+        const double scale = __hiloint2double(__double2hiint(t) + (int)((uint32_t)(n & ~63) << 14), __double2loint(t));
         return (unsigned long long)__double_as_longlong(fma(scale, p, 4503599627370496.0));
     }
     static constexpr unsigned long long RAISED = 0x433ull << 52;  // 2^52
@@ -203,10 +239,8 @@ struct SampleRow {
     // V tokens from position i of the run on: their sum (v: each), and in n how many are kept.  A token that weighs nothing is taken at none_x, where the
     // rounding leaves 0; what the raised weights have too much goes off at the end.
     template <bool ONES>
-    __device__ __forceinline__ unsigned long long values(float value, int i, uint32_t &n, unsigned long long (&v)[V]) const
+    __device__ __forceinline__ unsigned long long values(float value, const float (&x)[V], int i, uint32_t &n, unsigned long long (&v)[V]) const
     {
-        float x[V];
-        get(i, x);
         unsigned long long sum = 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) v[j] = 0;
@@ -214,10 +248,7 @@ struct SampleRow {
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] = x[j] == value, sum += v[j];
         } else {
-            float most = x[0];
-#pragma unroll
-            for (int j = 1; j < V; ++j) most = fmaxf(most, x[j]);
-            if (most >= cut_x) {
+            if (largest(x) >= cut_x) {
                 uint32_t m = 0;
                 if (cut_i == INT_MAX) {
 #pragma unroll
@@ -255,7 +286,7 @@ struct SampleRow {
         uint32_t n = 0;
         {
             const Span span = run_of(warp);
-            for (int i = span.i0 + lane * V; i < span.i1; i += 32 * V) sum += values<ONES>(value, i, n, v);
+            stream<2>(span.i0, span.i1, 32 * V, [&](const float (&x)[V], int i) { sum += values<ONES>(value, x, i, n, v); });
         }
         __syncwarp();
         sum = warp_sum(sum);
@@ -285,7 +316,13 @@ struct SampleRow {
             for (int base = span.i0; base < span.i1; base += THREADS * V) {
                 const int i = base + tid * V;
                 unsigned long long s = 0;
-                if (i < span.i1) s = values<ONES>(value, i, n, v);
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] = 0;
+                if (i < span.i1) {
+                    float x[V];
+                    get(i, x);
+                    s = values<ONES>(value, x, i, n, v);
+                }
                 __syncwarp();
                 unsigned long long run = warp_scan(s, lane);
                 __syncthreads();
@@ -351,19 +388,13 @@ struct SampleRow {
         };
         bool room = true;
         if (near) {
-            for (int i = tid; i < (int)S.near_count && room; i += THREADS) room = take((int)S.near[i]);
+            for (int i = lane; i < (int)S.near_of[warp] && room; i += 32) room = take((int)S.near[warp][i]);
         } else {
-            for (int i0 = tid * V; i0 < padded && room; i0 += 4 * THREADS * V) {
-                float m[4];  // four loads at once
-#pragma unroll
-                for (int q = 0; q < 4; ++q) m[q] = i0 + q * THREADS * V < padded ? largest_at(i0 + q * THREADS * V) : -CUDART_INF_F;
+            stream_all<4>([&](const float (&x)[V], int i0) {
+                if (room && largest(x) >= which.low)
 #pragma unroll 1
-                for (int q = 0; q < 4; ++q) {
-                    if (m[0] >= which.low)
-                        for (int i = i0 + q * THREADS * V; i < min(i0 + q * THREADS * V + V, len) && room; ++i) room = take(i);
-                    m[0] = m[1], m[1] = m[2], m[2] = m[3];
-                }
-            }
+                    for (int i = i0; i < min(i0 + V, len) && room; ++i) room = take(i);
+            });
         }
         __syncwarp();
     }
@@ -410,9 +441,10 @@ struct SampleRow {
     {
         for (int i = tid; i < SAMPLE_BUCKETS; i += THREADS) S.count[i] = 0, S.mass[i] = 0;
         __syncthreads();
-        const int n = near ? (int)S.near_count : len;
-        for (int i = tid; i < n; i += THREADS) {
-            const float x = at(near ? (int)S.near[i] : i);
+        const int n = near ? (int)S.near_of[warp] : len;
+#pragma unroll 2
+        for (int i = near ? lane : tid; i < n; i += near ? 32 : THREADS) {
+            const float x = at(near ? (int)S.near[warp][i] : i);
             if (!(x >= which.low)) continue;
             uint32_t b;
             if (which.shift < 0) {
@@ -429,6 +461,7 @@ struct SampleRow {
             }
             atomicAdd(&S.count[b], 1u);
         }
+        __syncwarp();
     }
     // The first bucket at which the cluster's counts (or weights) from the largest on reach the goal, into S.bucket, .members and .above; false: they
     // never do.
@@ -494,32 +527,20 @@ struct SampleRow {
     // `near` <- where this block's tokens from `low` on are, so that weights, which cost much for a token here and there, are computed densely
     __device__ __forceinline__ bool bring_near(float low) const
     {
-        if (tid == 0) S.near_count = 0;
-        __syncthreads();
+        uint32_t to = 0;  // a list for every warp, of its own tokens
         const unsigned lower = (1u << lane) - 1;
-        for (int i0 = 0; i0 < padded; i0 += THREADS * V) {  // all lanes alike
-            const int i = i0 + tid * V;
-            float x[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = -CUDART_INF_F;
-            if (i < padded) get(i, x);
-            unsigned who[V];
-            uint32_t count = 0;
-#pragma unroll
-            for (int j = 0; j < V; ++j) who[j] = __ballot_sync(FULL, x[j] >= low), count += __popc(who[j]);
-            if (count == 0) continue;
-            uint32_t to = 0;
-            if (lane == 0) to = atomicAdd(&S.near_count, count);
-            to = __shfl_sync(FULL, to, 0);
+        stream_all<4>([&](const float (&x)[V], int i) {
+            if (!__any_sync(FULL, largest(x) >= low)) return;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const uint32_t at_ = to + __popc(who[j] & lower);
-                if (x[j] >= low && at_ < SampleShared<THREADS>::NEAR) S.near[at_] = (uint32_t)(i + j);
-                to += __popc(who[j]);
+                const unsigned who = __ballot_sync(FULL, x[j] >= low);
+                const uint32_t at_ = to + __popc(who & lower);
+                if (x[j] >= low && at_ < SampleShared<THREADS>::NEAR) S.near[warp][at_] = (uint32_t)(i + j);
+                to += __popc(who);
             }
-        }
-        __syncthreads();
-        return S.near_count <= SampleShared<THREADS>::NEAR;
+        });
+        if (lane == 0) S.near_of[warp] = to;
+        return !__syncthreads_or(to > SampleShared<THREADS>::NEAR);
     }
 
     // (cut_x, cut_i) <- the token of the rank at which the counts (or weights) of the tokens from `low` on reach the goal
@@ -704,7 +725,7 @@ struct SampleRow {
     {
         // the run, and its largest logit
         float most = -CUDART_INF_F;
-        if (P.resident) {
+        if constexpr (RESIDENT) {
             T *const to = const_cast<T *>(mine);
             const T *const from = row + begin;
             int done = 0;
@@ -733,12 +754,7 @@ struct SampleRow {
                 most = fmaxf(most, x);
             }
         } else {
-            for (int i = tid * V; i < padded; i += 4 * THREADS * V) {
-                float m[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) m[q] = i + q * THREADS * V < padded ? largest_at(i + q * THREADS * V) : -CUDART_INF_F;
-                most = fmaxf(fmaxf(fmaxf(most, m[0]), fmaxf(m[1], m[2])), m[3]);
-            }
+            stream_all<4>([&](const float (&x)[V], int) { most = fmaxf(most, largest(x)); });
         }
         __syncwarp();
         uint32_t key = key_of(most), group = key;
@@ -779,11 +795,11 @@ struct SampleRow {
             wait();
             return;
         }
-        factor = 512 * 1.4426950408889634074 / T_;
+        factor = 64 * 1.4426950408889634074 / T_;
         constexpr float LOWEST = -3.402823466e38f;
         none_x = fmaxf(fminf(__double2float_rd((double)top - T_ * 0.69314718055994530942 * (P.bits + 2)), nextafterf(top, -CUDART_INF_F)), LOWEST);
         // where the next logit below already weighs nothing, it is put where the exponent still has room
-        if (none_x == nextafterf(top, -CUDART_INF_F)) factor = fmin(factor, 512.0 * (P.bits + 4) / ((double)top - (double)none_x));
+        if (none_x == nextafterf(top, -CUDART_INF_F)) factor = fmin(factor, 64.0 * (P.bits + 4) / ((double)top - (double)none_x));
         cut_x = LOWEST, cut_i = INT_MAX;
         if (m > 0) {  // the least x with (top - x) / T <= -log(min_p)
             const double far = -log(m), inv = 1.0 / T_;
@@ -854,26 +870,28 @@ struct SampleRow {
     }
 };
 
-// Clusters as many as fit at once walk over the rows, so a block that has done its part of a row loads the next one while another finishes.
-template <typename T, int THREADS>
+template <typename T, int THREADS, bool RESIDENT>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const SampleArgs P)
 {
     extern __shared__ __align__(16) uint8_t raw[];
     SampleShared<THREADS> &S = *reinterpret_cast<SampleShared<THREADS> *>(raw);
-    static_assert(THREADS >= SAMPLE_LIST && THREADS >= SAMPLE_GROUPS, "a thread per item");
-    if (threadIdx.x < 512) S.power[threadIdx.x] = exp2((double)threadIdx.x / 512 + P.bits);
+    static_assert(THREADS >= SAMPLE_LIST && THREADS >= SAMPLE_GROUPS && THREADS % 64 == 0, "a thread per item");
+    {
+        const double power = exp2((double)(threadIdx.x & 63) / 64 + P.bits);
+#pragma unroll
+        for (int i = (int)threadIdx.x >> 6; i < 16; i += THREADS / 64) S.power[(threadIdx.x & 63) * 16 + i] = power;
+    }
+    if (threadIdx.x == 0) S.list_count = 0, S.key_max = 0;
     pdl_wait();
+    __syncthreads();
     const uint32_t rank = P.cluster > 1 ? cluster_rank() : 0;
     const int begin = min((int)rank * P.chunk, P.vocab), len = min(P.chunk, P.vocab - begin);
-    for (int64_t r = blockIdx.x / P.cluster; r < P.rows; r += gridDim.x / P.cluster) {
-        if (threadIdx.x == 0) S.list_count = 0, S.key_max = 0;  // the last row's readers are through
-        __syncthreads();
-        const T *const row = static_cast<const T *>(P.logits) + r * P.stride;
-        SampleRow<T, THREADS> s{P, S, row, reinterpret_cast<const T *>(raw + sizeof(S)), begin, len, (len + Io<T>::V - 1) / Io<T>::V * Io<T>::V,
-                                (reinterpret_cast<uintptr_t>(row + begin) & 15) == 0, rank, (uint32_t)(r % P.cluster), (int)threadIdx.x,
-                                (int)threadIdx.x & 31, (int)threadIdx.x >> 5};
-        s.run(r);
-    }
+    const int64_t r = blockIdx.x / P.cluster;
+    const T *const row = static_cast<const T *>(P.logits) + r * P.stride;
+    SampleRow<T, THREADS, RESIDENT> s{P, S, row, reinterpret_cast<const T *>(raw + sizeof(S)), begin, len, (len + Io<T>::V - 1) / Io<T>::V * Io<T>::V,
+                                      (reinterpret_cast<uintptr_t>(row + begin) & 15) == 0, rank, (uint32_t)(r % P.cluster), (int)threadIdx.x,
+                                      (int)threadIdx.x & 31, (int)threadIdx.x >> 5};
+    s.run(r);
 }
 
 }  // namespace lapsum

@@ -16,63 +16,39 @@ namespace {
 // ------------------------------------------------------------------ sample ----
 constexpr int SAMPLE_BLOCK_BYTES = 64 << 10, SMEM_MOST = 226 << 10;
 
-// Clusters of a kernel that the device holds at once; more would wait for a whole turn of the others.  The answer is kept for the last question.
-template <typename K>
-int clusters_at_once(K kernel, int cluster, int threads, size_t smem, int dev, int *out)
+template <typename T, int THREADS, bool RESIDENT>
+int sample_launch(const SampleArgs &A, int64_t rows, cudaStream_t st)
 {
-    static thread_local int last[3] = {-1, -1, -1}, answer = 0;
-    if (last[0] != dev || last[1] != cluster || last[2] != (int)smem) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(cluster * 1024));
-        cfg.blockDim = dim3((unsigned)threads);
-        cfg.dynamicSmemBytes = smem;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)cluster;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        CU_OK(cudaOccupancyMaxActiveClusters(&answer, kernel, &cfg));
-        if (answer < 1) answer = 1;
-        last[0] = dev, last[1] = cluster, last[2] = (int)smem;
-    }
-    *out = answer;
-    return LAPSUM_OK;
-}
-
-template <typename T, int THREADS>
-int sample_launch(SampleArgs &A, int cluster, cudaStream_t st)
-{
-    constexpr int FIXED = (int)sizeof(SampleShared<THREADS>);
-    A.cluster = cluster;
-    A.chunk = (int)(ceil_div(ceil_div(A.vocab, cluster), 128) * 128);
-    const size_t run = (size_t)A.chunk * sizeof(T);
-    A.resident = run + FIXED <= SMEM_MOST;
-    const size_t smem = FIXED + (A.resident ? run : 0);
+    const auto kernel = sample_kernel<T, THREADS, RESIDENT>;
+    const size_t smem = sizeof(SampleShared<THREADS>) + (RESIDENT ? (size_t)A.chunk * sizeof(T) : 0);
     static thread_local int dev_ready = -1;  // the attribute belongs to the device's context
-    int dev = 0, fit = 0;
+    int dev = 0;
     CU_OK(cudaGetDevice(&dev));
     if (dev != dev_ready) {
-        CU_OK(cudaFuncSetAttribute(sample_kernel<T, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST));
+        CU_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST));
         dev_ready = dev;
     }
-    RUN(clusters_at_once(sample_kernel<T, THREADS>, cluster, THREADS, smem, dev, &fit));
-    const int64_t clusters = A.rows < fit ? A.rows : fit;
-    return launch_clusters((unsigned)cluster, sample_kernel<T, THREADS>, (unsigned)(clusters * cluster), THREADS, smem, st, A);
+    return launch_clusters((unsigned)A.cluster, kernel, (unsigned)(rows * A.cluster), THREADS, smem, st, A);
 }
-// A block per row where the rows occupy two thirds of the SMs; otherwise blocks as many as keep a block's run at 64 KB (two blocks per SM), and more, down
-// to runs of 4096 tokens, while SMs are without work.
+// Few rows, or a top-p that may have to look far: blocks as many as keep a block's run at 64 KB (two blocks per SM), and more, down to runs of 4096 tokens,
+// while SMs are without work.  Rows for two thirds of the SMs, long and without top-p: a block of 1024 threads each.  Measured at 256 x 128000 fp32, a block
+// each / clusters, us: no filter 109 / 121, top-k 40 82 / 111, top-p 0.9 over some 3000 tokens 366 / 424, rows of all kinds 324 / 193 (a single row of the
+// last kind takes 200 on one SM); 512 x 1000 75 / 36.
 template <typename T>
-int sample_t(SampleArgs A, cudaStream_t st)
+int sample_t(SampleArgs A, int64_t rows, cudaStream_t st)
 {
     int sms = 0;
     RUN(sm_count(&sms));
-    if (3 * A.rows >= 2 * sms) return sample_launch<T, 1024>(A, 1, st);
+    const bool many = 3 * rows >= 2 * sms && A.vocab >= 32768 && !A.top_p_row && A.top_p >= 1;
     int cluster = 1;
-    while (cluster < 8 && ((int64_t)A.vocab * (int)sizeof(T) > (int64_t)cluster * SAMPLE_BLOCK_BYTES ||
-                           (A.rows * cluster < 2 * sms && A.vocab >= 2 * 4096 * cluster)))
+    while (!many && cluster < 8 && ((int64_t)A.vocab * (int)sizeof(T) > (int64_t)cluster * SAMPLE_BLOCK_BYTES ||
+                           (rows * cluster < 2 * sms && A.vocab >= 2 * 4096 * cluster)))
         cluster *= 2;
-    return sample_launch<T, 512>(A, cluster, st);
+    A.cluster = cluster;
+    A.chunk = (int)(ceil_div(ceil_div(A.vocab, cluster), 128) * 128);
+    if (many) return sample_launch<T, 1024, false>(A, rows, st);
+    if ((size_t)A.chunk * sizeof(T) + sizeof(SampleShared<512>) <= SMEM_MOST) return sample_launch<T, 512, true>(A, rows, st);
+    return sample_launch<T, 512, false>(A, rows, st);
 }
 
 // ------------------------------------------------------------------- embed ----
@@ -161,14 +137,14 @@ int lapsum_sample(const void *logits, int64_t rows, int64_t vocab, int64_t strid
     if (!logits || !u || !token) return LAPSUM_ERR_NULL;
     SampleArgs A;
     std::memset(&A, 0, sizeof(A));
-    A.logits = logits, A.stride = stride, A.rows = rows, A.u = u;
+    A.logits = logits, A.stride = stride, A.u = u;
     A.temperature_row = temperature, A.top_k_row = top_k, A.top_p_row = top_p, A.min_p_row = min_p;
     A.temperature = prm->temperature, A.top_p = prm->top_p, A.min_p = prm->min_p, A.top_k = prm->top_k;
     A.token = token, A.logprob = logprob, A.kept = kept;
     A.vocab = (int)vocab;
     A.bits = 45;
     while (A.bits > 0 && vocab > (int64_t)1 << (62 - A.bits)) --A.bits;
-    return BY_TYPE(sample_t, prm->io_dtype, A, static_cast<cudaStream_t>(stream));
+    return BY_TYPE(sample_t, prm->io_dtype, A, rows, static_cast<cudaStream_t>(stream));
 }
 
 int lapsum_embed_forward(const void *ids, int32_t id_bytes, int64_t tokens, const void *table, int64_t table_stride, int64_t vocab, int64_t d,
