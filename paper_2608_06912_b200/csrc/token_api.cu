@@ -70,7 +70,7 @@ EmbedLayout embed_layout(int64_t tokens, int64_t vocab, int64_t d)
     X.off_start = at, at += align_up((size_t)(vocab + 1) * 4);
     X.off_order = at, at += align_up((size_t)tokens * 4);
     X.off_long = at, at += align_up((size_t)(tokens / EMBED_LONG + 1) * 4);
-    X.off_partial = at, at += align_up((size_t)ceil_div(tokens, EMBED_LONG) * 2 * (size_t)d * 4);
+    X.off_partial = at, at += align_up((size_t)ceil_div(tokens, EMBED_LONG) * 2 * (size_t)(ceil_div(d, 4) * 4) * 4);
     X.bytes = at;
     return X;
 }
@@ -94,17 +94,19 @@ int embed_backward_t(EmbedArgs A, cudaStream_t st)
     const bool vec = A.d % V == 0 && A.grad_stride % V == 0 && aligned(A.grad_out, 16) && aligned(A.grad, 16);
     const int64_t parts = vec ? embed_parts<T, true>(A.d) : embed_parts<T, false>(A.d);
     A.chunk_blocks = ceil_div(ceil_div(A.tokens, EMBED_LONG) * parts, 8);
-    const int64_t blocks = A.chunk_blocks + ceil_div(A.vocab * parts, 8);
+    const int64_t blocks = A.chunk_blocks + ceil_div(ceil_div(A.vocab, EMBED_ROWS) * parts, 8);
     if (blocks >= (int64_t)1 << 31) return LAPSUM_ERR_SHAPE;
     int sms = 0, dev = 0;
     RUN(sm_count(&sms));
     static thread_local int dev_ready = -1;  // the attribute belongs to the device's context
     CU_OK(cudaGetDevice(&dev));
     if (dev != dev_ready) {
-        CU_OK(cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        CU_OK(cudaFuncSetAttribute(embed_sort_kernel<int32_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        CU_OK(cudaFuncSetAttribute(embed_sort_kernel<int64_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
         dev_ready = dev;
     }
-    RUN(launch_pdl(embed_sort_kernel, (unsigned)ceil_div(A.vocab, EMBED_RANGE), 32 * EMBED_WARPS, smem, st, A));
+    RUN(launch_pdl(A.wide_ids ? embed_sort_kernel<int64_t> : embed_sort_kernel<int32_t>, (unsigned)ceil_div(A.vocab, EMBED_RANGE), 32 * EMBED_WARPS,
+                   smem, st, A));
     RUN(launch_pdl(vec ? embed_grad_kernel<T, true> : embed_grad_kernel<T, false>, (unsigned)blocks, 256, 0, st, A));
     if (A.tokens <= EMBED_LONG) return LAPSUM_OK;  // no row can be long
     return launch_pdl(embed_join_kernel<T>, (unsigned)(4 * sms), 256, 0, st, A);
@@ -191,6 +193,7 @@ int lapsum_embed_backward(const void *grad_out, int64_t grad_stride, const void 
     A.long_count = reinterpret_cast<uint32_t *>(at);
     A.row_start = reinterpret_cast<int32_t *>(at + X.off_start), A.order = reinterpret_cast<int32_t *>(at + X.off_order);
     A.long_rows = reinterpret_cast<int32_t *>(at + X.off_long), A.partial = reinterpret_cast<float *>(at + X.off_partial);
+    A.partial_stride = ceil_div(d, 4) * 4;
     return BY_TYPE(embed_backward_t, io_dtype, A, st);
 }
 
