@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
         if (lane == 0 && (!PAIR || rank == 0)) {
             constexpr uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
             constexpr uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | ((A_MN ? 1u : 0u) << 15) | ((B_MN ? 1u : 0u) << 16) |
-                                       ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
+                                   ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
             constexpr uint32_t step_a = A_MN ? 2048 : 32, step_b = B_MN ? 2048 : 32;  // 16 along the contraction
             uint32_t fill = 0, it = 0;
             bool ok = true, any = false;
@@ -350,6 +350,13 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
             const int l = t.l0 + 32 * ew + lane;
             float bias = 0.f;
             if (P.bias != nullptr && l < P.L && !split) bias = load_either<T>(P.bias, l, P.bias_f32);
+            // the residual's tile comes into L2 while the products run: waiting for it afterwards, 16 columns at a time, took as long as they did
+            if (P.residual != nullptr && l < P.L)
+                for (int c = lane; c < BN / 2; c += 32) {
+                    const int row = t.c0 + c / 16 * 32 + 16 * set + c % 16;
+                    const int64_t at = (int64_t)row * P.residual_stride + t.l0 + 32 * ew;
+                    if (row < P.C) asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t *>(P.residual) + at * (P.out_f32 ? 4 : 2)) : "memory");
+                }
             const auto finish = [&](float (&v)[16], int c0) {  // columns c0 .. of the tile
                 if (split) {
                     // the ring is free: all products of this block's only tile have ended.  [column][lane]
@@ -505,11 +512,17 @@ __global__ void __launch_bounds__(256) linear_few_kernel(const T *x, int64_t x_s
 }
 
 // ---------------------------------------------------------- dP and its column sums ----
-// dP = dy act'(P) in 16 bits, the operand of both products, and the sums over GRAD_ROWS rows of the values before that rounding, which linear_bias_kernel adds in order.  A warp has 256 columns, eight per lane, and every eighth row of the block.
+// dP = dy act'(P) in 16 bits, the operand of both products, and the sums over a block's rows of the values before that rounding, which linear_bias_kernel adds in order.  A warp has 256 columns, eight per lane, and every eighth row of the block.
 // One rounding of dP is of the size of a 16-bit result's own.  Where grad_w is fp32 it would be the largest error by far (2^-9 against
 // 2^-20), so there what the rounding left is kept in 16 bits as well, and the contraction of dW runs over both: twice the products for
 // gradients with the digits of an fp32 sum (3e-6).
-constexpr int GRAD_ROWS = 64;
+// Rows of a block: 64, or as few as 16 while there are no 128 blocks of rows.
+inline int64_t grad_blocks_most(int64_t rows)  // never less for more rows, for workspaces
+{
+    const int64_t few = (rows + 15) / 16, many = (rows + 63) / 64;
+    return few < 128 ? few : many < 128 ? 128 : many;
+}
+inline int grad_block_rows(int64_t rows) { return rows <= 128 * 16 ? 16 : rows <= 128 * 32 ? 32 : 64; }
 struct LinearGradArgs {
     const void *grad_y;  // fp32 (y_f32) or T
     const void *pre;     // fp32 (pre_f32) or T, null without an activation
@@ -517,7 +530,7 @@ struct LinearGradArgs {
     void *dp_low;        // T, dP less its rounding, null where grad_w is 16-bit
     float *partial;      // [blocks of rows][n], null without a bias
     int64_t y_stride, pre_stride, dp_stride, rows;
-    int n, y_f32, pre_f32;
+    int n, y_f32, pre_f32, block_rows;
 };
 __device__ __forceinline__ void load8f(const float *p, float (&x)[8])
 {
@@ -530,45 +543,64 @@ __global__ void __launch_bounds__(256) linear_grad_kernel(const LinearGradArgs P
     pdl_wait();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ float part[8][256];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = (int)blockIdx.y * 256 + 8 * lane;
-    const int64_t row0 = (int64_t)blockIdx.x * GRAD_ROWS, row1 = min(P.rows, row0 + GRAD_ROWS);
+    // eight columns of a lane: side by side (VEC), or 32 apart, so that single values are read side by side as well
+    constexpr int STEP = VEC ? 1 : 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = (int)blockIdx.y * 256 + (VEC ? 8 * lane : lane);
+    const int64_t row0 = (int64_t)blockIdx.x * P.block_rows, row1 = min(P.rows, row0 + P.block_rows);
     float sum[8] = {};
     if (c < P.n) {
 #pragma unroll 2
         for (int64_t r = row0 + warp; r < row1; r += 8) {
-            float g[8];
+            float g[8], p[8];
             if (VEC) {
                 if (P.y_f32) load8f(static_cast<const float *>(P.grad_y) + r * P.y_stride + c, g);
                 else Io<T>::unpack(ld(reinterpret_cast<const uint4 *>(static_cast<const T *>(P.grad_y) + r * P.y_stride + c)), g);
+                if constexpr (ACT != LAPSUM_ACT_NONE) {
+                    if (P.pre_f32) load8f(static_cast<const float *>(P.pre) + r * P.pre_stride + c, p);
+                    else Io<T>::unpack(ld(reinterpret_cast<const uint4 *>(static_cast<const T *>(P.pre) + r * P.pre_stride + c)), p);
+                }
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = c + i < P.n ? load_either<T>(P.grad_y, r * P.y_stride + c + i, P.y_f32) : 0.f;
+                for (int i = 0; i < 8; ++i) {
+                    g[i] = c + STEP * i < P.n ? load_either<T>(P.grad_y, r * P.y_stride + c + STEP * i, P.y_f32) : 0.f;
+                    if constexpr (ACT != LAPSUM_ACT_NONE) p[i] = c + STEP * i < P.n ? load_either<T>(P.pre, r * P.pre_stride + c + STEP * i, P.pre_f32) : 0.f;
+                }
             }
             if constexpr (ACT != LAPSUM_ACT_NONE) {
-                float p[8];  // rows of pre are whole vectors
-                if (P.pre_f32) load8f(static_cast<const float *>(P.pre) + r * P.pre_stride + c, p);
-                else Io<T>::unpack(ld(reinterpret_cast<const uint4 *>(static_cast<const T *>(P.pre) + r * P.pre_stride + c)), p);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = c + i < P.n ? g[i] * slope_of<ACT>(p[i]) : 0.f;  // the padding is nobody's
+                for (int i = 0; i < 8; ++i) g[i] *= slope_of<ACT>(p[i]);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += g[i];
             if (P.dp != nullptr) {
                 const uint4 q = Io<T>::pack(g);
-                *reinterpret_cast<uint4 *>(static_cast<T *>(P.dp) + r * P.dp_stride + c) = q;
+                float h[8];
+                Io<T>::unpack(q, h);
+                const int64_t at = r * P.dp_stride + c;
+                if (VEC) {
+                    *reinterpret_cast<uint4 *>(static_cast<T *>(P.dp) + at) = q;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (c + STEP * i < P.n) Io<T>::store1(static_cast<T *>(P.dp) + at + STEP * i, h[i]);
+                }
                 if (P.dp_low != nullptr) {
-                    float h[8];
-                    Io<T>::unpack(q, h);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) h[i] = isfinite(h[i]) ? g[i] - h[i] : 0.f;  // beyond the range the rounding stands
-                    *reinterpret_cast<uint4 *>(static_cast<T *>(P.dp_low) + r * P.dp_stride + c) = Io<T>::pack(h);
+                    if (VEC) {
+                        *reinterpret_cast<uint4 *>(static_cast<T *>(P.dp_low) + at) = Io<T>::pack(h);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (c + STEP * i < P.n) Io<T>::store1(static_cast<T *>(P.dp_low) + at + STEP * i, h[i]);
+                    }
                 }
             }
         }
     }
     if (P.partial == nullptr) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) part[warp][8 * lane + i] = sum[i];
+    for (int i = 0; i < 8; ++i) part[warp][VEC ? 8 * lane + i : lane + 32 * i] = sum[i];
     __syncthreads();
     const int mine = (int)blockIdx.y * 256 + threadIdx.x;
     if (mine < P.n) {

@@ -26,11 +26,11 @@ int linear_layout(const lapsum_linear_dims *p, LinearLayout &X, lapsum_linear_la
         if (t != p->io_dtype && t != LAPSUM_IO_F32) return LAPSUM_ERR_UNSUPPORTED;
     if (p->activation < LAPSUM_ACT_NONE || p->activation > LAPSUM_ACT_GELU_TANH || (p->training != 0 && p->training != 1)) return LAPSUM_ERR_PARAM;
     X.ld = (p->n + 7) / 8 * 8;
-    X.parts = ceil_div(p->rows, GRAD_ROWS);
+    X.parts = ceil_div(p->rows, grad_block_rows(p->rows));
     size_t at = 256;  // control block: the status word
     X.off_dp = at, at += p->training ? align_up((size_t)p->rows * (size_t)X.ld * 2) : 0;
     X.off_low = at, at += p->training ? align_up((size_t)p->rows * (size_t)X.ld * 2) : 0;
-    X.off_partial = at, at += p->training ? align_up((size_t)X.parts * (size_t)p->n * 4) : 0;
+    X.off_partial = at, at += p->training ? align_up((size_t)grad_blocks_most(p->rows) * (size_t)p->n * 4) : 0;
     out->workspace_bytes = at;
     out->pre_bytes = p->training && p->activation != LAPSUM_ACT_NONE ? (size_t)p->rows * (size_t)X.ld * (p->pre_dtype == LAPSUM_IO_F32 ? 4 : 2) : 0;
     out->pre_stride = X.ld;
@@ -39,7 +39,10 @@ int linear_layout(const lapsum_linear_dims *p, LinearLayout &X, lapsum_linear_la
 
 // Tiles of a product of L lanes, C columns and K along the contraction.  For every form of tile the time is taken as rounds of the SMs times
 // (steps of 64 x clocks per step + the tile's own time), and the least wins.  Clocks per step: the tensor core's 2 x BN, or the operands' bytes
-// at 65 per clock and SM, whichever is more; a pair of blocks shares its operands.
+// at BYTES_PER_CLOCK for each SM, whichever is more; a pair of blocks shares its operands.  A shared contraction costs its join.
+// Measured, tile columns / blocks per tile, us: 1021 x 2048 x 5632 128 43, 128 / 2 52, 256 / 2 39, pairs 47; 512 x 2048 x 2048 64 19, 128 21, 128 / 2 19,
+// 128 / 4 27; 16384 x 8192 x 2048 128 617, 256 461, pairs 428 (of 224 columns, which leave no round half empty, 4 % slower: the power limit); 65536 x 128 x 2048 64 84, 128 70, 256 68, pairs 86; 48 x 2048 x 1024 64 15, 64 / 4 14, 64 / 8 21.
+constexpr double BYTES_PER_CLOCK = 45.0;
 struct Choice {
     int bn, split;
     bool pair;
@@ -50,19 +53,19 @@ Choice choose(int64_t L, int64_t C, int64_t K, bool b_mn, int sms)
     Choice best{b_mn ? 64 : 16, 1, false};
     double least = 1e300;
     for (int bn = b_mn ? 64 : 16; bn <= 256; bn *= 2) {
-        if (bn > 16 && bn >= 2 * C && bn > (b_mn ? 64 : 16)) break;  // half of the tile and more would be empty
+        if (bn >= 2 * C && bn > (b_mn ? 64 : 16)) break;  // half of the tile and more would be empty
         const int64_t tiles = ceil_div(L, 128) * ceil_div(C, bn);
-        const double bytes = 128 * (128 + bn) / 65.0, step = bytes > 2.0 * bn ? bytes : 2.0 * bn;
-        for (int split = 1; split <= 8; split *= 2) {
-            if (split > 1 && (steps < 2 * split || tiles * split > sms)) break;
+        const double bytes = 128 * (128 + bn) / BYTES_PER_CLOCK, step = bytes > 2.0 * bn ? bytes : 2.0 * bn;
+        for (int split = 1; split <= 4; split *= 2) {
+            if (split > 1 && (steps < 4 * split || tiles * split > sms)) break;
             if ((split - 1) * ceil_div(steps, split) >= steps) continue;  // a block without a part
             const int64_t rounds = ceil_div(tiles * split, sms);
-            const double t = (double)rounds * ((double)ceil_div(steps, split) * step + 10.0 * bn) + (split > 1 ? 2500.0 : 0.0);
+            const double t = (double)rounds * ((double)ceil_div(steps, split) * step + 10.0 * bn) + (split > 1 ? 2000.0 + 20.0 * bn : 0.0);
             if (t < least) least = t, best = Choice{bn, split, false};
         }
     }
     const int64_t tiles = ceil_div(L, 256) * ceil_div(C, 256);
-    const double t = (double)ceil_div(tiles, sms / 2) * ((double)steps * 540.0 + 2560.0);
+    const double t = (double)ceil_div(tiles, sms / 2) * ((double)steps * 256 * 128 / BYTES_PER_CLOCK + 2560.0);
     if (t < least && C > 128) best = Choice{256, 1, true};
     return best;
 }
@@ -177,7 +180,7 @@ int backward_t(const lapsum_linear_dims &p, const LinearLayout &X, const void *g
         G.partial = grad_bias ? reinterpret_cast<float *>(ws + X.off_partial) : nullptr;
         if (G.dp && keep_low) G.dp_low = ws + X.off_low;
         G.pre_f32 = p.pre_dtype == LAPSUM_IO_F32;
-        G.y_stride = gy_stride, G.pre_stride = G.dp_stride = X.ld, G.rows = p.rows, G.n = (int)p.n, G.y_f32 = y_f32;
+        G.y_stride = gy_stride, G.pre_stride = G.dp_stride = X.ld, G.rows = p.rows, G.n = (int)p.n, G.y_f32 = y_f32, G.block_rows = grad_block_rows(p.rows);
         const bool vec = gy_stride % 8 == 0 && p.n % 8 == 0 && aligned(grad_y, 16);
         const dim3 grid((unsigned)X.parts, (unsigned)ceil_div(p.n, 256));
         switch (p.activation) {

@@ -46,6 +46,7 @@ class LinearWorkspace(_Memory):
         _check(lib().lapsum_linear_describe(C.byref(self.dims), C.byref(out)), "lapsum_linear_describe")
         self.rows, self.n, self.k, self.training = int(rows), int(n), int(k), bool(training)
         self.dtype, self.out_dtype, self.pre_dtype = IO_TORCH[io_dtype], IO_TORCH[out_dtype], IO_TORCH[pre_dtype]
+        self._dims = {}  # a call's dims by its rows and types
         self.bytes, self.pre_bytes, self.pre_stride = out.workspace_bytes, out.pre_bytes, out.pre_stride
         with torch.cuda.device(dev), torch.cuda.stream(stream) if stream is not None else nullcontext():
             self._allocate(self.bytes, dev)
@@ -65,14 +66,24 @@ class LinearWorkspace(_Memory):
         _check(lib().lapsum_linear_status(self.ptr, self._use(stream), C.byref(out)), "lapsum_linear_status")
         return out.value
 
-    def _call(self, x: torch.Tensor) -> tuple:
+    def _call(self, x: torch.Tensor, wide_bias: bool, wide_grad: bool = False) -> tuple:
         """(dims of this call, x's row stride)"""
         stride = _rows(x, self.dtype, "x", self.gpu)
         rows = x.shape[0]
         if x.shape[1] != self.k or rows > self.rows:
             raise ValueError(f"x must have up to {self.rows} rows of {self.k}, not shape {tuple(x.shape)}")
-        dims = LinearDims.from_buffer_copy(self.dims)
-        dims.rows = rows
+        key = (rows, wide_bias, wide_grad)
+        dims = self._dims.get(key)
+        if dims is None:
+            dims = LinearDims.from_buffer_copy(self.dims)
+            dims.rows = rows
+            if wide_bias:
+                dims.bias_dtype = IO_F32
+            if wide_grad:
+                dims.grad_w_dtype = IO_F32
+            if len(self._dims) >= 256:
+                self._dims.clear()
+            self._dims[key] = dims
         return dims, stride
 
     def _kept(self, pre: Optional[torch.Tensor], rows: int) -> tuple:
@@ -94,9 +105,7 @@ def lapsum_linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch
     """y (rows x n, the workspace's out_dtype) <- act(x w^T + bias) + residual.  x: rows x k with contiguous rows; w: n x k; bias: n, the
     workspace's 16-bit type or float32; residual like y (or y itself)."""
     gpu = ws.gpu
-    dims, stride = ws._call(x)
-    if bias is not None and bias.dtype == torch.float32:
-        dims.bias_dtype = IO_F32
+    dims, stride = ws._call(x, bias is not None and bias.dtype == torch.float32)
     out = (dims.rows, ws.n)
     at, room = ws._kept(pre, dims.rows)
     rc = lib().lapsum_linear_forward(
@@ -114,11 +123,7 @@ def lapsum_linear_backward(grad_y: torch.Tensor, x: torch.Tensor, w: torch.Tenso
     """The gradients of lapsum_linear_forward that are not None; grad_w and grad_bias have the workspace's 16-bit type or float32.  The
     residual's gradient is grad_y."""
     gpu = ws.gpu
-    dims, stride = ws._call(x)
-    if grad_w is not None and grad_w.dtype == torch.float32:
-        dims.grad_w_dtype = IO_F32
-    if grad_bias is not None and grad_bias.dtype == torch.float32:
-        dims.bias_dtype = IO_F32
+    dims, stride = ws._call(x, grad_bias is not None and grad_bias.dtype == torch.float32, grad_w is not None and grad_w.dtype == torch.float32)
     at, room = ws._kept(pre, dims.rows)
     rc = lib().lapsum_linear_backward(
         grad_y.data_ptr(), _matrix(grad_y, ws.out_dtype, (dims.rows, ws.n), "grad_y", gpu), x.data_ptr(), stride,
