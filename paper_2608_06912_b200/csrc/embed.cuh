@@ -5,6 +5,9 @@
 //
 // The gradient in three kernels: a stable sort of the positions by id (embed_sort_kernel), the sums of all rows with few positions and
 // partial sums of pieces of the others (embed_grad_kernel), the sums of the pieces (embed_join_kernel).  Every sum has a fixed order.
+//
+// Measured: 65536 ids into 128000 x 2048 bf16: forward 65 us (380 MB, 5.8 TB/s); gradient in fp32 324 us: sort 35, sums 261 (1.32 GB, most of it the zeros of rows
+// that do not occur, 5.0 TB/s), pieces 12; in bf16 245.  4093 ids into 50021 x 1000 fp16: 10 and 42 us (100 MB of zeros take 16), three dependent kernels.
 #pragma once
 #include <type_traits>
 
@@ -32,7 +35,8 @@ struct EmbedArgs {
     int64_t partial_stride;   // d, rounded up to whole vectors
 };
 
-// Rows of more than EMBED_LONG positions are summed in pieces: runs of EMBED_LONG sorted positions (chunks) cut them.
+// Rows of more than EMBED_LONG positions are summed in pieces: runs of EMBED_LONG sorted positions (chunks) cut them.  A warp takes four positions at
+// a time, so this bounds its longest chain.  16 / 32, us: 4093 ids into 50021 x 1000 42 / 53, 65536 into 128000 x 2048 324 / 314.
 constexpr int EMBED_LONG = 16;
 // Ids that one block of the sort takes care of, and its warps
 constexpr int EMBED_RANGE = 512, EMBED_WARPS = 32;
@@ -98,7 +102,7 @@ __global__ void __launch_bounds__(256) embed_forward_kernel(const EmbedArgs P)
 
 // A block has EMBED_RANGE neighbouring ids and reads all of them: it counts, per warp (a run of positions) and id, and how many ids lie below its
 // range, which is where its part of the order begins; then it reads them again and puts its positions where the counts say.  No
-// block waits for another.
+// block waits for another.  Bound by instructions, some eight per id in every block: 35 us for 65536 ids and 250 blocks, with 64-bit comparisons 59.
 template <typename Id>
 __global__ void __launch_bounds__(32 * EMBED_WARPS) embed_sort_kernel(const EmbedArgs P)
 {

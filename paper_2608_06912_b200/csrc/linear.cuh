@@ -13,6 +13,12 @@
 // so a few tokens are a narrow column tile beside full 128-row tiles of weights, and in the epilogue the 32 lanes of a warp hold
 // 32 neighbouring values of one row of the result: loads and stores of it are contiguous whatever n, the strides and the alignment,
 // and a bias is one value per thread.
+//
+// Measured in bf16, operands not in L2 (a library's product of the same shape beside it): 16384 x 8192 x 2048 forward without an epilogue 378 - 396 us,
+// 1.39 - 1.45 PFLOP/s (343 - 352), with silu and P kept in fp32 (805 MB of results) 427 - 439; dx 358 - 379 (348 - 357), dW 398 - 440 (340 - 350), both at the power limit;
+// dW with fp32 digits 1000 for twice the products.  Logits of 48 rows, 128000 x 2048, 107 us, 5.1 TB/s of weights (107); the router 65536 x 128 x 2048 65 - 68 us,
+// 4.5 TB/s (69); a prompt of 1021 rows, 2048 x 5632, 39 us (27): 32 large or 128 small tiles leave SMs idle or their operands' copies the bound, 45 bytes per
+// clock and SM; one row of 2048 x 1024 9 us, the host's call.
 #pragma once
 #include <type_traits>
 
