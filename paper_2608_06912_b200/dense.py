@@ -22,8 +22,19 @@ ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
 ACTIVATIONS = {"none": ACT_NONE, "relu": ACT_RELU, "silu": ACT_SILU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH}
 
 
+# A call's checks are most of a small call's time (a dense layer of one row takes 3 us on the GPU), so what is right is found so by one condition; _dense
+# and _rows name what is wrong.
+def _flat(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str, gpu: int) -> int:
+    """The address of a contiguous tensor."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == gpu and t.is_contiguous():
+        return t.data_ptr()
+    return _dense(t, dtype, shape, name, gpu)
+
+
 def _matrix(t: torch.Tensor, dtype: torch.dtype, shape: tuple, name: str, gpu: int) -> int:
     """The row stride of a matrix of this shape with contiguous rows."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == gpu and t.is_contiguous():
+        return shape[1]
     stride = _rows(t, dtype, name, gpu)
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
@@ -46,7 +57,7 @@ class LinearWorkspace(_Memory):
         _check(lib().lapsum_linear_describe(C.byref(self.dims), C.byref(out)), "lapsum_linear_describe")
         self.rows, self.n, self.k, self.training = int(rows), int(n), int(k), bool(training)
         self.dtype, self.out_dtype, self.pre_dtype = IO_TORCH[io_dtype], IO_TORCH[out_dtype], IO_TORCH[pre_dtype]
-        self._dims = {}  # a call's dims by its rows and types
+        self._dims, self._w, self._b = {}, (self.n, self.k), (self.n,)  # _dims: a call's dims by its rows and types
         self.bytes, self.pre_bytes, self.pre_stride = out.workspace_bytes, out.pre_bytes, out.pre_stride
         with torch.cuda.device(dev), torch.cuda.stream(stream) if stream is not None else nullcontext():
             self._allocate(self.bytes, dev)
@@ -67,24 +78,20 @@ class LinearWorkspace(_Memory):
         return out.value
 
     def _call(self, x: torch.Tensor, wide_bias: bool, wide_grad: bool = False) -> tuple:
-        """(dims of this call, x's row stride)"""
-        stride = _rows(x, self.dtype, "x", self.gpu)
-        rows = x.shape[0]
-        if x.shape[1] != self.k or rows > self.rows:
-            raise ValueError(f"x must have up to {self.rows} rows of {self.k}, not shape {tuple(x.shape)}")
-        key = (rows, wide_bias, wide_grad)
-        dims = self._dims.get(key)
-        if dims is None:
-            dims = LinearDims.from_buffer_copy(self.dims)
-            dims.rows = rows
-            if wide_bias:
-                dims.bias_dtype = IO_F32
-            if wide_grad:
-                dims.grad_w_dtype = IO_F32
+        """(reference to this call's dims, rows, x's row stride)"""
+        shape = x.shape
+        rows = shape[0] if len(shape) == 2 else -1
+        dims = self._dims.get((rows, wide_bias, wide_grad))
+        if dims is None or shape[1] != self.k:
+            _rows(x, self.dtype, "x", self.gpu)
+            if shape[1] != self.k or rows > self.rows:
+                raise ValueError(f"x must have up to {self.rows} rows of {self.k}, not shape {tuple(shape)}")
+            made = LinearDims.from_buffer_copy(self.dims)
+            made.rows, made.bias_dtype, made.grad_w_dtype = rows, IO_F32 if wide_bias else made.bias_dtype, IO_F32 if wide_grad else made.grad_w_dtype
             if len(self._dims) >= 256:
                 self._dims.clear()
-            self._dims[key] = dims
-        return dims, stride
+            dims = self._dims[rows, wide_bias, wide_grad] = C.byref(made)
+        return dims, rows, _matrix(x, self.dtype, (rows, self.k), "x", self.gpu)
 
     def _kept(self, pre: Optional[torch.Tensor], rows: int) -> tuple:
         if not self.pre_bytes:
@@ -104,15 +111,15 @@ def lapsum_linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch
                           ws: LinearWorkspace, pre: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """y (rows x n, the workspace's out_dtype) <- act(x w^T + bias) + residual.  x: rows x k with contiguous rows; w: n x k; bias: n, the
     workspace's 16-bit type or float32; residual like y (or y itself)."""
-    gpu = ws.gpu
-    dims, stride = ws._call(x, bias is not None and bias.dtype == torch.float32)
-    out = (dims.rows, ws.n)
-    at, room = ws._kept(pre, dims.rows)
+    gpu, kind = ws.gpu, ws.out_dtype
+    wide = bias is not None and bias.dtype is torch.float32
+    dims, rows, stride = ws._call(x, wide)
+    out = (rows, ws.n)
+    at, room = ws._kept(pre, rows) if pre is not None or ws.pre_bytes else (None, 0)
     rc = lib().lapsum_linear_forward(
-        x.data_ptr(), stride, _dense(w, ws.dtype, (ws.n, ws.k), "w", gpu),
-        None if bias is None else _dense(bias, IO_TORCH[dims.bias_dtype], (ws.n,), "bias", gpu), None if residual is None else residual.data_ptr(),
-        0 if residual is None else _matrix(residual, ws.out_dtype, out, "residual", gpu), y.data_ptr(), _matrix(y, ws.out_dtype, out, "y", gpu),
-        at, room, C.byref(dims), ws.ptr, ws.bytes, ws._use(stream))
+        x.data_ptr(), stride, _flat(w, ws.dtype, ws._w, "w", gpu), None if bias is None else _flat(bias, torch.float32 if wide else ws.dtype, ws._b, "bias", gpu),
+        None if residual is None else residual.data_ptr(), 0 if residual is None else _matrix(residual, kind, out, "residual", gpu), y.data_ptr(),
+        _matrix(y, kind, out, "y", gpu), at, room, dims, ws.ptr, ws.bytes, ws._use(stream))
     if rc:
         _check(rc, "lapsum_linear_forward")
 
@@ -123,14 +130,14 @@ def lapsum_linear_backward(grad_y: torch.Tensor, x: torch.Tensor, w: torch.Tenso
     """The gradients of lapsum_linear_forward that are not None; grad_w and grad_bias have the workspace's 16-bit type or float32.  The
     residual's gradient is grad_y."""
     gpu = ws.gpu
-    dims, stride = ws._call(x, grad_bias is not None and grad_bias.dtype == torch.float32, grad_w is not None and grad_w.dtype == torch.float32)
-    at, room = ws._kept(pre, dims.rows)
+    wide, wide_w = grad_bias is not None and grad_bias.dtype is torch.float32, grad_w is not None and grad_w.dtype is torch.float32
+    dims, rows, stride = ws._call(x, wide, wide_w)
+    at, room = ws._kept(pre, rows) if pre is not None or ws.pre_bytes else (None, 0)
     rc = lib().lapsum_linear_backward(
-        grad_y.data_ptr(), _matrix(grad_y, ws.out_dtype, (dims.rows, ws.n), "grad_y", gpu), x.data_ptr(), stride,
-        _dense(w, ws.dtype, (ws.n, ws.k), "w", gpu), at, room, None if grad_x is None else grad_x.data_ptr(),
-        0 if grad_x is None else _matrix(grad_x, ws.dtype, (dims.rows, ws.k), "grad_x", gpu),
-        None if grad_w is None else _dense(grad_w, IO_TORCH[dims.grad_w_dtype], (ws.n, ws.k), "grad_w", gpu),
-        None if grad_bias is None else _dense(grad_bias, IO_TORCH[dims.bias_dtype], (ws.n,), "grad_bias", gpu), C.byref(dims), ws.ptr, ws.bytes,
+        grad_y.data_ptr(), _matrix(grad_y, ws.out_dtype, (rows, ws.n), "grad_y", gpu), x.data_ptr(), stride, _flat(w, ws.dtype, ws._w, "w", gpu), at, room,
+        None if grad_x is None else grad_x.data_ptr(), 0 if grad_x is None else _matrix(grad_x, ws.dtype, (rows, ws.k), "grad_x", gpu),
+        None if grad_w is None else _flat(grad_w, torch.float32 if wide_w else ws.dtype, ws._w, "grad_w", gpu),
+        None if grad_bias is None else _flat(grad_bias, torch.float32 if wide else ws.dtype, ws._b, "grad_bias", gpu), dims, ws.ptr, ws.bytes,
         ws._use(stream))
     if rc:
         _check(rc, "lapsum_linear_backward")
@@ -156,39 +163,43 @@ def lapsum_sample(logits: torch.Tensor, u: torch.Tensor, params: SampleParams, t
     temperature, top_p, min_p (float32) and top_k (int32), one per row, replace the params' value for all rows."""
     stride = _rows(logits, IO_TORCH[params.io_dtype], "logits")
     rows, vocab = logits.shape
-    gpu, f, i = logits.get_device(), torch.float32, torch.int32
-
-    def vec(t, dtype, name):
-        return None if t is None else _dense(t, dtype, (rows,), name, gpu)
-
+    gpu, f, i, n = logits.get_device(), torch.float32, torch.int32, (rows,)
     rc = lib().lapsum_sample(
-        logits.data_ptr(), rows, vocab, stride, _dense(u, f, (rows,), "u", gpu), C.byref(params), vec(temperature, f, "temperature"),
-        vec(top_k, i, "top_k"), vec(top_p, f, "top_p"), vec(min_p, f, "min_p"), _dense(token, i, (rows,), "token", gpu),
-        vec(logprob, f, "logprob"), vec(kept, i, "kept"), _stream(stream, gpu))
+        logits.data_ptr(), rows, vocab, stride, _flat(u, f, n, "u", gpu), C.byref(params),
+        None if temperature is None else _flat(temperature, f, n, "temperature", gpu), None if top_k is None else _flat(top_k, i, n, "top_k", gpu),
+        None if top_p is None else _flat(top_p, f, n, "top_p", gpu), None if min_p is None else _flat(min_p, f, n, "min_p", gpu),
+        _flat(token, i, n, "token", gpu), None if logprob is None else _flat(logprob, f, n, "logprob", gpu),
+        None if kept is None else _flat(kept, i, n, "kept", gpu), _stream(stream, gpu))
     if rc:
         _check(rc, "lapsum_sample")
 
 
 # ------------------------------------------------------------------------------------------------------------- embed
+_ID_BYTES = {torch.int32: 4, torch.int64: 8}
+
+
 def _ids(ids: torch.Tensor, gpu: int) -> tuple:
-    if not (ids.is_cuda and ids.dtype in (torch.int32, torch.int64) and ids.dim() == 1 and ids.is_contiguous()):
+    size, shape = _ID_BYTES.get(ids.dtype), ids.shape
+    if size is None or len(shape) != 1 or not ids.is_contiguous() or not ids.is_cuda:
         raise TypeError("ids must be a contiguous int32 or int64 CUDA vector")
     if ids.get_device() != gpu:
         _elsewhere(ids, gpu, "ids")
-    return ids.data_ptr(), ids.element_size(), ids.shape[0]
+    return ids.data_ptr(), size, shape[0]
 
 
 def lapsum_embed_forward(ids: torch.Tensor, table: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
                          stream: Optional[torch.cuda.Stream] = None) -> None:
     """out (tokens x d) <- scale * table[ids]; ids outside the table give zeros.  ids: int32 or int64; table: vocab x d, float32, float16
     or bfloat16, contiguous rows; out like the table."""
-    if table.dtype not in IO_OF:
+    dtype = table.dtype
+    io = IO_OF.get(dtype)
+    if io is None:
         raise TypeError("table must be float32, float16 or bfloat16")
-    stride, gpu = _rows(table, table.dtype, "table"), table.get_device()
+    stride, gpu = _rows(table, dtype, "table"), table.get_device()
     at, size, tokens = _ids(ids, gpu)
     vocab, d = table.shape
-    rc = lib().lapsum_embed_forward(at, size, tokens, table.data_ptr(), stride, vocab, d, scale, IO_OF[table.dtype], out.data_ptr(),
-                                    _matrix(out, table.dtype, (tokens, d), "out", gpu), _stream(stream, gpu))
+    rc = lib().lapsum_embed_forward(at, size, tokens, table.data_ptr(), stride, vocab, d, scale, io, out.data_ptr(),
+                                    _matrix(out, dtype, (tokens, d), "out", gpu), _stream(stream, gpu))
     if rc:
         _check(rc, "lapsum_embed_forward")
 
@@ -217,6 +228,6 @@ def lapsum_embed_backward(grad_out: torch.Tensor, ids: torch.Tensor, grad_table:
     wide = torch.float32 if grad_table.dtype == torch.float32 else grad_out.dtype
     rc = lib().lapsum_embed_backward(
         grad_out.data_ptr(), _matrix(grad_out, grad_out.dtype, (tokens, ws.d), "grad_out", gpu), at, size, tokens, ws.vocab, ws.d, scale, skip,
-        IO_OF[grad_out.dtype], IO_OF[wide], _dense(grad_table, wide, (ws.vocab, ws.d), "grad_table", gpu), ws.ptr, ws.bytes, ws._use(stream))
+        IO_OF[grad_out.dtype], IO_OF[wide], _flat(grad_table, wide, (ws.vocab, ws.d), "grad_table", gpu), ws.ptr, ws.bytes, ws._use(stream))
     if rc:
         _check(rc, "lapsum_embed_backward")
