@@ -809,7 +809,7 @@ struct SampleRow {
             for (int i = 0; i < 4 && !inside(x); ++i) x = nextafterf(x, CUDART_INF_F);
 #pragma unroll 1
             for (int i = 0; i < 4 && inside(nextafterf(x, -CUDART_INF_F)); ++i) x = nextafterf(x, -CUDART_INF_F);
-            cut_x = fmaxf(cut_x, x);
+            cut_x = fmaxf(cut_x, fminf(x, top));  // at a temperature whose reciprocal is infinite nothing is inside
         }
         // turns: the cut of top-k; the sum, the cut of top-p; the sum, the draw
         bool need_k = k > 0 && k < P.vocab, need_p = p < 1;

@@ -130,6 +130,16 @@ def test_extreme_temperatures(temperature):
         check(x, u, temperature=temperature, **kw)
 
 
+def test_a_temperature_whose_reciprocal_is_infinite():
+    x, u = make(5, 2000, seed=14)
+    token, kept = (torch.full((5,), -7, device="cuda", dtype=torch.int32) for _ in range(2))
+    for kw in (dict(min_p=0.5), dict(top_p=0.5), dict(top_k=9, min_p=1.0), {}):
+        L.lapsum_sample(x, u, L.sample_params(temperature=1e-310, **kw), token, None, kept)
+        assert torch.equal(token.long(), x.argmax(1)), kw
+        if kw:
+            assert (kept == 1).all() or "top_k" in kw
+
+
 @pytest.mark.parametrize("scale,shift", [(1e-6, 0.0), (1e-3, 1000.0), (1e4, 0.0), (1.0, -1e5), (1e30, 0.0)])
 def test_logits_of_any_size(scale, shift):
     x, u = make(8, 20000, seed=13)
