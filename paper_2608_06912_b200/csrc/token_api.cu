@@ -31,7 +31,7 @@ int sample_launch(const SampleArgs &A, int64_t rows, cudaStream_t st)
     return launch_clusters((unsigned)A.cluster, kernel, (unsigned)(rows * A.cluster), THREADS, smem, st, A);
 }
 // Few rows, or a top-p that may have to look far: blocks as many as keep a block's run at 64 KB (two blocks per SM), and more, down to runs of 4096 tokens,
-// while SMs are without work.  Rows for two thirds of the SMs, long and without top-p: a block of 1024 threads each.  Measured at 256 x 128000 fp32, a block
+// while all of them find a place at once.  Rows for two thirds of the SMs, long and without top-p: a block of 1024 threads each.  Measured at 256 x 128000 fp32, a block
 // each / clusters, us: no filter 109 / 121, top-k 40 82 / 111, top-p 0.9 over some 3000 tokens 366 / 424, rows of all kinds 324 / 193 (a single row of the
 // last kind takes 200 on one SM); 512 x 1000 75 / 36.
 template <typename T>
@@ -42,7 +42,7 @@ int sample_t(SampleArgs A, int64_t rows, cudaStream_t st)
     const bool many = 3 * rows >= 2 * sms && A.vocab >= 32768 && !A.top_p_row && A.top_p >= 1;
     int cluster = 1;
     while (!many && cluster < 8 && ((int64_t)A.vocab * (int)sizeof(T) > (int64_t)cluster * SAMPLE_BLOCK_BYTES ||
-                           (rows * cluster < 2 * sms && A.vocab >= 2 * 4096 * cluster)))
+                           (rows * cluster * 2 <= 2 * sms && A.vocab >= 2 * 4096 * cluster)))
         cluster *= 2;
     A.cluster = cluster;
     A.chunk = (int)(ceil_div(ceil_div(A.vocab, cluster), 128) * 128);
