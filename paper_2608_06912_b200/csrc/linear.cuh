@@ -17,8 +17,8 @@
 // Measured in bf16, operands not in L2 (a library's product of the same shape beside it): 16384 x 8192 x 2048 forward without an epilogue 378 - 396 us,
 // 1.39 - 1.45 PFLOP/s (343 - 352), with silu and P kept in fp32 (805 MB of results) 427 - 439; dx 358 - 379 (348 - 357), dW 398 - 440 (340 - 350), both at the power limit;
 // dW with fp32 digits 1000 for twice the products.  Logits of 48 rows, 128000 x 2048, 107 us, 5.1 TB/s of weights (107); the router 65536 x 128 x 2048 65 - 68 us,
-// 4.5 TB/s (69); a prompt of 1021 rows, 2048 x 5632, 39 us (27): 32 large or 128 small tiles leave SMs idle or their operands' copies the bound, 45 bytes per
-// clock and SM; one row of 2048 x 1024 9 us, the host's call.
+// 4.5 TB/s (69); a prompt of 1021 rows, 2048 x 5632, 33 us (27): 32 large tiles, their contraction shared by two pairs each, so a join; one row of
+// 2048 x 1024 9 us, the host's call (3 in a graph).
 #pragma once
 #include <type_traits>
 
@@ -190,7 +190,7 @@ __device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N]
 //   WIDE   the tensor core's own additions truncate: an error of about 2^-25 of the sum each, all towards zero, 2e-6 at K = 2048 and 2e-5 at 16384.
 //          That is nothing to a 16-bit result.  For an fp32 result an accumulator takes ROUND steps (512 of the contraction), and the epilogue adds
 //          the rounds' sums in fp32 registers, rounded to nearest, while the next round is computed in the other accumulator: 5e-7.
-//   split  a cluster of `split` blocks shares the contraction of one tile, for shapes with few tiles: each leaves its sums in its shared
+//   split  a cluster of `split` blocks, or pairs, shares the contraction of one tile, for shapes with few tiles: each leaves its sums in its shared
 //          memory, and after a cluster barrier adds its share of the columns over the blocks, in their order.
 template <int BN, bool PAIR_>
 struct LinearShape {
@@ -218,8 +218,9 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
     __shared__ uint32_t tmem_at;
     __shared__ int abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const bool split = !PAIR && P.split > 1;
-    const uint32_t rank = PAIR || split ? cluster_rank() : 0;
+    const bool split = P.split > 1;
+    // of a pair: its first block's rank, which of the two this is; of a shared contraction: which part of it
+    const uint32_t rank = PAIR || split ? cluster_rank() : 0, first = rank & ~1u, half = PAIR ? rank & 1 : 0, part = PAIR ? rank >> 1 : rank;
 
     if (tid == 0) {
         abort_flag = 0;
@@ -249,12 +250,12 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
     const uint32_t tmem = tmem_at;
     pdl_wait();
 
-    const int half = (P.K + 63) / 64, steps = P.twice ? 2 * half : half;
+    const int once = (P.K + 63) / 64, steps = P.twice ? 2 * once : once;
     const int share = split ? (steps + P.split - 1) / P.split : steps;
-    const int k_first = split ? min((int)rank * share, steps) : 0, nkb = min(share, steps - k_first);  // 0: a block without a part
+    const int k_first = split ? min((int)part * share, steps) : 0, nkb = min(share, steps - k_first);  // 0: a block without a part
     const int round = WIDE ? S::ROUND : nkb;
     const int64_t tiles = (int64_t)P.lane_tiles * P.col_tiles;
-    const int64_t group = PAIR ? 2 : split ? P.split : 1, tile0 = blockIdx.x / group, tile_step = gridDim.x / group;
+    const int64_t group = (PAIR ? 2 : 1) * P.split, tile0 = blockIdx.x / group, tile_step = gridDim.x / group;
 
     // Tiles in groups of eight column tiles, lane tiles outside: what the SMs work on at one time shares its operands in L2.
     struct Tile {
@@ -264,7 +265,7 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
         const int64_t per = (int64_t)8 * P.lane_tiles, g = i / per;
         const int rest = (int)(i - g * per), wide = (int)min((int64_t)8, P.col_tiles - 8 * g);
         const int lt = rest / wide, ct = (int)(8 * g) + rest - lt * wide;
-        return Tile{(PAIR ? 256 : 128) * lt + (PAIR ? 128 * (int)rank : 0), BN * ct};
+        return Tile{(PAIR ? 256 : 128) * lt + 128 * (int)half, BN * ct};
     };
     Waits waits{&abort_flag, P.status, P.wait_ns, LAPSUM_ST_LINEAR_TIMEOUT};
 
@@ -278,17 +279,17 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
         };
         for (int64_t i = tile0; i < tiles && ok; i += tile_step) {
             const Tile t = tile_at(i);
-            const int c0 = t.c0 + (PAIR ? (int)rank * S::COLS : 0);
+            const int c0 = t.c0 + (int)half * S::COLS;
             for (int kb = 0; kb < nkb; ++kb, ++fill) {
                 const uint32_t s = fill % S::STAGES, phase = (fill / S::STAGES) & 1;
                 ok = waits.wait(empty + 8 * s, phase ^ 1);
                 ok = __all_sync(FULL, ok);
                 if (!ok || P.hold) break;
-                const uint32_t bar = PAIR ? in_block(full + 8 * s, 0) : full + 8 * s;  // a pair's first block counts for both
-                if (lane == 0 && (!PAIR || rank == 0)) mbar_expect_tx(full + 8 * s, PAIR ? 2 * S::STAGE : S::STAGE);
+                const uint32_t bar = PAIR ? in_block(full + 8 * s, first) : full + 8 * s;  // a pair's first block counts for both
+                if (lane == 0 && half == 0) mbar_expect_tx(full + 8 * s, PAIR ? 2 * S::STAGE : S::STAGE);
                 __syncwarp();
-                const bool low = k_first + kb >= half;
-                const int k0 = (k_first + kb - (low ? half : 0)) * 64;
+                const bool low = k_first + kb >= once;
+                const int k0 = (k_first + kb - (low ? once : 0)) * 64;
                 const CUtensorMap *const map_b = low ? &maps.b_low : &maps.b;
                 const uint32_t a = ring_a + s * S::A_BYTES, b = ring_b + s * S::B_BYTES;
                 if constexpr (A_MN) {
@@ -308,12 +309,12 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
         const uint32_t first = fill > S::STAGES ? fill - S::STAGES : 0;
         for (uint32_t f = first; f < fill; ++f) {
             const uint32_t s = f % S::STAGES, phase = (f / S::STAGES) & 1;
-            if (!PAIR || rank == 0) waits.plain(full + 8 * s, phase, false);
+            if (half == 0) waits.plain(full + 8 * s, phase, false);
             if (ok) waits.wait(empty + 8 * s, phase);
         }
     } else if (warp == 1) {
         // ------------------------------------------------ one thread issues the products (a pair's: one of its first block)
-        if (lane == 0 && (!PAIR || rank == 0)) {
+        if (lane == 0 && half == 0) {
             constexpr uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
             constexpr uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | ((A_MN ? 1u : 0u) << 15) | ((B_MN ? 1u : 0u) << 16) |
                                    ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((PAIR ? 256 : 128) >> 4) << 24);
@@ -336,12 +337,12 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
 #pragma unroll
                         for (int q = 0; q < 4; ++q) tc_mma<PAIR>(d, a + q * (step_a >> 4), b + q * (step_b >> 4), idesc, (kb - k0) | q ? 1 : 0);
                         any = true;
-                        tc_commit<PAIR>(empty + 8 * s);
+                        tc_commit<PAIR>(empty + 8 * s, first);
                     }
-                    if (ok) tc_commit<PAIR>(acc_full + 8 * buf);
+                    if (ok) tc_commit<PAIR>(acc_full + 8 * buf, first);
                 }
             if (!ok && any) {  // a wait ran out: the products already issued end before the block does
-                tc_commit<PAIR>(drain);
+                tc_commit<PAIR>(drain, first);
                 waits.plain(drain, 0, false);
             }
         }
@@ -407,7 +408,7 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(PAIR ? in_block(acc_empty + 8 * buf, 0) : acc_empty + 8 * buf);
+                if (lane == 0) mbar_arrive_cluster(PAIR ? in_block(acc_empty + 8 * buf, first) : acc_empty + 8 * buf);
             }
             if (!ok) break;
             if constexpr (WIDE) {
@@ -425,41 +426,38 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
     }
     __syncwarp();
     __syncthreads();
-    if constexpr (PAIR) cluster_barrier();
-    if constexpr (!PAIR) {
-        if (split) {
-            cluster_barrier();
-            const Tile t = tile_at(tile0);
-            const int l = tid & 127, per = BN / P.split;  // columns of one block: two or more, for BN >= 16 and up to eight blocks
-            const int c1 = ((int)rank + 1) * per;
-            if (t.l0 + l < P.L) {
-                const float bias = P.bias != nullptr ? load_either<T>(P.bias, t.l0 + l, P.bias_f32) : 0.f;
+    if (PAIR || split) cluster_barrier();
+    if (split) {
+        const Tile t = tile_at(tile0);
+        const int l = tid & 127, per = BN / P.split;  // columns of one block: four or more, for BN >= 16 and up to four blocks
+        const int c1 = ((int)part + 1) * per;
+        if (t.l0 + l < P.L) {
+            const float bias = P.bias != nullptr ? load_either<T>(P.bias, t.l0 + l, P.bias_f32) : 0.f;
 #pragma unroll 1
-                for (int c = (int)rank * per + 8 * (tid >> 7); c < c1 && t.c0 + c < P.C; c += 24) {
-                    float v[8] = {};
+            for (int c = (int)part * per + 8 * (tid >> 7); c < c1 && t.c0 + c < P.C; c += 24) {
+                float v[8] = {};
 #pragma unroll
-                    for (int s = 0; s < 8; ++s)
-                        if (s < P.split) {
-                            const uint32_t from = in_block(ring_a + 4 * (c * 128 + l), s);
-                            float part[8];
+                for (int s = 0; s < 4; ++s)
+                    if (s < P.split) {
+                        const uint32_t from = in_block(ring_a + 4 * (c * 128 + l), PAIR ? 2 * s + half : s);
+                        float sums[8];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[j]) : "r"(from + 512 * j) : "memory");
+                        for (int j = 0; j < 8; ++j)
+                            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(sums[j]) : "r"(from + 512 * j) : "memory");
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) v[j] += part[j];
-                        }
-                    if (per >= 8) {
-                        linear_finish<T>(P, v, t.l0 + l, t.c0 + c, bias);
-                    } else {
-                        LinearArgs Q = P;  // the next columns are another block's
-                        Q.C = min(P.C, t.c0 + c1);
-                        linear_finish<T>(Q, v, t.l0 + l, t.c0 + c, bias);
+                        for (int j = 0; j < 8; ++j) v[j] += sums[j];
                     }
+                if (per >= 8) {
+                    linear_finish<T>(P, v, t.l0 + l, t.c0 + c, bias);
+                } else {
+                    LinearArgs Q = P;  // the next columns are another block's
+                    Q.C = min(P.C, t.c0 + c1);
+                    linear_finish<T>(Q, v, t.l0 + l, t.c0 + c, bias);
                 }
             }
-            __syncwarp();
-            cluster_barrier();  // nobody leaves while others read
         }
+        __syncwarp();
+        cluster_barrier();  // nobody leaves while others read
     }
     if (warp == 2) {
         tc_fence_after();

@@ -40,7 +40,7 @@ int linear_layout(const lapsum_linear_dims *p, LinearLayout &X, lapsum_linear_la
 // Tiles of a product of L lanes, C columns and K along the contraction.  For every form of tile the time is taken as rounds of the SMs times
 // (steps of 64 x clocks per step + the tile's own time), and the least wins.  Clocks per step: the tensor core's 2 x BN, or the operands' bytes
 // at BYTES_PER_CLOCK for each SM, whichever is more; a pair of blocks shares its operands.  A shared contraction costs its join.
-// Measured, tile columns / blocks per tile, us: 1021 x 2048 x 5632 128 43, 128 / 2 52, 256 / 2 39, pairs 47; 512 x 2048 x 2048 64 19, 128 21, 128 / 2 19,
+// Measured, tile columns / blocks per tile, us: 1021 x 2048 x 5632 128 41, 128 / 2 49, 256 / 2 35, pairs 45, pairs / 2 33; 512 x 2048 x 2048 64 19, 128 18, 128 / 2 18,
 // 128 / 4 27; 16384 x 8192 x 2048 128 617, 256 461, pairs 428 (of 224 columns, which leave no round half empty, 4 % slower: the power limit); 65536 x 128 x 2048 64 84, 128 70, 256 68, pairs 86; 48 x 2048 x 1024 64 15, 64 / 4 14, 64 / 8 21.
 constexpr double BYTES_PER_CLOCK = 45.0;
 struct Choice {
@@ -65,8 +65,11 @@ Choice choose(int64_t L, int64_t C, int64_t K, bool b_mn, int sms)
         }
     }
     const int64_t tiles = ceil_div(L, 256) * ceil_div(C, 256);
-    const double t = (double)ceil_div(tiles, sms / 2) * ((double)steps * 256 * 128 / BYTES_PER_CLOCK + 2560.0);
-    if (t < least && C > 128) best = Choice{256, 1, true};
+    for (int split = 1; split <= 2 && C > 128; split *= 2) {
+        if (split > 1 && (steps < 4 * split || 2 * split * tiles > sms)) break;
+        const double t = (double)ceil_div(2 * split * tiles, sms) * ((double)ceil_div(steps, split) * 256 * 128 / BYTES_PER_CLOCK + 2560.0) + (split > 1 ? 7120.0 : 0.0);
+        if (t < least) least = t, best = Choice{256, split, true};
+    }
     return best;
 }
 
@@ -82,8 +85,8 @@ int run_tiles(const LinearMaps &maps, const LinearArgs &A, int sms, cudaStream_t
         CU_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
         dev_ready = dev;
     }
-    const int64_t tiles = (int64_t)A.lane_tiles * A.col_tiles, units = PAIR ? sms / 2 : A.split > 1 ? tiles : sms;
-    const int cluster = PAIR ? 2 : A.split;
+    const int64_t tiles = (int64_t)A.lane_tiles * A.col_tiles, units = A.split > 1 ? tiles : PAIR ? sms / 2 : sms;
+    const int cluster = (PAIR ? 2 : 1) * A.split;
     return launch_clusters((unsigned)cluster, kernel, (unsigned)((tiles < units ? tiles : units) * cluster), S::THREADS, S::SMEM, st, maps, A);
 }
 template <bool A_MN, bool B_MN, bool WIDE, typename T>

@@ -126,11 +126,11 @@ __device__ __forceinline__ void tmem_wait_ld(float (&v)[16])
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 template <bool PAIR>
-__device__ __forceinline__ void tc_commit(uint32_t bar)  // PAIR: on the barrier of this name in both blocks
+__device__ __forceinline__ void tc_commit(uint32_t bar, uint32_t first = 0)  // PAIR: on the barrier of this name in both blocks, of ranks first and first + 1
 {
     if constexpr (PAIR)
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                     "h"((uint16_t)3)
+                     "h"((uint16_t)(3u << first))
                      : "memory");
     else
         asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");

@@ -117,7 +117,7 @@ def test_back_to_back_calls_that_overlap_see_each_other_s_results():
     assert all(torch.equal(o[0], x) and torch.equal(o[1], y) for o in outs)
 
 
-@pytest.mark.parametrize("rows,n,k", [(48, 1000, 512), (600, 600, 256), (4096, 2048, 512), (16, 128, 4096)])
+@pytest.mark.parametrize("rows,n,k", [(48, 1000, 512), (600, 600, 256), (4096, 2048, 512), (16, 128, 4096), (1021, 2048, 5632)])
 def test_waits_that_run_out_end_with_a_status(rows, n, k):
     ws = L.LinearWorkspace(rows, n, k)
     x, w, y = (torch.zeros(*s, device="cuda", dtype=torch.bfloat16) for s in ((rows, k), (n, k), (rows, n)))

@@ -113,6 +113,12 @@ def test_fp32_results_keep_fp32_digits_over_a_long_contraction(rows, n, k):
         assert (got[name].double() - value).norm() <= 2.0 ** -17 * value.norm(), name
 
 
+@pytest.mark.parametrize("rows,n,k,out", [(1021, 2048, 5632, "same"), (1000, 2040, 4104, "f32"), (129, 300, 2048, "f32"), (512, 1024, 1000, "same"), (300, 4000, 8192, "same")])
+def test_shared_contractions(rows, n, k, out):
+    run(rows, n, k, bias="same", residual=True, out=out, extra=1, seed=k)
+    run(rows, n, k, act="silu", bias="f32", out=out, backward=True, grad_w="f32", seed=k)
+
+
 def test_no_rows():
     ws = L.LinearWorkspace(4, 16, 8, training=True)
     e = torch.empty(0, 8, device="cuda", dtype=torch.bfloat16)
