@@ -42,6 +42,7 @@ struct LinearArgs {
     int act, out_f32, bias_f32, pre_f32;
     int twice;             // the contraction runs over (a, b), then over (a, b_low)
     int split;             // blocks of a cluster that share the contraction of one tile
+    int parts;             // of the contraction, each a block's of its own, whose results lie one behind the other (fp32, C rows each)
     int hold;              // test hook: the producer brings nothing, so the waits run out
     uint32_t *status;
     unsigned long long wait_ns;
@@ -152,7 +153,7 @@ __device__ __forceinline__ void store_rows(void *base, int64_t at, int64_t strid
 }
 // N values of lane l, rows r0 .. : bias, pre-activation, activation, residual, result
 template <typename T, int N>
-__device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N], int l, int r0, float bias)
+__device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N], int l, int r0, float bias, int64_t shift = 0)
 {
     const int n = P.C - r0;
     float res[N];
@@ -177,7 +178,7 @@ __device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N]
 #pragma unroll
         for (int j = 0; j < N; ++j) v[j] += res[j];
     }
-    const int64_t at = (int64_t)r0 * P.out_stride + l;
+    const int64_t at = shift + (int64_t)r0 * P.out_stride + l;
     if (P.out_f32) store_rows<float>(P.out, at, P.out_stride, n, v);
     else store_rows<T>(P.out, at, P.out_stride, n, v);
 }
@@ -187,6 +188,7 @@ __device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N]
 // into one of two accumulators in TMEM, warps 4 to 11 (two sets of four; a set reads the 128 lanes) finish the previous tile.
 //   PAIR   a cluster of two blocks works on one 256 x 256 tile (cta_group::2): each block brings 128 rows of A and half of B, 64 bytes per
 //          clock of tensor work instead of the 96 that a 128 x 256 tile of one block needs.
+//   parts  the same without a cluster: blocks of their own leave fp32 results one behind the other, for linear_parts_kernel to add.
 //   WIDE   the tensor core's own additions truncate: an error of about 2^-25 of the sum each, all towards zero, 2e-6 at K = 2048 and 2e-5 at 16384.
 //          That is nothing to a 16-bit result.  For an fp32 result an accumulator takes ROUND steps (512 of the contraction), and the epilogue adds
 //          the rounds' sums in fp32 registers, rounded to nearest, while the next round is computed in the other accumulator: 5e-7.
@@ -218,7 +220,7 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
     __shared__ uint32_t tmem_at;
     __shared__ int abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const bool split = P.split > 1;
+    const bool split = P.split > 1, spread = !PAIR && P.parts > 1;
     // of a pair: its first block's rank, which of the two this is; of a shared contraction: which part of it
     const uint32_t rank = PAIR || split ? cluster_rank() : 0, first = rank & ~1u, half = PAIR ? rank & 1 : 0, part = PAIR ? rank >> 1 : rank;
 
@@ -251,12 +253,13 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
     pdl_wait();
 
     const int once = (P.K + 63) / 64, steps = P.twice ? 2 * once : once;
-    const int share = split ? (steps + P.split - 1) / P.split : steps;
-    const int k_first = split ? min((int)part * share, steps) : 0, nkb = min(share, steps - k_first);  // 0: a block without a part
-    const int round = WIDE ? S::ROUND : nkb;
+    const int ways = spread ? P.parts : P.split, share = (steps + ways - 1) / ways;
     const int64_t tiles = (int64_t)P.lane_tiles * P.col_tiles;
-    const int64_t group = (PAIR ? 2 : 1) * P.split, tile0 = blockIdx.x / group, tile_step = gridDim.x / group;
-
+    const int64_t group = (PAIR ? 2 : 1) * P.split, tile0 = spread ? blockIdx.x % tiles : blockIdx.x / group, tile_step = spread ? tiles : gridDim.x / group;
+    const int mine = spread ? (int)(blockIdx.x / tiles) : (int)part;  // which part of the contraction
+    const int64_t shift = spread ? (int64_t)mine * P.C * P.out_stride : 0;
+    const int k_first = split || spread ? min(mine * share, steps) : 0, nkb = min(share, steps - k_first);
+    const int round = WIDE ? S::ROUND : nkb;
     // Tiles in groups of eight column tiles, lane tiles outside: what the SMs work on at one time shares its operands in L2.
     struct Tile {
         int l0, c0;
@@ -371,7 +374,7 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
                     for (int j = 0; j < 16; ++j)
                         asm volatile("st.shared.f32 [%0], %1;" ::"r"(ring_a + 4 * ((c0 + j) * 128 + 32 * ew + lane)), "f"(v[j]) : "memory");
                 } else if (l < P.L) {
-                    linear_finish<T>(P, v, l, t.c0 + c0, bias);
+                    linear_finish<T>(P, v, l, t.c0 + c0, bias, shift);
                 }
             };
             float sum[WIDE ? S::CHUNKS : 1][16];
@@ -466,6 +469,20 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
         else
             asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(S::TMEM) : "memory");
     }
+}
+
+// The parts' results added in order: a long contraction for few tiles (the gradients of a router's weights) that clusters do not spread over the SMs.
+template <typename T>
+__global__ void __launch_bounds__(256) linear_parts_kernel(const float *partial, int parts, int C, int L, void *out, int64_t out_stride, int out_f32)
+{
+    pdl_wait();
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)C * L;
+    if (i >= n) return;
+    float s = 0.f;
+#pragma unroll 8
+    for (int p = 0; p < parts; ++p) s += ld(partial + p * n + i);
+    const int64_t c = i / L;
+    store_either<T>(out, c * out_stride + i - c * L, out_f32, s);
 }
 
 // ------------------------------------------------------------- a few rows ----

@@ -12,10 +12,15 @@ using namespace lapsum;
 namespace {
 
 struct LinearLayout {
-    size_t off_dp, off_low, off_partial;
+    size_t off_dp, off_low, off_partial, off_parts;
     int64_t ld, parts;  // row stride of pre and dP, blocks of rows of the bias' partial sums
 };
 
+// A gradient whose tiles are fewer than an eighth of the SMs, with a long contraction: as many parts of it as fill the SMs, of 16 steps of 64 at least, each with
+// a tile's fp32 results in the workspace.  Measured, dW without / with parts, us: 65536 x 128 x 2048 86 / 71, in fp32 186 / 130; 65536 x 64 x 512 83 / 30, 177 / 56;
+// 65536 x 11 x 72 100 / 36; 4096 x 128 x 256 17 / 16; dx of 100 x 60000 x 128 78 / 22.
+constexpr int PARTS_UNITS = 148;
+constexpr size_t PARTS_BYTES = (size_t)PARTS_UNITS * 128 * 128 * 4;
 int linear_layout(const lapsum_linear_dims *p, LinearLayout &X, lapsum_linear_layout *out)
 {
     if (!p) return LAPSUM_ERR_NULL;
@@ -31,6 +36,7 @@ int linear_layout(const lapsum_linear_dims *p, LinearLayout &X, lapsum_linear_la
     X.off_dp = at, at += p->training ? align_up((size_t)p->rows * (size_t)X.ld * 2) : 0;
     X.off_low = at, at += p->training ? align_up((size_t)p->rows * (size_t)X.ld * 2) : 0;
     X.off_partial = at, at += p->training ? align_up((size_t)grad_blocks_most(p->rows) * (size_t)p->n * 4) : 0;
+    X.off_parts = at, at += p->training ? PARTS_BYTES : 0;
     out->workspace_bytes = at;
     out->pre_bytes = p->training && p->activation != LAPSUM_ACT_NONE ? (size_t)p->rows * (size_t)X.ld * (p->pre_dtype == LAPSUM_IO_F32 ? 4 : 2) : 0;
     out->pre_stride = X.ld;
@@ -85,9 +91,9 @@ int run_tiles(const LinearMaps &maps, const LinearArgs &A, int sms, cudaStream_t
         CU_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
         dev_ready = dev;
     }
-    const int64_t tiles = (int64_t)A.lane_tiles * A.col_tiles, units = A.split > 1 ? tiles : PAIR ? sms / 2 : sms;
+    const int64_t tiles = (int64_t)A.lane_tiles * A.col_tiles, units = A.split > 1 || A.parts > 1 ? tiles * A.parts : PAIR ? sms / 2 : sms;
     const int cluster = (PAIR ? 2 : 1) * A.split;
-    return launch_clusters((unsigned)cluster, kernel, (unsigned)((tiles < units ? tiles : units) * cluster), S::THREADS, S::SMEM, st, maps, A);
+    return launch_clusters((unsigned)cluster, kernel, (unsigned)((tiles * A.parts < units ? tiles * A.parts : units) * cluster), S::THREADS, S::SMEM, st, maps, A);
 }
 template <bool A_MN, bool B_MN, bool WIDE, typename T>
 int run_choice(const LinearMaps &m, const LinearArgs &A, const Choice &ch, int sms, cudaStream_t st)
@@ -112,13 +118,26 @@ struct Operand {
 };
 
 // One product.  A: [L][K] or, A_MN, [K][L]; B: [C][K] or, B_MN, [K][C].
+// `partial`: room for parts of the contraction (PARTS_BYTES), gradients only.
 template <bool A_MN, bool B_MN, typename T>
-int product(const Operand &a, const Operand &b, LinearArgs A, int dtype, cudaStream_t st, const void *low = nullptr)
+int product(const Operand &a, const Operand &b, LinearArgs A, int dtype, cudaStream_t st, float *partial = nullptr, const void *low = nullptr)
 {
     int sms = 0;
     RUN(sm_count(&sms));
     A.twice = low != nullptr;
-    const Choice ch = choose(A.L, A.C, A.K * (low ? 2ll : 1ll), B_MN, sms);
+    Choice ch = choose(A.L, A.C, A.K * (low ? 2ll : 1ll), B_MN, sms);
+    const LinearArgs whole = A;
+    if (partial) {
+        const int64_t steps = ceil_div(A.K, 64) * (low ? 2 : 1), bn = A.C > 64 ? 128 : 64, tiles = ceil_div(A.L, 128) * ceil_div(A.C, bn);
+        int64_t parts = PARTS_UNITS / tiles;
+        if (parts > steps / 16) parts = steps / 16;
+        if (parts >= 8) {
+            parts = ceil_div(steps, ceil_div(steps, parts));  // none without a part
+            ch = Choice{(int)bn, 1, false};
+            A.parts = (int)parts;
+            A.out = partial, A.out_stride = A.L, A.out_f32 = 1;
+        }
+    }
     A.split = ch.split;
     A.lane_tiles = (int)ceil_div(A.L, ch.pair ? 256 : 128), A.col_tiles = (int)ceil_div(A.C, ch.bn);
     LinearMaps m;
@@ -126,6 +145,13 @@ int product(const Operand &a, const Operand &b, LinearArgs A, int dtype, cudaStr
     RUN(map_2d(&m.b, dtype, b.base, b.cols, b.rows, b.stride, B_MN ? 64 : ch.pair ? 128 : ch.bn));
     m.b_low = m.b;
     if (low) RUN(map_2d(&m.b_low, dtype, low, b.cols, b.rows, b.stride, B_MN ? 64 : ch.pair ? 128 : ch.bn));
+    if constexpr (A_MN) {
+        if (A.parts > 1) {
+            RUN((ch.bn == 128 ? run_tiles<A_MN, B_MN, 128, false, true, T>(m, A, sms, st) : run_tiles<A_MN, B_MN, 64, false, true, T>(m, A, sms, st)));
+            return launch_pdl(linear_parts_kernel<T>, (unsigned)ceil_div((int64_t)A.C * A.L, 256), 256, 0, st, partial, A.parts, A.C, A.L, whole.out,
+                              whole.out_stride, whole.out_f32);
+        }
+    }
     if constexpr (A_MN && !B_MN) return run_choice<A_MN, B_MN, false, T>(m, A, ch, sms, st);  // grad_x is 16-bit
     else return A.out_f32 ? run_choice<A_MN, B_MN, true, T>(m, A, ch, sms, st) : run_choice<A_MN, B_MN, false, T>(m, A, ch, sms, st);
 }
@@ -156,7 +182,7 @@ LinearArgs base_args(void *ws)
 {
     LinearArgs A;
     std::memset(&A, 0, sizeof(A));
-    A.split = 1;
+    A.split = A.parts = 1;
     A.status = static_cast<uint32_t *>(ws);
     A.wait_ns = 2000000000ull;
     return A;
@@ -199,15 +225,16 @@ int backward_t(const lapsum_linear_dims &p, const LinearLayout &X, const void *g
     }
     const Operand dp = direct ? Operand{grad_y, p.n, p.rows, gy_stride} : Operand{ws + X.off_dp, p.n, p.rows, X.ld};
     LinearArgs A = base_args(ws);
+    float *const partial = reinterpret_cast<float *>(ws + X.off_parts);
     if (grad_x) {
         A.out = grad_x, A.out_stride = gx_stride, A.out_f32 = 0;
         A.L = (int)p.k, A.C = (int)p.rows, A.K = (int)p.n;
-        RUN((product<true, false, T>(Operand{w, p.k, p.n, p.k}, dp, A, p.io_dtype, st)));
+        RUN((product<true, false, T>(Operand{w, p.k, p.n, p.k}, dp, A, p.io_dtype, st, partial)));
     }
     if (grad_w) {
         A.out = grad_w, A.out_stride = p.k, A.out_f32 = p.grad_w_dtype == LAPSUM_IO_F32;
         A.L = (int)p.k, A.C = (int)p.n, A.K = (int)p.rows;
-        RUN((product<true, true, T>(Operand{x, p.k, p.rows, x_stride}, dp, A, p.io_dtype, st, keep_low ? ws + X.off_low : nullptr)));
+        RUN((product<true, true, T>(Operand{x, p.k, p.rows, x_stride}, dp, A, p.io_dtype, st, partial, keep_low ? ws + X.off_low : nullptr)));
     }
     return LAPSUM_OK;
 }

@@ -119,6 +119,14 @@ def test_shared_contractions(rows, n, k, out):
     run(rows, n, k, act="silu", bias="f32", out=out, backward=True, grad_w="f32", seed=k)
 
 
+@pytest.mark.parametrize("rows,n,k,grad_w,act", [(20011, 11, 72, "f32", "none"), (9000, 130, 256, "same", "silu"), (300, 6011, 136, "f32", "gelu"), (40, 9000, 64, "same", "none"),
+                                                   (16384, 1, 8, "f32", "silu"), (3000, 64, 520, "same", "relu")])
+def test_gradients_of_few_tiles_and_a_long_contraction(rows, n, k, grad_w, act):
+    a = run(rows, n, k, act=act, bias="f32", backward=True, grad_w=grad_w, extra=1, seed=n)
+    b = run(rows, n, k, act=act, bias="f32", backward=True, grad_w=grad_w, extra=1, seed=n)
+    assert all(torch.equal(a[name], b[name]) for name in a)
+
+
 def test_no_rows():
     ws = L.LinearWorkspace(4, 16, 8, training=True)
     e = torch.empty(0, 8, device="cuda", dtype=torch.bfloat16)
