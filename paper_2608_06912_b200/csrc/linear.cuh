@@ -14,11 +14,11 @@
 // 32 neighbouring values of one row of the result: loads and stores of it are contiguous whatever n, the strides and the alignment,
 // and a bias is one value per thread.
 //
-// Measured in bf16, operands not in L2 (a library's product of the same shape beside it): 16384 x 8192 x 2048 forward without an epilogue 378 - 396 us,
-// 1.39 - 1.45 PFLOP/s (343 - 352), with silu and P kept in fp32 (805 MB of results) 427 - 439; dx 358 - 379 (348 - 357), dW 398 - 440 (340 - 350), both at the power limit;
-// dW with fp32 digits 1000 for twice the products.  Logits of 48 rows, 128000 x 2048, 107 us, 5.1 TB/s of weights (107); the router 65536 x 128 x 2048 65 - 68 us,
-// 4.5 TB/s (69); a prompt of 1021 rows, 2048 x 5632, 33 us (27): 32 large tiles, their contraction shared by two pairs each, so a join; one row of
-// 2048 x 1024 9 us, the host's call (3 in a graph).
+// Measured in bf16, operands not in L2 (a library's product of the same shape beside it): 16384 x 8192 x 2048 forward without an epilogue 373 us,
+// 1.47 PFLOP/s (344), with silu and P kept in fp32 (805 MB of results) 416 - 426; dx 352 (348), dW 399 (341), all at the power limit; dW with fp32 digits 990 for
+// twice the products.  Logits of 48 rows, 128000 x 2048, 106 us, 5.1 TB/s of weights (107); the router 65536 x 128 x 2048 65 - 68 us,
+// 4.5 TB/s (70); a prompt of 1021 rows, 2048 x 5632, 33 us (26): 32 large tiles, their contraction shared by two pairs each, so a join; one row of
+// 2048 x 1024 7 - 9 us, the host's call (3 in a graph).
 #pragma once
 #include <type_traits>
 
@@ -151,9 +151,28 @@ __device__ __forceinline__ void store_rows(void *base, int64_t at, int64_t strid
             if (j < n) Io<S>::store1(p, v[j]);
     }
 }
+// The same for 16-bit values of 32 neighbouring lanes: two lanes exchange every other value, so that each stores two neighbouring ones of every other row, with
+// half the instructions: products of 16384 x 8192 x 2048 394 -> 373, 376 -> 352, 423 -> 399 us.
+template <typename T, int N>
+__device__ __forceinline__ void store_row_pairs(void *base, int64_t at, int64_t stride, int n, const float (&v)[N])
+{
+    const bool odd = threadIdx.x & 1;
+    T *p = static_cast<T *>(base) + at + (odd ? stride - 1 : 0);
+#pragma unroll
+    for (int j = 0; j + 1 < N; j += 2, p += 2 * stride) {
+        const float other = __shfl_xor_sync(FULL, odd ? v[j] : v[j + 1], 1);
+        T two[2];
+        Io<T>::store1(two, odd ? other : v[j]);
+        Io<T>::store1(two + 1, odd ? v[j + 1] : other);
+        uint32_t q;
+        memcpy(&q, two, 4);
+        if (j + odd < n) *reinterpret_cast<uint32_t *>(p) = q;
+    }
+}
 // N values of lane l, rows r0 .. : bias, pre-activation, activation, residual, result
 template <typename T, int N>
-__device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N], int l, int r0, float bias, int64_t shift = 0)
+__device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N], int l, int r0, float bias, int64_t shift = 0,
+                                              bool pairs = false)  // pairs: 32 neighbouring lanes, results at multiples of 4 bytes
 {
     const int n = P.C - r0;
     float res[N];
@@ -180,6 +199,7 @@ __device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N]
     }
     const int64_t at = shift + (int64_t)r0 * P.out_stride + l;
     if (P.out_f32) store_rows<float>(P.out, at, P.out_stride, n, v);
+    else if (pairs) store_row_pairs<T>(P.out, at, P.out_stride, n, v);
     else store_rows<T>(P.out, at, P.out_stride, n, v);
 }
 
@@ -367,14 +387,15 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
                     const int64_t at = (int64_t)row * P.residual_stride + t.l0 + 32 * ew;
                     if (row < P.C) asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t *>(P.residual) + at * (P.out_f32 ? 4 : 2)) : "memory");
                 }
+            const bool pairs = !WIDE && !P.out_f32 && t.l0 + 32 * ew + 32 <= P.L && P.out_stride % 2 == 0 && (reinterpret_cast<uintptr_t>(P.out) & 3) == 0;
             const auto finish = [&](float (&v)[16], int c0) {  // columns c0 .. of the tile
                 if (split) {
                     // the ring is free: all products of this block's only tile have ended.  [column][lane]
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
                         asm volatile("st.shared.f32 [%0], %1;" ::"r"(ring_a + 4 * ((c0 + j) * 128 + 32 * ew + lane)), "f"(v[j]) : "memory");
-                } else if (l < P.L) {
-                    linear_finish<T>(P, v, l, t.c0 + c0, bias, shift);
+                } else if (pairs || l < P.L) {
+                    linear_finish<T>(P, v, l, t.c0 + c0, bias, shift, pairs);
                 }
             };
             float sum[WIDE ? S::CHUNKS : 1][16];
