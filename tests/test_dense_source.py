@@ -16,7 +16,7 @@ def test_no_load_promises_that_its_data_stays_constant(name):
 def test_the_last_kernel_of_a_call_lets_no_other_start_early():
     """Its results go to any kernel of the library, some of which read their inputs through the non-coherent path."""
     text = code("linear.cuh")
-    for kernel in ("linear_kernel", "linear_few_kernel", "linear_bias_kernel"):
+    for kernel in ("linear_kernel", "linear_few_kernel", "linear_bias_kernel", "linear_parts_kernel"):
         assert "launch_dependents" not in body(text, kernel), kernel
     text = code("embed.cuh")
     for kernel in ("embed_forward_kernel", "embed_join_kernel"):
@@ -26,7 +26,7 @@ def test_the_last_kernel_of_a_call_lets_no_other_start_early():
 
 
 def test_every_kernel_waits_for_the_one_before_it():
-    for name, kernels in (("linear.cuh", ("linear_kernel", "linear_few_kernel", "linear_grad_kernel", "linear_bias_kernel")),
+    for name, kernels in (("linear.cuh", ("linear_kernel", "linear_few_kernel", "linear_grad_kernel", "linear_bias_kernel", "linear_parts_kernel")),
                           ("embed.cuh", ("embed_forward_kernel", "embed_sort_kernel", "embed_grad_kernel", "embed_join_kernel")),
                           ("sample.cuh", ("sample_kernel",))):
         for kernel in kernels:

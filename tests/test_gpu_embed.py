@@ -64,9 +64,9 @@ def test_backward(n, vocab, d, dtype, wide):
     backward(draw_ids(n, vocab, seed=n), vocab, d, dtype, scale=1.5, wide=wide)
 
 
-@pytest.mark.parametrize("count", [31, 32, 33, 63, 64, 65, 96, 97, 4096])
+@pytest.mark.parametrize("count", [15, 16, 17, 31, 32, 33, 63, 64, 65, 96, 97, 4096])
 def test_rows_of_many_positions_wherever_their_pieces_begin(count):
-    for before in (0, 1, 31, 32, 40):
+    for before in (0, 1, 15, 16, 31, 32, 40):
         ids = torch.cat([torch.arange(before), torch.full((count,), 50), torch.arange(51, 60)]).to(torch.int32)
         ids = ids[torch.randperm(len(ids), generator=torch.Generator().manual_seed(count))].cuda()
         backward(ids, 64, 24, "f32")
