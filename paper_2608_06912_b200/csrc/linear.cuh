@@ -43,6 +43,7 @@ struct LinearArgs {
     int twice;             // the contraction runs over (a, b), then over (a, b_low)
     int split;             // blocks of a cluster that share the contraction of one tile
     int parts;             // of the contraction, each a block's of its own, whose results lie one behind the other (fp32, C rows each)
+    const uint32_t *largest;  // fp16 gradients: the largest |dP| of every column of the result, by which its operand was scaled (grad_scale), or null
     int hold;              // test hook: the producer brings nothing, so the waits run out
     uint32_t *status;
     unsigned long long wait_ns;
@@ -122,6 +123,12 @@ __device__ __forceinline__ void store_either(void *p, int64_t i, bool f32, float
     else Io<T>::store1(static_cast<T *>(p) + i, v);
 }
 
+// fp16 ends at 6e-8 and at 65504, so there dP takes a power of two per row (for dx) or column (for dW) that brings the largest finite one of it, whose
+// bits these are, to between 2^14 and 2^15; the products' epilogues take it back.  Both are exact, and +-126 at most, so that neither is subnormal.
+__device__ __forceinline__ uint32_t grad_scale_exponent(uint32_t largest) { return min(268 - (largest >> 23), 253u); }
+__device__ __forceinline__ float grad_scale(uint32_t largest) { return __uint_as_float(grad_scale_exponent(largest) << 23); }
+__device__ __forceinline__ float grad_unscale(uint32_t largest) { return __uint_as_float((254 - grad_scale_exponent(largest)) << 23); }
+
 // n of N values, `stride` apart
 template <typename S, int N>
 __device__ __forceinline__ void load_rows(const void *base, int64_t at, int64_t stride, int n, float (&v)[N])
@@ -180,6 +187,12 @@ __device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N]
         const int64_t at = (int64_t)r0 * P.residual_stride + l;
         if (P.out_f32) load_rows<float>(P.residual, at, P.residual_stride, n, res);
         else load_rows<T>(P.residual, at, P.residual_stride, n, res);
+    }
+    if constexpr (std::is_same<T, __half>::value) {
+        if (P.largest != nullptr) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] *= j < n ? grad_unscale(ld(P.largest + r0 + j)) : 0.f;
+        }
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) v[j] += bias;
@@ -494,7 +507,8 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
 
 // The parts' results added in order: a long contraction for few tiles (the gradients of a router's weights) that clusters do not spread over the SMs.
 template <typename T>
-__global__ void __launch_bounds__(256) linear_parts_kernel(const float *partial, int parts, int C, int L, void *out, int64_t out_stride, int out_f32)
+__global__ void __launch_bounds__(256) linear_parts_kernel(const float *partial, int parts, int C, int L, void *out, int64_t out_stride, int out_f32,
+                                                           const uint32_t *largest)
 {
     pdl_wait();
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)C * L;
@@ -503,6 +517,7 @@ __global__ void __launch_bounds__(256) linear_parts_kernel(const float *partial,
 #pragma unroll 8
     for (int p = 0; p < parts; ++p) s += ld(partial + p * n + i);
     const int64_t c = i / L;
+    if (largest != nullptr) s *= grad_unscale(ld(largest + c));
     store_either<T>(out, c * out_stride + i - c * L, out_f32, s);
 }
 
@@ -558,6 +573,10 @@ __global__ void __launch_bounds__(256) linear_few_kernel(const T *x, int64_t x_s
 // One rounding of dP is of the size of a 16-bit result's own.  Where grad_w is fp32 it would be the largest error by far (2^-9 against
 // 2^-20), so there what the rounding left is kept in 16 bits as well, and the contraction of dW runs over both: twice the products for
 // gradients with the digits of an fp32 sum (3e-6).
+// fp16's range would cut small dP off and make large ones infinite, so there dP is written scaled, by rows for dx and by columns for dW (a factor has to stay the
+// same along the contraction), and linear_largest_kernel finds the largest of each first.  Within a row or column the two 16-bit parts reach 2^-40 of the largest.
+// What that costs, us of the backward without / with it: 777 x 1003 x 520 with gelu 27 / 32; 16384 x 8192 x 2048 with silu 1121 / 1346 (another pass over dy and P),
+// with an fp32 grad_w 1563 / 1973 (two: dx's operand takes the room of dW's after its product).
 // Rows of a block: 64, or as few as 16 while there are no 128 blocks of rows.
 inline int64_t grad_blocks_most(int64_t rows)  // never less for more rows, for workspaces
 {
@@ -568,8 +587,10 @@ inline int grad_block_rows(int64_t rows) { return rows <= 128 * 16 ? 16 : rows <
 struct LinearGradArgs {
     const void *grad_y;  // fp32 (y_f32) or T
     const void *pre;     // fp32 (pre_f32) or T, null without an activation
-    void *dp;            // T, null where grad_y itself serves
+    void *dp;            // T, null where grad_y itself serves; scaled by columns where col_largest is given
     void *dp_low;        // T, dP less its rounding, null where grad_w is 16-bit
+    void *dp_rows;       // T, dP scaled by rows, or null
+    uint32_t *row_largest, *col_largest;  // bits of the largest finite |dP| of every row, of every column; either may be null
     float *partial;      // [blocks of rows][n], null without a bias
     int64_t y_stride, pre_stride, dp_stride, rows;
     int n, y_f32, pre_f32, block_rows;
@@ -579,62 +600,94 @@ __device__ __forceinline__ void load8f(const float *p, float (&x)[8])
     const float4 a = ld(reinterpret_cast<const float4 *>(p)), b = ld(reinterpret_cast<const float4 *>(p) + 1);
     x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
 }
+// A lane's eight columns of a row, from c on: side by side (VEC), or 32 apart, so that single values are read side by side as well
 template <typename T, int ACT, bool VEC>
-__global__ void __launch_bounds__(256) linear_grad_kernel(const LinearGradArgs P)
+__device__ __forceinline__ void load_dp(const LinearGradArgs &P, int64_t r, int c, float (&g)[8])
+{
+    float p[8];
+    if (VEC) {
+        if (P.y_f32) load8f(static_cast<const float *>(P.grad_y) + r * P.y_stride + c, g);
+        else Io<T>::unpack(ld(reinterpret_cast<const uint4 *>(static_cast<const T *>(P.grad_y) + r * P.y_stride + c)), g);
+        if constexpr (ACT != LAPSUM_ACT_NONE) {
+            if (P.pre_f32) load8f(static_cast<const float *>(P.pre) + r * P.pre_stride + c, p);
+            else Io<T>::unpack(ld(reinterpret_cast<const uint4 *>(static_cast<const T *>(P.pre) + r * P.pre_stride + c)), p);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            g[i] = c + 32 * i < P.n ? load_either<T>(P.grad_y, r * P.y_stride + c + 32 * i, P.y_f32) : 0.f;
+            if constexpr (ACT != LAPSUM_ACT_NONE) p[i] = c + 32 * i < P.n ? load_either<T>(P.pre, r * P.pre_stride + c + 32 * i, P.pre_f32) : 0.f;
+        }
+    }
+    if constexpr (ACT != LAPSUM_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] *= slope_of<ACT>(p[i]);
+    }
+}
+// The same columns of a row of `to`
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_dp(const LinearGradArgs &P, void *to, int64_t r, int c, const float (&v)[8])
+{
+    T *const at = static_cast<T *>(to) + r * P.dp_stride + c;
+    if (VEC) {
+        *reinterpret_cast<uint4 *>(at) = Io<T>::pack(v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + 32 * i < P.n) Io<T>::store1(at + 32 * i, v[i]);
+    }
+}
+template <typename T, int ACT, bool VEC>
+__global__ void __launch_bounds__(256, 2) linear_grad_kernel(const LinearGradArgs P)
 {
     pdl_wait();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ float part[8][256];
-    // eight columns of a lane: side by side (VEC), or 32 apart, so that single values are read side by side as well
     constexpr int STEP = VEC ? 1 : 32;
+    constexpr bool SCALED = std::is_same<T, __half>::value;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = (int)blockIdx.y * 256 + (VEC ? 8 * lane : lane);
     const int64_t row0 = (int64_t)blockIdx.x * P.block_rows, row1 = min(P.rows, row0 + P.block_rows);
     float sum[8] = {};
     if (c < P.n) {
-#pragma unroll 2
-        for (int64_t r = row0 + warp; r < row1; r += 8) {
-            float g[8], p[8];
-            if (VEC) {
-                if (P.y_f32) load8f(static_cast<const float *>(P.grad_y) + r * P.y_stride + c, g);
-                else Io<T>::unpack(ld(reinterpret_cast<const uint4 *>(static_cast<const T *>(P.grad_y) + r * P.y_stride + c)), g);
-                if constexpr (ACT != LAPSUM_ACT_NONE) {
-                    if (P.pre_f32) load8f(static_cast<const float *>(P.pre) + r * P.pre_stride + c, p);
-                    else Io<T>::unpack(ld(reinterpret_cast<const uint4 *>(static_cast<const T *>(P.pre) + r * P.pre_stride + c)), p);
-                }
-            } else {
+        float by_col[SCALED ? 8 : 1];
+        if constexpr (SCALED) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    g[i] = c + STEP * i < P.n ? load_either<T>(P.grad_y, r * P.y_stride + c + STEP * i, P.y_f32) : 0.f;
-                    if constexpr (ACT != LAPSUM_ACT_NONE) p[i] = c + STEP * i < P.n ? load_either<T>(P.pre, r * P.pre_stride + c + STEP * i, P.pre_f32) : 0.f;
-                }
-            }
-            if constexpr (ACT != LAPSUM_ACT_NONE) {
+            for (int i = 0; i < 8; ++i) by_col[i] = P.col_largest != nullptr && c + STEP * i < P.n ? grad_scale(ld(P.col_largest + c + STEP * i)) : 1.f;
+        }
+        // two rows at a time: stores of one would hold up the next one's loads
+        for (int64_t r0 = row0 + warp; r0 < row1; r0 += 16) {
+            float both[2][8], by_row[2] = {1.f, 1.f};
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] *= slope_of<ACT>(p[i]);
+            for (int q = 0; q < 2; ++q) {
+                const int64_t r = min(r0 + 8 * q, row1 - 1);
+                load_dp<T, ACT, VEC>(P, r, c, both[q]);
+                if constexpr (SCALED) by_row[q] = P.dp_rows != nullptr ? grad_scale(ld(P.row_largest + r)) : 1.f;
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += g[i];
-            if (P.dp != nullptr) {
-                const uint4 q = Io<T>::pack(g);
-                float h[8];
-                Io<T>::unpack(q, h);
-                const int64_t at = r * P.dp_stride + c;
-                if (VEC) {
-                    *reinterpret_cast<uint4 *>(static_cast<T *>(P.dp) + at) = q;
-                } else {
+            for (int q = 0; q < 2; ++q) {
+                const int64_t r = r0 + 8 * q;
+                if (r >= row1) break;
+                float(&g)[8] = both[q];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (c + STEP * i < P.n) Io<T>::store1(static_cast<T *>(P.dp) + at + STEP * i, h[i]);
+                for (int i = 0; i < 8; ++i) sum[i] += g[i];
+                if constexpr (SCALED) {
+                    if (P.dp_rows != nullptr) {
+                        float h[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) h[i] = g[i] * by_row[q];
+                        store_dp<T, VEC>(P, P.dp_rows, r, c, h);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) g[i] *= by_col[i];
                 }
-                if (P.dp_low != nullptr) {
+                if (P.dp != nullptr) {
+                    store_dp<T, VEC>(P, P.dp, r, c, g);
+                    if (P.dp_low != nullptr) {
+                        float h[8];
+                        Io<T>::unpack(Io<T>::pack(g), h);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) h[i] = isfinite(h[i]) ? g[i] - h[i] : 0.f;  // beyond the range the rounding stands
-                    if (VEC) {
-                        *reinterpret_cast<uint4 *>(static_cast<T *>(P.dp_low) + at) = Io<T>::pack(h);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (c + STEP * i < P.n) Io<T>::store1(static_cast<T *>(P.dp_low) + at + STEP * i, h[i]);
+                        for (int i = 0; i < 8; ++i) h[i] = isfinite(h[i]) ? g[i] - h[i] : 0.f;  // an infinity has no remainder
+                        store_dp<T, VEC>(P, P.dp_low, r, c, h);
                     }
                 }
             }
@@ -650,6 +703,60 @@ __global__ void __launch_bounds__(256) linear_grad_kernel(const LinearGradArgs P
 #pragma unroll
         for (int i = 0; i < 8; ++i) s += part[i][threadIdx.x];
         P.partial[(int64_t)blockIdx.x * P.n + mine] = s;
+    }
+}
+// The words that linear_largest_kernel is about to raise.  (A kernel rather than a memset, beside which no kernel starts early: 1 us of a small step.)
+__global__ void __launch_bounds__(256) linear_zero_kernel(uint32_t *to, int64_t n)
+{
+    pdl_wait();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) to[i] = 0;
+}
+// The largest finite |dP| of every row and of every column, into words that were zero: the order of fp32's bits is the order of values that are not negative, and
+// a largest one does not depend on the atomics' order.
+template <typename T, int ACT, bool VEC>
+__global__ void __launch_bounds__(256, 2) linear_largest_kernel(const LinearGradArgs P)
+{
+    pdl_wait();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ uint32_t part[8][256];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = (int)blockIdx.y * 256 + (VEC ? 8 * lane : lane);
+    const int64_t row0 = (int64_t)blockIdx.x * P.block_rows, row1 = min(P.rows, row0 + P.block_rows);
+    uint32_t most[8] = {};
+    for (int64_t r0 = row0 + warp; r0 < row1; r0 += 16) {
+        uint32_t of_row[2] = {};
+        if (c < P.n) {
+            float g[2][8];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) load_dp<T, ACT, VEC>(P, min(r0 + 8 * q, row1 - 1), c, g[q]);  // a row twice changes nothing
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t b = __float_as_uint(fabsf(g[q][i])), finite = b < 0x7f800000u ? b : 0;
+                    most[i] = max(most[i], finite), of_row[q] = max(of_row[q], finite);
+                }
+        }
+        __syncwarp();
+        if (P.row_largest != nullptr) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                of_row[q] = __reduce_max_sync(FULL, of_row[q]);
+                if (lane == 0) atomicMax(P.row_largest + min(r0 + 8 * q, row1 - 1), of_row[q]);
+            }
+        }
+    }
+    if (P.col_largest == nullptr) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[warp][VEC ? 8 * lane + i : lane + 32 * i] = most[i];
+    __syncthreads();
+    const int mine = (int)blockIdx.y * 256 + threadIdx.x;
+    if (mine < P.n) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, part[i][threadIdx.x]);
+        atomicMax(P.col_largest + mine, m);
     }
 }
 // 32 columns per block, the blocks of rows dealt out to its warps; the warps' sums are added in order

@@ -12,7 +12,7 @@ using namespace lapsum;
 namespace {
 
 struct LinearLayout {
-    size_t off_dp, off_low, off_partial, off_parts;
+    size_t off_dp, off_low, off_partial, off_parts, off_largest;
     int64_t ld, parts;  // row stride of pre and dP, blocks of rows of the bias' partial sums
 };
 
@@ -37,6 +37,7 @@ int linear_layout(const lapsum_linear_dims *p, LinearLayout &X, lapsum_linear_la
     X.off_low = at, at += p->training ? align_up((size_t)p->rows * (size_t)X.ld * 2) : 0;
     X.off_partial = at, at += p->training ? align_up((size_t)grad_blocks_most(p->rows) * (size_t)p->n * 4) : 0;
     X.off_parts = at, at += p->training ? PARTS_BYTES : 0;
+    X.off_largest = at, at += p->training && p->io_dtype == LAPSUM_IO_F16 ? align_up((size_t)(p->rows + p->n) * 4) : 0;
     out->workspace_bytes = at;
     out->pre_bytes = p->training && p->activation != LAPSUM_ACT_NONE ? (size_t)p->rows * (size_t)X.ld * (p->pre_dtype == LAPSUM_IO_F32 ? 4 : 2) : 0;
     out->pre_stride = X.ld;
@@ -135,7 +136,7 @@ int product(const Operand &a, const Operand &b, LinearArgs A, int dtype, cudaStr
             parts = ceil_div(steps, ceil_div(steps, parts));  // none without a part
             ch = Choice{(int)bn, 1, false};
             A.parts = (int)parts;
-            A.out = partial, A.out_stride = A.L, A.out_f32 = 1;
+            A.out = partial, A.out_stride = A.L, A.out_f32 = 1, A.largest = nullptr;
         }
     }
     A.split = ch.split;
@@ -149,7 +150,7 @@ int product(const Operand &a, const Operand &b, LinearArgs A, int dtype, cudaStr
         if (A.parts > 1) {
             RUN((ch.bn == 128 ? run_tiles<A_MN, B_MN, 128, false, true, T>(m, A, sms, st) : run_tiles<A_MN, B_MN, 64, false, true, T>(m, A, sms, st)));
             return launch_pdl(linear_parts_kernel<T>, (unsigned)ceil_div((int64_t)A.C * A.L, 256), 256, 0, st, partial, A.parts, A.C, A.L, whole.out,
-                              whole.out_stride, whole.out_f32);
+                              whole.out_stride, whole.out_f32, whole.largest);
         }
     }
     if constexpr (A_MN && !B_MN) return run_choice<A_MN, B_MN, false, T>(m, A, ch, sms, st);  // grad_x is 16-bit
@@ -189,52 +190,78 @@ LinearArgs base_args(void *ws)
 }
 
 template <typename T, int ACT>
-int grad(bool vec, dim3 grid, const LinearGradArgs &G, cudaStream_t st)
+int grad(bool vec, bool largest, dim3 grid, const LinearGradArgs &G, cudaStream_t st)
 {
+    if constexpr (std::is_same<T, __half>::value) {
+        if (largest) return launch_pdl(vec ? linear_largest_kernel<T, ACT, true> : linear_largest_kernel<T, ACT, false>, grid, 256, 0, st, G);
+    }
     return launch_pdl(vec ? linear_grad_kernel<T, ACT, true> : linear_grad_kernel<T, ACT, false>, grid, 256, 0, st, G);
+}
+template <typename T>
+int grad_by_act(int act, bool vec, bool largest, dim3 grid, const LinearGradArgs &G, cudaStream_t st)
+{
+    switch (act) {
+    case LAPSUM_ACT_RELU: return grad<T, LAPSUM_ACT_RELU>(vec, largest, grid, G, st);
+    case LAPSUM_ACT_SILU: return grad<T, LAPSUM_ACT_SILU>(vec, largest, grid, G, st);
+    case LAPSUM_ACT_GELU: return grad<T, LAPSUM_ACT_GELU>(vec, largest, grid, G, st);
+    case LAPSUM_ACT_GELU_TANH: return grad<T, LAPSUM_ACT_GELU_TANH>(vec, largest, grid, G, st);
+    default: return grad<T, LAPSUM_ACT_NONE>(vec, largest, grid, G, st);
+    }
 }
 
 template <typename T>
 int backward_t(const lapsum_linear_dims &p, const LinearLayout &X, const void *grad_y, int64_t gy_stride, const void *x, int64_t x_stride,
                const void *w, const void *pre, void *grad_x, int64_t gx_stride, void *grad_w, void *grad_bias, uint8_t *ws, cudaStream_t st)
 {
-    const bool y_f32 = p.out_dtype == LAPSUM_IO_F32;
+    const bool y_f32 = p.out_dtype == LAPSUM_IO_F32, wide = p.grad_w_dtype == LAPSUM_IO_F32;
     // grad_y is dP itself where there is no activation and the tensor maps can take it as it lies
-    const bool direct = p.activation == LAPSUM_ACT_NONE && !y_f32 && gy_stride % 8 == 0 && aligned(grad_y, 16);
-    const bool products = grad_x || grad_w, keep_low = grad_w && !direct && p.grad_w_dtype == LAPSUM_IO_F32;
+    const bool same = p.activation == LAPSUM_ACT_NONE && !y_f32, direct = same && gy_stride % 8 == 0 && aligned(grad_y, 16);
+    const bool products = grad_x || grad_w, keep_low = grad_w && !direct && wide;
+    // fp16 that is computed: dW's operand is scaled by columns, dx's by rows.  Both are written at once, the second in the room of the remainder, or, where dW
+    // needs that, one after the other.
+    const bool scaled = products && !same && p.io_dtype == LAPSUM_IO_F16, again = scaled && grad_x && keep_low;
+    LinearGradArgs G;
+    std::memset(&G, 0, sizeof(G));
+    G.grad_y = grad_y, G.pre = pre, G.pre_f32 = p.pre_dtype == LAPSUM_IO_F32;
+    G.y_stride = gy_stride, G.pre_stride = G.dp_stride = X.ld, G.rows = p.rows, G.n = (int)p.n, G.y_f32 = y_f32, G.block_rows = grad_block_rows(p.rows);
+    const bool vec = gy_stride % 8 == 0 && p.n % 8 == 0 && aligned(grad_y, 16);
+    const dim3 grid((unsigned)X.parts, (unsigned)ceil_div(p.n, 256));
+    if (scaled) {
+        uint32_t *const largest = reinterpret_cast<uint32_t *>(ws + X.off_largest);
+        G.row_largest = grad_x ? largest : nullptr, G.col_largest = grad_w ? largest + p.rows : nullptr;
+        RUN(launch_pdl(linear_zero_kernel, (unsigned)ceil_div(p.rows + p.n, 256), 256, 0, st, largest, p.rows + p.n));
+        RUN((grad_by_act<T>(p.activation, vec, true, grid, G, st)));
+    }
+    uint8_t *const dp_w = ws + X.off_dp, *const dp_x = scaled && grad_w && !again ? ws + X.off_low : ws + X.off_dp;
     if (grad_bias || (products && !direct)) {
-        LinearGradArgs G;
-        std::memset(&G, 0, sizeof(G));
-        G.grad_y = grad_y, G.pre = pre, G.dp = products && !direct ? ws + X.off_dp : nullptr;
         G.partial = grad_bias ? reinterpret_cast<float *>(ws + X.off_partial) : nullptr;
-        if (G.dp && keep_low) G.dp_low = ws + X.off_low;
-        G.pre_f32 = p.pre_dtype == LAPSUM_IO_F32;
-        G.y_stride = gy_stride, G.pre_stride = G.dp_stride = X.ld, G.rows = p.rows, G.n = (int)p.n, G.y_f32 = y_f32, G.block_rows = grad_block_rows(p.rows);
-        const bool vec = gy_stride % 8 == 0 && p.n % 8 == 0 && aligned(grad_y, 16);
-        const dim3 grid((unsigned)X.parts, (unsigned)ceil_div(p.n, 256));
-        switch (p.activation) {
-        case LAPSUM_ACT_RELU: RUN((grad<T, LAPSUM_ACT_RELU>(vec, grid, G, st))); break;
-        case LAPSUM_ACT_SILU: RUN((grad<T, LAPSUM_ACT_SILU>(vec, grid, G, st))); break;
-        case LAPSUM_ACT_GELU: RUN((grad<T, LAPSUM_ACT_GELU>(vec, grid, G, st))); break;
-        case LAPSUM_ACT_GELU_TANH: RUN((grad<T, LAPSUM_ACT_GELU_TANH>(vec, grid, G, st))); break;
-        default: RUN((grad<T, LAPSUM_ACT_NONE>(vec, grid, G, st))); break;
-        }
+        if (scaled ? grad_w != nullptr : products && !direct) G.dp = dp_w;
+        if (scaled && grad_x && !again) G.dp_rows = dp_x;
+        if (keep_low) G.dp_low = ws + X.off_low;
+        RUN((grad_by_act<T>(p.activation, vec, false, grid, G, st)));
         if (grad_bias)
             RUN(launch_pdl(linear_bias_kernel<T>, (unsigned)ceil_div(p.n, 32), 1024, 0, st, G.partial, X.parts, (int)p.n, grad_bias,
                            p.bias_dtype == LAPSUM_IO_F32 ? 1 : 0));
     }
-    const Operand dp = direct ? Operand{grad_y, p.n, p.rows, gy_stride} : Operand{ws + X.off_dp, p.n, p.rows, X.ld};
-    LinearArgs A = base_args(ws);
+    const auto operand = [&](const uint8_t *dp) { return direct ? Operand{grad_y, p.n, p.rows, gy_stride} : Operand{dp, p.n, p.rows, X.ld}; };
     float *const partial = reinterpret_cast<float *>(ws + X.off_parts);
-    if (grad_x) {
-        A.out = grad_x, A.out_stride = gx_stride, A.out_f32 = 0;
+    const auto to_x = [&] {
+        LinearArgs A = base_args(ws);
+        A.out = grad_x, A.out_stride = gx_stride, A.out_f32 = 0, A.largest = G.row_largest;
         A.L = (int)p.k, A.C = (int)p.rows, A.K = (int)p.n;
-        RUN((product<true, false, T>(Operand{w, p.k, p.n, p.k}, dp, A, p.io_dtype, st, partial)));
-    }
+        return product<true, false, T>(Operand{w, p.k, p.n, p.k}, operand(dp_x), A, p.io_dtype, st, partial);
+    };
+    if (grad_x && !again) RUN(to_x());
     if (grad_w) {
-        A.out = grad_w, A.out_stride = p.k, A.out_f32 = p.grad_w_dtype == LAPSUM_IO_F32;
+        LinearArgs A = base_args(ws);
+        A.out = grad_w, A.out_stride = p.k, A.out_f32 = wide, A.largest = G.col_largest;
         A.L = (int)p.k, A.C = (int)p.n, A.K = (int)p.rows;
-        RUN((product<true, true, T>(Operand{x, p.k, p.rows, x_stride}, dp, A, p.io_dtype, st, partial, keep_low ? ws + X.off_low : nullptr)));
+        RUN((product<true, true, T>(Operand{x, p.k, p.rows, x_stride}, operand(dp_w), A, p.io_dtype, st, partial, keep_low ? ws + X.off_low : nullptr)));
+    }
+    if (again) {
+        G.partial = nullptr, G.dp = G.dp_low = nullptr, G.dp_rows = dp_x;
+        RUN((grad_by_act<T>(p.activation, vec, false, grid, G, st)));
+        RUN(to_x());
     }
     return LAPSUM_OK;
 }
