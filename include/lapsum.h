@@ -594,7 +594,8 @@ int lapsum_debug_experts_timeout(int64_t wait_us, void *ws, size_t ws_bytes, con
  * lapsum_linear_backward:  dP = grad_y act'(P),  grad_x = dP W,  grad_w = dP^T x,  grad_bias = sum over rows of dP.
  * grad_y: rows x n of out_dtype, any row stride >= n; grad_x: rows x k of io_dtype, any row stride >= k; grad_w: n x k of grad_w_dtype
  * (io_dtype or fp32); grad_bias: n of bias_dtype.  Each result may be NULL.  The residual's gradient is grad_y.  dP is rounded to
- * io_dtype for the products (the tensor core's operands); for an fp32 grad_w the remainder takes part as well, and grad_bias sums it unrounded.  fp16 operands are
+ * io_dtype for the products (the tensor core's operands); for an fp32 grad_w the remainder takes part as well (an infinite x gives the infinities of the formula all
+ * the same), and grad_bias sums it unrounded.  fp16 operands are
  * scaled by powers of two, for grad_x by rows and for grad_w by columns of dP, so that dP may have any size in fp32's range: what counts is the largest finite
  * one of its own row or column, of which 2^-40 is resolved.  With rows = 0 grad_w and grad_bias are zeros.
  * Results do not depend on scheduling.

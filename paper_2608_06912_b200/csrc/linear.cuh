@@ -20,6 +20,7 @@
 // 4.5 TB/s (70); a prompt of 1021 rows, 2048 x 5632, 33 us (26): 32 large tiles, their contraction shared by two pairs each, so a join; one row of
 // 2048 x 1024 7 - 9 us, the host's call (3 in a graph).
 #pragma once
+#include <climits>
 #include <type_traits>
 
 #include "common.cuh"
@@ -292,7 +293,9 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
     const int mine = spread ? (int)(blockIdx.x / tiles) : (int)part;  // which part of the contraction
     const int64_t shift = spread ? (int64_t)mine * P.C * P.out_stride : 0;
     const int k_first = split || spread ? min(mine * share, steps) : 0, nkb = min(share, steps - k_first);
-    const int round = WIDE ? S::ROUND : nkb;
+    // An accumulator takes `round` steps, and never steps of both b and b_low: those of b_low begin at `turn`.
+    const int round = WIDE ? S::ROUND : nkb, turn = P.twice ? once - k_first : INT_MAX;
+    auto round_end = [&](int k0) { return min(k0 < turn ? min(k0 + round, turn) : k0 + round, nkb); };
     // Tiles in groups of eight column tiles, lane tiles outside: what the SMs work on at one time shares its operands in L2.
     struct Tile {
         int l0, c0;
@@ -358,13 +361,14 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
             uint32_t fill = 0, it = 0;
             bool ok = true, any = false;
             for (int64_t i = tile0; i < tiles && ok; i += tile_step)
-                for (int k0 = 0; k0 < nkb && ok; k0 += round, ++it) {
+                for (int k0 = 0, k1; k0 < nkb && ok; k0 = k1, ++it) {
+                    k1 = round_end(k0);
                     const uint32_t buf = it % S::ACC, phase = (it / S::ACC) & 1;
                     ok = waits.wait(acc_empty + 8 * buf, phase ^ 1);
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t d = tmem + buf * BN;
-                    for (int kb = k0; kb < min(nkb, k0 + round); ++kb, ++fill) {
+                    for (int kb = k0; kb < k1; ++kb, ++fill) {
                         const uint32_t s = fill % S::STAGES;
                         ok = waits.wait(full + 8 * s, (fill / S::STAGES) & 1);
                         if (!ok) break;
@@ -418,7 +422,7 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
 #pragma unroll
                     for (int j = 0; j < 16; ++j) sum[c][j] = 0.f;
             }
-            for (int k0 = 0; k0 < nkb; k0 += round, ++it) {
+            for (int k0 = 0; k0 < nkb; k0 = round_end(k0), ++it) {
                 const uint32_t buf = it % S::ACC, phase = (it / S::ACC) & 1;
                 ok = waits.wait(acc_full + 8 * buf, phase);
                 ok = __all_sync(FULL, ok);
@@ -426,6 +430,8 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
                 tc_fence_after();
                 const uint32_t d = tmem + buf * BN + lanes + 16 * set;
                 if constexpr (WIDE) {
+                    // an infinity or NaN of a's has reached the sums of b: beside the remainders, zeros or of the other sign, it would only make a NaN
+                    const bool low = k0 >= turn;
 #pragma unroll
                     for (int c = 0; c < S::CHUNKS; ++c) {
                         if (16 * set + 32 * c >= BN) continue;
@@ -433,7 +439,7 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
                         tmem_ld16(d + 32 * c, v);
                         tmem_wait_ld(v);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) sum[c][j] += v[j];
+                        for (int j = 0; j < 16; ++j) sum[c][j] += low && !(fabsf(v[j]) <= 3.402823466e38f) ? 0.f : v[j];
                     }
                 } else {
 #pragma unroll 1
