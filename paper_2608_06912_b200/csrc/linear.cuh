@@ -594,7 +594,7 @@ struct LinearGradArgs {
     const void *grad_y;  // fp32 (y_f32) or T
     const void *pre;     // fp32 (pre_f32) or T, null without an activation
     void *dp;            // T, null where grad_y itself serves; scaled by columns where col_largest is given
-    void *dp_low;        // T, dP less its rounding, null where grad_w is 16-bit
+    void *dp_low;        // T, dP less its rounding, null where grad_w is 16-bit or dP a copy of grad_y
     void *dp_rows;       // T, dP scaled by rows, or null
     uint32_t *row_largest, *col_largest;  // bits of the largest finite |dP| of every row, of every column; either may be null
     float *partial;      // [blocks of rows][n], null without a bias

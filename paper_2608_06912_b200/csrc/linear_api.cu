@@ -34,10 +34,12 @@ int linear_layout(const lapsum_linear_dims *p, LinearLayout &X, lapsum_linear_la
     X.parts = ceil_div(p->rows, grad_block_rows(p->rows));
     size_t at = 256;  // control block: the status word
     X.off_dp = at, at += p->training ? align_up((size_t)p->rows * (size_t)X.ld * 2) : 0;
-    X.off_low = at, at += p->training ? align_up((size_t)p->rows * (size_t)X.ld * 2) : 0;
+    // a 16-bit grad_y without an activation is dP itself, copied at most: no remainder, nothing to scale
+    const bool computed = p->activation != LAPSUM_ACT_NONE || p->out_dtype == LAPSUM_IO_F32;
+    X.off_low = at, at += p->training && computed ? align_up((size_t)p->rows * (size_t)X.ld * 2) : 0;
     X.off_partial = at, at += p->training ? align_up((size_t)grad_blocks_most(p->rows) * (size_t)p->n * 4) : 0;
     X.off_parts = at, at += p->training ? PARTS_BYTES : 0;
-    X.off_largest = at, at += p->training && p->io_dtype == LAPSUM_IO_F16 ? align_up((size_t)(p->rows + p->n) * 4) : 0;
+    X.off_largest = at, at += p->training && computed && p->io_dtype == LAPSUM_IO_F16 ? align_up((size_t)(p->rows + p->n) * 4) : 0;
     out->workspace_bytes = at;
     out->pre_bytes = p->training && p->activation != LAPSUM_ACT_NONE ? (size_t)p->rows * (size_t)X.ld * (p->pre_dtype == LAPSUM_IO_F32 ? 4 : 2) : 0;
     out->pre_stride = X.ld;
@@ -216,7 +218,7 @@ int backward_t(const lapsum_linear_dims &p, const LinearLayout &X, const void *g
     const bool y_f32 = p.out_dtype == LAPSUM_IO_F32, wide = p.grad_w_dtype == LAPSUM_IO_F32;
     // grad_y is dP itself where there is no activation and the tensor maps can take it as it lies
     const bool same = p.activation == LAPSUM_ACT_NONE && !y_f32, direct = same && gy_stride % 8 == 0 && aligned(grad_y, 16);
-    const bool products = grad_x || grad_w, keep_low = grad_w && !direct && wide;
+    const bool products = grad_x || grad_w, keep_low = grad_w && !same && wide;
     // fp16 that is computed: dW's operand is scaled by columns, dx's by rows.  Both are written at once, the second in the room of the remainder, or, where dW
     // needs that, one after the other.
     const bool scaled = products && !same && p.io_dtype == LAPSUM_IO_F16, again = scaled && grad_x && keep_low;

@@ -1,0 +1,27 @@
+"""What the dense operators ask for and accept, without a GPU: room for what a call can use, sizes whose results are exact and whose grids exist."""
+import ctypes as C
+
+import pytest
+
+import paper_2608_06912_b200 as L
+from paper_2608_06912_b200 import binding as B
+
+FAKE = 4096  # 256-byte aligned, never dereferenced: the checks return first
+F32, F16, BF16 = L.IO_F32, L.IO_F16, L.IO_BF16
+
+
+def linear_bytes(rows, n, k, act=L.ACT_NONE, io=BF16, out=BF16):
+    layout = B.LinearLayout()
+    dims = B.LinearDims(rows, n, k, act, io, out, io, io, F32, 1)
+    assert L.lib().lapsum_linear_describe(C.byref(dims), C.byref(layout)) == 0
+    return layout.workspace_bytes
+
+
+@pytest.mark.parametrize("io", [BF16, F16])
+def test_a_copied_gradient_has_no_remainder(io):
+    """a 16-bit grad_y without an activation is dP: its remainder is zero, so neither room nor a product is spent on it"""
+    rows, n, k = 4096, 1000, 64
+    plain, one = linear_bytes(rows, n, k, io=io, out=io), rows * n * 2
+    assert one <= linear_bytes(rows, n, k, io=io, out=F32) - plain <= one + 4 * (rows + n) + 512
+    assert linear_bytes(rows, n, k, io=io, out=io, act=L.ACT_SILU) == linear_bytes(rows, n, k, io=io, out=F32)
+    assert plain < 2 * one + 64 * n * 4 * 2 + 148 * 128 * 128 * 4
