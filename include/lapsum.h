@@ -598,7 +598,8 @@ int lapsum_debug_experts_timeout(int64_t wait_us, void *ws, size_t ws_bytes, con
  * the same), and grad_bias sums it unrounded.  fp16 operands are
  * scaled by powers of two, for grad_x by rows and for grad_w by columns of dP, so that dP may have any size in fp32's range: what counts is the largest finite
  * one of its own row or column, of which 2^-40 is resolved.  With rows = 0 grad_w and grad_bias are zeros.
- * Results do not depend on scheduling.
+ * Results do not depend on scheduling.  Sums of any length are right to about 1.3e-5 for 16-bit results of more than 8192 (bf16: 65536) terms, to 6.3e-9 a term
+ * below, to 3e-6 for fp32 results (5e-7 where the terms' signs are mixed).
  *
  * A workspace made for some rows serves calls of fewer.  It serves one stream at a time.  lapsum_linear_workspace_init clears its status
  * word; lapsum_linear_status synchronises and reads it (LAPSUM_ST_LINEAR_TIMEOUT: a bounded wait inside a kernel gave up).

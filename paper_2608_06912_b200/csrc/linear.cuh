@@ -42,6 +42,7 @@ struct LinearArgs {
     int lane_tiles, col_tiles;
     int act, out_f32, bias_f32, pre_f32;
     int twice;             // the contraction runs over (a, b), then over (a, b_low)
+    int round;             // WIDE: steps of 64 that one accumulator takes
     int split;             // blocks of a cluster that share the contraction of one tile
     int parts;             // of the contraction, each a block's of its own, whose results lie one behind the other (fp32, C rows each)
     const uint32_t *largest;  // fp16 gradients: the largest |dP| of every column of the result, by which its operand was scaled (grad_scale), or null
@@ -223,9 +224,10 @@ __device__ __forceinline__ void linear_finish(const LinearArgs &P, float (&v)[N]
 //   PAIR   a cluster of two blocks works on one 256 x 256 tile (cta_group::2): each block brings 128 rows of A and half of B, 64 bytes per
 //          clock of tensor work instead of the 96 that a 128 x 256 tile of one block needs.
 //   parts  the same without a cluster: blocks of their own leave fp32 results one behind the other, for linear_parts_kernel to add.
-//   WIDE   the tensor core's own additions truncate: an error of about 2^-25 of the sum each, all towards zero, 2e-6 at K = 2048 and 2e-5 at 16384.
-//          That is nothing to a 16-bit result.  For an fp32 result an accumulator takes ROUND steps (512 of the contraction), and the epilogue adds
-//          the rounds' sums in fp32 registers, rounded to nearest, while the next round is computed in the other accumulator: 5e-7.
+//   WIDE   the tensor core's own additions truncate, all towards zero: 2e-6 of the sum at K = 2048 and 2e-5 at 16384 where signs are mixed, five times that where all terms
+//          have one sign.  A 16-bit result of a short contraction does not show it.  For an fp32 result, or a long contraction, an accumulator takes some steps (512 of the
+//          contraction, 2048), and the epilogue adds the rounds' sums in fp32 registers, rounded to nearest, while the next round is computed in the other accumulator:
+//          5e-7 for fp32, with one sign 3e-6.
 //   split  a cluster of `split` blocks, or pairs, shares the contraction of one tile, for shapes with few tiles: each leaves its sums in its shared
 //          memory, and after a cluster barrier adds its share of the columns over the blocks, in their order.
 template <int BN, bool PAIR_>
@@ -235,7 +237,6 @@ struct LinearShape {
     static constexpr int A_BYTES = 128 * 128, B_BYTES = COLS * 128, STAGE = A_BYTES + B_BYTES;
     static constexpr int FIT = 229376 / STAGE, STAGES = FIT < 12 ? FIT : 12;
     static constexpr int ACC = 2, TMEM = ACC * BN;
-    static constexpr int ROUND = 8;                // steps of 64 that one accumulator of a WIDE result takes
     static constexpr int CHUNKS = (BN + 31) / 32;  // runs of 16 columns of one set of epilogue warps
     static constexpr int THREADS = 384;
     static constexpr int SMEM = STAGES * STAGE + 1024 + 512;
@@ -294,7 +295,7 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
     const int64_t shift = spread ? (int64_t)mine * P.C * P.out_stride : 0;
     const int k_first = split || spread ? min(mine * share, steps) : 0, nkb = min(share, steps - k_first);
     // An accumulator takes `round` steps, and never steps of both b and b_low: those of b_low begin at `turn`.
-    const int round = WIDE ? S::ROUND : nkb, turn = P.twice ? once - k_first : INT_MAX;
+    const int round = WIDE ? P.round : nkb, turn = P.twice ? once - k_first : INT_MAX;
     auto round_end = [&](int k0) { return min(k0 < turn ? min(k0 + round, turn) : k0 + round, nkb); };
     // Tiles in groups of eight column tiles, lane tiles outside: what the SMs work on at one time shares its operands in L2.
     struct Tile {

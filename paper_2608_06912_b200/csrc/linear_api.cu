@@ -120,6 +120,13 @@ struct Operand {
     int64_t cols, rows, stride;  // as it lies in memory; the contraction runs along the columns, or (MN-major) along the rows
 };
 
+// Steps of 64 that one accumulator takes for a 16-bit result.  The tensor core's additions truncate; where all terms have one sign that adds up to 6.3e-9 of the
+// sum per term (measured: fp16 sums of 16384 terms off by -1.0e-4 in the mean, of 400003 by -6.4e-4 in four parts).  Up to here it stays below a ninth of the largest
+// rounding of the type, 2^-11 or 2^-8; beyond, rounds are summed in registers: of 2048 (off by 1.3e-5), which cost 7 % (dW of 16384 x 8192 x 2048 fp16 410 -> 438 us);
+// rounds of 512, as fp32 results have them, 16 %.
+constexpr int64_t LONG_F16 = 8192 / 64, LONG_BF16 = 65536 / 64;
+constexpr int ROUND_F32 = 512 / 64, ROUND_16 = 2048 / 64;
+
 // One product.  A: [L][K] or, A_MN, [K][L]; B: [C][K] or, B_MN, [K][C].
 // `partial`: room for parts of the contraction (PARTS_BYTES), gradients only.
 template <bool A_MN, bool B_MN, typename T>
@@ -128,6 +135,7 @@ int product(const Operand &a, const Operand &b, LinearArgs A, int dtype, cudaStr
     int sms = 0;
     RUN(sm_count(&sms));
     A.twice = low != nullptr;
+    A.round = A.out_f32 ? ROUND_F32 : ROUND_16;
     Choice ch = choose(A.L, A.C, A.K * (low ? 2ll : 1ll), B_MN, sms);
     const LinearArgs whole = A;
     if (partial) {
@@ -155,8 +163,8 @@ int product(const Operand &a, const Operand &b, LinearArgs A, int dtype, cudaStr
                               whole.out_stride, whole.out_f32, whole.largest);
         }
     }
-    if constexpr (A_MN && !B_MN) return run_choice<A_MN, B_MN, false, T>(m, A, ch, sms, st);  // grad_x is 16-bit
-    else return A.out_f32 ? run_choice<A_MN, B_MN, true, T>(m, A, ch, sms, st) : run_choice<A_MN, B_MN, false, T>(m, A, ch, sms, st);
+    const bool rounds = A.out_f32 || ceil_div(ceil_div(A.K, 64), ch.split) > (dtype == LAPSUM_IO_F16 ? LONG_F16 : LONG_BF16);
+    return rounds ? run_choice<A_MN, B_MN, true, T>(m, A, ch, sms, st) : run_choice<A_MN, B_MN, false, T>(m, A, ch, sms, st);
 }
 
 constexpr int64_t FEW_ROWS = 4;
