@@ -657,8 +657,10 @@ int lapsum_debug_linear_timeout(int64_t wait_us, const void *x, const void *w, v
  *   token: int32; logprob (nullable): log of the probability with which it was drawn, fp32; kept (nullable): number of kept tokens, int32
  * A row without a usable logit gets token -1, logprob -inf, kept 0; a row with a setting out of range (temperature negative or not
  * finite, top_p <= 0, min_p outside [0, 1], u outside [0, 1), any of them NaN) token -1, logprob NaN, kept 0.
- * Sums are exact integers of weights with 45 fractional bits (fewer beyond 2^17 tokens): the result does not depend on scheduling,
- * and it is the definition's unless u or top_p meets a border to within about 2^-37.  rows <= 2^27, vocab <= 2^30.
+ * Sums are exact integers of weights with S fractional bits, S = 45 up to 2^18 tokens and one less for each doubling, so the result does not depend on scheduling.
+ * Each weight is rounded by at most 2^-(S + 1) of the largest: the result is the definition's unless u or top_p meets a border to within
+ * vocab 2^-(S + 1) of it (2^-28 at 2^18 tokens, 2^-22 at 2^21; typically, as the roundings differ, 2^-37 at 2^17), and logprob is off by at most as much beside its own
+ * rounding.  rows <= 2^27, vocab <= 2^21.
  */
 typedef struct lapsum_sample_params {
     double temperature; /* default 1                                    */

@@ -12,8 +12,8 @@
 // 256 x 128000 (131 MB, 20 us by its bytes): without filters 109 us, the exponentials, 9 operations in 64 bits and some 14 others per token, of which an SM
 // does 2.6 tokens a clock; with top-k, where only listed tokens are weighed, 82 us; rows of all kinds 193 us.
 //
-// Weights are integers, e_i 2^S rounded (S = 45 up to 2^17 tokens), from an exponential in 64 bits: their sums are exact in any order, so the
-// result depends neither on the cluster nor on atomics, and it is the definition's unless u or top_p falls within about 2^-37 of a border.
+// Weights are integers, e_i 2^S rounded (S = 45 up to 2^18 tokens), from an exponential in 64 bits: their sums are exact in any order, so the
+// result depends neither on the cluster nor on atomics, and it is the definition's unless u or top_p falls within vocab 2^-(S + 1) of a border, mostly some 2^-37.
 // With fp32 sums one draw in a few hundred over a vocabulary of 2^17 would pick a neighbour.
 //
 // The short way: the row's threads form 128 groups, and the largest logits of k groups are k tokens, so nothing below the k-th of them is among

@@ -14,6 +14,9 @@ using namespace lapsum;
 namespace {
 
 // ------------------------------------------------------------------ sample ----
+// Every weight is off by half a unit of 2^-S at most, the sums by vocab times that, and a long tail of small weights all to one side: 2^-28 of the largest weight at 2^18 tokens,
+// where S is 45, four times more for each doubling.  Up to here, 2^-22, that is of the size of what u and logprob resolve.
+constexpr int64_t SAMPLE_VOCAB = (int64_t)1 << 21;
 constexpr int SAMPLE_BLOCK_BYTES = 64 << 10, SMEM_MOST = 226 << 10;
 
 template <typename T, int THREADS, bool RESIDENT>
@@ -130,7 +133,7 @@ int lapsum_sample(const void *logits, int64_t rows, int64_t vocab, int64_t strid
                   int32_t *kept, void *stream)
 {
     if (!prm) return LAPSUM_ERR_NULL;
-    if (rows < 0 || rows > (int64_t)1 << 27 || vocab < 1 || vocab > (int64_t)1 << 30 || stride < vocab) return LAPSUM_ERR_SHAPE;
+    if (rows < 0 || rows > (int64_t)1 << 27 || vocab < 1 || vocab > SAMPLE_VOCAB || stride < vocab) return LAPSUM_ERR_SHAPE;
     // a setting for all rows has to be in range (one per row voids its row instead)
     if (prm->io_dtype < LAPSUM_IO_F32 || prm->io_dtype > LAPSUM_IO_BF16 || (!temperature && !(prm->temperature >= 0 && std::isfinite(prm->temperature))) ||
         (!top_p && !(prm->top_p > 0)) || (!min_p && !(prm->min_p >= 0 && prm->min_p <= 1)))
@@ -145,7 +148,7 @@ int lapsum_sample(const void *logits, int64_t rows, int64_t vocab, int64_t strid
     A.token = token, A.logprob = logprob, A.kept = kept;
     A.vocab = (int)vocab;
     A.bits = 45;
-    while (A.bits > 0 && vocab > (int64_t)1 << (62 - A.bits)) --A.bits;
+    while (vocab > (int64_t)1 << (63 - A.bits)) --A.bits;  // sums of up to vocab 2^S fit 64 bits
     return BY_TYPE(sample_t, prm->io_dtype, A, rows, static_cast<cudaStream_t>(stream));
 }
 

@@ -25,3 +25,11 @@ def test_a_copied_gradient_has_no_remainder(io):
     assert one <= linear_bytes(rows, n, k, io=io, out=F32) - plain <= one + 4 * (rows + n) + 512
     assert linear_bytes(rows, n, k, io=io, out=io, act=L.ACT_SILU) == linear_bytes(rows, n, k, io=io, out=F32)
     assert plain < 2 * one + 64 * n * 4 * 2 + 148 * 128 * 128 * 4
+
+
+def test_rows_whose_weights_would_be_too_coarse_are_refused():
+    """the sampler's integer weights lose a bit for each doubling of the vocabulary, and their sums two; beyond 2^21 tokens that would show"""
+    def call(vocab):
+        return L.lib().lapsum_sample(FAKE, 1, vocab, vocab, FAKE, C.byref(L.sample_params()), None, None, None, None, FAKE, None, None, None)
+
+    assert call((1 << 21) + 1) == call(1 << 24) == call(1 << 30) == -2
