@@ -660,7 +660,8 @@ int lapsum_debug_linear_timeout(int64_t wait_us, const void *x, const void *w, v
  * Sums are exact integers of weights with S fractional bits, S = 45 up to 2^18 tokens and one less for each doubling, so the result does not depend on scheduling.
  * Each weight is rounded by at most 2^-(S + 1) of the largest: the result is the definition's unless u or top_p meets a border to within
  * vocab 2^-(S + 1) of it (2^-28 at 2^18 tokens, 2^-22 at 2^21; typically, as the roundings differ, 2^-37 at 2^17), and logprob is off by at most as much beside its own
- * rounding.  rows <= 2^27, vocab <= 2^21.
+ * rounding.  Differences of logits are right to 2^-126, so this holds for temperatures from 1e-27 on (and 0); below, logits under fp32's normal range count as about its end.
+ * rows <= 2^27, vocab <= 2^21.
  */
 typedef struct lapsum_sample_params {
     double temperature; /* default 1                                    */
