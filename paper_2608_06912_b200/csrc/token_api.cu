@@ -86,7 +86,7 @@ int embed_forward_t(const EmbedArgs &A, cudaStream_t st)
     constexpr int V = Io<T>::V;
     const bool vec = A.d % V == 0 && A.table_stride % V == 0 && A.out_stride % V == 0 && aligned(A.table, 16) && aligned(A.out, 16);
     const int64_t units = A.tokens * (vec ? embed_parts<T, true>(A.d) : embed_parts<T, false>(A.d));
-    if (units > (int64_t)8 << 31) return LAPSUM_ERR_SHAPE;
+    if (ceil_div(units, 8) >= (int64_t)1 << 31) return LAPSUM_ERR_SHAPE;  // a grid ends at 2^31 - 1 blocks
     return launch_pdl(vec ? embed_forward_kernel<T, true> : embed_forward_kernel<T, false>, (unsigned)ceil_div(units, 8), 256, 0, st, A);
 }
 

@@ -33,3 +33,9 @@ def test_rows_whose_weights_would_be_too_coarse_are_refused():
         return L.lib().lapsum_sample(FAKE, 1, vocab, vocab, FAKE, C.byref(L.sample_params()), None, None, None, None, FAKE, None, None, None)
 
     assert call((1 << 21) + 1) == call(1 << 24) == call(1 << 30) == -2
+
+
+def test_a_forward_beyond_the_largest_grid_is_refused():
+    """2^30 ids with rows of 16 warps each are 2^31 blocks of eight warps, one more than a grid has"""
+    rc = L.lib().lapsum_embed_forward(FAKE, 4, 1 << 30, FAKE, 8192, 9, 8192, 1.0, BF16, FAKE, 8192, None)
+    assert rc == -2
