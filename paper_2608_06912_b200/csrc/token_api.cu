@@ -66,6 +66,10 @@ int embed_check(const void *ids, int32_t id_bytes, int64_t tokens, int64_t vocab
 struct EmbedLayout {
     size_t off_start, off_order, off_long, off_partial, bytes;
 };
+// Every block of the sort reads all ids, once per range of the table: 1.2e12 products of ids and ranges a second (2^20 ids into 2^20 rows 2.1 ms, 2^22 into 2^24 117).  Sizes
+// whose sort would hold the GPU for more than a quarter of a second are refused.
+constexpr int64_t EMBED_PRODUCTS = (int64_t)1 << 38;
+bool embed_sorts(int64_t tokens, int64_t vocab) { return tokens == 0 || ceil_div(vocab, EMBED_RANGE) <= EMBED_PRODUCTS / tokens; }
 EmbedLayout embed_layout(int64_t tokens, int64_t vocab, int64_t d)
 {
     EmbedLayout X;
@@ -169,7 +173,8 @@ int lapsum_embed_forward(const void *ids, int32_t id_bytes, int64_t tokens, cons
 int lapsum_embed_workspace_bytes(int64_t tokens, int64_t vocab, int64_t d, size_t *bytes)
 {
     if (!bytes) return LAPSUM_ERR_NULL;
-    if (tokens < 0 || tokens > (int64_t)1 << 30 || vocab < 1 || vocab > (int64_t)1 << 30 || d < 1 || d > (int64_t)1 << 20) return LAPSUM_ERR_SHAPE;
+    if (tokens < 0 || tokens > (int64_t)1 << 30 || vocab < 1 || vocab > (int64_t)1 << 30 || d < 1 || d > (int64_t)1 << 20 || !embed_sorts(tokens, vocab))
+        return LAPSUM_ERR_SHAPE;
     *bytes = embed_layout(tokens, vocab, d).bytes;
     return LAPSUM_OK;
 }
@@ -178,7 +183,7 @@ int lapsum_embed_backward(const void *grad_out, int64_t grad_stride, const void 
                           double scale, int64_t skip, int32_t io_dtype, int32_t grad_dtype, void *grad_table, void *ws, size_t ws_bytes, void *stream)
 {
     RUN(embed_check(ids, id_bytes, tokens, vocab, d, scale, io_dtype));
-    if (grad_stride < d) return LAPSUM_ERR_SHAPE;
+    if (grad_stride < d || !embed_sorts(tokens, vocab)) return LAPSUM_ERR_SHAPE;
     if (grad_dtype != io_dtype && grad_dtype != LAPSUM_IO_F32) return LAPSUM_ERR_UNSUPPORTED;
     if (!grad_table || !ws || (tokens > 0 && !grad_out)) return LAPSUM_ERR_NULL;
     const EmbedLayout X = embed_layout(tokens, vocab, d);

@@ -39,3 +39,17 @@ def test_a_forward_beyond_the_largest_grid_is_refused():
     """2^30 ids with rows of 16 warps each are 2^31 blocks of eight warps, one more than a grid has"""
     rc = L.lib().lapsum_embed_forward(FAKE, 4, 1 << 30, FAKE, 8192, 9, 8192, 1.0, BF16, FAKE, 8192, None)
     assert rc == -2
+
+
+def test_a_sort_that_would_hold_the_gpu_for_minutes_is_refused():
+    """every 512 rows of the table cost a pass over the ids: 2^30 ids into 2^30 rows would be 2^51 reads"""
+    def size(tokens, vocab):
+        return L.lib().lapsum_embed_workspace_bytes(tokens, vocab, 8, C.byref(C.c_size_t()))
+
+    def back(tokens, vocab):
+        return L.lib().lapsum_embed_backward(FAKE, 8, FAKE, 4, tokens, vocab, 8, 1.0, -1, F32, F32, FAKE, FAKE, 1 << 60, None)
+
+    for tokens, vocab in ((1 << 30, 1 << 30), (1 << 23, (1 << 24) + 1), (1 << 30, (1 << 17) + 1)):
+        assert size(tokens, vocab) == back(tokens, vocab) == -2
+    for tokens, vocab in ((1 << 22, 1 << 24), (1 << 23, 1 << 24), (1 << 30, 1 << 17), (1, 1 << 30), (0, 1 << 30)):
+        assert size(tokens, vocab) == 0
