@@ -54,9 +54,9 @@ constexpr int SAMPLE_BUCKETS = 1024, SAMPLE_LIST = 256, SAMPLE_GROUPS = 128;
 // tokens that the groups' bound lets through: 128 ln(1 / (1 - k / 128)) if the order is random, 177 for this k
 constexpr int SAMPLE_SHORT_K = 96;
 
-template <int THREADS>
+template <int THREADS, bool TOP_P>
 struct alignas(16) SampleShared {
-    static constexpr int NEAR = THREADS == 1024 ? 1024 : 128;  // tokens of a warp's near list: with 64 KB of the row two blocks of 512 threads fit an SM
+    static constexpr int NEAR = TOP_P ? 128 : 1;  // tokens of a warp's near list, which top-p alone needs: with 64 KB of the row two blocks of 512 threads fit an SM
     double power[64 * 16];  // 2^(j / 64 + S), sixteen of each: a lane reads its own, so that no two meet in a bank
     unsigned long long mass[SAMPLE_BUCKETS];
     uint32_t count[SAMPLE_BUCKETS];
@@ -119,11 +119,11 @@ __device__ __forceinline__ void far_all(const uint32_t *p, int cluster, uint32_t
 }
 
 // One row as one block sees it
-template <typename T, int THREADS, bool RESIDENT>
+template <typename T, int THREADS, bool RESIDENT, bool TOP_P>
 struct SampleRow {
     static constexpr int V = Io<T>::V, WARPS = THREADS / 32;
     const SampleArgs &P;
-    SampleShared<THREADS> &S;
+    SampleShared<THREADS, TOP_P> &S;
     const T *row, *mine;     // the row in memory; this block's run of it in shared memory
     int begin, len, padded;  // the run; `padded` is a multiple of V
     bool whole;              // vectors of the run in memory are aligned
@@ -536,12 +536,12 @@ struct SampleRow {
             for (int j = 0; j < V; ++j) {
                 const unsigned who = __ballot_sync(FULL, x[j] >= low);
                 const uint32_t at_ = to + __popc(who & lower);
-                if (x[j] >= low && at_ < SampleShared<THREADS>::NEAR) S.near[warp][at_] = (uint32_t)(i + j);
+                if (x[j] >= low && at_ < SampleShared<THREADS, TOP_P>::NEAR) S.near[warp][at_] = (uint32_t)(i + j);
                 to += __popc(who);
             }
         });
         if (lane == 0) S.near_of[warp] = to;
-        return !__syncthreads_or(to > SampleShared<THREADS>::NEAR);
+        return !__syncthreads_or(to > SampleShared<THREADS, TOP_P>::NEAR);
     }
 
     // (cut_x, cut_i) <- the token of the rank at which the counts (or weights) of the tokens from `low` on reach the goal
@@ -772,7 +772,7 @@ struct SampleRow {
         top = key_to_float(key);
 
         const double T_ = P.temperature_row ? (double)ld(P.temperature_row + r) : P.temperature;
-        const double p = P.top_p_row ? (double)ld(P.top_p_row + r) : P.top_p, m = P.min_p_row ? (double)ld(P.min_p_row + r) : P.min_p;
+        const double p = !TOP_P ? 1.0 : P.top_p_row ? (double)ld(P.top_p_row + r) : P.top_p, m = P.min_p_row ? (double)ld(P.min_p_row + r) : P.min_p;
         const int64_t k = P.top_k_row ? (int64_t)ld(P.top_k_row + r) : P.top_k;
         const float u = ld(P.u + r);
         const bool valid = T_ >= 0 && T_ < CUDART_INF && p > 0 && m >= 0 && m <= 1 && u >= 0.f && u < 1.f;  // false for NaN
@@ -863,7 +863,7 @@ struct SampleRow {
                 low = fmaxf(low, light > 0 ? __double2float_rd((double)top + T_ * log(light)) : none_x);
                 range = top - low;
             }
-            descend(!need_k, low, range, goal);
+            descend(TOP_P && !need_k, low, range, goal);
             if (need_k) need_k = false;
             else need_p = false;
         }
@@ -871,11 +871,11 @@ struct SampleRow {
     }
 };
 
-template <typename T, int THREADS, bool RESIDENT>
+template <typename T, int THREADS, bool RESIDENT, bool TOP_P>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const SampleArgs P)
 {
     extern __shared__ __align__(16) uint8_t raw[];
-    SampleShared<THREADS> &S = *reinterpret_cast<SampleShared<THREADS> *>(raw);
+    SampleShared<THREADS, TOP_P> &S = *reinterpret_cast<SampleShared<THREADS, TOP_P> *>(raw);
     static_assert(THREADS >= SAMPLE_LIST && THREADS >= SAMPLE_GROUPS && THREADS % 64 == 0, "a thread per item");
     {
         const double power = exp2((double)(threadIdx.x & 63) / 64 + P.bits);
@@ -889,7 +889,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) sample_kernel(const S
     const int begin = min((int)rank * P.chunk, P.vocab), len = min(P.chunk, P.vocab - begin);
     const int64_t r = blockIdx.x / P.cluster;
     const T *const row = static_cast<const T *>(P.logits) + r * P.stride;
-    SampleRow<T, THREADS, RESIDENT> s{P, S, row, reinterpret_cast<const T *>(raw + sizeof(S)), begin, len, (len + Io<T>::V - 1) / Io<T>::V * Io<T>::V,
+    SampleRow<T, THREADS, RESIDENT, TOP_P> s{P, S, row, reinterpret_cast<const T *>(raw + sizeof(S)), begin, len, (len + Io<T>::V - 1) / Io<T>::V * Io<T>::V,
                                       (reinterpret_cast<uintptr_t>(row + begin) & 15) == 0, rank, (uint32_t)(r % P.cluster), (int)threadIdx.x,
                                       (int)threadIdx.x & 31, (int)threadIdx.x >> 5};
     s.run(r);

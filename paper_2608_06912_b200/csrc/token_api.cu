@@ -19,11 +19,11 @@ namespace {
 constexpr int64_t SAMPLE_VOCAB = (int64_t)1 << 21;
 constexpr int SAMPLE_BLOCK_BYTES = 64 << 10, SMEM_MOST = 226 << 10;
 
-template <typename T, int THREADS, bool RESIDENT>
+template <typename T, int THREADS, bool RESIDENT, bool TOP_P>
 int sample_launch(const SampleArgs &A, int64_t rows, cudaStream_t st)
 {
-    const auto kernel = sample_kernel<T, THREADS, RESIDENT>;
-    const size_t smem = sizeof(SampleShared<THREADS>) + (RESIDENT ? (size_t)A.chunk * sizeof(T) : 0);
+    const auto kernel = sample_kernel<T, THREADS, RESIDENT, TOP_P>;
+    const size_t smem = sizeof(SampleShared<THREADS, TOP_P>) + (RESIDENT ? (size_t)A.chunk * sizeof(T) : 0);
     static thread_local int dev_ready = -1;  // the attribute belongs to the device's context
     int dev = 0;
     CU_OK(cudaGetDevice(&dev));
@@ -49,9 +49,9 @@ int sample_t(SampleArgs A, int64_t rows, cudaStream_t st)
         cluster *= 2;
     A.cluster = cluster;
     A.chunk = (int)(ceil_div(ceil_div(A.vocab, cluster), 128) * 128);
-    if (many) return sample_launch<T, 1024, false>(A, rows, st);
-    if ((size_t)A.chunk * sizeof(T) + sizeof(SampleShared<512>) <= SMEM_MOST) return sample_launch<T, 512, true>(A, rows, st);
-    return sample_launch<T, 512, false>(A, rows, st);
+    if (many) return sample_launch<T, 1024, false, false>(A, rows, st);
+    if ((size_t)A.chunk * sizeof(T) + sizeof(SampleShared<512, true>) <= SMEM_MOST) return sample_launch<T, 512, true, true>(A, rows, st);
+    return sample_launch<T, 512, false, true>(A, rows, st);
 }
 
 // ------------------------------------------------------------------- embed ----
