@@ -19,7 +19,7 @@ struct LinearLayout {
 // A gradient whose tiles are fewer than an eighth of the SMs, with a long contraction: as many parts of it as fill the SMs, of 16 steps of 64 at least, each with
 // a tile's fp32 results in the workspace.  Measured, dW without / with parts, us: 65536 x 128 x 2048 86 / 71, in fp32 186 / 130; 65536 x 64 x 512 83 / 30, 177 / 56;
 // 65536 x 11 x 72 100 / 36; 4096 x 128 x 256 17 / 16; dx of 100 x 60000 x 128 78 / 22.
-constexpr int PARTS_UNITS = 148;
+constexpr int PARTS_UNITS = 148;  // the SMs of a B200: a workspace is described without a device
 constexpr size_t PARTS_BYTES = (size_t)PARTS_UNITS * 128 * 128 * 4;
 int linear_layout(const lapsum_linear_dims *p, LinearLayout &X, lapsum_linear_layout *out)
 {

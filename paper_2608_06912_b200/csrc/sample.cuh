@@ -8,7 +8,7 @@
 // Or, for many long rows without top-p, one block of 1024 threads has one and reads it again, from L2: no cluster barriers and no loads from other
 // blocks' memory, which take 2000 clocks and more.
 //
-// What bounds it.  One row (50021 tokens, 15 us with the call): a chain of three to nine cluster barriers and the fetch of code that runs once.
+// What bounds it.  One row (50021 tokens, 9 to 32 us with the call, by the way that its settings take): a chain of three to nine cluster barriers and the fetch of code that runs once.
 // 256 x 128000 (131 MB, 20 us by its bytes): without filters 109 us, the exponentials, 9 operations in 64 bits and some 14 others per token, of which an SM
 // does 2.6 tokens a clock; with top-k, where only listed tokens are weighed, 82 us; rows of all kinds 193 us.
 //
@@ -54,6 +54,14 @@ constexpr int SAMPLE_BUCKETS = 1024, SAMPLE_LIST = 256, SAMPLE_GROUPS = 128;
 // tokens that the groups' bound lets through: 128 ln(1 / (1 - k / 128)) if the order is random, 177 for this k
 constexpr int SAMPLE_SHORT_K = 96;
 
+// Read by the cluster's other blocks, each behind the barrier that follows its writing, and written again only behind another one (or a row's first time):
+//   key_max, groups      behind the row's first barrier; groups are never written again, key_min and key_max in descend(), behind crossing()'s
+//   block_mass, _count   sum_and_find(): the next one comes behind the barriers of what lies between, crossing() or finish_short(), or was the row's last
+//   mass, count          as histograms, between crossing()'s two barriers; before and afterwards they are this block's own
+//   slice_...            behind crossing()'s second; written between the next one's two
+//   list, list_count     written by all blocks, read behind finish_list()'s or finish_short()'s; the count is cleared behind crossing()'s first
+//   index                descend(), between its last two; elsewhere this block's own
+// All the rest, warp_mass among it, is this block's alone.  How many barriers a block passes depends on values that all blocks read alike.
 template <int THREADS, bool TOP_P>
 struct alignas(16) SampleShared {
     static constexpr int NEAR = TOP_P ? 128 : 1;  // tokens of a warp's near list, which top-p alone needs: with 64 KB of the row two blocks of 512 threads fit an SM
@@ -67,8 +75,7 @@ struct alignas(16) SampleShared {
     uint32_t groups[SAMPLE_GROUPS], ranked[SAMPLE_GROUPS];  // this block's groups' largest keys; those of all blocks, largest first
     unsigned long long warp_mass[THREADS / 32];
     uint32_t warp_count[THREADS / 32];
-    unsigned long long part_mass[THREADS / 32];  // for this block alone: warp_mass is read by the others until the row's last barrier
-    unsigned long long block_mass, slice_total;  // read by the cluster's other blocks
+    unsigned long long block_mass, slice_total;
     uint32_t block_count, list_count;
     uint32_t key_min, key_max;
     int index;
@@ -327,13 +334,13 @@ struct SampleRow {
                 __syncwarp();
                 unsigned long long run = warp_scan(s, lane);
                 __syncthreads();
-                if (lane == 31) S.part_mass[warp] = run;
+                if (lane == 31) S.warp_mass[warp] = run;
                 __syncthreads();
                 unsigned long long lower = before;
 #pragma unroll 4
                 for (int w = 0; w < WARPS; ++w) {
-                    if (w < warp) lower += S.part_mass[w];
-                    before += S.part_mass[w];
+                    if (w < warp) lower += S.warp_mass[w];
+                    before += S.warp_mass[w];
                 }
                 run += lower - s;
                 if (run <= goal && goal < run + s) {
@@ -691,7 +698,7 @@ struct SampleRow {
             const unsigned long long w = first ? weight(x) : 0;
             // running sums in the rank's order
             unsigned long long run = warp_scan(w, lane);
-            if (lane == 31) S.part_mass[warp] = run;
+            if (lane == 31) S.warp_mass[warp] = run;
             S.mass[tid] = w;
             if (tid < SAMPLE_LIST) S.list[tid] = back;
             if (tid == 0) S.members = 0;
@@ -699,8 +706,8 @@ struct SampleRow {
             unsigned long long total = 0;
 #pragma unroll 1
             for (int i = 0; i < SAMPLE_LIST / 32; ++i) {
-                if (i < warp) run += S.part_mass[i];
-                total += S.part_mass[i];
+                if (i < warp) run += S.warp_mass[i];
+                total += S.warp_mass[i];
             }
             const unsigned long long goal = p < 1 ? reach(p, k > 0 ? total : all) : ~0ull;
             if (first && run - w < goal) atomicAdd(&S.members, 1u);  // all before the goal is reached, and the one that reaches it

@@ -34,9 +34,13 @@ int sample_launch(const SampleArgs &A, int64_t rows, cudaStream_t st)
     return launch_clusters((unsigned)A.cluster, kernel, (unsigned)(rows * A.cluster), THREADS, smem, st, A);
 }
 // Few rows, or a top-p that may have to look far: blocks as many as keep a block's run at 64 KB (two blocks per SM), and more, down to runs of 4096 tokens,
-// while all of them find a place at once.  Rows for two thirds of the SMs, long and without top-p: a block of 1024 threads each.  Measured at 256 x 128000 fp32, a block
-// each / clusters, us: no filter 109 / 121, top-k 40 82 / 111, top-p 0.9 over some 3000 tokens 366 / 424, rows of all kinds 324 / 193 (a single row of the
-// last kind takes 200 on one SM); 512 x 1000 75 / 36.
+// while all of them find a place at once.  Rows for two thirds of the SMs, long and without top-p: a block of 1024 threads each.  Measured, a block each / clusters, us, no
+// filter and top-k 40:
+//   fp32   74 x 128000 40 / 41, 26 / 34     99 x 32768 17 / 17, 15 / 16     148 x 50257 27 / 36, 24 / 36    256 x 128000 90 / 121, 63 / 111   600 x 128000 226 / 268, 139 / 235
+//          48 x 128000 39 / 29, 25 / 25     99 x 16384 13 / 13, 14 / 15     296 x 16384 25 / 16, 25 / 17    600 x 24000 70 / 59, 69 / 67
+//   bf16   99 x 128000 36 / 37, 25 / 32     148 x 65536 23 / 25, 19 / 20    296 x 128000 72 / 98, 45 / 78   but 600 x 32768 73 / 53, 67 / 49
+// With top-p clusters win: 0.9 over some 3000 tokens 366 / 424 of 256 x 128000, but rows of all kinds 324 / 193 (a single row of the last kind takes 200 on one SM).  The
+// host sees no values of settings per row, so a given top-p counts as one.
 template <typename T>
 int sample_t(SampleArgs A, int64_t rows, cudaStream_t st)
 {
