@@ -310,7 +310,8 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
     const uint32_t tmem = tmem_at;
     pdl_wait();
 
-    const int once = (P.K + 63) / 64, steps = P.twice ? 2 * once : once;
+    constexpr bool LOW = WIDE && A_MN && B_MN;  // dW alone has a b_low
+    const int once = (P.K + 63) / 64, steps = LOW && P.twice ? 2 * once : once;
     const int ways = spread ? P.parts : P.split, share = (steps + ways - 1) / ways;
     const int64_t tiles = (int64_t)P.lane_tiles * P.col_tiles;
     const int64_t group = (PAIR ? 2 : 1) * P.split, tile0 = spread ? blockIdx.x % tiles : blockIdx.x / group, tile_step = spread ? tiles : gridDim.x / group;
@@ -318,7 +319,7 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
     const int64_t shift = spread ? (int64_t)mine * P.C * P.out_stride : 0;
     const int k_first = split || spread ? min(mine * share, steps) : 0, nkb = min(share, steps - k_first);
     // An accumulator takes `round` steps, and never steps of both b and b_low: those of b_low begin at `turn`.
-    const int round = WIDE ? P.round : nkb, turn = P.twice ? once - k_first : INT_MAX;
+    const int round = WIDE ? P.round : nkb, turn = LOW && P.twice ? once - k_first : INT_MAX;
     auto round_end = [&](int k0) { return min(k0 < turn ? min(k0 + round, turn) : k0 + round, nkb); };
     // Tiles in groups of eight column tiles, lane tiles outside: what the SMs work on at one time shares its operands in L2.
     struct Tile {
@@ -454,16 +455,19 @@ __global__ void __launch_bounds__(384, 1) linear_kernel(const __grid_constant__ 
                 tc_fence_after();
                 const uint32_t d = tmem + buf * BN + lanes + 16 * set;
                 if constexpr (WIDE) {
-                    // an infinity or NaN of a's has reached the sums of b: beside the remainders, zeros or of the other sign, it would only make a NaN
-                    const bool low = k0 >= turn;
 #pragma unroll
                     for (int c = 0; c < S::CHUNKS; ++c) {
                         if (16 * set + 32 * c >= BN) continue;
                         float v[16];
                         tmem_ld16(d + 32 * c, v);
                         tmem_wait_ld(v);
+                        if (LOW && k0 >= turn) {
+                            // an infinity or NaN of a's has reached the sums of b: beside the remainders, zeros or of the other sign, it would only make a NaN
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) sum[c][j] += low && !(fabsf(v[j]) <= 3.402823466e38f) ? 0.f : v[j];
+                            for (int j = 0; j < 16; ++j) v[j] = fabsf(v[j]) <= 3.402823466e38f ? v[j] : 0.f;
+                        }
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sum[c][j] += v[j];
                     }
                 } else {
 #pragma unroll 1
