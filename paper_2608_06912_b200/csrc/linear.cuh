@@ -14,11 +14,11 @@
 // 32 neighbouring values of one row of the result: loads and stores of it are contiguous whatever n, the strides and the alignment,
 // and a bias is one value per thread.
 //
-// Measured in bf16, operands not in L2 (a library's product of the same shape beside it): 16384 x 8192 x 2048 forward without an epilogue 373 us,
-// 1.47 PFLOP/s (344), with silu and P kept in fp32 (805 MB of results) 416 - 426; dx 352 (348), dW 399 (341), all at the power limit; dW with fp32 digits 990 for
-// twice the products.  Logits of 48 rows, 128000 x 2048, 106 us, 5.1 TB/s of weights (107); the router 65536 x 128 x 2048 65 - 68 us,
-// 4.5 TB/s (70); a prompt of 1021 rows, 2048 x 5632, 33 us (26): 32 large tiles, their contraction shared by two pairs each, so a join; one row of
-// 2048 x 1024 7 - 9 us, the host's call (3 in a graph).
+// Measured in bf16 on two boards, operands not in L2 (a library's product of the same shape beside it): 16384 x 8192 x 2048 forward without an epilogue 373 - 393 us,
+// 1.47 PFLOP/s (344 - 358), with silu and P kept in fp32 (805 MB of results) 416 - 453; dx 352 - 373 (348), dW 399 - 455 (341), all at the power limit; dW with fp32 digits
+// 990 - 1110 for twice the products.  Logits of 48 rows, 128000 x 2048, 106 us, 5.1 TB/s of weights (107); the router 65536 x 128 x 2048 65 - 68 us,
+// 4.5 TB/s (70), 256 tiles on 148 SMs, so that 40 of them have one and the others two; a prompt of 1021 rows, 2048 x 5632, 33 us (26): 32 large tiles, their contraction
+// shared by two pairs each, so a join; one row of 2048 x 1024 7 - 9 us, the host's call (2.6 in a graph).
 #pragma once
 #include <climits>
 #include <type_traits>

@@ -158,8 +158,8 @@ def sample_params(**overrides) -> SampleParams:
 def lapsum_sample(logits: torch.Tensor, u: torch.Tensor, params: SampleParams, token: torch.Tensor, logprob: Optional[torch.Tensor] = None,
                   kept: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
                   top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
-    """token (int32, one per row) <- the next token of every row of logits (rows x vocab of the params' io_dtype, contiguous rows, any row
-    stride) for the random numbers u (float32, one per row, in [0, 1)).  logprob (float32), kept (int32): see lapsum_sample in the header.
+    """token (int32, one per row) <- the next token of every row of logits (rows x vocab of the params' io_dtype, up to 2^21 tokens, contiguous
+    rows, any row stride) for the random numbers u (float32, one per row, in [0, 1)).  logprob (float32), kept (int32): see lapsum_sample in the header.
     temperature, top_p, min_p (float32) and top_k (int32), one per row, replace the params' value for all rows."""
     stride = _rows(logits, IO_TORCH[params.io_dtype], "logits")
     rows, vocab = logits.shape
