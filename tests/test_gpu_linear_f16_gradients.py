@@ -100,3 +100,41 @@ def test_results_do_not_depend_on_scheduling():
     for grad_w in (F, H):
         a, b = (gradients(777, 515, 520, "silu", upstream(777, 515) * 1e-6, grad_w) for _ in range(2))
         assert all(torch.equal(a[name], b[name]) for name in a)
+
+
+@pytest.mark.parametrize("grad_w", [F, H])
+def test_a_captured_backward_finds_each_replay_s_own_sizes(grad_w):
+    """what was largest in one replay, or in a call of more rows on the same workspace, has no part in the next"""
+    rows, n, k = 300, 131, 72
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn(rows, k, device="cuda", generator=gen).to(H)
+    w = (torch.randn(n, k, device="cuda", generator=gen) * k ** -0.5).to(H)
+    ws = L.LinearWorkspace(2 * rows, n, k, activation=L.ACT_SILU, io_dtype=L.IO_F16, out_dtype=L.IO_F32, training=True)
+    pre, y, gy = ws.new_pre(), torch.empty(rows, n, device="cuda"), torch.empty(rows, n, device="cuda")
+    L.lapsum_linear_forward(x, w, None, None, y, ws, pre=pre)
+    out = torch.empty_like(x), torch.empty(n, k, device="cuda", dtype=grad_w)
+
+    def backward(workspace, into):
+        L.lapsum_linear_backward(gy, x, w, pre, into[0], into[1], None, workspace)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        backward(ws, out)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        backward(ws, out)
+    for size in (1e8, 1.0, 1e-9, 1e3):
+        gy.copy_(upstream(rows, n, seed=int(size)) * size)
+        graph.replay()
+        fresh = L.LinearWorkspace(rows, n, k, activation=L.ACT_SILU, io_dtype=L.IO_F16, out_dtype=L.IO_F32, training=True)
+        want = torch.empty_like(out[0]), torch.empty_like(out[1])
+        backward(fresh, want)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), size
+        big = torch.full((2 * rows, n), 1e20, device="cuda")
+        x2, pre2, gx2 = x.repeat(2, 1), ws.new_pre(), torch.empty(2 * rows, k, device="cuda", dtype=H)
+        pre2.zero_()
+        L.lapsum_linear_backward(big, x2, w, pre2, gx2, torch.empty_like(out[1]), None, ws)
+    assert ws.status() == 0
